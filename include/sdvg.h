@@ -33,7 +33,7 @@ typedef enum {
   SDVG_ERR_DEVICE = -6       /* a HIP runtime call failed (see sdvg_last_device_error) */
 } sdvg_status;
 
-enum { SDVG_BF16 = 0, SDVG_F32 = 1 };
+enum { SDVG_BF16 = 0, SDVG_F32 = 1, SDVG_F16 = 2, SDVG_E4M3 = 3 }; /* the last two: paged cache only */
 
 /* Key-split policy of sdvg_block_attn_batch (see there). */
 enum { SDVG_SPLIT_NEVER = 0, SDVG_SPLIT_AUTO = 1, SDVG_SPLIT_ALWAYS = 2 };
@@ -294,6 +294,60 @@ int sdvg_avg_frame_route(const float *frame_scores, int32_t n_frames, float tau,
 int sdvg_avg_frame_route_batch(const float *frame_scores, int32_t n_blocks, int32_t n_frames,
                                float tau, const int32_t *block_idx, int32_t first_block_idx,
                                int32_t *decisions_out, float *q_b_out, void *stream);
+
+/*
+ * ---- Paged cache -----------------------------------------------------------------------------
+ * Where many requests of different lengths are generated at once, token by token (a draft of a few tokens, then
+ * their verification), a cache per request sized for the longest one does not pay. The paged cache is one pool
+ * of pages of page_tokens tokens; a row of the block table lists a request's pages in order. One step of a model:
+ *   sdvg_page_plan     once per step: pages for the new tokens, their slots and positions, from the requests' lengths
+ *   sdvg_paged_commit  per layer: the new tokens' K (rotated) and V into their slots, q rotated in the same launch
+ *   sdvg_paged_attn    per layer: every new token's attention over its request's cached tokens and itself
+ * Undoing rejected tokens needs no call: the next plan is given the shorter lengths, the pages stay held. All
+ * lengths, tables and slots are read on the device, so a captured graph of the step may be replayed with other values in
+ * the same arrays. Device values out of range are never followed out of the arrays they index (each call says what
+ * they mean).
+ */
+
+/* One layer's pools k and v: device, logical [n_pages][page_tokens][n_kv_heads][128], strides alike. */
+typedef struct {
+  void *k, *v;                    /* device, 16-byte aligned */
+  const float *k_scale, *v_scale; /* device [n_kv_heads], nullable (1): a stored number x stands for x * scale */
+  int32_t n_pages, page_tokens;   /* page_tokens: a multiple of 8; n_pages * page_tokens < 2^31 */
+  int32_t n_kv_heads, head_dim;   /* head_dim must be 128 */
+  int64_t page_stride, token_stride, head_stride; /* elements, multiples of 16 bytes; rows must not overlap */
+  int32_t dtype;                  /* SDVG_BF16, SDVG_F16 or SDVG_E4M3 (largest 448, no infinities); scales with SDVG_E4M3 only */
+} sdvg_paged_kv;
+
+/*
+ * Plan of one step: from c = cached[r] tokens in the cache and n = new_tokens[r] new ones of each of n_requests requests
+ *   q_start[0] = 0, q_start[r + 1] = q_start[r] + n        rows of request r among all new tokens
+ *   kv_lens[r] = c + n
+ *   block_table[r][j], held[r] <= j < ceil((c + n) / page_tokens): the next pages of free_pages, request by request
+ *                      in order, from place *next_free on; other entries stay as they are
+ *   positions[t] = c + i, slots[t] = page * page_tokens + position % page_tokens    of the new token t = q_start[r] + i
+ * A token without a page (free_pages ran out, the table is too narrow, the entry is negative) has slot -1; rows t
+ * behind the last token have slot -1 and position 0. held_out[r] is the number of pages the request holds now and
+ * *next_free_out = *next_free + all pages asked for: more than n_free says by how many they ran out.
+ * Negative lengths count as 0. New tokens past max_tokens have pages, but no row: q_start, kv_lens,
+ * positions and slots count them as not there.
+ *   held     device [n_requests], or NULL: every page a request needs is in its row of the table already, none is taken
+ *            (free_pages, next_free, held_out and next_free_out are then not used and may be NULL).
+ *   next_free device, one int32, or NULL (0). free_pages may be NULL with n_free == 0.
+ * Outputs must not overlap inputs or each other (SDVG_ERR_RANGE): the same call again gives the same answer. n_requests and
+ * max_tokens may be 0. One launch, asynchronous on `stream`.
+ */
+typedef struct {
+  int32_t n_requests, page_tokens; /* page_tokens: a multiple of 8 */
+  int32_t table_width;             /* entries per row of the table, >= 1 */
+  int32_t n_free;                  /* entries of free_pages */
+  int64_t table_stride;            /* elements between rows of the table, >= table_width */
+  int64_t max_tokens;              /* length of positions and slots, < 2^31 */
+  const int32_t *cached, *new_tokens, *free_pages, *held, *next_free;               /* device */
+  int32_t *block_table, *q_start, *kv_lens, *positions, *held_out, *next_free_out;  /* device */
+  int64_t *slots;                                                                   /* device */
+} sdvg_page_plan_args;
+int sdvg_page_plan(const sdvg_page_plan_args *args, void *stream);
 
 /*
  * Measurement aid (no passage of the paper: it exists so that a benchmark can report what the

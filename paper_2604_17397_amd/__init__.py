@@ -20,9 +20,13 @@ from .binding import (  # noqa: F401
     buffer_snapshot,
     worst_frame_route,
     worst_frame_route_batch,
+    PagePlan,
+    page_plan,
     probe_mfma,
     lib,
     status_string,
     SDVG_BF16,
     SDVG_F32,
+    SDVG_F16,
+    SDVG_E4M3,
 )

@@ -19,7 +19,7 @@ LIB_PATH = os.environ.get("SDVG_LIBRARY") or os.path.join(HERE, "libsdvg.so")
 
 NATIVE_PATH = os.path.join(HERE, "_native.so")
 
-SDVG_BF16, SDVG_F32 = 0, 1
+SDVG_BF16, SDVG_F32, SDVG_F16, SDVG_E4M3 = 0, 1, 2, 3
 SDVG_SPLIT_NEVER, SDVG_SPLIT_AUTO, SDVG_SPLIT_ALWAYS = 0, 1, 2
 _SPLIT = {"never": 0, "auto": 1, "always": 2}
 
@@ -47,6 +47,22 @@ class sdvg_attn_desc(ctypes.Structure):
                 ("kv_token_stride", ctypes.c_int64), ("kv_head_stride", ctypes.c_int64),
                 ("blk_token_stride", ctypes.c_int64), ("blk_head_stride", ctypes.c_int64),
                 ("scale", ctypes.c_float), ("dtype", ctypes.c_int32)]
+
+
+class sdvg_paged_kv(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class sdvg_page_plan_args(ctypes.Structure):
+    _fields_ = [("n_requests", ctypes.c_int32), ("page_tokens", ctypes.c_int32), ("table_width", ctypes.c_int32),
+                ("n_free", ctypes.c_int32), ("table_stride", ctypes.c_int64), ("max_tokens", ctypes.c_int64),
+                ("cached", ctypes.c_void_p), ("new_tokens", ctypes.c_void_p), ("free_pages", ctypes.c_void_p),
+                ("held", ctypes.c_void_p), ("next_free", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+                ("q_start", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("held_out", ctypes.c_void_p), ("next_free_out", ctypes.c_void_p), ("slots", ctypes.c_void_p)]
 
 
 _LIB = None
@@ -96,6 +112,8 @@ def lib():
         L.sdvg_avg_frame_route.argtypes = [vp, i32, f32, i32, ctypes.POINTER(f32), vp]
         L.sdvg_avg_frame_route_batch.restype = ctypes.c_int
         L.sdvg_avg_frame_route_batch.argtypes = [vp, i32, i32, f32, vp, i32, vp, vp, vp]
+        L.sdvg_page_plan.restype = ctypes.c_int
+        L.sdvg_page_plan.argtypes = [ctypes.POINTER(sdvg_page_plan_args), vp]
         L.sdvg_probe_mfma.restype = ctypes.c_int
         L.sdvg_probe_mfma.argtypes = [vp, i64, vp, i32, ctypes.POINTER(ctypes.c_double), vp]
         L.sdvg_probe_mfma_changing.restype = ctypes.c_int
@@ -493,6 +511,80 @@ def worst_frame_route_batch(frame_scores, tau, block_idx=None, first_block_idx=0
     if st != 0:
         raise SdvgError(st, "sdvg_worst_frame_route_batch")
     return dec, qb
+
+
+# ---- paged cache
+
+def _check_here(*tensors):
+    """Device tensors on the current device, which is the one that calls launch on."""
+    _check_dev(*tensors)
+    for t in tensors:
+        if t is not None and t.device.index != torch.cuda.current_device():
+            raise ValueError("all tensors live on the current device")
+
+
+class PagePlan:
+    """What page_plan computes, in device tensors of its own that every plan of up to this size may reuse: q_start
+    int32 [requests + 1], kv_lens and held int32 [requests], positions int32 and slots int64 [max_tokens], next_free
+    int32 [1] (held and next_free are written only by plans that take pages)."""
+
+    def __init__(self, n_requests, max_tokens, device="cuda"):
+        n_requests, max_tokens = int(n_requests), int(max_tokens)
+        if n_requests < 0 or max_tokens < 0:
+            raise ValueError("negative size")
+        ints = torch.zeros(3 * n_requests + 2 + max_tokens, dtype=torch.int32, device=device)
+        self.q_start, self.kv_lens, self.held, self.next_free, self.positions = ints.split(
+            [n_requests + 1, n_requests, n_requests, 1, max_tokens])
+        self.slots = torch.zeros(max_tokens, dtype=torch.int64, device=device)
+
+
+def _int_array(name, t, n, dtype=torch.int32):
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError("%s must be a dense %s tensor of %d elements" % (name, str(dtype)[6:], n))
+
+
+def page_plan(cached, new_tokens, block_table, page_tokens, free_pages=None, held=None, next_free=None, max_tokens=None,
+              out=None, stream=None):
+    """sdvg_page_plan: cached, new_tokens int32 [requests]; block_table int32 [requests, pages] (written in place);
+    held int32 [requests], free_pages int32 [n] and next_free int32 [1] say which pages may be taken (held=None: none is).
+    `out`: a PagePlan for as many requests (its positions and slots hold the new tokens), or None for a new one
+    of `max_tokens` tokens. Returns the PagePlan."""
+    if out is None:
+        if max_tokens is None:
+            raise ValueError("page_plan needs max_tokens or out")
+        out = PagePlan(cached.shape[0], max_tokens, cached.device)
+    elif max_tokens is not None and max_tokens != out.slots.shape[0]:
+        raise ValueError("out holds another number of tokens than max_tokens")
+    n = cached.shape[0]
+    _check_here(cached, new_tokens, block_table, free_pages, held, next_free, out.q_start, out.slots)
+    _int_array("cached", cached, n)
+    _int_array("new_tokens", new_tokens, n)
+    _int_array("out.kv_lens", out.kv_lens, n)
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or block_table.shape[0] != n or (
+            block_table.shape[1] > 1 and block_table.stride(1) != 1):
+        raise ValueError("block_table must be int32 [requests, pages] with unit stride along the pages")
+    if held is None and (free_pages is not None or next_free is not None):
+        raise ValueError("free_pages and next_free come with held")
+    if held is not None:
+        _int_array("held", held, n)
+    if free_pages is not None:
+        _int_array("free_pages", free_pages, free_pages.shape[0])
+    if next_free is not None:
+        _int_array("next_free", next_free, 1)
+
+    def p(t):
+        return None if t is None or t.numel() == 0 else t.data_ptr()
+    a = sdvg_page_plan_args(n, int(page_tokens), block_table.shape[1], 0 if free_pages is None else free_pages.shape[0],
+                            block_table.stride(0) if n > 1 else block_table.shape[1], out.slots.shape[0],
+                            p(cached), p(new_tokens), p(free_pages),
+                            # (without requests an empty `held` has no address, and still says that pages may be taken)
+                            None if held is None else p(held) or p(out.q_start),
+                            p(next_free), p(block_table), p(out.q_start), p(out.kv_lens), p(out.positions), p(out.held),
+                            p(out.next_free), p(out.slots))
+    st = lib().sdvg_page_plan(ctypes.byref(a), _stream_ptr(stream))
+    if st != 0:
+        raise SdvgError(st, "sdvg_page_plan")
+    return out
 
 
 def probe_mfma(iters=20000, stream=None, changing=False):
