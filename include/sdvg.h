@@ -350,6 +350,55 @@ typedef struct {
 int sdvg_page_plan(const sdvg_page_plan_args *args, void *stream);
 
 /*
+ * Rotary embedding by positions. For pair p < rotary_dim / 2 of every row's vector, at angle = position * freqs[p],
+ *     (a, b) -> (a c - b s, a s + b c),   c = gain * cos(angle), s = gain * sin(angle),
+ * where (a, b) are elements (p, p + rotary_dim / 2) in SDVG_ROPE_HALF and (2p, 2p + 1) in SDVG_ROPE_INTERLEAVED; elements from
+ * rotary_dim on are copied. The angle is a product in 64 bits taken modulo one turn before anything is rounded to
+ * 32, so positions up to 2^31 keep full accuracy; the rest is fp32, the result rounded once. Scaling for contexts
+ * longer than the original one is in freqs and gain (the Python package's rope_frequencies makes them).
+ *   positions device int32 [n_tokens], 4-byte aligned, of either sign; freqs device double [rotary_dim / 2], 8-byte aligned,
+ *   in radians per position. rotary_dim: a multiple of 16, at most 128.
+ */
+enum { SDVG_ROPE_INTERLEAVED = 0, SDVG_ROPE_HALF = 1 };
+typedef struct {
+  const int32_t *positions; /* device */
+  const double *freqs;      /* device */
+  int32_t rotary_dim, layout;
+  float gain;               /* finite */
+} sdvg_rope_desc;
+
+/* Rows [n_tokens][n_heads][128] that are read at in and written at out (which may be in itself, with the same strides;
+ * otherwise they must not overlap). 16-byte aligned; strides in elements, multiples of 16 bytes, those of dimensions of size 1
+ * are not looked at. */
+typedef struct {
+  const void *in; /* device */
+  void *out;      /* device */
+  int32_t n_heads;
+  int64_t in_token_stride, in_head_stride, out_token_stride, out_head_stride;
+} sdvg_rows;
+
+/*
+ * Rotates x and, in the same launch, y (nullable: e.g. q and k of a layer), both of n_tokens tokens and of type `dtype`
+ * (SDVG_BF16, SDVG_F16, SDVG_F32). n_tokens < 2^26; 0 is a no-op. Asynchronous on `stream`.
+ */
+int sdvg_rope_positions(const sdvg_rope_desc *rope, const sdvg_rows *x, const sdvg_rows *y, int64_t n_tokens,
+                        int32_t head_dim, int32_t dtype, void *stream);
+
+/*
+ * Commit into the paged cache: k->in and v->in, rows [n_tokens][n_kv_heads][128] of type `dtype` (SDVG_BF16 or SDVG_F16; the
+ * cache's own type unless that is SDVG_E4M3), go to slots[t] = page * page_tokens + place in the page. Rows whose slot is
+ * negative or past the pools are not written. Slots that are written must differ (two rows of one slot: either may win, in parts).
+ *   rope      nullable. K is rotated on its way (v is not); a 16-bit cache then holds what sdvg_rope_positions would give.
+ *   q         nullable, needs rope: rows that are rotated to q->out in the same launch.
+ *   SDVG_E4M3: stored = round(x / scale), clamped to +-448 first (NaN stays NaN); x is not rounded to `dtype` after
+ *             the rotation.
+ * k->out and v->out are not looked at. The sources must not overlap the pools (SDVG_ERR_RANGE). n_tokens < 2^26; 0 is a no-op.
+ * Asynchronous on `stream`.
+ */
+int sdvg_paged_commit(const sdvg_paged_kv *cache, const sdvg_rows *k, const sdvg_rows *v, const int64_t *slots,
+                      int64_t n_tokens, int32_t dtype, const sdvg_rope_desc *rope, const sdvg_rows *q, void *stream);
+
+/*
  * Measurement aid (no passage of the paper: it exists so that a benchmark can report what the
  * matrix cores of the chip it runs on deliver, next to the attention kernel's rate). Launches
  * 256 workgroups of 4 waves (one wave per SIMD of the chip); every wave issues iters x 16 v_mfma_f32_32x32x16_bf16 from

@@ -22,6 +22,10 @@ from .binding import (  # noqa: F401
     worst_frame_route_batch,
     PagePlan,
     page_plan,
+    rope_frequencies,
+    rope_positions,
+    PagedKV,
+    paged_commit,
     probe_mfma,
     lib,
     status_string,

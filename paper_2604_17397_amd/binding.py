@@ -7,6 +7,7 @@ leaves every call it does not recognise as valid to the Python code here, which 
 """
 import ctypes
 import importlib.util
+import math
 import os
 import warnings
 
@@ -21,6 +22,8 @@ NATIVE_PATH = os.path.join(HERE, "_native.so")
 
 SDVG_BF16, SDVG_F32, SDVG_F16, SDVG_E4M3 = 0, 1, 2, 3
 SDVG_SPLIT_NEVER, SDVG_SPLIT_AUTO, SDVG_SPLIT_ALWAYS = 0, 1, 2
+SDVG_ROPE_INTERLEAVED, SDVG_ROPE_HALF = 0, 1
+_LAYOUT = {"interleaved": 0, "half": 1}
 _SPLIT = {"never": 0, "auto": 1, "always": 2}
 
 
@@ -54,6 +57,17 @@ class sdvg_paged_kv(ctypes.Structure):
                 ("n_pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
                 ("head_stride", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+class sdvg_rope_desc(ctypes.Structure):
+    _fields_ = [("positions", ctypes.c_void_p), ("freqs", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("gain", ctypes.c_float)]
+
+
+class sdvg_rows(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n_heads", ctypes.c_int32),
+                ("in_token_stride", ctypes.c_int64), ("in_head_stride", ctypes.c_int64),
+                ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64)]
 
 
 class sdvg_page_plan_args(ctypes.Structure):
@@ -114,6 +128,11 @@ def lib():
         L.sdvg_avg_frame_route_batch.argtypes = [vp, i32, i32, f32, vp, i32, vp, vp, vp]
         L.sdvg_page_plan.restype = ctypes.c_int
         L.sdvg_page_plan.argtypes = [ctypes.POINTER(sdvg_page_plan_args), vp]
+        rd, rows = ctypes.POINTER(sdvg_rope_desc), ctypes.POINTER(sdvg_rows)
+        L.sdvg_rope_positions.restype = ctypes.c_int
+        L.sdvg_rope_positions.argtypes = [rd, rows, rows, i64, i32, i32, vp]
+        L.sdvg_paged_commit.restype = ctypes.c_int
+        L.sdvg_paged_commit.argtypes = [ctypes.POINTER(sdvg_paged_kv), rows, rows, vp, i64, i32, rd, rows, vp]
         L.sdvg_probe_mfma.restype = ctypes.c_int
         L.sdvg_probe_mfma.argtypes = [vp, i64, vp, i32, ctypes.POINTER(ctypes.c_double), vp]
         L.sdvg_probe_mfma_changing.restype = ctypes.c_int
@@ -585,6 +604,142 @@ def page_plan(cached, new_tokens, block_table, page_tokens, free_pages=None, hel
     if st != 0:
         raise SdvgError(st, "sdvg_page_plan")
     return out
+
+
+def rope_frequencies(rotary_dim, theta=10000.0, scaling="none", factor=1.0, original=None, beta_fast=32.0, beta_slow=1.0,
+                     device="cuda"):
+    """(freqs, gain) for rope_positions and paged_commit: radians per position of every pair, theta^(-2p / rotary_dim), as
+    float64 [rotary_dim / 2], and the factor of cos and sin. For contexts `factor` times the original length:
+    "linear" divides every frequency by factor; "ntk" takes theta * factor^(rotary_dim / (rotary_dim - 2)), which leaves
+    the fastest pair alone and divides the slowest by factor; "yarn" (Peng et al., 2023) interpolates pairs that turn at
+    most beta_slow times over `original` positions, leaves those that turn at least beta_fast times, mixes in between, and
+    has gain 0.1 ln(factor) + 1."""
+    rotary_dim, theta, factor = int(rotary_dim), float(theta), float(factor)
+    if rotary_dim < 16 or rotary_dim > 128 or rotary_dim % 16:
+        raise ValueError("rotary_dim must be a multiple of 16, at most 128")
+    if not (0 < theta < math.inf and 1 <= factor < math.inf):
+        raise ValueError("theta must be positive and factor at least 1")
+    if scaling not in ("none", "linear", "ntk", "yarn"):
+        raise ValueError("scaling must be none, linear, ntk or yarn")
+    p = torch.arange(0, rotary_dim, 2, dtype=torch.float64)
+    if scaling == "ntk":
+        theta *= factor ** (rotary_dim / (rotary_dim - 2))
+    w = theta ** (-p / rotary_dim)
+    gain = 1.0
+    if scaling == "linear":
+        w = w / factor
+    elif scaling == "yarn":
+        if original is None or not original > 0 or not 0 <= beta_slow < beta_fast:
+            raise ValueError("yarn needs the original length and 0 <= beta_slow < beta_fast")
+        keep = ((original * w / (2 * math.pi) - beta_slow) / (beta_fast - beta_slow)).clamp(0, 1)
+        w = w * keep + w / factor * (1 - keep)
+        gain = 0.1 * math.log(factor) + 1.0
+    return w.to(device), gain
+
+
+_ROW_TYPES = {torch.bfloat16: SDVG_BF16, torch.float32: SDVG_F32, torch.float16: SDVG_F16}
+
+
+def _rope_desc(positions, freqs, layout, gain, n_tokens):
+    _check_here(positions, freqs)
+    _int_array("positions", positions, n_tokens)
+    if freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
+        raise ValueError("freqs must be a dense float64 tensor [rotary_dim / 2]")
+    if layout not in _LAYOUT:
+        raise ValueError("layout must be half or interleaved")
+    return sdvg_rope_desc(positions.data_ptr(), freqs.data_ptr(), 2 * freqs.shape[0], _LAYOUT[layout], float(gain))
+
+
+def _check_rows(name, t, like=None):
+    if t.dim() != 3 or t.shape[2] != 128 or t.stride(2) != 1 or t.dtype not in _ROW_TYPES:
+        raise ValueError("%s must be [tokens, heads, 128] of 16 or 32 bit floats with unit dim stride" % name)
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
+        raise ValueError("%s must match its input" % name)
+
+
+def _rows(t, out):
+    return sdvg_rows(t.data_ptr(), None if out is None else out.data_ptr(), t.shape[1], t.stride(0), t.stride(1),
+                     0 if out is None else out.stride(0), 0 if out is None else out.stride(1))
+
+
+def rope_positions(x, positions, freqs, y=None, layout="half", gain=1.0, out=None, y_out=None, stream=None):
+    """sdvg_rope_positions: rotary embedding of x [tokens, heads, 128], and of y (as many tokens and the same dtype, any
+    number of heads) in the same launch, at int32 positions [tokens] with float64 freqs [rotary_dim / 2] (rope_frequencies).
+    layout "half" pairs elements p and p + rotary_dim / 2, "interleaved" 2p and 2p + 1. out / y_out default to new tensors;
+    pass the input for in place. Returns out, or (out, y_out) with y."""
+    _check_here(x, y, out, y_out)
+    _check_rows("x", x)
+    if y is None and y_out is not None:
+        raise ValueError("y_out comes with y")
+    if y is not None:
+        _check_rows("y", y)
+        if y.dtype != x.dtype or y.shape[0] != x.shape[0]:
+            raise ValueError("y must have x's tokens and dtype")
+    rope = _rope_desc(positions, freqs, layout, gain, x.shape[0])
+    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    _check_rows("out", out, x)
+    if y is not None:
+        y_out = torch.empty(y.shape, dtype=y.dtype, device=y.device) if y_out is None else y_out
+        _check_rows("y_out", y_out, y)
+    st = lib().sdvg_rope_positions(ctypes.byref(rope), ctypes.byref(_rows(x, out)),
+                                   None if y is None else ctypes.byref(_rows(y, y_out)), x.shape[0], 128,
+                                   _ROW_TYPES[x.dtype], _stream_ptr(stream))
+    if st != 0:
+        raise SdvgError(st, "sdvg_rope_positions")
+    return out if y is None else (out, y_out)
+
+
+class PagedKV:
+    """Caller-owned paged KV cache of one layer: k, v device tensors [pages, page_tokens, kv_heads, 128] (any page / token /
+    head strides, unit dim stride) of bfloat16, float16 or float8_e4m3fn; the latter with optional float32 scales
+    [kv_heads] (a stored number x stands for x * scale)."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        _check_dev(k, v, k_scale, v_scale)
+        types = {torch.bfloat16: SDVG_BF16, torch.float16: SDVG_F16, torch.float8_e4m3fn: SDVG_E4M3}
+        if k.dtype not in types or v.dtype != k.dtype:
+            raise TypeError("k and v must both be bfloat16, float16 or float8_e4m3fn")
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1 or v.device != k.device:
+            raise ValueError("k and v must be [pages, page_tokens, kv_heads, 128] with the same strides and unit dim stride")
+        for t in (k_scale, v_scale):
+            if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (k.shape[2],) or not t.is_contiguous()
+                                  or t.device != k.device):
+                raise ValueError("k_scale and v_scale must be dense float32 [kv_heads] on the cache's device")
+            if t is not None and k.dtype != torch.float8_e4m3fn:
+                raise ValueError("scales come with a float8 cache")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.c = sdvg_paged_kv(k.data_ptr(), v.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
+                               None if v_scale is None else v_scale.data_ptr(), k.shape[0], k.shape[1], k.shape[2], k.shape[3],
+                               k.stride(0), k.stride(1), k.stride(2), types[k.dtype])
+
+
+def paged_commit(cache, k, v, slots, positions=None, freqs=None, q=None, q_out=None, layout="half", gain=1.0, stream=None):
+    """sdvg_paged_commit: rows k, v [tokens, kv_heads, 128] of bfloat16 or float16 into the int64 slots [tokens] of a PagedKV;
+    a negative slot writes nothing. With positions and freqs (as for rope_positions) K is rotated on its way, and so is
+    q [tokens, heads, 128] into q_out (default: a new tensor; pass q for in place). Returns q_out, or None without q."""
+    _check_here(cache.k, k, v, slots, q, q_out)
+    for name, t in (("k", k), ("v", v)):
+        _check_rows(name, t)
+        if t.shape[1] != cache.c.n_kv_heads or t.shape[0] != k.shape[0] or t.dtype != k.dtype:
+            raise ValueError("k and v must have the cache's heads, the same tokens and dtype")
+    if k.dtype == torch.float32 or (cache.k.dtype != torch.float8_e4m3fn and cache.k.dtype != k.dtype):
+        raise ValueError("k and v must be bfloat16 or float16, of the cache's own dtype unless that is float8")
+    _int_array("slots", slots, k.shape[0], torch.int64)
+    if (positions is None) != (freqs is None) or (q is not None and positions is None) or (q is None and q_out is not None):
+        raise ValueError("positions and freqs come together, q with both, q_out with q")
+    rope = None if positions is None else _rope_desc(positions, freqs, layout, gain, k.shape[0])
+    if q is not None:
+        _check_rows("q", q)
+        if q.dtype != k.dtype or q.shape[0] != k.shape[0]:
+            raise ValueError("q must have k's tokens and dtype")
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+        _check_rows("q_out", q_out, q)
+    st = lib().sdvg_paged_commit(ctypes.byref(cache.c), ctypes.byref(_rows(k, None)), ctypes.byref(_rows(v, None)),
+                                 _ptr(slots), k.shape[0], _ROW_TYPES[k.dtype], None if rope is None else ctypes.byref(rope),
+                                 None if q is None else ctypes.byref(_rows(q, q_out)), _stream_ptr(stream))
+    if st != 0:
+        raise SdvgError(st, "sdvg_paged_commit")
+    return q_out
 
 
 def probe_mfma(iters=20000, stream=None, changing=False):

@@ -59,3 +59,127 @@ def test_page_plan_binding_checks(b, monkeypatch):
             b.page_plan(**a)
     with pytest.raises(ValueError):
         b.PagePlan(-1, 4, device="cpu")
+
+
+def rope_desc(b, **kw):
+    d = b.sdvg_rope_desc(positions=FAKE, freqs=FAKE, rotary_dim=64, layout=1, gain=1.0)
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return d
+
+
+def rows(b, **kw):
+    r = b.sdvg_rows(in_=FAKE, out=FAKE + (1 << 20), n_heads=2, in_token_stride=256, in_head_stride=128, out_token_stride=256,
+                    out_head_stride=128)
+    for k, v in kw.items():
+        setattr(r, k, v)
+    return r
+
+
+ROPE_BAD = [(dict(positions=None), -1), (dict(freqs=None), -1), (dict(rotary_dim=0), -2), (dict(rotary_dim=144), -2),
+            (dict(rotary_dim=24), -4), (dict(layout=2), -5), (dict(gain=float("inf")), -3), (dict(gain=float("nan")), -3),
+            (dict(positions=FAKE + 2), -4), (dict(freqs=FAKE + 4), -4)]
+ROWS_BAD = [(dict(in_=None), -1), (dict(n_heads=0), -2), (dict(in_token_stride=127), -2), (dict(in_token_stride=260), -4),
+            (dict(in_head_stride=1 << 41), -5), (dict(in_=FAKE + 8), -4)]
+OUT_BAD = [(dict(out=None), -1), (dict(out_head_stride=0), -2), (dict(out_token_stride=132), -4), (dict(out=FAKE + (1 << 20) + 2), -4),
+           (dict(out=FAKE, out_token_stride=512), -3)]
+
+
+def test_rope_positions_rejects_bad_arguments(b):
+    ref = ctypes.byref
+
+    def call(rope=None, x=None, y=None, n=4, d=128, dtype=0):
+        return b.lib().sdvg_rope_positions(ref(rope or rope_desc(b)), ref(x or rows(b)), y and ref(y), n, d, dtype, None)
+    for kw, want in ROPE_BAD:
+        assert call(rope=rope_desc(b, **kw)) == want, kw
+    for kw, want in ROWS_BAD + OUT_BAD:
+        assert call(x=rows(b, **kw)) == want, kw
+        assert call(y=rows(b, **kw)) == want, kw
+    assert call(n=-1) == -2 and call(d=64) == -5 and call(dtype=3) == -5 and call(dtype=9) == -5 and call(n=1 << 26) == -5
+    assert call(n=0) == 0 and call(n=0, x=rows(b, in_=None, out=None)) == 0
+    assert b.lib().sdvg_rope_positions(None, ref(rows(b)), None, 4, 128, 0, None) == -1
+    assert b.lib().sdvg_rope_positions(ref(rope_desc(b)), None, None, 4, 128, 0, None) == -1
+
+
+def paged_kv(b, **kw):
+    c = b.sdvg_paged_kv(k=FAKE << 4, v=FAKE << 5, n_pages=4, page_tokens=8, n_kv_heads=2, head_dim=128,
+                        page_stride=8 * 256, token_stride=256, head_stride=128, dtype=0)
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+PAGED_BAD = [(dict(k=None), -1), (dict(v=None), -1), (dict(head_dim=64), -5), (dict(dtype=1), -5), (dict(dtype=7), -5),
+             (dict(k_scale=FAKE), -5), (dict(n_pages=0), -2), (dict(page_tokens=0), -2), (dict(page_tokens=12), -4),
+             (dict(n_kv_heads=0), -2), (dict(n_pages=1 << 28), -5), (dict(k=FAKE + 8), -4), (dict(token_stride=260), -4),
+             (dict(token_stride=128), -2), (dict(page_stride=7 * 256), -2), (dict(head_stride=64), -2),
+             (dict(head_stride=7 * 128, token_stride=128), -2),          # head-major, a head too short for its tokens
+             (dict(dtype=3, k_scale=FAKE + 2), -4)]
+
+
+def test_paged_commit_rejects_bad_arguments(b):
+    ref = ctypes.byref
+
+    def call(c=None, k=None, v=None, slots=FAKE, n=4, dtype=0, rope=None, q=None):
+        return b.lib().sdvg_paged_commit(ref(c or paged_kv(b)), ref(k or rows(b)), ref(v or rows(b)), slots, n, dtype,
+                                         rope and ref(rope), q and ref(q), None)
+    for kw, want in PAGED_BAD:
+        assert call(c=paged_kv(b, **kw)) == want, kw
+    for kw, want in ROWS_BAD:
+        want = -2 if "n_heads" in kw else want
+        assert call(k=rows(b, **kw)) == want and call(v=rows(b, **kw)) == want, kw
+    for kw, want in ROPE_BAD:
+        assert call(rope=rope_desc(b, **kw)) == want, kw
+    for kw, want in ROWS_BAD + OUT_BAD:
+        assert call(rope=rope_desc(b), q=rows(b, **kw)) == want, kw
+    assert call(q=rows(b)) == -1                                        # q without a rotation
+    assert call(slots=None) == -1 and call(slots=FAKE + 4) == -4 and call(n=-1) == -2 and call(n=1 << 26) == -5
+    assert call(dtype=1) == -5 and call(dtype=2) == -5                  # fp32 rows; half rows into a bfloat16 cache
+    assert call(k=rows(b, n_heads=3)) == -2
+    assert call(v=rows(b, in_=(FAKE << 4) + 4096)) == -3                # v inside the pool of k
+    assert call(n=0, slots=None) == 0
+
+
+def test_paged_binding_checks(b, monkeypatch):
+    for name in ("_check_here", "_check_dev"):
+        monkeypatch.setattr(b, name, lambda *a: None)
+    monkeypatch.setattr(b, "_LIB", type("Trap", (), {"__getattr__": lambda s, n: pytest.fail("the C library must not be reached")})())
+    x = torch.zeros((4, 2, 128), dtype=torch.bfloat16)
+    pos, freqs = torch.zeros(4, dtype=torch.int32), torch.zeros(32, dtype=torch.float64)
+    for kw in [dict(x=x.double()), dict(x=x[..., :64]), dict(x=x[0]), dict(positions=pos[:3]), dict(positions=pos.long()),
+               dict(freqs=freqs.float()), dict(layout="both"), dict(out=x[:3]), dict(out=x.half()), dict(y=x[:2]), dict(y=x.half()),
+               dict(y_out=x), dict(y=x, y_out=x[:, :1])]:
+        with pytest.raises(ValueError):
+            b.rope_positions(**{**dict(x=x, positions=pos, freqs=freqs), **kw})
+    pool = torch.zeros((3, 8, 2, 128), dtype=torch.bfloat16)
+    with pytest.raises(TypeError):
+        b.PagedKV(pool.float(), pool.float())
+    for args in [(pool, pool[:2]), (pool[0], pool[0]), (pool, pool, torch.ones(2)), (pool.to(torch.float8_e4m3fn),) * 2 + (torch.ones(3),)]:
+        with pytest.raises(ValueError):
+            b.PagedKV(*args)
+    c = b.PagedKV(pool, pool)
+    slots = torch.zeros(4, dtype=torch.int64)
+    for kw in [dict(k=x[:, :1]), dict(k=x.half(), v=x.half()), dict(v=x[:3]), dict(slots=slots[:2]), dict(slots=slots.int()),
+               dict(positions=pos), dict(freqs=freqs), dict(q=x), dict(q_out=x), dict(positions=pos, freqs=freqs, q=x[:2]),
+               dict(positions=pos, freqs=freqs, q=x, q_out=x.half())]:
+        with pytest.raises(ValueError):
+            b.paged_commit(**{**dict(cache=c, k=x, v=x, slots=slots), **kw})
+
+
+def test_rope_frequencies(b):
+    import math
+    w, gain = b.rope_frequencies(64, theta=1e4, device="cpu")
+    assert w.dtype == torch.float64 and gain == 1.0 and torch.allclose(w, 1e4 ** (-torch.arange(32).double() / 32), rtol=1e-14)
+    assert torch.equal(b.rope_frequencies(64, scaling="linear", factor=4, device="cpu")[0], w / 4)
+    ntk, _ = b.rope_frequencies(64, scaling="ntk", factor=4, device="cpu")
+    assert ntk[0] == w[0] and abs(ntk[-1] / w[-1] * 4 - 1) < 1e-12 and (ntk[1:] < w[1:]).all() and (ntk > w / 4 - 1e-18).all()
+    yarn, gain = b.rope_frequencies(64, scaling="yarn", factor=4, original=2048, device="cpu")
+    turns = 2048 * w / (2 * math.pi)
+    assert torch.equal(yarn[turns >= 32], w[turns >= 32]) and torch.equal(yarn[turns <= 1], w[turns <= 1] / 4)
+    mid = (turns > 1) & (turns < 32)
+    assert mid.any() and ((yarn < w) & (yarn > w / 4))[mid].all() and abs(gain - (0.1 * math.log(4) + 1)) < 1e-15
+    for bad in [dict(rotary_dim=24), dict(rotary_dim=0), dict(rotary_dim=160), dict(rotary_dim=64, theta=0), dict(rotary_dim=64, factor=0.5),
+                dict(rotary_dim=64, scaling="other"), dict(rotary_dim=64, scaling="yarn"),
+                dict(rotary_dim=64, scaling="yarn", original=100, beta_fast=1, beta_slow=1)]:
+        with pytest.raises(ValueError):
+            b.rope_frequencies(device="cpu", **bad)
