@@ -399,6 +399,41 @@ int sdvg_paged_commit(const sdvg_paged_kv *cache, const sdvg_rows *k, const sdvg
                       int64_t n_tokens, int32_t dtype, const sdvg_rope_desc *rope, const sdvg_rows *q, void *stream);
 
 /*
+ * Attention of the new tokens of every request over its pages. New token i of the n = q_start[r + 1] - q_start[r] tokens of
+ * request r has position kv_lens[r] - n + i and sees the keys of its request at positions up to its own, with
+ * window > 0 only the last `window` of them; its own K and V are in the cache already (sdvg_paged_commit). Query head h
+ * belongs to key head h / (n_heads / n_kv_heads):
+ *     out[t,h,:] = sum_j p_j V[j,:],  p = softmax_j(scale * q[t,h,:] . K[j,:]),  lse[t,h] = log sum_j exp(scale * q . K[j]).
+ *   desc      host. dtype SDVG_BF16 or SDVG_F16 of q and out; the cache's own type unless that is SDVG_E4M3.
+ *   q, out    device [n_tokens][n_heads][128]; out may be q itself (same strides). lse device float, dense
+ *             [n_tokens][n_heads], nullable. Rows from q_start[n_requests] on, and below q_start[0], are left as they are.
+ *   block_table  device int32 [n_requests][table_width]; q_start device int32 [n_requests + 1], not decreasing;
+ *             kv_lens device int32 [n_requests], kv_lens[r] >= n: all as sdvg_page_plan leaves them.
+ *             Keys on a page whose number is negative or not below n_pages, or past the table, count as not there. A row without any key gets
+ *             out = 0 and lse = -infinity. Numbers out of range in q_start and kv_lens are clamped.
+ *   workspace device, nullable, 16-byte aligned: with at least sdvg_paged_attn_workspace_bytes(desc, cache) bytes the keys of long
+ *             requests are split over workgroups and the pieces joined by a second small launch; without, every
+ *             request's keys are one workgroup's per key head and tile of rows. Scratch: overlapping calls need their own.
+ *   Arithmetic: products on the matrix cores with fp32 accumulation, fp32 softmax statistics and sums; probabilities are
+ *   rounded to `dtype` before the product with V (their sum is not, so that lse has 32 bits), e4m3 numbers are exact in it. What
+ *   lies in the cache behind a request's last key may be anything; keys that any row of a request sees must be finite.
+ *   Made for few new tokens per request (1 .. some 16); longer ones are right, but read the keys once per 64 rows.
+ * scale as in sdvg_attn_desc. n_requests and n_tokens may be 0 (no-op). Asynchronous on `stream`; launches kernels only.
+ */
+typedef struct {
+  int32_t n_requests, n_tokens, n_heads, head_dim; /* n_heads: a multiple of the cache's; head_dim must be 128 */
+  int32_t table_width, window;                     /* window: 0 = none */
+  int64_t table_stride;                            /* elements */
+  int64_t q_token_stride, q_head_stride, o_token_stride, o_head_stride;
+  float scale;
+  int32_t dtype;
+} sdvg_paged_attn_desc;
+int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_paged_kv *cache, const void *q, const int32_t *block_table,
+                    const int32_t *q_start, const int32_t *kv_lens, void *out, float *lse, void *workspace,
+                    int64_t workspace_bytes, void *stream);
+int64_t sdvg_paged_attn_workspace_bytes(const sdvg_paged_attn_desc *desc, const sdvg_paged_kv *cache);
+
+/*
  * Measurement aid (no passage of the paper: it exists so that a benchmark can report what the
  * matrix cores of the chip it runs on deliver, next to the attention kernel's rate). Launches
  * 256 workgroups of 4 waves (one wave per SIMD of the chip); every wave issues iters x 16 v_mfma_f32_32x32x16_bf16 from

@@ -26,6 +26,8 @@ from .binding import (  # noqa: F401
     rope_positions,
     PagedKV,
     paged_commit,
+    paged_attn,
+    paged_attn_workspace_bytes,
     probe_mfma,
     lib,
     status_string,

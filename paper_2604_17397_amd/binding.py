@@ -70,6 +70,14 @@ class sdvg_rows(ctypes.Structure):
                 ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64)]
 
 
+class sdvg_paged_attn_desc(ctypes.Structure):
+    _fields_ = [("n_requests", ctypes.c_int32), ("n_tokens", ctypes.c_int32), ("n_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("table_width", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("table_stride", ctypes.c_int64), ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+                ("o_token_stride", ctypes.c_int64), ("o_head_stride", ctypes.c_int64), ("scale", ctypes.c_float),
+                ("dtype", ctypes.c_int32)]
+
+
 class sdvg_page_plan_args(ctypes.Structure):
     _fields_ = [("n_requests", ctypes.c_int32), ("page_tokens", ctypes.c_int32), ("table_width", ctypes.c_int32),
                 ("n_free", ctypes.c_int32), ("table_stride", ctypes.c_int64), ("max_tokens", ctypes.c_int64),
@@ -133,6 +141,11 @@ def lib():
         L.sdvg_rope_positions.argtypes = [rd, rows, rows, i64, i32, i32, vp]
         L.sdvg_paged_commit.restype = ctypes.c_int
         L.sdvg_paged_commit.argtypes = [ctypes.POINTER(sdvg_paged_kv), rows, rows, vp, i64, i32, rd, rows, vp]
+        pa, pc = ctypes.POINTER(sdvg_paged_attn_desc), ctypes.POINTER(sdvg_paged_kv)
+        L.sdvg_paged_attn.restype = ctypes.c_int
+        L.sdvg_paged_attn.argtypes = [pa, pc, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.sdvg_paged_attn_workspace_bytes.restype = ctypes.c_int64
+        L.sdvg_paged_attn_workspace_bytes.argtypes = [pa, pc]
         L.sdvg_probe_mfma.restype = ctypes.c_int
         L.sdvg_probe_mfma.argtypes = [vp, i64, vp, i32, ctypes.POINTER(ctypes.c_double), vp]
         L.sdvg_probe_mfma_changing.restype = ctypes.c_int
@@ -740,6 +753,53 @@ def paged_commit(cache, k, v, slots, positions=None, freqs=None, q=None, q_out=N
     if st != 0:
         raise SdvgError(st, "sdvg_paged_commit")
     return q_out
+
+
+def _paged_attn_desc(q, cache, block_table, out, scale, window):
+    _check_rows("q", q)
+    if q.dtype == torch.float32 or (cache.k.dtype != torch.float8_e4m3fn and cache.k.dtype != q.dtype):
+        raise ValueError("q must be bfloat16 or float16, of the cache's dtype unless that is float8")
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+        raise ValueError("block_table must be int32 [requests, pages] with unit stride along the pages")
+    _check_rows("out", out, q)
+    n = block_table.shape[0]
+    return sdvg_paged_attn_desc(n, q.shape[0], q.shape[1], q.shape[2], block_table.shape[1], int(window),
+                                block_table.stride(0), q.stride(0), q.stride(1), out.stride(0), out.stride(1),
+                                0.0 if scale is None else float(scale), _ROW_TYPES[q.dtype])
+
+
+def paged_attn_workspace_bytes(q, cache, block_table):
+    """sdvg_paged_attn_workspace_bytes for the shapes of these tensors."""
+    _check_here(q, cache.k, block_table)
+    d = _paged_attn_desc(q, cache, block_table, q, None, 0)
+    n = lib().sdvg_paged_attn_workspace_bytes(ctypes.byref(d), ctypes.byref(cache.c))
+    if n < 0:
+        raise SdvgError(n, "sdvg_paged_attn_workspace_bytes")
+    return int(n)
+
+
+def paged_attn(q, cache, block_table, q_start, kv_lens, out=None, lse=None, scale=None, window=0, workspace=None, stream=None):
+    """sdvg_paged_attn: attention of the new tokens q [tokens, heads, 128] of several requests over their pages in a PagedKV.
+    block_table int32 [requests, pages], q_start int32 [requests + 1] and kv_lens int32 [requests] as page_plan leaves
+    them. `window` > 0: every token sees the last `window` keys only. `lse`: optional float32 [tokens, heads] for the log of the sums.
+    `workspace`: optional device tensor of paged_attn_workspace_bytes, with which the keys of long requests are split
+    over the chip. `scale=None` is 1/sqrt(128). out defaults to a new tensor; pass out=q for in place. Returns out."""
+    _check_here(q, cache.k, block_table, q_start, kv_lens, out, lse, workspace)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    d = _paged_attn_desc(q, cache, block_table, out, scale, window)
+    _int_array("q_start", q_start, d.n_requests + 1)
+    _int_array("kv_lens", kv_lens, d.n_requests)
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous()):
+        raise ValueError("lse must be dense float32 [tokens, heads]")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    st = lib().sdvg_paged_attn(ctypes.byref(d), ctypes.byref(cache.c), _ptr(q), _ptr(block_table), _ptr(q_start), _ptr(kv_lens),
+                               _ptr(out), _ptr(lse), _ptr(workspace),
+                               0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+    if st != 0:
+        raise SdvgError(st, "sdvg_paged_attn")
+    return out
 
 
 def probe_mfma(iters=20000, stream=None, changing=False):

@@ -1,0 +1,552 @@
+// Attention of a few new tokens per request over a paged cache (one decoding or verification step), with the keys of
+// long requests split over workgroups and joined.
+//
+// What bounds it: every cached row of K and V is read once, 512 bytes per key and head in 16 bits, for 4 x 128 FLOP per
+// query row; up to some hundred rows per key head the time is the HBM's. So there is no staging through LDS: the matrix
+// instructions take both K and V straight from registers as they come from memory.
+//
+// A wave takes 32 keys per step, the 16 (NT tiles of 16) query rows of a request that share a key head as columns:
+//   S^T = K Q^T with v_mfma_f32_16x16x32: lane l holds 8 consecutive dims of key row l % 16, one 16-byte load. The
+//     key rows of the two 16-row products are dealt out so that lane l's 8 scores (rows 4 (l / 16) .. + 3 of both) belong to
+//     the keys 8 (l / 16) .. + 7 of the step, in order, and to query row l % 16.
+//   O^T = V^T P^T: that is the B operand of this product as it is (8 consecutive keys of column l % 16): P never
+//     moves between lanes. The A operand wants 8 consecutive keys of one dim per lane, and memory has 8 consecutive dims of one key:
+//     lane l loads dims 8 (l % 16) .. + 7 of its 8 keys (a row of 256 bytes per 16 lanes) and transposes this 8 x 8 block among its own
+//     registers with 32 v_perm; product d of 8 then has rows 8 m + d of O^T.
+// Pages hold multiples of 8 tokens, so such a block of 8 keys lies on one page.
+#include <math.h>
+
+#include <mutex>
+
+#include "paged_attn_plan.h"
+#include "paged_kv.h"
+#include "row_map.h"
+
+namespace {
+
+namespace pg = sdvg::paged;
+
+typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kRows = 16;               // query rows per matrix product
+constexpr int kPad = 132;               // floats per row of O in LDS
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct AttnParams {
+  const void *q, *k, *v;
+  void *out;
+  float *lse;
+  const float *k_scale, *v_scale;
+  const int32_t *table, *q_start, *kv_lens;
+  float *part_o, *part_ml;            // partial results: O [slot][key head][row][128], (m, l) [slot][key head][row][2]
+  int64_t q_ts, q_hs, o_ts, o_hs, page_stride, token_stride, head_stride, table_stride;
+  int64_t capacity;                   // keys a row of the table can name
+  int32_t n_requests, n_tokens, n_heads, n_kv_heads, group, n_pages, table_width, window, target;
+  sdvg::FastDiv by_group, by_page;    // rows -> tokens; blocks of 8 keys -> pages
+  float scale_log2e;
+};
+
+// ---- the two 16-bit types
+struct Bf16 {
+  typedef bf16x8 frag;
+  static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ unsigned pack(float x, float y) {
+    const f32x2 f = {x, y};
+    return __builtin_bit_cast(unsigned, __builtin_convertvector(f, bf16x2));
+  }
+  // elements 2i, 2i + 1 of a dword of four e4m3 numbers (exact in 16 bits)
+  static __device__ __forceinline__ unsigned lo8(unsigned w) {
+    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
+  }
+  static __device__ __forceinline__ unsigned hi8(unsigned w) {
+    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true));
+  }
+};
+struct F16 {
+  static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ unsigned pack(float x, float y) {
+    const f16x2 h = {static_cast<_Float16>(x), static_cast<_Float16>(y)};
+    return __builtin_bit_cast(unsigned, h);
+  }
+  static __device__ __forceinline__ unsigned lo8(unsigned w) {
+    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false));
+  }
+  static __device__ __forceinline__ unsigned hi8(unsigned w) {
+    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true));
+  }
+};
+template <typename T>
+__device__ __forceinline__ u32x4 widen(u32x2 w) {
+  return u32x4{T::lo8(w[0]), T::hi8(w[0]), T::lo8(w[1]), T::hi8(w[1])};
+}
+
+// ---- over the 4 lanes that hold one query row (l, l ^ 16, l ^ 32, l ^ 48)
+__device__ __forceinline__ float rows_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float rows_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// ---- which part of the work a workgroup has
+// Found by every wave for itself: lane i looks at request 64 b + i. Batches of 64 requests at a time.
+struct Found {
+  pg::Request q;
+  int32_t request, tile, piece, pieces, slot;   // row tile of the request; slot of its first piece
+};
+template <int kRowTile>
+__device__ __forceinline__ pg::Request load_request(const AttnParams &p, int r) {
+  if (r >= p.n_requests) return pg::Request{0, 0, 0, 0, 0, 0};
+  return pg::request_of(p.q_start[r], p.q_start[r + 1], p.kv_lens[r], p.n_tokens, p.group, kRowTile, p.window, p.capacity);
+}
+// Number `x` among the items (kItems) or among the split row tiles.
+template <int kRowTile, bool kItems>
+__device__ __forceinline__ bool find(const AttnParams &p, int x, Found &f) {
+  const int lane = threadIdx.x & 63;
+  pg::Request q = load_request<kRowTile>(p, lane);
+  int64_t total = pg::work_of(q);
+  for (int b = 64; b < p.n_requests; b += 64) {
+    const pg::Request o = load_request<kRowTile>(p, b + lane);
+    total += pg::work_of(o);
+  }
+  for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
+  const int32_t chunk = pg::chunk_of(total, p.target);
+  int before = 0, slots_before = 0;
+  for (int b = 0; b < p.n_requests; b += 64) {
+    if (b > 0) q = load_request<kRowTile>(p, b + lane);
+    const int32_t pieces = pg::pieces_of(q, chunk);
+    const int32_t slots = pieces > 1 ? q.row_tiles * pieces : 0;
+    const int32_t mine = kItems ? q.row_tiles * pieces : pieces > 1 ? q.row_tiles : 0;
+    int upto = mine, slots_upto = slots;  // inclusive
+    for (int d = 1; d < 64; d <<= 1) {
+      const int a = __shfl_up(upto, d), c = __shfl_up(slots_upto, d);
+      if (lane >= d) {
+        upto += a;
+        slots_upto += c;
+      }
+    }
+    const int at = x - before - (upto - mine);
+    const uint64_t hit = __ballot(at >= 0 && at < mine);
+    if (hit) {
+      const int src = __ffsll(static_cast<unsigned long long>(hit)) - 1;
+      const auto get = [src](int v) { return __builtin_amdgcn_readlane(v, src); };
+      f.q = pg::Request{get(q.row0), get(q.n), get(q.len), get(q.first_tile), get(q.tiles), get(q.row_tiles)};
+      f.request = b + src;
+      f.pieces = get(pieces);
+      const int i = get(at), slot0 = slots_before + get(slots_upto - slots);
+      f.tile = kItems ? i / f.pieces : i;
+      f.piece = kItems ? i - f.tile * f.pieces : 0;
+      f.slot = slot0 + f.tile * f.pieces;
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+    slots_before += __builtin_amdgcn_readlane(slots_upto, 63);
+  }
+  return false;
+}
+
+// T: type of q, of P and of the output. kF8: the cache holds e4m3 numbers. NT: tiles of 16 query rows.
+template <typename T, bool kF8, int NT>
+__global__ __launch_bounds__(kThreads) void paged_attn_kernel(AttnParams p) {
+  constexpr int kRowTile = kRows * NT;
+  constexpr int kBytes = kF8 ? 1 : 2;
+  __shared__ float o_s[kWaves][kRows][kPad];
+  __shared__ float ml_s[kWaves][kRows][2];
+  Found f;
+  if (!find<kRowTile, true>(p, blockIdx.x, f)) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
+  const int head = blockIdx.y;
+  const int rows = f.q.n * p.group - f.tile * kRowTile;   // rows of this tile, those past kRowTile included
+
+  // the query rows of this lane: column col of every tile of 16
+  u32x4 qf[NT][4];
+  int32_t sees[NT], from[NT];   // keys from[..] <= j < sees[..]
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int row = t * kRows + col;
+    const uint32_t all = f.tile * kRowTile + row, i = p.by_group.div(all), h = all - i * p.group;
+    sees[t] = from[t] = 0;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) qf[t][s] = u32x4{0, 0, 0, 0};
+    if (row < rows) {
+      sees[t] = f.q.len - f.q.n + static_cast<int>(i) + 1;
+      from[t] = p.window > 0 && sees[t] > p.window ? sees[t] - p.window : 0;
+      const uint16_t *src = static_cast<const uint16_t *>(p.q) + (f.q.row0 + static_cast<int64_t>(i)) * p.q_ts +
+                            (static_cast<int64_t>(head) * p.group + h) * p.q_hs;
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        // dims of product s in this lane: as K's load has them (below)
+        const int d = kF8 ? 64 * (s >> 1) + 16 * quad + 8 * (s & 1) : 32 * s + 8 * quad;
+        qf[t][s] = *reinterpret_cast<const u32x4 *>(src + d);
+      }
+    }
+  }
+  // tiles in which every row of the workgroup sees every key
+  const int last_row = rows < kRowTile ? rows - 1 : kRowTile - 1;
+  const int first_i = static_cast<int>(p.by_group.div(f.tile * kRowTile)),
+            last_i = static_cast<int>(p.by_group.div(f.tile * kRowTile + last_row));
+  const int all_sees = f.q.len - f.q.n + first_i + 1, last_sees = f.q.len - f.q.n + last_i + 1;
+  const int all_from = p.window > 0 && last_sees > p.window ? last_sees - p.window : 0;
+
+  const float scale = p.scale_log2e * (kF8 && p.k_scale ? p.k_scale[head] : 1.0f);
+  f32x4 o[NT][8];
+  float m[NT], l[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    m[t] = -INFINITY;
+    l[t] = 0.f;
+#pragma unroll
+    for (int d = 0; d < 8; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const int begin = f.q.first_tile + pg::piece_begin(f.q.tiles, f.piece, f.pieces);
+  const int end = f.q.first_tile + pg::piece_begin(f.q.tiles, f.piece + 1, f.pieces);
+  const int32_t *table = p.table + f.request * p.table_stride;
+  const char *k_head = static_cast<const char *>(p.k) + head * p.head_stride * kBytes,
+             *v_head = static_cast<const char *>(p.v) + head * p.head_stride * kBytes;
+  // the page of a block of 8 keys, -1 if there is none
+  const auto page_of = [&](uint32_t block, uint32_t &place) {
+    const uint32_t i = p.by_page.div(block);
+    place = (block - i * p.by_page.d) * 8;
+    const int32_t page = i < static_cast<uint32_t>(p.table_width) ? table[i] : -1;
+    return page >= 0 && page < p.n_pages ? page : -1;
+  };
+  for (int tile = begin + wave; tile < end; tile += kWaves) {
+    const int key0 = tile * pg::kKeyTile;
+    uint32_t k_place, v_place;
+    const int32_t k_page = page_of(key0 / 8 + (col >> 2), k_place), v_page = page_of(key0 / 8 + quad, v_place);
+    // (a page that is not there reads page 0, which is memory of the pool; its keys do not count)
+    const char *kp = k_head + ((k_page < 0 ? 0 : k_page) * p.page_stride + (k_place + (col & 3)) * p.token_stride) * kBytes;
+    const char *vp = v_head + ((v_page < 0 ? 0 : v_page) * p.page_stride + v_place * p.token_stride) * kBytes;
+    u32x4 kf[2][4];
+    u32x4 vf[8];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const char *row = kp + 4 * t * p.token_stride * kBytes;
+      if constexpr (kF8) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const u32x4 w = *reinterpret_cast<const u32x4 *>(row + 64 * s + 16 * quad);
+          kf[t][2 * s] = widen<T>(u32x2{w[0], w[1]});
+          kf[t][2 * s + 1] = widen<T>(u32x2{w[2], w[3]});
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) kf[t][s] = *reinterpret_cast<const u32x4 *>(row + 64 * s + 16 * quad);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const char *row = vp + j * p.token_stride * kBytes + col * (8 * kBytes);
+      if constexpr (kF8)
+        vf[j] = widen<T>(*reinterpret_cast<const u32x2 *>(row));
+      else
+        vf[j] = *reinterpret_cast<const u32x4 *>(row);
+    }
+    // keys of this lane's block of 8 that are there; V of the others is cleared (0 times anything but a number is no 0)
+    int there = f.q.len - (key0 + 8 * quad);
+    there = v_page < 0 ? 0 : there < 0 ? 0 : there > 8 ? 8 : there;
+    const bool gaps = __any(there < 8);
+    if (gaps) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j >= there) vf[j] = u32x4{0, 0, 0, 0};
+    }
+    const bool masked = gaps || key0 + pg::kKeyTile > all_sees || key0 < all_from;
+    // V^T: dim 2e + h of keys 2c, 2c + 1 from dword e of both
+    u32x4 vt[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        vt[2 * e][c] = __builtin_amdgcn_perm(vf[2 * c + 1][e], vf[2 * c][e], 0x05040100u);
+        vt[2 * e + 1][c] = __builtin_amdgcn_perm(vf[2 * c + 1][e], vf[2 * c][e], 0x07060302u);
+      }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        s[0] = T::mfma(kf[0][c], qf[t][c], s[0]);
+        s[1] = T::mfma(kf[1][c], qf[t][c], s[1]);
+      }
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * scale;
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int key = key0 + 8 * quad + e;
+          x[e] = e < there && key < sees[t] && key >= from[t] ? x[e] : -INFINITY;
+        }
+      }
+      float top = x[0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
+      top = fmaxf(m[t], rows_max(top));
+      const float base = top == -INFINITY ? 0.f : top;   // no key so far: every probability is 2^-inf
+      const float keep = exp2f(m[t] - base);
+      m[t] = top;
+      l[t] *= keep;
+#pragma unroll
+      for (int d = 0; d < 8; ++d) o[t][d] *= keep;
+      u32x4 pf;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const float a = exp2f(x[2 * c] - base), b = exp2f(x[2 * c + 1] - base);
+        pf[c] = T::pack(a, b);
+        l[t] += a + b;
+      }
+#pragma unroll
+      for (int d = 0; d < 8; ++d) o[t][d] = T::mfma(vt[d], pf, o[t][d]);
+    }
+  }
+
+  // The 4 waves' results of a tile of 16 rows meet in LDS; 16 threads finish a row.
+  const float v_scale = kF8 && p.v_scale ? p.v_scale[head] : 1.0f;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    if (t * kRows >= rows) break;
+    if (t > 0) __syncthreads();
+    const float sum = rows_sum(l[t]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {  // dims 8 (4 quad + i) + d
+      float *dst = &o_s[wave][col][8 * (4 * quad + i)];
+      *reinterpret_cast<f32x4 *>(dst) = f32x4{o[t][0][i], o[t][1][i], o[t][2][i], o[t][3][i]};
+      *reinterpret_cast<f32x4 *>(dst + 4) = f32x4{o[t][4][i], o[t][5][i], o[t][6][i], o[t][7][i]};
+    }
+    if (quad == 0) {
+      ml_s[wave][col][0] = m[t];
+      ml_s[wave][col][1] = sum;
+    }
+    __syncthreads();
+    const int r = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * 8;
+    const int row = t * kRows + r;
+    if (row >= rows) continue;   // (all waves come to the barriers: `rows` is the workgroup's)
+    float top = ml_s[0][r][0], total = 0.f, acc[8] = {};
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ml_s[w][r][0]);
+    const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float weight = exp2f(ml_s[w][r][0] - base);
+      total += weight * ml_s[w][r][1];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] += weight * o_s[w][r][d0 + j];
+    }
+    if (f.pieces > 1) {
+      const int64_t at = (static_cast<int64_t>(f.slot + f.piece) * p.n_kv_heads + head) * kRowTile + row;
+      f32x4 *dst = reinterpret_cast<f32x4 *>(p.part_o + at * 128 + d0);
+      dst[0] = f32x4{acc[0], acc[1], acc[2], acc[3]};
+      dst[1] = f32x4{acc[4], acc[5], acc[6], acc[7]};
+      if (d0 == 0) {
+        p.part_ml[at * 2] = top;
+        p.part_ml[at * 2 + 1] = total;
+      }
+      continue;
+    }
+    const uint32_t all = f.tile * kRowTile + row, i = p.by_group.div(all), h = all - i * p.group;
+    const int64_t token = f.q.row0 + static_cast<int64_t>(i), q_head = static_cast<int64_t>(head) * p.group + h;
+    const float norm = top == -INFINITY ? 0.f : v_scale / total;   // (sum 0 only without a key)
+    u32x4 w;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) w[c] = T::pack(acc[2 * c] * norm, acc[2 * c + 1] * norm);
+    *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(p.out) + token * p.o_ts + q_head * p.o_hs + d0) = w;
+    if (p.lse && d0 == 0) p.lse[token * p.n_heads + q_head] = top == -INFINITY ? -INFINITY : (top + log2f(total)) * kLn2;
+  }
+}
+
+// Joins the pieces of one row: 32 threads have its dims, 8 sets of them every 8th piece.
+template <typename T, bool kF8, int NT>
+__global__ __launch_bounds__(kThreads) void paged_join_kernel(AttnParams p) {
+  constexpr int kRowTile = kRows * NT;
+  __shared__ f32x4 o_s[kThreads / 32][32];
+  Found f;
+  if (!find<kRowTile, false>(p, blockIdx.x, f)) return;
+  const int head = blockIdx.y, row = blockIdx.z, lane = threadIdx.x & 63;
+  if (f.tile * kRowTile + row >= f.q.n * p.group) return;
+  const int64_t step = static_cast<int64_t>(p.n_kv_heads) * kRowTile;   // rows between two pieces
+  const int64_t at = (static_cast<int64_t>(f.slot) * p.n_kv_heads + head) * kRowTile + row;
+  float top = -INFINITY, total = 0.f;
+  for (int i = lane; i < f.pieces; i += 64) top = fmaxf(top, p.part_ml[(at + i * step) * 2]);
+  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float base = top == -INFINITY ? 0.f : top;
+  for (int i = lane; i < f.pieces; i += 64)
+    total += exp2f(p.part_ml[(at + i * step) * 2] - base) * p.part_ml[(at + i * step) * 2 + 1];
+  for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
+  const int d4 = threadIdx.x & 31, set = threadIdx.x >> 5;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int i = set; i < f.pieces; i += kThreads / 32) {
+    const float weight = exp2f(p.part_ml[(at + i * step) * 2] - base);
+    acc += weight * reinterpret_cast<const f32x4 *>(p.part_o + (at + i * step) * 128)[d4];
+  }
+  o_s[set][d4] = acc;
+  __syncthreads();
+  if (set != 0) return;
+#pragma unroll
+  for (int w = 1; w < kThreads / 32; ++w) acc += o_s[w][d4];
+  const uint32_t all = f.tile * kRowTile + row, i = p.by_group.div(all), h = all - i * p.group;
+  const int64_t token = f.q.row0 + static_cast<int64_t>(i), q_head = static_cast<int64_t>(head) * p.group + h;
+  const float norm = top == -INFINITY ? 0.f : (kF8 && p.v_scale ? p.v_scale[head] : 1.0f) / total;
+  acc *= norm;
+  const u32x2 w = {T::pack(acc[0], acc[1]), T::pack(acc[2], acc[3])};
+  *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(p.out) + token * p.o_ts + q_head * p.o_hs + 4 * d4) = w;
+  if (p.lse && d4 == 0) p.lse[token * p.n_heads + q_head] = top == -INFINITY ? -INFINITY : (top + log2f(total)) * kLn2;
+}
+
+constexpr int kMaxDevices = 64;
+int compute_units(int &n) {
+  static std::once_flag once[kMaxDevices];
+  static int units[kMaxDevices];
+  static hipError_t status[kMaxDevices];
+  int dev = 0;
+  SDVG_HIP_CHECK(hipGetDevice(&dev));
+  if (dev < 0 || dev >= kMaxDevices) return SDVG_ERR_UNSUPPORTED;
+  std::call_once(once[dev], [dev] { status[dev] = hipDeviceGetAttribute(&units[dev], hipDeviceAttributeMultiprocessorCount, dev); });
+  SDVG_HIP_CHECK(status[dev]);
+  n = units[dev];
+  return SDVG_OK;
+}
+
+// Tiles of 16 rows per workgroup, by the average request: K and V are then read once per key head.
+int row_tiles_of(int64_t n_requests, int64_t n_tokens, int group) {
+  const int64_t rows = (n_tokens + n_requests - 1) / n_requests * group;
+  return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+}
+
+// Items per key head that a launch aims at.
+int target_of(int n_cu, int n_kv_heads) {
+  const int t = 4 * n_cu / n_kv_heads;
+  return t > 1 ? t : 1;
+}
+
+int64_t workspace_of(int target, int n_kv_heads, int nt) {
+  return pg::max_slots(target) * n_kv_heads * (kRows * nt) * (128 + 2) * 4;
+}
+
+int check_attn(const sdvg_paged_attn_desc *d, const sdvg_paged_kv *c) {
+  if (!d) return SDVG_ERR_NULL;
+  const int st = sdvg::check_paged_kv(c);
+  if (st != SDVG_OK) return st;
+  if (d->head_dim != 128) return SDVG_ERR_UNSUPPORTED;
+  if (d->dtype != SDVG_BF16 && d->dtype != SDVG_F16) return SDVG_ERR_UNSUPPORTED;
+  if (c->dtype != d->dtype && c->dtype != SDVG_E4M3) return SDVG_ERR_UNSUPPORTED;
+  if (d->n_requests < 0 || d->n_tokens < 0 || d->n_heads < 1 || d->n_heads % c->n_kv_heads != 0 || d->table_width < 1 ||
+      d->window < 0)
+    return SDVG_ERR_SHAPE;
+  if (c->n_kv_heads > 65535 || int64_t{d->n_tokens} * d->n_heads > INT32_MAX) return SDVG_ERR_UNSUPPORTED;
+  if (d->n_requests > 1 && d->table_stride < d->table_width) return SDVG_ERR_SHAPE;
+  if (!(d->scale >= 0.f) || !isfinite(d->scale)) return SDVG_ERR_RANGE;
+  return SDVG_OK;
+}
+
+template <typename T, bool kF8, int NT>
+int launch_attn(const AttnParams &p, hipStream_t s) {
+  const int64_t tiles = pg::max_row_tiles(p.n_requests, p.n_tokens, p.group, kRows * NT);
+  const int64_t items = pg::max_items(tiles, p.target);
+  if (items > (INT32_MAX / kThreads)) return SDVG_ERR_UNSUPPORTED;
+  hipLaunchKernelGGL((paged_attn_kernel<T, kF8, NT>), dim3(static_cast<uint32_t>(items), p.n_kv_heads), dim3(kThreads), 0, s, p);
+  SDVG_HIP_CHECK(hipGetLastError());
+  if (p.target > 0) {
+    const int64_t rows = static_cast<int64_t>(p.n_tokens) * p.group;
+    hipLaunchKernelGGL((paged_join_kernel<T, kF8, NT>),
+                       dim3(p.target, p.n_kv_heads, static_cast<uint32_t>(rows < kRows * NT ? rows : kRows * NT)),
+                       dim3(kThreads), 0, s, p);
+    SDVG_HIP_CHECK(hipGetLastError());
+  }
+  return SDVG_OK;
+}
+template <typename T, bool kF8>
+int launch_attn(const AttnParams &p, int nt, hipStream_t s) {
+  return nt == 1 ? launch_attn<T, kF8, 1>(p, s) : nt == 2 ? launch_attn<T, kF8, 2>(p, s) : launch_attn<T, kF8, 4>(p, s);
+}
+
+}  // namespace
+
+extern "C" int64_t sdvg_paged_attn_workspace_bytes(const sdvg_paged_attn_desc *desc, const sdvg_paged_kv *cache) {
+  int st = check_attn(desc, cache), n_cu = 0;
+  if (st != SDVG_OK) return st;
+  if (desc->n_requests == 0 || desc->n_tokens == 0) return 0;
+  if ((st = compute_units(n_cu)) != SDVG_OK) return st;
+  return workspace_of(target_of(n_cu, cache->n_kv_heads), cache->n_kv_heads,
+                      row_tiles_of(desc->n_requests, desc->n_tokens, desc->n_heads / cache->n_kv_heads));
+}
+
+extern "C" int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_paged_kv *cache, const void *q,
+                               const int32_t *block_table, const int32_t *q_start, const int32_t *kv_lens, void *out,
+                               float *lse, void *workspace, int64_t workspace_bytes, void *stream) {
+  int st = check_attn(desc, cache);
+  if (st != SDVG_OK) return st;
+  if (workspace_bytes < 0) return SDVG_ERR_SHAPE;
+  if (desc->n_requests == 0 || desc->n_tokens == 0) return SDVG_OK;
+  if (!q || !block_table || !q_start || !kv_lens || !out) return SDVG_ERR_NULL;
+  for (const int64_t s : {desc->q_token_stride, desc->o_token_stride})
+    if ((st = sdvg::check_stride(desc->n_tokens, s, 2)) != SDVG_OK) return st;
+  for (const int64_t s : {desc->q_head_stride, desc->o_head_stride})
+    if ((st = sdvg::check_stride(desc->n_heads, s, 2)) != SDVG_OK) return st;
+  if (!sdvg::aligned16(q) || !sdvg::aligned16(out) || !sdvg::aligned16(workspace)) return SDVG_ERR_ALIGN;
+  if ((reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(q_start) | reinterpret_cast<uintptr_t>(kv_lens) |
+       reinterpret_cast<uintptr_t>(lse)) & 3)
+    return SDVG_ERR_ALIGN;
+  if (q == out && ((desc->n_tokens > 1 && desc->q_token_stride != desc->o_token_stride) ||
+                   (desc->n_heads > 1 && desc->q_head_stride != desc->o_head_stride)))
+    return SDVG_ERR_RANGE;
+  int n_cu = 0;
+  if ((st = compute_units(n_cu)) != SDVG_OK) return st;
+  AttnParams p{};
+  p.q = q;
+  p.k = cache->k;
+  p.v = cache->v;
+  p.out = out;
+  p.lse = lse;
+  p.k_scale = cache->k_scale;
+  p.v_scale = cache->v_scale;
+  p.table = block_table;
+  p.q_start = q_start;
+  p.kv_lens = kv_lens;
+  p.q_ts = desc->q_token_stride;
+  p.q_hs = desc->q_head_stride;
+  p.o_ts = desc->o_token_stride;
+  p.o_hs = desc->o_head_stride;
+  p.page_stride = cache->page_stride;
+  p.token_stride = cache->token_stride;
+  p.head_stride = cache->head_stride;
+  p.table_stride = desc->table_stride;
+  p.capacity = int64_t{desc->table_width} * cache->page_tokens;
+  if (p.capacity > INT32_MAX - 2 * pg::kKeyTile) p.capacity = INT32_MAX - 2 * pg::kKeyTile;  // (more than any pool holds)
+  p.n_requests = desc->n_requests;
+  p.n_tokens = desc->n_tokens;
+  p.n_heads = desc->n_heads;
+  p.n_kv_heads = cache->n_kv_heads;
+  p.group = desc->n_heads / cache->n_kv_heads;
+  p.n_pages = cache->n_pages;
+  p.table_width = desc->table_width;
+  p.window = desc->window;
+  p.by_group = sdvg::FastDiv::of(p.group);
+  p.by_page = sdvg::FastDiv::of(cache->page_tokens / 8);
+  p.scale_log2e = (desc->scale == 0.f ? 1.0f / sqrtf(128.0f) : desc->scale) * kLog2e;
+  const int nt = row_tiles_of(p.n_requests, p.n_tokens, p.group), target = target_of(n_cu, p.n_kv_heads);
+  if (workspace && workspace_bytes >= workspace_of(target, p.n_kv_heads, nt)) {
+    p.target = target;
+    p.part_o = static_cast<float *>(workspace);
+    p.part_ml = p.part_o + pg::max_slots(target) * p.n_kv_heads * (kRows * nt) * 128;
+  }
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const bool f8 = cache->dtype == SDVG_E4M3;
+  if (desc->dtype == SDVG_BF16) return f8 ? launch_attn<Bf16, true>(p, nt, s) : launch_attn<Bf16, false>(p, nt, s);
+  return f8 ? launch_attn<F16, true>(p, nt, s) : launch_attn<F16, false>(p, nt, s);
+}

@@ -1,0 +1,78 @@
+// How the work of a paged attention launch is cut into workgroups: integer arithmetic on the requests' lengths, which the
+// kernels do on the device (lengths are device data) and a host test repeats.
+//
+// The rows of a request that share a key head (its new tokens x the query heads of the group) are cut into tiles of
+// row_tile rows. Work is counted in (row tile, key tile) pairs; `chunk` key tiles at most go to one workgroup ("item"), so
+// that the launch has about `target` items per key head whatever the lengths are. A request whose keys fit one chunk is
+// written by its workgroup; the others leave a partial result per item in a numbered slot, and the join adds up a
+// group of consecutive slots per row tile.
+#pragma once
+#include <stdint.h>
+
+#if defined(__HIPCC__)
+#include <hip/hip_runtime.h>
+#define SDVG_PAGED_HD __host__ __device__ inline __attribute__((always_inline))
+#else
+#define SDVG_PAGED_HD inline
+#endif
+
+namespace sdvg {
+namespace paged {
+
+constexpr int kKeyTile = 32;   // keys a wave takes per step
+constexpr int kMinChunk = 4;   // key tiles: one per wave of a workgroup
+
+// What a request asks for.
+struct Request {
+  int32_t row0, n;              // first row among all tokens, new tokens
+  int32_t len;                  // keys of the last token: positions 0 .. len - 1
+  int32_t first_tile, tiles;    // key tiles that any of its rows sees
+  int32_t row_tiles;
+};
+SDVG_PAGED_HD int32_t clamp(int32_t x, int32_t lo, int32_t hi) { return x < lo ? lo : x > hi ? hi : x; }
+
+// start, end: q_start[r], q_start[r + 1]; capacity: keys that a row of the block table can name.
+SDVG_PAGED_HD Request request_of(int32_t start, int32_t end, int32_t len, int32_t n_tokens, int32_t group, int32_t row_tile,
+                                 int32_t window, int64_t capacity) {
+  Request q;
+  q.row0 = clamp(start, 0, n_tokens);
+  q.n = clamp(end, q.row0, n_tokens) - q.row0;
+  q.len = len > 0 ? len : 0;
+  const int64_t first = static_cast<int64_t>(q.len) - q.n + 1 - window;  // of the first token's window
+  const int32_t lo = window > 0 && first > 0 ? static_cast<int32_t>(first) : 0;
+  const int32_t hi = q.len < capacity ? q.len : static_cast<int32_t>(capacity);
+  q.first_tile = lo / kKeyTile;
+  q.tiles = hi > lo ? static_cast<int32_t>((static_cast<int64_t>(hi) + kKeyTile - 1) / kKeyTile) - q.first_tile : 0;
+  q.row_tiles = static_cast<int32_t>((static_cast<int64_t>(q.n) * group + row_tile - 1) / row_tile);
+  return q;
+}
+// (A row tile without keys still is an item: somebody has to write its zeros.)
+SDVG_PAGED_HD int64_t work_of(const Request &q) { return static_cast<int64_t>(q.row_tiles) * (q.tiles > 1 ? q.tiles : 1); }
+
+// Key tiles per item at most: total = the sum of work_of. target <= 0: no split.
+SDVG_PAGED_HD int32_t chunk_of(int64_t total, int32_t target) {
+  if (target <= 0) return INT32_MAX;
+  const int64_t c = (total + target - 1) / target;
+  return c > kMinChunk ? static_cast<int32_t>(c < INT32_MAX ? c : INT32_MAX) : kMinChunk;
+}
+// Items per row tile.
+SDVG_PAGED_HD int32_t pieces_of(const Request &q, int32_t chunk) {
+  return q.tiles > chunk ? static_cast<int32_t>((static_cast<int64_t>(q.tiles) + chunk - 1) / chunk) : 1;
+}
+// First key tile of piece i of n, counted from the request's first: even shares.
+SDVG_PAGED_HD int32_t piece_begin(int32_t tiles, int32_t i, int32_t n) {
+  return static_cast<int32_t>(static_cast<int64_t>(tiles) * i / n);
+}
+
+// Bounds for the launch, from what the host knows. Items: total / chunk <= target of full chunks, and one more per row tile.
+// Slots: a split row tile of t > chunk tiles has ceil(t / chunk) < 2 t / chunk pieces. Groups (split row tiles): t > chunk each.
+SDVG_PAGED_HD int64_t max_row_tiles(int64_t n_requests, int64_t n_tokens, int32_t group, int32_t row_tile) {
+  const int64_t rows = n_tokens * group;
+  const int64_t bound = rows / row_tile + n_requests;
+  return bound < rows ? bound : rows;
+}
+SDVG_PAGED_HD int64_t max_items(int64_t row_tiles, int32_t target) { return row_tiles + (target > 0 ? target : 0); }
+SDVG_PAGED_HD int64_t max_slots(int32_t target) { return 2 * static_cast<int64_t>(target); }
+
+}  // namespace paged
+}  // namespace sdvg

@@ -183,3 +183,66 @@ def test_rope_frequencies(b):
                 dict(rotary_dim=64, scaling="yarn", original=100, beta_fast=1, beta_slow=1)]:
         with pytest.raises(ValueError):
             b.rope_frequencies(device="cpu", **bad)
+
+
+def test_cut_of_paged_attention_on_the_host(tmp_path):
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = str(tmp_path / "plan")
+    subprocess.run(["g++", "-O2", "-std=c++17", "-Wall", "-I", os.path.join(root, "paper_2604_17397_amd", "csrc"),
+                    os.path.join(root, "tests", "host", "paged_attn_plan.cpp"), "-o", exe], check=True)
+    res = subprocess.run([exe], stdout=subprocess.PIPE, text=True, timeout=120)
+    assert res.returncode == 0 and res.stdout.strip() == "ok", res.stdout
+
+
+def attn_desc(b, **kw):
+    d = b.sdvg_paged_attn_desc(n_requests=3, n_tokens=5, n_heads=6, head_dim=128, table_width=4, window=0, table_stride=4,
+                               q_token_stride=6 * 128, q_head_stride=128, o_token_stride=6 * 128, o_head_stride=128,
+                               scale=0.0, dtype=0)
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return d
+
+
+def test_paged_attn_rejects_bad_arguments(b):
+    ref = ctypes.byref
+
+    def call(d=None, c=None, q=FAKE, table=FAKE, start=FAKE, lens=FAKE, out=FAKE << 1, lse=None, ws=None, n_ws=0):
+        return b.lib().sdvg_paged_attn(ref(d or attn_desc(b)), ref(c or paged_kv(b)), q, table, start, lens, out, lse, ws, n_ws, None)
+    for kw, want in PAGED_BAD:
+        assert call(c=paged_kv(b, **kw)) == want, kw
+    for kw, want in [(dict(head_dim=64), -5), (dict(dtype=1), -5), (dict(dtype=2), -5), (dict(dtype=3), -5), (dict(n_requests=-1), -2),
+                     (dict(n_tokens=-1), -2), (dict(n_heads=0), -2), (dict(n_heads=5), -2), (dict(table_width=0), -2),
+                     (dict(window=-1), -2), (dict(table_stride=3), -2), (dict(scale=-1.0), -3), (dict(scale=float("nan")), -3),
+                     (dict(q_token_stride=100), -2), (dict(q_head_stride=132), -4), (dict(o_token_stride=772), -4),
+                     (dict(n_tokens=1 << 29), -5)]:
+        assert call(d=attn_desc(b, **kw)) == want, kw
+        if "stride" not in next(iter(kw)) or "table" in next(iter(kw)):
+            assert b.lib().sdvg_paged_attn_workspace_bytes(ref(attn_desc(b, **kw)), ref(paged_kv(b))) == want, kw
+    for kw in (dict(q=None), dict(table=None), dict(start=None), dict(lens=None), dict(out=None)):
+        assert call(**kw) == -1
+    for kw in (dict(q=FAKE + 8), dict(table=FAKE + 2), dict(start=FAKE + 1), dict(lens=FAKE + 2), dict(out=FAKE + 2), dict(lse=FAKE + 2),
+               dict(ws=FAKE + 8, n_ws=1 << 20)):
+        assert call(**kw) == -4
+    assert call(n_ws=-1) == -2
+    assert call(d=attn_desc(b, o_token_stride=1024), out=FAKE) == -3       # in place with other strides
+    assert call(d=attn_desc(b, n_requests=0), q=None) == 0 and call(d=attn_desc(b, n_tokens=0), q=None) == 0
+    assert b.lib().sdvg_paged_attn_workspace_bytes(ref(attn_desc(b, n_tokens=0)), ref(paged_kv(b))) == 0
+
+
+def test_paged_attn_binding_checks(b, monkeypatch):
+    for name in ("_check_here", "_check_dev"):
+        monkeypatch.setattr(b, name, lambda *a: None)
+    pool = torch.zeros((3, 8, 2, 128), dtype=torch.bfloat16)
+    c = b.PagedKV(pool, pool)
+    monkeypatch.setattr(b, "_LIB", type("Trap", (), {"__getattr__": lambda s, n: pytest.fail("the C library must not be reached")})())
+    q = torch.zeros((4, 6, 128), dtype=torch.bfloat16)
+    n = torch.zeros(2, dtype=torch.int32)
+    ok = dict(q=q, cache=c, block_table=torch.zeros((2, 3), dtype=torch.int32), q_start=torch.zeros(3, dtype=torch.int32), kv_lens=n)
+    for kw in [dict(q=q.half()), dict(q=q.float()), dict(q=q[0]), dict(block_table=n), dict(block_table=ok["block_table"].long()),
+               dict(block_table=torch.zeros((3, 2), dtype=torch.int32).t()), dict(q_start=n), dict(kv_lens=n[:1]), dict(kv_lens=n.long()),
+               dict(out=q[:3]), dict(out=q.half()), dict(lse=torch.zeros((4, 6), dtype=torch.float64)), dict(lse=torch.zeros((4, 5))),
+               dict(lse=torch.zeros((6, 4)).t()), dict(workspace=torch.zeros((8, 8)).t())]:
+        with pytest.raises(ValueError):
+            b.paged_attn(**{**ok, **kw})
