@@ -163,6 +163,7 @@ def lib():
 class _PythonOnly:
     """Stands in for the marshalling module where it has not been built: Python handles every call."""
     block_attn = rope = route = batch = commit = rollback = snapshot = staticmethod(lambda *args: None)
+    page_plan = rope_positions = paged_commit = paged_attn = staticmethod(lambda *args: None)
 
 
 _NATIVE = None
@@ -184,8 +185,9 @@ def _bind_native(L):
     entry = [ctypes.cast(f, ctypes.c_void_p).value for f in
              (L.sdvg_block_attn, L.sdvg_block_attn_commit, L.sdvg_rope, L.sdvg_worst_frame_route, L.sdvg_avg_frame_route,
               L.sdvg_block_attn_batch, L.sdvg_block_attn_batch_static, L.sdvg_kv_commit, L.sdvg_kv_commit_rope,
-              L.sdvg_kv_rollback, L.sdvg_buffer_snapshot)]
-    module.init(*entry, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, np.float32, sdvg_kv_cache)
+              L.sdvg_kv_rollback, L.sdvg_buffer_snapshot, L.sdvg_page_plan, L.sdvg_rope_positions, L.sdvg_paged_commit,
+              L.sdvg_paged_attn)]
+    module.init(*entry, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, np.float32, sdvg_kv_cache, sdvg_paged_kv)
     _NATIVE = module
 
 
@@ -587,6 +589,13 @@ def page_plan(cached, new_tokens, block_table, page_tokens, free_pages=None, hel
         out = PagePlan(cached.shape[0], max_tokens, cached.device)
     elif max_tokens is not None and max_tokens != out.slots.shape[0]:
         raise ValueError("out holds another number of tokens than max_tokens")
+    r = (_NATIVE or _native()).page_plan(cached, new_tokens, block_table, page_tokens, free_pages, held, next_free, out.q_start,
+                                        out.kv_lens, out.positions, out.held, out.next_free, out.slots,
+                                        None if stream is None else stream.cuda_stream)
+    if r is not None:
+        if r != 0:
+            raise SdvgError(r, "sdvg_page_plan")
+        return out
     n = cached.shape[0]
     _check_here(cached, new_tokens, block_table, free_pages, held, next_free, out.q_start, out.slots)
     _int_array("cached", cached, n)
@@ -680,6 +689,13 @@ def rope_positions(x, positions, freqs, y=None, layout="half", gain=1.0, out=Non
     number of heads) in the same launch, at int32 positions [tokens] with float64 freqs [rotary_dim / 2] (rope_frequencies).
     layout "half" pairs elements p and p + rotary_dim / 2, "interleaved" 2p and 2p + 1. out / y_out default to new tensors;
     pass the input for in place. Returns out, or (out, y_out) with y."""
+    if type(layout) is str and layout in _LAYOUT:
+        r = (_NATIVE or _native()).rope_positions(x, positions, freqs, y, _LAYOUT[layout], gain, out, y_out,
+                                                 None if stream is None else stream.cuda_stream)
+        if r is not None:
+            if type(r) is int:
+                raise SdvgError(r, "sdvg_rope_positions")
+            return r
     _check_here(x, y, out, y_out)
     _check_rows("x", x)
     if y is None and y_out is not None:
@@ -730,6 +746,15 @@ def paged_commit(cache, k, v, slots, positions=None, freqs=None, q=None, q_out=N
     """sdvg_paged_commit: rows k, v [tokens, kv_heads, 128] of bfloat16 or float16 into the int64 slots [tokens] of a PagedKV;
     a negative slot writes nothing. With positions and freqs (as for rope_positions) K is rotated on its way, and so is
     q [tokens, heads, 128] into q_out (default: a new tensor; pass q for in place). Returns q_out, or None without q."""
+    if type(layout) is str and layout in _LAYOUT:
+        r = (_NATIVE or _native()).paged_commit(cache.c, cache.k, k, v, slots, positions, freqs, q, q_out, _LAYOUT[layout], gain,
+                                               None if stream is None else stream.cuda_stream)
+        if r is not None:
+            if type(r) is int:
+                if r != 0:
+                    raise SdvgError(r, "sdvg_paged_commit")
+                return None
+            return r
     _check_here(cache.k, k, v, slots, q, q_out)
     for name, t in (("k", k), ("v", v)):
         _check_rows(name, t)
@@ -784,6 +809,12 @@ def paged_attn(q, cache, block_table, q_start, kv_lens, out=None, lse=None, scal
     them. `window` > 0: every token sees the last `window` keys only. `lse`: optional float32 [tokens, heads] for the log of the sums.
     `workspace`: optional device tensor of paged_attn_workspace_bytes, with which the keys of long requests are split
     over the chip. `scale=None` is 1/sqrt(128). out defaults to a new tensor; pass out=q for in place. Returns out."""
+    r = (_NATIVE or _native()).paged_attn(q, cache.c, cache.k, block_table, q_start, kv_lens, out, lse, scale, window, workspace,
+                                         None if stream is None else stream.cuda_stream)
+    if r is not None:
+        if type(r) is int:
+            raise SdvgError(r, "sdvg_paged_attn")
+        return r
     _check_here(q, cache.k, block_table, q_start, kv_lens, out, lse, workspace)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)

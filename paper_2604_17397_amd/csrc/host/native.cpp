@@ -1,12 +1,13 @@
 // Argument marshalling of the calls a denoising loop makes most often (attention, rotary embedding, the routing
-// decision, commit, rollback, snapshot), in C++: the same checks and the same call into libsdvg as
+// decision, commit, rollback, snapshot) and of the paged cache's, in C++: the same checks and the same call into libsdvg as
 // binding.py makes. Every function either finds all checks of its Python counterpart satisfied and
 // makes the call, or returns None without having done anything; the Python counterpart then takes
 // over, raises what it always raised, or handles the rarer form (fp32, tensor subclasses, ...).
 //
 // Why: on a small layer the GPU is done in 4 to 16 us, while checking and converting six tensors
 // through ctypes took 15 us per attention call and 12 per rotary pass. A batch of 1, 2 or 3 items took 21, 32 and 43 us,
-// commit, rollback and snapshot 7 to 10, which the GPU waits for behind a routing decision.
+// commit, rollback and snapshot 7 to 10, which the GPU waits for behind a routing decision. The paged cache's calls took 15
+// (plan) to 23 us (attention).
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ops/empty.h>
@@ -35,6 +36,12 @@ using commit_fn = int (*)(sdvg_kv_cache *, const void *, const void *, int32_t, 
 using commit_rope_fn = int (*)(sdvg_kv_cache *, const void *, const void *, int32_t, const float *, const float *, void *);
 using rollback_fn = int (*)(sdvg_kv_cache *, int64_t, void *);
 using snapshot_fn = int (*)(void *, const void *, int64_t, void *);
+using page_plan_fn = int (*)(const sdvg_page_plan_args *, void *);
+using rope_positions_fn = int (*)(const sdvg_rope_desc *, const sdvg_rows *, const sdvg_rows *, int64_t, int32_t, int32_t, void *);
+using paged_commit_fn = int (*)(const sdvg_paged_kv *, const sdvg_rows *, const sdvg_rows *, const int64_t *, int64_t, int32_t,
+                                const sdvg_rope_desc *, const sdvg_rows *, void *);
+using paged_attn_fn = int (*)(const sdvg_paged_attn_desc *, const sdvg_paged_kv *, const void *, const int32_t *, const int32_t *,
+                              const int32_t *, void *, float *, void *, int64_t, void *);
 
 // Entry points of the libsdvg that binding.py has loaded, and torch's current-stream functions.
 struct Api {
@@ -48,7 +55,11 @@ struct Api {
   commit_rope_fn commit_rope = nullptr;
   rollback_fn rollback = nullptr;
   snapshot_fn snapshot = nullptr;
-  PyObject *get_device = nullptr, *get_raw_stream = nullptr, *float32 = nullptr, *cache_type = nullptr;
+  page_plan_fn page_plan = nullptr;
+  rope_positions_fn rope_positions = nullptr;
+  paged_commit_fn paged_commit = nullptr;
+  paged_attn_fn paged_attn = nullptr;
+  PyObject *get_device = nullptr, *get_raw_stream = nullptr, *float32 = nullptr, *cache_type = nullptr, *paged_type = nullptr;
 } api;
 
 // A plain strided GPU tensor, or null (subclasses, wrappers and CPU tensors are Python's).
@@ -249,23 +260,24 @@ PyObject *batch_impl(PyObject *const *a, Py_ssize_t n_args) {
   return PyLong_FromLong(status);
 }
 
-// The sdvg_kv_cache inside a ctypes structure of binding.py, for as long as this lives.
-struct CacheRef {
+// The descriptor S inside a ctypes structure of binding.py (of class `type`), for as long as this lives.
+template <typename S>
+struct DescRef {
   Py_buffer view{};
-  sdvg_kv_cache *c = nullptr;
-  explicit CacheRef(PyObject *o) {
-    if (reinterpret_cast<PyObject *>(Py_TYPE(o)) != api.cache_type) return;
+  S *c = nullptr;
+  DescRef(PyObject *o, PyObject *type) {
+    if (reinterpret_cast<PyObject *>(Py_TYPE(o)) != type) return;
     if (PyObject_GetBuffer(o, &view, PyBUF_WRITABLE) != 0) {
       PyErr_Clear();
       return;
     }
-    if (view.len == static_cast<Py_ssize_t>(sizeof(sdvg_kv_cache))) c = static_cast<sdvg_kv_cache *>(view.buf);
+    if (view.len == static_cast<Py_ssize_t>(sizeof(S))) c = static_cast<S *>(view.buf);
   }
-  ~CacheRef() {
+  ~DescRef() {
     if (view.obj) PyBuffer_Release(&view);
   }
-  CacheRef(const CacheRef &) = delete;
-  CacheRef &operator=(const CacheRef &) = delete;
+  DescRef(const DescRef &) = delete;
+  DescRef &operator=(const DescRef &) = delete;
 };
 
 // A dense bf16 [layers][T][heads][dim] block of the cache's shape.
@@ -280,7 +292,7 @@ const at::Tensor *block_tensor(PyObject *o, const sdvg_kv_cache &c) {
 // (cache.c, k_blk, v_blk, slot, stream), and cos, sin with the rotation of K
 PyObject *commit_impl(PyObject *const *a, Py_ssize_t n) {
   if (n != 5 && n != 7) PYTHON_TAKES_OVER;
-  const CacheRef cache(a[0]);
+  const DescRef<sdvg_kv_cache> cache(a[0], api.cache_type);
   int64_t slot;
   if (!cache.c || !integer(a[3], slot) || slot != static_cast<int32_t>(slot)) PYTHON_TAKES_OVER;
   const at::Tensor *kb = block_tensor(a[1], *cache.c), *vb = block_tensor(a[2], *cache.c);
@@ -307,7 +319,7 @@ PyObject *commit_impl(PyObject *const *a, Py_ssize_t n) {
 // (cache.c, new_len, stream)
 PyObject *rollback_impl(PyObject *const *a, Py_ssize_t n) {
   if (n != 3) PYTHON_TAKES_OVER;
-  const CacheRef cache(a[0]);
+  const DescRef<sdvg_kv_cache> cache(a[0], api.cache_type);
   int64_t new_len;
   void *stream;
   if (!cache.c || !integer(a[1], new_len) || !stream_ptr(a[2], stream)) PYTHON_TAKES_OVER;
@@ -388,6 +400,210 @@ PyObject *route_impl(PyObject *const *a, Py_ssize_t n) {
   return scalar ? Py_BuildValue("(iN)", status, scalar) : nullptr;
 }
 
+// ---- paged cache
+
+// The current device, which all tensors of a call have to be on, and the stream to launch on.
+bool launch_place(PyObject *stream, int64_t &device, void *&s) {
+  PyObject *dev = PyObject_CallNoArgs(api.get_device);
+  bool ok = dev && integer(dev, device);
+  if (ok && stream == Py_None) {
+    PyObject *raw = PyObject_CallOneArg(api.get_raw_stream, dev);
+    int64_t v = 0;
+    ok = raw && integer(raw, v);
+    Py_XDECREF(raw);
+    s = reinterpret_cast<void *>(v);
+  } else if (ok) {
+    ok = stream_ptr(stream, s);
+  }
+  Py_XDECREF(dev);
+  if (!ok) PyErr_Clear();
+  return ok;
+}
+
+// A dense tensor of n elements of one type, in one dimension.
+const at::Tensor *array(PyObject *o, at::ScalarType type, int64_t n, int64_t device) {
+  const at::Tensor *t = gpu_tensor(o);
+  return t && t->scalar_type() == type && t->dim() == 1 && t->size(0) == n && t->is_contiguous() && t->get_device() == device ? t : nullptr;
+}
+bool optional_array(PyObject *o, int64_t n, int64_t device, const int32_t *&p) {
+  p = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor *t = array(o, at::kInt, n, device);
+  if (t) p = static_cast<const int32_t *>(t->data_ptr());
+  return t;
+}
+const at::Tensor *table_tensor(PyObject *o, int64_t device) {
+  const at::Tensor *t = gpu_tensor(o);
+  return t && t->scalar_type() == at::kInt && t->dim() == 2 && (t->size(1) <= 1 || t->stride(1) == 1) && t->get_device() == device &&
+                 t->size(0) <= INT32_MAX && t->size(1) <= INT32_MAX
+             ? t
+             : nullptr;
+}
+// Rows [tokens][heads][128]; their type as sdvg.h has it, or -1.
+const at::Tensor *rows_tensor(PyObject *o, int64_t device) {
+  const at::Tensor *t = gpu_tensor(o);
+  return t && t->dim() == 3 && t->size(2) == 128 && t->stride(2) == 1 && t->get_device() == device && t->size(0) <= INT32_MAX &&
+                 t->size(1) <= INT32_MAX
+             ? t
+             : nullptr;
+}
+int type_of(const at::Tensor &t) {
+  switch (t.scalar_type()) {
+    case at::kBFloat16: return SDVG_BF16;
+    case at::kFloat: return SDVG_F32;
+    case at::kHalf: return SDVG_F16;
+    default: return -1;
+  }
+}
+sdvg_rows rows_of(const at::Tensor &in, const at::Tensor *out) {
+  return sdvg_rows{in.data_ptr(), out ? out->data_ptr() : nullptr, static_cast<int32_t>(in.size(1)), in.stride(0), in.stride(1),
+                   out ? out->stride(0) : 0, out ? out->stride(1) : 0};
+}
+bool rope_of(PyObject *positions, PyObject *freqs, PyObject *layout, PyObject *gain, int64_t n_tokens, int64_t device,
+             sdvg_rope_desc &d) {
+  const at::Tensor *p = array(positions, at::kInt, n_tokens, device), *f = gpu_tensor(freqs);
+  int64_t how;
+  if (!p || !f || f->scalar_type() != at::kDouble || f->dim() != 1 || !f->is_contiguous() || f->get_device() != device ||
+      f->size(0) > 64 || !integer(layout, how) || !PyFloat_CheckExact(gain))
+    return false;
+  d = sdvg_rope_desc{static_cast<const int32_t *>(p->data_ptr()), static_cast<const double *>(f->data_ptr()),
+                     static_cast<int32_t>(2 * f->size(0)), static_cast<int32_t>(how), static_cast<float>(PyFloat_AS_DOUBLE(gain))};
+  return true;
+}
+
+// (cached, new_tokens, block_table, page_tokens, free_pages, held, next_free, q_start, kv_lens, positions, held_out,
+// next_free_out, slots, stream) -> 0, a negative status, or None
+PyObject *page_plan_impl(PyObject *const *a, Py_ssize_t n_args) {
+  if (n_args != 14) PYTHON_TAKES_OVER;
+  int64_t device, page;
+  void *stream;
+  if (!launch_place(a[13], device, stream) || !integer(a[3], page) || page != static_cast<int32_t>(page)) PYTHON_TAKES_OVER;
+  const at::Tensor *table = table_tensor(a[2], device), *slots = gpu_tensor(a[12]);
+  if (!table || !slots || slots->dim() != 1) PYTHON_TAKES_OVER;
+  const int64_t n = table->size(0), m = slots->size(0);
+  if (n < 1 || m < 1) PYTHON_TAKES_OVER;  // (empty tensors have no address)
+  const at::Tensor *const cached = array(a[0], at::kInt, n, device), *const fresh = array(a[1], at::kInt, n, device),
+                   *const starts = array(a[7], at::kInt, n + 1, device), *const lens = array(a[8], at::kInt, n, device),
+                   *const positions = array(a[9], at::kInt, m, device), *const held_out = array(a[10], at::kInt, n, device),
+                   *const next_out = array(a[11], at::kInt, 1, device);
+  if (!cached || !fresh || !starts || !lens || !positions || !held_out || !next_out || !array(a[12], at::kLong, m, device)) PYTHON_TAKES_OVER;
+  const at::Tensor *const free = a[4] == Py_None ? nullptr : gpu_tensor(a[4]);
+  if (a[4] != Py_None && (!free || free->dim() != 1 || free->size(0) > INT32_MAX || !array(a[4], at::kInt, free->size(0), device)))
+    PYTHON_TAKES_OVER;
+  const int32_t *held, *next;
+  if (!optional_array(a[5], n, device, held) || !optional_array(a[6], 1, device, next) || (!held && (free || next))) PYTHON_TAKES_OVER;
+  const auto ints = [](const at::Tensor *t) { return static_cast<int32_t *>(t->data_ptr()); };
+  const sdvg_page_plan_args args{static_cast<int32_t>(n), static_cast<int32_t>(page), static_cast<int32_t>(table->size(1)),
+                                 free ? static_cast<int32_t>(free->size(0)) : 0, n > 1 ? table->stride(0) : table->size(1), m,
+                                 ints(cached), ints(fresh), free && free->size(0) > 0 ? ints(free) : nullptr, held, next, ints(table),
+                                 ints(starts), ints(lens), ints(positions), ints(held_out), ints(next_out),
+                                 static_cast<int64_t *>(slots->data_ptr())};
+  int status;
+  Py_BEGIN_ALLOW_THREADS
+  status = api.page_plan(&args, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(status);
+}
+
+// (x, positions, freqs, y, layout, gain, out, y_out, stream) -> out or (out, y_out), a negative status, or None
+PyObject *rope_positions_impl(PyObject *const *a, Py_ssize_t n_args) {
+  if (n_args != 9) PYTHON_TAKES_OVER;
+  int64_t device;
+  void *stream;
+  if (!launch_place(a[8], device, stream)) PYTHON_TAKES_OVER;
+  const bool two = a[3] != Py_None;
+  const at::Tensor *x = rows_tensor(a[0], device), *y = two ? rows_tensor(a[3], device) : nullptr;
+  if (!x || type_of(*x) < 0 || x->size(0) < 1) PYTHON_TAKES_OVER;
+  if (two ? (!y || y->scalar_type() != x->scalar_type() || y->size(0) != x->size(0)) : a[7] != Py_None) PYTHON_TAKES_OVER;
+  sdvg_rope_desc rope;
+  if (!rope_of(a[1], a[2], a[4], a[5], x->size(0), device, rope)) PYTHON_TAKES_OVER;
+  const at::Tensor out = output(a[6], *x), y_out = two ? output(a[7], *y) : at::Tensor();
+  if (!out.defined() || (two && !y_out.defined())) PYTHON_TAKES_OVER;
+  const sdvg_rows rx = rows_of(*x, &out), ry = two ? rows_of(*y, &y_out) : sdvg_rows{};
+  const int64_t n = x->size(0);
+  const int32_t type = type_of(*x);
+  int status;
+  Py_BEGIN_ALLOW_THREADS
+  status = api.rope_positions(&rope, &rx, two ? &ry : nullptr, n, 128, type, stream);
+  Py_END_ALLOW_THREADS
+  PyObject *first = result(status, a[6], out);
+  if (status != 0 || !two || !first) return first;
+  PyObject *second = result(status, a[7], y_out);
+  return Py_BuildValue("(NN)", first, second);
+}
+
+// (cache.c, cache.k, k, v, slots, positions, freqs, q, q_out, layout, gain, stream) -> q_out, 0 without q, a negative status, or None
+PyObject *paged_commit_impl(PyObject *const *a, Py_ssize_t n_args) {
+  if (n_args != 12) PYTHON_TAKES_OVER;
+  int64_t device;
+  void *stream;
+  if (!launch_place(a[11], device, stream)) PYTHON_TAKES_OVER;
+  const DescRef<const sdvg_paged_kv> cache(a[0], api.paged_type);
+  const at::Tensor *pool = gpu_tensor(a[1]), *k = rows_tensor(a[2], device), *v = rows_tensor(a[3], device);
+  if (!cache.c || !pool || pool->get_device() != device || !k || !v || k->size(0) < 1 || k->sizes() != v->sizes() ||
+      k->scalar_type() != v->scalar_type() || k->size(1) != cache.c->n_kv_heads)
+    PYTHON_TAKES_OVER;
+  const int type = type_of(*k);
+  if ((type != SDVG_BF16 && type != SDVG_F16) || (cache.c->dtype != type && cache.c->dtype != SDVG_E4M3)) PYTHON_TAKES_OVER;
+  const int64_t n = k->size(0);
+  const at::Tensor *slots = array(a[4], at::kLong, n, device);
+  if (!slots) PYTHON_TAKES_OVER;
+  const bool turn = a[5] != Py_None, with_q = a[7] != Py_None;
+  sdvg_rope_desc rope;
+  if (turn != (a[6] != Py_None) || (with_q && !turn) || (!with_q && a[8] != Py_None)) PYTHON_TAKES_OVER;
+  if (turn && !rope_of(a[5], a[6], a[9], a[10], n, device, rope)) PYTHON_TAKES_OVER;
+  const at::Tensor *q = with_q ? rows_tensor(a[7], device) : nullptr;
+  if (with_q && (!q || q->size(0) != n || q->scalar_type() != k->scalar_type())) PYTHON_TAKES_OVER;
+  const at::Tensor q_out = with_q ? output(a[8], *q) : at::Tensor();
+  if (with_q && !q_out.defined()) PYTHON_TAKES_OVER;
+  const sdvg_rows rk = rows_of(*k, nullptr), rv = rows_of(*v, nullptr), rq = with_q ? rows_of(*q, &q_out) : sdvg_rows{};
+  const int64_t *const sp = static_cast<const int64_t *>(slots->data_ptr());
+  int status;
+  Py_BEGIN_ALLOW_THREADS
+  status = api.paged_commit(cache.c, &rk, &rv, sp, n, type, turn ? &rope : nullptr, with_q ? &rq : nullptr, stream);
+  Py_END_ALLOW_THREADS
+  return with_q ? result(status, a[8], q_out) : PyLong_FromLong(status);
+}
+
+// (q, cache.c, cache.k, block_table, q_start, kv_lens, out, lse, scale, window, workspace, stream)
+PyObject *paged_attn_impl(PyObject *const *a, Py_ssize_t n_args) {
+  if (n_args != 12) PYTHON_TAKES_OVER;
+  int64_t device, window;
+  void *stream;
+  double scale;
+  if (!launch_place(a[11], device, stream) || !integer(a[9], window) || window != static_cast<int32_t>(window) || !scale_of(a[8], scale))
+    PYTHON_TAKES_OVER;
+  const DescRef<const sdvg_paged_kv> cache(a[1], api.paged_type);
+  const at::Tensor *pool = gpu_tensor(a[2]), *q = rows_tensor(a[0], device), *table = table_tensor(a[3], device);
+  if (!cache.c || !pool || pool->get_device() != device || !q || !table || q->size(0) < 1 || table->size(0) < 1) PYTHON_TAKES_OVER;
+  const int type = type_of(*q);
+  if ((type != SDVG_BF16 && type != SDVG_F16) || (cache.c->dtype != type && cache.c->dtype != SDVG_E4M3)) PYTHON_TAKES_OVER;
+  const int64_t n = table->size(0);
+  const at::Tensor *starts = array(a[4], at::kInt, n + 1, device), *lens = array(a[5], at::kInt, n, device);
+  if (!starts || !lens) PYTHON_TAKES_OVER;
+  const at::Tensor *lse = a[7] == Py_None ? nullptr : gpu_tensor(a[7]), *ws = a[10] == Py_None ? nullptr : gpu_tensor(a[10]);
+  if (a[7] != Py_None && (!lse || lse->scalar_type() != at::kFloat || lse->dim() != 2 || lse->size(0) != q->size(0) ||
+                          lse->size(1) != q->size(1) || !lse->is_contiguous() || lse->get_device() != device))
+    PYTHON_TAKES_OVER;
+  if (a[10] != Py_None && (!ws || !ws->is_contiguous() || ws->get_device() != device)) PYTHON_TAKES_OVER;
+  const at::Tensor out = output(a[6], *q);
+  if (!out.defined()) PYTHON_TAKES_OVER;
+  const sdvg_paged_attn_desc d{static_cast<int32_t>(n), static_cast<int32_t>(q->size(0)), static_cast<int32_t>(q->size(1)), 128,
+                               static_cast<int32_t>(table->size(1)), static_cast<int32_t>(window), table->stride(0), q->stride(0),
+                               q->stride(1), out.stride(0), out.stride(1), static_cast<float>(scale), type};
+  const auto ints = [](const at::Tensor *t) { return static_cast<const int32_t *>(t->data_ptr()); };
+  const void *const qp = q->data_ptr();
+  const int32_t *const tp = ints(table), *const sp = ints(starts), *const lp = ints(lens);
+  void *const op = out.data_ptr(), *const wp = ws ? ws->data_ptr() : nullptr;
+  float *const ep = lse ? static_cast<float *>(lse->data_ptr()) : nullptr;
+  const int64_t w_bytes = ws ? static_cast<int64_t>(ws->nbytes()) : 0;
+  int status;
+  Py_BEGIN_ALLOW_THREADS
+  status = api.paged_attn(&d, cache.c, qp, tp, sp, lp, op, ep, wp, w_bytes, stream);
+  Py_END_ALLOW_THREADS
+  return result(status, a[6], out);
+}
+
 // Anything torch throws (a tensor without storage, ...) happens before the launch: Python repeats
 // the call and reports it its own way.
 template <PyObject *(*F)(PyObject *const *, Py_ssize_t)>
@@ -401,12 +617,13 @@ PyObject *guarded(PyObject *, PyObject *const *args, Py_ssize_t n) {
 }
 
 // (addresses of attn, attn_commit, rope, route_min, route_mean, batch, batch_static, commit, commit_rope, rollback,
-// snapshot; torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, numpy.float32, the ctypes class of the cache)
+// snapshot, page_plan, rope_positions, paged_commit, paged_attn; torch._C._cuda_getDevice,
+// torch._C._cuda_getCurrentRawStream, numpy.float32, the ctypes classes of the cache and of the paged cache)
 PyObject *init(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  constexpr int kEntries = 11;
+  constexpr int kEntries = 15;
   int64_t p[kEntries];
-  if (n != kEntries + 4) {
-    PyErr_SetString(PyExc_TypeError, "init takes 15 arguments");
+  if (n != kEntries + 5) {
+    PyErr_SetString(PyExc_TypeError, "init takes 20 arguments");
     return nullptr;
   }
   for (int i = 0; i < kEntries; ++i)
@@ -418,7 +635,9 @@ PyObject *init(PyObject *, PyObject *const *a, Py_ssize_t n) {
   api = Api{reinterpret_cast<attn_fn>(p[0]),    reinterpret_cast<attn_commit_fn>(p[1]),  reinterpret_cast<rope_fn>(p[2]),
             reinterpret_cast<route_fn>(p[3]),   reinterpret_cast<route_fn>(p[4]),        reinterpret_cast<batch_fn>(p[5]),
             reinterpret_cast<batch_static_fn>(p[6]), reinterpret_cast<commit_fn>(p[7]),  reinterpret_cast<commit_rope_fn>(p[8]),
-            reinterpret_cast<rollback_fn>(p[9]), reinterpret_cast<snapshot_fn>(p[10]),   a[11], a[12], a[13], a[14]};
+            reinterpret_cast<rollback_fn>(p[9]), reinterpret_cast<snapshot_fn>(p[10]),   reinterpret_cast<page_plan_fn>(p[11]),
+            reinterpret_cast<rope_positions_fn>(p[12]), reinterpret_cast<paged_commit_fn>(p[13]),
+            reinterpret_cast<paged_attn_fn>(p[14]), a[15], a[16], a[17], a[18], a[19]};
   Py_RETURN_NONE;
 }
 
@@ -428,6 +647,8 @@ PyMethodDef methods[] = {METHOD("init", init), METHOD("block_attn", guarded<bloc
                          METHOD("rope", guarded<rope_impl>), METHOD("route", guarded<route_impl>),
                          METHOD("batch", guarded<batch_impl>), METHOD("commit", guarded<commit_impl>),
                          METHOD("rollback", guarded<rollback_impl>), METHOD("snapshot", guarded<snapshot_impl>),
+                         METHOD("page_plan", guarded<page_plan_impl>), METHOD("rope_positions", guarded<rope_positions_impl>),
+                         METHOD("paged_commit", guarded<paged_commit_impl>), METHOD("paged_attn", guarded<paged_attn_impl>),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", "Argument marshalling of libsdvg's most frequent calls.",
                           -1, methods, nullptr, nullptr, nullptr, nullptr};
