@@ -17,6 +17,7 @@
 #include <math.h>
 
 #include <mutex>
+#include <type_traits>
 
 #include "paged_attn_plan.h"
 #include "paged_kv.h"
@@ -38,6 +39,7 @@ typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kRows = 16;               // query rows per matrix product
 constexpr int kPad = 132;               // floats per row of O in LDS
+constexpr float kSlack = 8.0f;          // powers of two by which a probability may pass 1
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttnParams {
@@ -50,9 +52,12 @@ struct AttnParams {
   int64_t q_ts, q_hs, o_ts, o_hs, page_stride, token_stride, head_stride, table_stride;
   int64_t capacity;                   // keys a row of the table can name
   int32_t n_requests, n_tokens, n_heads, n_kv_heads, group, n_pages, table_width, window, target;
-  sdvg::FastDiv by_group, by_page;    // rows -> tokens; blocks of 8 keys -> pages
+  sdvg::FastDiv by_group, by_page, by_heads;  // rows -> tokens; blocks of 8 keys -> pages; workgroups -> items
   float scale_log2e;
 };
+
+// Workgroups per compute unit that registers leave room for.
+constexpr int resident(int nt) { return nt == 4 ? 1 : 2; }
 
 // ---- the two 16-bit types
 struct Bf16 {
@@ -92,15 +97,33 @@ __device__ __forceinline__ u32x4 widen(u32x2 w) {
   return u32x4{T::lo8(w[0]), T::hi8(w[0]), T::lo8(w[1]), T::hi8(w[1])};
 }
 
-// ---- over the 4 lanes that hold one query row (l, l ^ 16, l ^ 32, l ^ 48)
+// ---- over the 4 lanes that hold one query row (l, l ^ 16, l ^ 32, l ^ 48). A swap of a register with itself leaves the
+// pair's two values in its two results.
 __device__ __forceinline__ float rows_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 __device__ __forceinline__ float rows_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+// Sum over lanes 0 .. own of a wave: within rows of 16 lanes, then rows to the rows behind them.
+__device__ __forceinline__ int scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // last lane of rows 0, 2 to rows 1, 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2, 3
+  return x;
+}
+// 2^x; results below 2^-126 are 0, which a probability beside a largest one of 1 may be.
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(scan(x), 63); }
 
 // ---- which part of the work a workgroup has
 // Found by every wave for itself: lane i looks at request 64 b + i. Batches of 64 requests at a time.
@@ -117,28 +140,25 @@ __device__ __forceinline__ pg::Request load_request(const AttnParams &p, int r) 
 template <int kRowTile, bool kItems>
 __device__ __forceinline__ bool find(const AttnParams &p, int x, Found &f) {
   const int lane = threadIdx.x & 63;
-  pg::Request q = load_request<kRowTile>(p, lane);
-  int64_t total = pg::work_of(q);
-  for (int b = 64; b < p.n_requests; b += 64) {
-    const pg::Request o = load_request<kRowTile>(p, b + lane);
-    total += pg::work_of(o);
+  const pg::Request mine0 = load_request<kRowTile>(p, lane);
+  int32_t chunk = INT32_MAX;
+  if (p.target > 0) {
+    int64_t total = 0, row_tiles = 0;
+    for (int b = 0; b < p.n_requests; b += 64) {
+      const pg::Request q = b ? load_request<kRowTile>(p, b + lane) : mine0;
+      const int64_t w = pg::work_of(q);
+      row_tiles += wave_total(q.row_tiles);
+      total += wave_total(static_cast<int>(w & 0xffff)) + (static_cast<int64_t>(wave_total(static_cast<int>(w >> 16))) << 16);
+    }
+    chunk = pg::chunk_of(total, row_tiles, p.target);
   }
-  for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
-  const int32_t chunk = pg::chunk_of(total, p.target);
   int before = 0, slots_before = 0;
   for (int b = 0; b < p.n_requests; b += 64) {
-    if (b > 0) q = load_request<kRowTile>(p, b + lane);
+    const pg::Request q = b ? load_request<kRowTile>(p, b + lane) : mine0;
     const int32_t pieces = pg::pieces_of(q, chunk);
     const int32_t slots = pieces > 1 ? q.row_tiles * pieces : 0;
     const int32_t mine = kItems ? q.row_tiles * pieces : pieces > 1 ? q.row_tiles : 0;
-    int upto = mine, slots_upto = slots;  // inclusive
-    for (int d = 1; d < 64; d <<= 1) {
-      const int a = __shfl_up(upto, d), c = __shfl_up(slots_upto, d);
-      if (lane >= d) {
-        upto += a;
-        slots_upto += c;
-      }
-    }
+    const int upto = scan(mine), slots_upto = scan(slots);  // inclusive
     const int at = x - before - (upto - mine);
     const uint64_t hit = __ballot(at >= 0 && at < mine);
     if (hit) {
@@ -161,15 +181,16 @@ __device__ __forceinline__ bool find(const AttnParams &p, int x, Found &f) {
 
 // T: type of q, of P and of the output. kF8: the cache holds e4m3 numbers. NT: tiles of 16 query rows.
 template <typename T, bool kF8, int NT>
-__global__ __launch_bounds__(kThreads) void paged_attn_kernel(AttnParams p) {
+__global__ __launch_bounds__(kThreads, resident(NT)) void paged_attn_kernel(AttnParams p) {
   constexpr int kRowTile = kRows * NT;
   constexpr int kBytes = kF8 ? 1 : 2;
   __shared__ float o_s[kWaves][kRows][kPad];
   __shared__ float ml_s[kWaves][kRows][2];
   Found f;
-  if (!find<kRowTile, true>(p, blockIdx.x, f)) return;
+  // the key heads of an item are neighbours: together they read whole rows of the cache's tokens
+  const int item = p.by_heads.div(blockIdx.x), head = blockIdx.x - item * p.n_kv_heads;
+  if (!find<kRowTile, true>(p, item, f)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
-  const int head = blockIdx.y;
   const int rows = f.q.n * p.group - f.tile * kRowTile;   // rows of this tile, those past kRowTile included
 
   // the query rows of this lane: column col of every tile of 16
@@ -218,72 +239,61 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(AttnParams p) {
   const int32_t *table = p.table + f.request * p.table_stride;
   const char *k_head = static_cast<const char *>(p.k) + head * p.head_stride * kBytes,
              *v_head = static_cast<const char *>(p.v) + head * p.head_stride * kBytes;
-  // the page of a block of 8 keys, -1 if there is none
-  const auto page_of = [&](uint32_t block, uint32_t &place) {
-    const uint32_t i = p.by_page.div(block);
-    place = (block - i * p.by_page.d) * 8;
-    const int32_t page = i < static_cast<uint32_t>(p.table_width) ? table[i] : -1;
-    return page >= 0 && page < p.n_pages ? page : -1;
+  // One step's worth of K and V on the way from memory, and where it lies. Loads are issued a step ahead: K's when the
+  // scores of the step before are done, V's when its values have been transposed, the pages of the step after those then. A wave
+  // waits for memory only where the loads of a whole step take longer than a step.
+  struct Place {
+    int32_t page;      // -1: not there
+    uint32_t token;    // in its page, of the first of the 8 keys
   };
-  for (int tile = begin + wave; tile < end; tile += kWaves) {
+  const auto place_of = [&](uint32_t block) {
+    const uint32_t i = p.by_page.div(block);
+    const int32_t page = i < static_cast<uint32_t>(p.table_width) ? table[i] : -1;
+    return Place{page < p.n_pages ? page : -1, (block - i * p.by_page.d) * 8};
+  };
+  typedef typename std::conditional<kF8, u32x2, u32x4>::type chunk;  // 8 numbers
+  u32x4 kf[2][kF8 ? 2 : 4];
+  chunk vf[8];
+  // (a page that is not there reads page 0, which is memory of the pool; its keys do not count)
+  const auto load_k = [&](const Place &at) {
+    const char *row = k_head + ((at.page < 0 ? 0 : at.page) * p.page_stride + (at.token + (col & 3)) * p.token_stride) * kBytes + 16 * quad;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int s = 0; s < (kF8 ? 2 : 4); ++s)
+        kf[t][s] = *reinterpret_cast<const u32x4 *>(row + 4 * t * p.token_stride * kBytes + 64 * s);
+  };
+  const auto load_v = [&](const Place &at) {
+    const char *row = v_head + ((at.page < 0 ? 0 : at.page) * p.page_stride + at.token * p.token_stride) * kBytes + col * (8 * kBytes);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) vf[j] = __builtin_nontemporal_load(reinterpret_cast<const chunk *>(row + j * p.token_stride * kBytes));
+  };
+  Place k_next, v_next;  // of the step after the one whose loads are under way
+  // One step; kMore: another one follows.
+  const auto step = [&](int tile, int32_t v_page, auto more) {
+    constexpr bool kMore = decltype(more)::value;
     const int key0 = tile * pg::kKeyTile;
-    uint32_t k_place, v_place;
-    const int32_t k_page = page_of(key0 / 8 + (col >> 2), k_place), v_page = page_of(key0 / 8 + quad, v_place);
-    // (a page that is not there reads page 0, which is memory of the pool; its keys do not count)
-    const char *kp = k_head + ((k_page < 0 ? 0 : k_page) * p.page_stride + (k_place + (col & 3)) * p.token_stride) * kBytes;
-    const char *vp = v_head + ((v_page < 0 ? 0 : v_page) * p.page_stride + v_place * p.token_stride) * kBytes;
-    u32x4 kf[2][4];
-    u32x4 vf[8];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const char *row = kp + 4 * t * p.token_stride * kBytes;
-      if constexpr (kF8) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const u32x4 w = *reinterpret_cast<const u32x4 *>(row + 64 * s + 16 * quad);
-          kf[t][2 * s] = widen<T>(u32x2{w[0], w[1]});
-          kf[t][2 * s + 1] = widen<T>(u32x2{w[2], w[3]});
-        }
-      } else {
-#pragma unroll
-        for (int s = 0; s < 4; ++s) kf[t][s] = *reinterpret_cast<const u32x4 *>(row + 64 * s + 16 * quad);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const char *row = vp + j * p.token_stride * kBytes + col * (8 * kBytes);
-      if constexpr (kF8)
-        vf[j] = widen<T>(*reinterpret_cast<const u32x2 *>(row));
-      else
-        vf[j] = *reinterpret_cast<const u32x4 *>(row);
-    }
-    // keys of this lane's block of 8 that are there; V of the others is cleared (0 times anything but a number is no 0)
+    // keys of this lane's block of 8 that are there
     int there = f.q.len - (key0 + 8 * quad);
     there = v_page < 0 ? 0 : there < 0 ? 0 : there > 8 ? 8 : there;
-    const bool gaps = __any(there < 8);
-    if (gaps) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j >= there) vf[j] = u32x4{0, 0, 0, 0};
-    }
-    const bool masked = gaps || key0 + pg::kKeyTile > all_sees || key0 < all_from;
-    // V^T: dim 2e + h of keys 2c, 2c + 1 from dword e of both
-    u32x4 vt[8];
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        vt[2 * e][c] = __builtin_amdgcn_perm(vf[2 * c + 1][e], vf[2 * c][e], 0x05040100u);
-        vt[2 * e + 1][c] = __builtin_amdgcn_perm(vf[2 * c + 1][e], vf[2 * c][e], 0x07060302u);
-      }
+    const bool gaps = __any(there < 8), masked = gaps || key0 + pg::kKeyTile > all_sees || key0 < all_from;
+    u32x4 pf[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        s[0] = T::mfma(kf[0][c], qf[t][c], s[0]);
-        s[1] = T::mfma(kf[1][c], qf[t][c], s[1]);
-      }
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          u32x4 k;
+          if constexpr (kF8)
+            k = widen<T>(u32x2{kf[h][c >> 1][2 * (c & 1)], kf[h][c >> 1][2 * (c & 1) + 1]});
+          else
+            k = kf[h][c];
+          s[h] = T::mfma(k, qf[t][c], s[h]);
+        }
+      if constexpr (kMore)
+        if (t == NT - 1) load_k(k_next);
       float x[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * scale;
@@ -294,26 +304,76 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(AttnParams p) {
           x[e] = e < there && key < sees[t] && key >= from[t] ? x[e] : -INFINITY;
         }
       }
-      float top = x[0];
+      const float high = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      // m is raised only when some row's scores pass it by more than 2^kSlack: numerator and denominator share it, whatever it is
+      if (__any(high > m[t] + kSlack)) {
+        const float top = fmaxf(m[t], rows_max(high));
+        const float keep = m[t] == -INFINITY ? 0.f : exp2_of(m[t] - top);
+        m[t] = top;
+        l[t] *= keep;
 #pragma unroll
-      for (int e = 1; e < 8; ++e) top = fmaxf(top, x[e]);
-      top = fmaxf(m[t], rows_max(top));
-      const float base = top == -INFINITY ? 0.f : top;   // no key so far: every probability is 2^-inf
-      const float keep = exp2f(m[t] - base);
-      m[t] = top;
-      l[t] *= keep;
-#pragma unroll
-      for (int d = 0; d < 8; ++d) o[t][d] *= keep;
-      u32x4 pf;
+        for (int d = 0; d < 8; ++d) o[t][d] *= keep;
+      }
+      const float base = m[t] == -INFINITY ? 0.f : m[t];   // no key so far: every probability is 2^-inf
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        const float a = exp2f(x[2 * c] - base), b = exp2f(x[2 * c + 1] - base);
-        pf[c] = T::pack(a, b);
+        const float a = exp2_of(x[2 * c] - base), b = exp2_of(x[2 * c + 1] - base);
+        pf[t][c] = T::pack(a, b);
         l[t] += a + b;
       }
-#pragma unroll
-      for (int d = 0; d < 8; ++d) o[t][d] = T::mfma(vt[d], pf, o[t][d]);
     }
+    // V of keys that are not there is cleared (0 times anything but a number is no 0)
+    if (gaps) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (j >= there) vf[j] = chunk{};
+    }
+    // V^T: dim 2e + h of keys 2c, 2c + 1 from dword e of both
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      unsigned w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (kF8)
+          w[j] = e & 1 ? T::hi8(vf[j][e >> 1]) : T::lo8(vf[j][e >> 1]);
+        else
+          w[j] = vf[j][e];
+      }
+      u32x4 vt[2];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        vt[0][c] = __builtin_amdgcn_perm(w[2 * c + 1], w[2 * c], 0x05040100u);
+        vt[1][c] = __builtin_amdgcn_perm(w[2 * c + 1], w[2 * c], 0x07060302u);
+      }
+      if constexpr (kMore) {
+        if (e == 3) {
+          load_v(v_next);
+          const int block = tile + 2 * kWaves < end ? (tile + 2 * kWaves) * 4 : key0 / 8;
+          k_next = place_of(block + (col >> 2));
+          v_next = place_of(block + quad);
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) o[t][2 * e + h] = T::mfma(vt[h], pf[t], o[t][2 * e + h]);
+    }
+  };
+  int tile = begin + wave;
+  if (tile < end) {
+    const Place k_at = place_of(tile * 4 + (col >> 2)), v_at = place_of(tile * 4 + quad);
+    const int next = tile + kWaves < end ? tile + kWaves : tile;
+    k_next = place_of(next * 4 + (col >> 2));
+    v_next = place_of(next * 4 + quad);
+    load_k(k_at);
+    load_v(v_at);
+    int32_t page = v_at.page;
+    for (; tile + kWaves < end; tile += kWaves) {
+      const int32_t page_next = v_next.page;
+      step(tile, page, std::true_type{});
+      page = page_next;
+    }
+    step(tile, page, std::false_type{});
   }
 
   // The 4 waves' results of a tile of 16 rows meet in LDS; 16 threads finish a row.
@@ -343,7 +403,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(AttnParams p) {
     const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float weight = exp2f(ml_s[w][r][0] - base);
+      const float weight = exp2_of(ml_s[w][r][0] - base);
       total += weight * ml_s[w][r][1];
 #pragma unroll
       for (int j = 0; j < 8; ++j) acc[j] += weight * o_s[w][r][d0 + j];
@@ -370,42 +430,61 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(AttnParams p) {
   }
 }
 
-// Joins the pieces of one row: 32 threads have its dims, 8 sets of them every 8th piece.
+// Joins the pieces of the rows of a split row tile. 32 threads have a row's dims; the 8 sets of them in a workgroup have
+// a row each where the pieces are few, and share the pieces of one row where they are many.
 template <typename T, bool kF8, int NT>
 __global__ __launch_bounds__(kThreads) void paged_join_kernel(AttnParams p) {
-  constexpr int kRowTile = kRows * NT;
-  __shared__ f32x4 o_s[kThreads / 32][32];
+  constexpr int kRowTile = kRows * NT, kSets = kThreads / 32;
+  __shared__ f32x4 o_s[kSets][32];
+  __shared__ float ml_s[kSets][2];
   Found f;
-  if (!find<kRowTile, false>(p, blockIdx.x, f)) return;
-  const int head = blockIdx.y, row = blockIdx.z, lane = threadIdx.x & 63;
-  if (f.tile * kRowTile + row >= f.q.n * p.group) return;
+  const int index = p.by_heads.div(blockIdx.x), head = blockIdx.x - index * p.n_kv_heads;
+  if (!find<kRowTile, false>(p, index, f)) return;
+  const int left = f.q.n * p.group - f.tile * kRowTile, rows = left < kRowTile ? left : kRowTile;
   const int64_t step = static_cast<int64_t>(p.n_kv_heads) * kRowTile;   // rows between two pieces
-  const int64_t at = (static_cast<int64_t>(f.slot) * p.n_kv_heads + head) * kRowTile + row;
-  float top = -INFINITY, total = 0.f;
-  for (int i = lane; i < f.pieces; i += 64) top = fmaxf(top, p.part_ml[(at + i * step) * 2]);
-  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  const float base = top == -INFINITY ? 0.f : top;
-  for (int i = lane; i < f.pieces; i += 64)
-    total += exp2f(p.part_ml[(at + i * step) * 2] - base) * p.part_ml[(at + i * step) * 2 + 1];
-  for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
   const int d4 = threadIdx.x & 31, set = threadIdx.x >> 5;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int i = set; i < f.pieces; i += kThreads / 32) {
-    const float weight = exp2f(p.part_ml[(at + i * step) * 2] - base);
-    acc += weight * reinterpret_cast<const f32x4 *>(p.part_o + (at + i * step) * 128)[d4];
+  const bool shared = f.pieces > 2 * kSets;
+  const int first = shared ? blockIdx.y : blockIdx.y * kSets + set, rows_step = shared ? gridDim.y : gridDim.y * kSets;
+  for (int row = first; row < rows; row += rows_step) {
+    const int64_t at = (static_cast<int64_t>(f.slot) * p.n_kv_heads + head) * kRowTile + row;
+    float top = -INFINITY, total = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = shared ? set : 0; i < f.pieces; i += shared ? kSets : 1) {
+      const f32x2 ml = *reinterpret_cast<const f32x2 *>(p.part_ml + (at + i * step) * 2);
+      const f32x4 o = reinterpret_cast<const f32x4 *>(p.part_o + (at + i * step) * 128)[d4];
+      const float high = fmaxf(top, ml[0]), base = high == -INFINITY ? 0.f : high;
+      const float keep = exp2_of(top - base), weight = exp2_of(ml[0] - base);
+      top = high;
+      total = total * keep + ml[1] * weight;
+      acc = acc * keep + o * weight;
+    }
+    if (shared) {   // (one row for the whole workgroup: all threads come here)
+      __syncthreads();
+      o_s[set][d4] = acc;
+      if (d4 == 0) {
+        ml_s[set][0] = top;
+        ml_s[set][1] = total;
+      }
+      __syncthreads();
+      if (set != 0) continue;
+      for (int w = 1; w < kSets; ++w) top = fmaxf(top, ml_s[w][0]);
+      const float base = top == -INFINITY ? 0.f : top;
+      acc = f32x4{0.f, 0.f, 0.f, 0.f};
+      total = 0.f;
+      for (int w = 0; w < kSets; ++w) {
+        const float weight = exp2_of(ml_s[w][0] - base);
+        total += weight * ml_s[w][1];
+        acc += weight * o_s[w][d4];
+      }
+    }
+    const uint32_t all = f.tile * kRowTile + row, i = p.by_group.div(all), h = all - i * p.group;
+    const int64_t token = f.q.row0 + static_cast<int64_t>(i), q_head = static_cast<int64_t>(head) * p.group + h;
+    acc *= top == -INFINITY ? 0.f : (kF8 && p.v_scale ? p.v_scale[head] : 1.0f) / total;
+    const u32x2 w = {T::pack(acc[0], acc[1]), T::pack(acc[2], acc[3])};
+    *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(p.out) + token * p.o_ts + q_head * p.o_hs + 4 * d4) = w;
+    if (p.lse && d4 == 0) p.lse[token * p.n_heads + q_head] = top == -INFINITY ? -INFINITY : (top + log2f(total)) * kLn2;
   }
-  o_s[set][d4] = acc;
-  __syncthreads();
-  if (set != 0) return;
-#pragma unroll
-  for (int w = 1; w < kThreads / 32; ++w) acc += o_s[w][d4];
-  const uint32_t all = f.tile * kRowTile + row, i = p.by_group.div(all), h = all - i * p.group;
-  const int64_t token = f.q.row0 + static_cast<int64_t>(i), q_head = static_cast<int64_t>(head) * p.group + h;
-  const float norm = top == -INFINITY ? 0.f : (kF8 && p.v_scale ? p.v_scale[head] : 1.0f) / total;
-  acc *= norm;
-  const u32x2 w = {T::pack(acc[0], acc[1]), T::pack(acc[2], acc[3])};
-  *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(p.out) + token * p.o_ts + q_head * p.o_hs + 4 * d4) = w;
-  if (p.lse && d4 == 0) p.lse[token * p.n_heads + q_head] = top == -INFINITY ? -INFINITY : (top + log2f(total)) * kLn2;
 }
 
 constexpr int kMaxDevices = 64;
@@ -428,9 +507,9 @@ int row_tiles_of(int64_t n_requests, int64_t n_tokens, int group) {
   return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
 }
 
-// Items per key head that a launch aims at.
-int target_of(int n_cu, int n_kv_heads) {
-  const int t = 4 * n_cu / n_kv_heads;
+// Items per key head that fill the chip once.
+int target_of(int n_cu, int n_kv_heads, int nt) {
+  const int t = resident(nt) * n_cu / n_kv_heads;
   return t > 1 ? t : 1;
 }
 
@@ -458,13 +537,18 @@ template <typename T, bool kF8, int NT>
 int launch_attn(const AttnParams &p, hipStream_t s) {
   const int64_t tiles = pg::max_row_tiles(p.n_requests, p.n_tokens, p.group, kRows * NT);
   const int64_t items = pg::max_items(tiles, p.target);
-  if (items > (INT32_MAX / kThreads)) return SDVG_ERR_UNSUPPORTED;
-  hipLaunchKernelGGL((paged_attn_kernel<T, kF8, NT>), dim3(static_cast<uint32_t>(items), p.n_kv_heads), dim3(kThreads), 0, s, p);
+  if (items * p.n_kv_heads >= (1 << 24)) return SDVG_ERR_UNSUPPORTED;  // (a grid holds fewer than 2^32 threads)
+  hipLaunchKernelGGL((paged_attn_kernel<T, kF8, NT>), dim3(static_cast<uint32_t>(items * p.n_kv_heads)), dim3(kThreads), 0, s, p);
   SDVG_HIP_CHECK(hipGetLastError());
   if (p.target > 0) {
-    const int64_t rows = static_cast<int64_t>(p.n_tokens) * p.group;
+    // Workgroups per row tile: one for every row of an average request's where that are few (then the pieces are many, and
+    // shared), otherwise one for every 8 rows. A workgroup takes more rows where there are more.
+    const int64_t groups = pg::max_groups(tiles, p.target) * p.n_kv_heads;
+    int64_t rows = (static_cast<int64_t>(p.n_tokens) + p.n_requests - 1) / p.n_requests * p.group;
+    rows = rows < kRows * NT ? rows : kRows * NT;
+    if (groups * rows > 1024) rows = (rows + 7) / 8;
     hipLaunchKernelGGL((paged_join_kernel<T, kF8, NT>),
-                       dim3(p.target, p.n_kv_heads, static_cast<uint32_t>(rows < kRows * NT ? rows : kRows * NT)),
+                       dim3(static_cast<uint32_t>(groups), static_cast<uint32_t>(rows)),
                        dim3(kThreads), 0, s, p);
     SDVG_HIP_CHECK(hipGetLastError());
   }
@@ -482,8 +566,8 @@ extern "C" int64_t sdvg_paged_attn_workspace_bytes(const sdvg_paged_attn_desc *d
   if (st != SDVG_OK) return st;
   if (desc->n_requests == 0 || desc->n_tokens == 0) return 0;
   if ((st = compute_units(n_cu)) != SDVG_OK) return st;
-  return workspace_of(target_of(n_cu, cache->n_kv_heads), cache->n_kv_heads,
-                      row_tiles_of(desc->n_requests, desc->n_tokens, desc->n_heads / cache->n_kv_heads));
+  const int nt = row_tiles_of(desc->n_requests, desc->n_tokens, desc->n_heads / cache->n_kv_heads);
+  return workspace_of(target_of(n_cu, cache->n_kv_heads, nt), cache->n_kv_heads, nt);
 }
 
 extern "C" int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_paged_kv *cache, const void *q,
@@ -537,9 +621,10 @@ extern "C" int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_page
   p.table_width = desc->table_width;
   p.window = desc->window;
   p.by_group = sdvg::FastDiv::of(p.group);
+  p.by_heads = sdvg::FastDiv::of(p.n_kv_heads);
   p.by_page = sdvg::FastDiv::of(cache->page_tokens / 8);
   p.scale_log2e = (desc->scale == 0.f ? 1.0f / sqrtf(128.0f) : desc->scale) * kLog2e;
-  const int nt = row_tiles_of(p.n_requests, p.n_tokens, p.group), target = target_of(n_cu, p.n_kv_heads);
+  const int nt = row_tiles_of(p.n_requests, p.n_tokens, p.group), target = target_of(n_cu, p.n_kv_heads, nt);
   if (workspace && workspace_bytes >= workspace_of(target, p.n_kv_heads, nt)) {
     p.target = target;
     p.part_o = static_cast<float *>(workspace);

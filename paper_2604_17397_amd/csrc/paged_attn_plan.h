@@ -2,8 +2,7 @@
 // kernels do on the device (lengths are device data) and a host test repeats.
 //
 // The rows of a request that share a key head (its new tokens x the query heads of the group) are cut into tiles of
-// row_tile rows. Work is counted in (row tile, key tile) pairs; `chunk` key tiles at most go to one workgroup ("item"), so
-// that the launch has about `target` items per key head whatever the lengths are. A request whose keys fit one chunk is
+// row_tile rows. Work is counted in (row tile, key tile) pairs; `chunk` key tiles at most go to one workgroup ("item"). A request whose keys fit one chunk is
 // written by its workgroup; the others leave a partial result per item in a numbered slot, and the join adds up a
 // group of consecutive slots per row tile.
 #pragma once
@@ -49,10 +48,15 @@ SDVG_PAGED_HD Request request_of(int32_t start, int32_t end, int32_t len, int32_
 // (A row tile without keys still is an item: somebody has to write its zeros.)
 SDVG_PAGED_HD int64_t work_of(const Request &q) { return static_cast<int64_t>(q.row_tiles) * (q.tiles > 1 ? q.tiles : 1); }
 
-// Key tiles per item at most: total = the sum of work_of. target <= 0: no split.
-SDVG_PAGED_HD int32_t chunk_of(int64_t total, int32_t target) {
+// Key tiles per item at most: total = the sum of work_of over all requests, row_tiles that of theirs, target the items that fill
+// the chip once (<= 0: no split). With few row tiles the items are made to be at most `target`, so that all run at once and
+// end together; every row tile may add one by rounding up. With many row tiles that would leave some items much
+// longer than others: then they are made kFiner times shorter, and the chip fills up again as they end.
+constexpr int kFiner = 2;
+SDVG_PAGED_HD int32_t chunk_of(int64_t total, int64_t row_tiles, int32_t target) {
   if (target <= 0) return INT32_MAX;
-  const int64_t c = (total + target - 1) / target;
+  const int64_t items = 4 * row_tiles <= target ? target - row_tiles : static_cast<int64_t>(kFiner) * target;
+  const int64_t c = (total + items - 1) / items;
   return c > kMinChunk ? static_cast<int32_t>(c < INT32_MAX ? c : INT32_MAX) : kMinChunk;
 }
 // Items per row tile.
@@ -64,15 +68,17 @@ SDVG_PAGED_HD int32_t piece_begin(int32_t tiles, int32_t i, int32_t n) {
   return static_cast<int32_t>(static_cast<int64_t>(tiles) * i / n);
 }
 
-// Bounds for the launch, from what the host knows. Items: total / chunk <= target of full chunks, and one more per row tile.
-// Slots: a split row tile of t > chunk tiles has ceil(t / chunk) < 2 t / chunk pieces. Groups (split row tiles): t > chunk each.
+// Bounds for the launch, from what the host knows, with most = kFiner * target >= total / chunk. Items: most full chunks, and one
+// more per row tile. Slots: a split row tile of t > chunk tiles has ceil(t / chunk) < 2 t / chunk pieces. Groups (split row tiles): t >
+// chunk each.
 SDVG_PAGED_HD int64_t max_row_tiles(int64_t n_requests, int64_t n_tokens, int32_t group, int32_t row_tile) {
   const int64_t rows = n_tokens * group;
   const int64_t bound = rows / row_tile + n_requests;
   return bound < rows ? bound : rows;
 }
-SDVG_PAGED_HD int64_t max_items(int64_t row_tiles, int32_t target) { return row_tiles + (target > 0 ? target : 0); }
-SDVG_PAGED_HD int64_t max_slots(int32_t target) { return 2 * static_cast<int64_t>(target); }
+SDVG_PAGED_HD int64_t max_items(int64_t row_tiles, int32_t target) { return row_tiles + (target > 0 ? kFiner * static_cast<int64_t>(target) : 0); }
+SDVG_PAGED_HD int64_t max_groups(int64_t row_tiles, int32_t target) { return row_tiles < kFiner * static_cast<int64_t>(target) ? row_tiles : kFiner * static_cast<int64_t>(target); }
+SDVG_PAGED_HD int64_t max_slots(int32_t target) { return 2 * kFiner * static_cast<int64_t>(target); }
 
 }  // namespace paged
 }  // namespace sdvg

@@ -50,8 +50,9 @@ static void one(int R, int longest, int most_new, int group, int row_tile, int w
     if (hi > lo) CHECK(q[r].first_tile * 32ll <= lo && (q[r].first_tile + int64_t{q[r].tiles}) * 32 >= hi && (q[r].first_tile + int64_t{q[r].tiles} - 1) * 32 < hi);
     else CHECK(q[r].tiles == 0);
   }
-  const int32_t chunk = pg::chunk_of(total, target);
-  int64_t items = 0, slots = 0, groups = 0, row_tiles = 0;
+  int64_t items = 0, slots = 0, groups = 0, row_tiles = 0, all_row_tiles = 0;
+  for (const pg::Request &x : q) all_row_tiles += x.row_tiles;
+  const int32_t chunk = pg::chunk_of(total, all_row_tiles, target);
   for (int r = 0; r < R; ++r) {
     const int n = pg::pieces_of(q[r], chunk);
     row_tiles += q[r].row_tiles;
@@ -66,10 +67,11 @@ static void one(int R, int longest, int most_new, int group, int row_tile, int w
       CHECK(share >= (n > 1 ? 1 : 0) && share <= chunk);
     }
   }
+  if (4 * row_tiles <= target) CHECK(items <= target);
   CHECK(row_tiles <= pg::max_row_tiles(R, tokens, group, row_tile));
   CHECK(items <= pg::max_items(pg::max_row_tiles(R, tokens, group, row_tile), target));
   CHECK(slots <= pg::max_slots(target > 0 ? target : 0));
-  CHECK(groups <= (target > 0 ? target : 0));
+  CHECK(groups <= (target > 0 ? pg::max_groups(row_tiles, target) : 0));
 }
 
 int main() {
