@@ -5,7 +5,7 @@
 // query row; up to some hundred rows per key head the time is the HBM's. So there is no staging through LDS: the matrix
 // instructions take both K and V straight from registers as they come from memory.
 //
-// A wave takes 32 keys per step, the 16 (NT tiles of 16) query rows of a request that share a key head as columns:
+// A wave takes 32 keys per step, and 16 query rows (NT tiles of 16) of a request that share a key head as columns:
 //   S^T = K Q^T with v_mfma_f32_16x16x32: lane l holds 8 consecutive dims of key row l % 16, one 16-byte load. The
 //     key rows of the two 16-row products are dealt out so that lane l's 8 scores (rows 4 (l / 16) .. + 3 of both) belong to
 //     the keys 8 (l / 16) .. + 7 of the step, in order, and to query row l % 16.
@@ -36,7 +36,7 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
 
-constexpr int kThreads = 256, kWaves = 4;
+constexpr int kJoinThreads = 256;
 constexpr int kRows = 16;               // query rows per matrix product
 constexpr int kPad = 132;               // floats per row of O in LDS
 constexpr float kSlack = 8.0f;          // powers of two by which a probability may pass 1
@@ -56,8 +56,11 @@ struct AttnParams {
   float scale_log2e;
 };
 
-// Workgroups per compute unit that registers leave room for.
-constexpr int resident(int nt) { return nt == 4 ? 1 : 2; }
+// Rows of a workgroup: NT tiles of 16 per wave, RS sets of 4 waves with different rows and the same keys (they share K and V
+// through the caches). Two waves per SIMD are what the registers leave room for.
+constexpr int kKeyWaves = 4;
+constexpr int row_tile(int nt, int rs) { return kRows * nt * rs; }
+constexpr int per_unit(int row_tile) { return row_tile == 64 ? 1 : 2; }  // workgroups per compute unit
 
 // ---- the two 16-bit types
 struct Bf16 {
@@ -179,10 +182,11 @@ __device__ __forceinline__ bool find(const AttnParams &p, int x, Found &f) {
   return false;
 }
 
-// T: type of q, of P and of the output. kF8: the cache holds e4m3 numbers. NT: tiles of 16 query rows.
-template <typename T, bool kF8, int NT>
-__global__ __launch_bounds__(kThreads, resident(NT)) void paged_attn_kernel(AttnParams p) {
-  constexpr int kRowTile = kRows * NT;
+// T: type of q, of P and of the output. kF8: the cache holds e4m3 numbers.
+template <typename T, bool kF8, int NT, int RS>
+__global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(AttnParams p) {
+  constexpr int kRowTile = row_tile(NT, RS), kWaves = kKeyWaves * RS, kThreads = 64 * kWaves;
+  constexpr int kDims = 128 * kRows * RS / kThreads;   // per thread where the workgroup finishes rows
   constexpr int kBytes = kF8 ? 1 : 2;
   __shared__ float o_s[kWaves][kRows][kPad];
   __shared__ float ml_s[kWaves][kRows][2];
@@ -192,13 +196,14 @@ __global__ __launch_bounds__(kThreads, resident(NT)) void paged_attn_kernel(Attn
   if (!find<kRowTile, true>(p, item, f)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
   const int rows = f.q.n * p.group - f.tile * kRowTile;   // rows of this tile, those past kRowTile included
+  const int row0 = wave / kKeyWaves * (NT * kRows);       // this wave's first
 
   // the query rows of this lane: column col of every tile of 16
   u32x4 qf[NT][4];
   int32_t sees[NT], from[NT];   // keys from[..] <= j < sees[..]
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const int row = t * kRows + col;
+    const int row = row0 + t * kRows + col;
     const uint32_t all = f.tile * kRowTile + row, i = p.by_group.div(all), h = all - i * p.group;
     sees[t] = from[t] = 0;
 #pragma unroll
@@ -348,7 +353,7 @@ __global__ __launch_bounds__(kThreads, resident(NT)) void paged_attn_kernel(Attn
       if constexpr (kMore) {
         if (e == 3) {
           load_v(v_next);
-          const int block = tile + 2 * kWaves < end ? (tile + 2 * kWaves) * 4 : key0 / 8;
+          const int block = tile + 2 * kKeyWaves < end ? (tile + 2 * kKeyWaves) * 4 : key0 / 8;
           k_next = place_of(block + (col >> 2));
           v_next = place_of(block + quad);
         }
@@ -359,16 +364,16 @@ __global__ __launch_bounds__(kThreads, resident(NT)) void paged_attn_kernel(Attn
         for (int t = 0; t < NT; ++t) o[t][2 * e + h] = T::mfma(vt[h], pf[t], o[t][2 * e + h]);
     }
   };
-  int tile = begin + wave;
-  if (tile < end) {
+  int tile = begin + wave % kKeyWaves;
+  if (tile < end && row0 < rows) {
     const Place k_at = place_of(tile * 4 + (col >> 2)), v_at = place_of(tile * 4 + quad);
-    const int next = tile + kWaves < end ? tile + kWaves : tile;
+    const int next = tile + kKeyWaves < end ? tile + kKeyWaves : tile;
     k_next = place_of(next * 4 + (col >> 2));
     v_next = place_of(next * 4 + quad);
     load_k(k_at);
     load_v(v_at);
     int32_t page = v_at.page;
-    for (; tile + kWaves < end; tile += kWaves) {
+    for (; tile + kKeyWaves < end; tile += kKeyWaves) {
       const int32_t page_next = v_next.page;
       step(tile, page, std::true_type{});
       page = page_next;
@@ -376,7 +381,7 @@ __global__ __launch_bounds__(kThreads, resident(NT)) void paged_attn_kernel(Attn
     step(tile, page, std::false_type{});
   }
 
-  // The 4 waves' results of a tile of 16 rows meet in LDS; 16 threads finish a row.
+  // The waves' results of a tile of 16 rows meet in LDS.
   const float v_scale = kF8 && p.v_scale ? p.v_scale[head] : 1.0f;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -394,47 +399,47 @@ __global__ __launch_bounds__(kThreads, resident(NT)) void paged_attn_kernel(Attn
       ml_s[wave][col][1] = sum;
     }
     __syncthreads();
-    const int r = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * 8;
-    const int row = t * kRows + r;
+    constexpr int kPerRow = 128 / kDims;
+    const int r = threadIdx.x / kPerRow, d0 = threadIdx.x % kPerRow * kDims, set = r / kRows, c = r % kRows;
+    const int row = set * (NT * kRows) + t * kRows + c;
     if (row >= rows) continue;   // (all waves come to the barriers: `rows` is the workgroup's)
-    float top = ml_s[0][r][0], total = 0.f, acc[8] = {};
+    const float(*const ml)[kRows][2] = ml_s + set * kKeyWaves;
+    float top = ml[0][c][0], total = 0.f;
+    f32x4 acc[kDims / 4] = {};
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ml_s[w][r][0]);
+    for (int w = 1; w < kKeyWaves; ++w) top = fmaxf(top, ml[w][c][0]);
     const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float weight = exp2_of(ml_s[w][r][0] - base);
-      total += weight * ml_s[w][r][1];
+    for (int w = 0; w < kKeyWaves; ++w) {
+      const float weight = exp2_of(ml[w][c][0] - base);
+      total += weight * ml[w][c][1];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] += weight * o_s[w][r][d0 + j];
+      for (int j = 0; j < kDims / 4; ++j)
+        acc[j] += weight * *reinterpret_cast<const f32x4 *>(&o_s[set * kKeyWaves + w][c][d0 + 4 * j]);
     }
     if (f.pieces > 1) {
       const int64_t at = (static_cast<int64_t>(f.slot + f.piece) * p.n_kv_heads + head) * kRowTile + row;
-      f32x4 *dst = reinterpret_cast<f32x4 *>(p.part_o + at * 128 + d0);
-      dst[0] = f32x4{acc[0], acc[1], acc[2], acc[3]};
-      dst[1] = f32x4{acc[4], acc[5], acc[6], acc[7]};
-      if (d0 == 0) {
-        p.part_ml[at * 2] = top;
-        p.part_ml[at * 2 + 1] = total;
-      }
+#pragma unroll
+      for (int j = 0; j < kDims / 4; ++j) reinterpret_cast<f32x4 *>(p.part_o + at * 128 + d0)[j] = acc[j];
+      if (d0 == 0) *reinterpret_cast<f32x2 *>(p.part_ml + at * 2) = f32x2{top, total};
       continue;
     }
     const uint32_t all = f.tile * kRowTile + row, i = p.by_group.div(all), h = all - i * p.group;
     const int64_t token = f.q.row0 + static_cast<int64_t>(i), q_head = static_cast<int64_t>(head) * p.group + h;
     const float norm = top == -INFINITY ? 0.f : v_scale / total;   // (sum 0 only without a key)
-    u32x4 w;
+    uint16_t *dst = static_cast<uint16_t *>(p.out) + token * p.o_ts + q_head * p.o_hs + d0;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) w[c] = T::pack(acc[2 * c] * norm, acc[2 * c + 1] * norm);
-    *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(p.out) + token * p.o_ts + q_head * p.o_hs + d0) = w;
+    for (int j = 0; j < kDims / 4; ++j)
+      reinterpret_cast<u32x2 *>(dst)[j] = u32x2{T::pack(acc[j][0] * norm, acc[j][1] * norm), T::pack(acc[j][2] * norm, acc[j][3] * norm)};
     if (p.lse && d0 == 0) p.lse[token * p.n_heads + q_head] = top == -INFINITY ? -INFINITY : (top + log2f(total)) * kLn2;
   }
 }
 
 // Joins the pieces of the rows of a split row tile. 32 threads have a row's dims; the 8 sets of them in a workgroup have
 // a row each where the pieces are few, and share the pieces of one row where they are many.
-template <typename T, bool kF8, int NT>
-__global__ __launch_bounds__(kThreads) void paged_join_kernel(AttnParams p) {
-  constexpr int kRowTile = kRows * NT, kSets = kThreads / 32;
+template <typename T, bool kF8, int NT, int RS>
+__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(AttnParams p) {
+  constexpr int kRowTile = row_tile(NT, RS), kSets = kJoinThreads / 32;
   __shared__ f32x4 o_s[kSets][32];
   __shared__ float ml_s[kSets][2];
   Found f;
@@ -501,20 +506,20 @@ int compute_units(int &n) {
   return SDVG_OK;
 }
 
-// Tiles of 16 rows per workgroup, by the average request: K and V are then read once per key head.
-int row_tiles_of(int64_t n_requests, int64_t n_tokens, int group) {
+// Rows per workgroup by the average request, so that K and V are read once per key head as a rule.
+int row_tile_of(int64_t n_requests, int64_t n_tokens, int group) {
   const int64_t rows = (n_tokens + n_requests - 1) / n_requests * group;
-  return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
 }
 
 // Items per key head that fill the chip once.
-int target_of(int n_cu, int n_kv_heads, int nt) {
-  const int t = resident(nt) * n_cu / n_kv_heads;
+int target_of(int n_cu, int n_kv_heads, int row_tile) {
+  const int t = per_unit(row_tile) * n_cu / n_kv_heads;
   return t > 1 ? t : 1;
 }
 
-int64_t workspace_of(int target, int n_kv_heads, int nt) {
-  return pg::max_slots(target) * n_kv_heads * (kRows * nt) * (128 + 2) * 4;
+int64_t workspace_of(int target, int n_kv_heads, int row_tile) {
+  return pg::max_slots(target) * n_kv_heads * row_tile * (128 + 2) * 4;
 }
 
 int check_attn(const sdvg_paged_attn_desc *d, const sdvg_paged_kv *c) {
@@ -533,30 +538,32 @@ int check_attn(const sdvg_paged_attn_desc *d, const sdvg_paged_kv *c) {
   return SDVG_OK;
 }
 
-template <typename T, bool kF8, int NT>
+template <typename T, bool kF8, int NT, int RS>
 int launch_attn(const AttnParams &p, hipStream_t s) {
-  const int64_t tiles = pg::max_row_tiles(p.n_requests, p.n_tokens, p.group, kRows * NT);
+  constexpr int kRowTile = row_tile(NT, RS), kThreads = 64 * kKeyWaves * RS;
+  const int64_t tiles = pg::max_row_tiles(p.n_requests, p.n_tokens, p.group, kRowTile);
   const int64_t items = pg::max_items(tiles, p.target);
-  if (items * p.n_kv_heads >= (1 << 24)) return SDVG_ERR_UNSUPPORTED;  // (a grid holds fewer than 2^32 threads)
-  hipLaunchKernelGGL((paged_attn_kernel<T, kF8, NT>), dim3(static_cast<uint32_t>(items * p.n_kv_heads)), dim3(kThreads), 0, s, p);
+  if (items * p.n_kv_heads >= (1 << 23)) return SDVG_ERR_UNSUPPORTED;  // (a grid holds fewer than 2^32 threads)
+  hipLaunchKernelGGL((paged_attn_kernel<T, kF8, NT, RS>), dim3(static_cast<uint32_t>(items * p.n_kv_heads)), dim3(kThreads), 0, s, p);
   SDVG_HIP_CHECK(hipGetLastError());
   if (p.target > 0) {
     // Workgroups per row tile: one for every row of an average request's where that are few (then the pieces are many, and
     // shared), otherwise one for every 8 rows. A workgroup takes more rows where there are more.
     const int64_t groups = pg::max_groups(tiles, p.target) * p.n_kv_heads;
     int64_t rows = (static_cast<int64_t>(p.n_tokens) + p.n_requests - 1) / p.n_requests * p.group;
-    rows = rows < kRows * NT ? rows : kRows * NT;
+    rows = rows < kRowTile ? rows : kRowTile;
     if (groups * rows > 1024) rows = (rows + 7) / 8;
-    hipLaunchKernelGGL((paged_join_kernel<T, kF8, NT>),
-                       dim3(static_cast<uint32_t>(groups), static_cast<uint32_t>(rows)),
-                       dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((paged_join_kernel<T, kF8, NT, RS>), dim3(static_cast<uint32_t>(groups), static_cast<uint32_t>(rows)),
+                       dim3(kJoinThreads), 0, s, p);
     SDVG_HIP_CHECK(hipGetLastError());
   }
   return SDVG_OK;
 }
 template <typename T, bool kF8>
-int launch_attn(const AttnParams &p, int nt, hipStream_t s) {
-  return nt == 1 ? launch_attn<T, kF8, 1>(p, s) : nt == 2 ? launch_attn<T, kF8, 2>(p, s) : launch_attn<T, kF8, 4>(p, s);
+int launch_attn(const AttnParams &p, int row_tile, hipStream_t s) {
+  return row_tile == 16   ? launch_attn<T, kF8, 1, 1>(p, s)
+         : row_tile == 32 ? launch_attn<T, kF8, 2, 1>(p, s)
+                          : launch_attn<T, kF8, 2, 2>(p, s);
 }
 
 }  // namespace
@@ -566,8 +573,8 @@ extern "C" int64_t sdvg_paged_attn_workspace_bytes(const sdvg_paged_attn_desc *d
   if (st != SDVG_OK) return st;
   if (desc->n_requests == 0 || desc->n_tokens == 0) return 0;
   if ((st = compute_units(n_cu)) != SDVG_OK) return st;
-  const int nt = row_tiles_of(desc->n_requests, desc->n_tokens, desc->n_heads / cache->n_kv_heads);
-  return workspace_of(target_of(n_cu, cache->n_kv_heads, nt), cache->n_kv_heads, nt);
+  const int tile = row_tile_of(desc->n_requests, desc->n_tokens, desc->n_heads / cache->n_kv_heads);
+  return workspace_of(target_of(n_cu, cache->n_kv_heads, tile), cache->n_kv_heads, tile);
 }
 
 extern "C" int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_paged_kv *cache, const void *q,
@@ -624,14 +631,14 @@ extern "C" int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_page
   p.by_heads = sdvg::FastDiv::of(p.n_kv_heads);
   p.by_page = sdvg::FastDiv::of(cache->page_tokens / 8);
   p.scale_log2e = (desc->scale == 0.f ? 1.0f / sqrtf(128.0f) : desc->scale) * kLog2e;
-  const int nt = row_tiles_of(p.n_requests, p.n_tokens, p.group), target = target_of(n_cu, p.n_kv_heads, nt);
-  if (workspace && workspace_bytes >= workspace_of(target, p.n_kv_heads, nt)) {
+  const int tile = row_tile_of(p.n_requests, p.n_tokens, p.group), target = target_of(n_cu, p.n_kv_heads, tile);
+  if (workspace && workspace_bytes >= workspace_of(target, p.n_kv_heads, tile)) {
     p.target = target;
     p.part_o = static_cast<float *>(workspace);
-    p.part_ml = p.part_o + pg::max_slots(target) * p.n_kv_heads * (kRows * nt) * 128;
+    p.part_ml = p.part_o + pg::max_slots(target) * p.n_kv_heads * tile * 128;
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool f8 = cache->dtype == SDVG_E4M3;
-  if (desc->dtype == SDVG_BF16) return f8 ? launch_attn<Bf16, true>(p, nt, s) : launch_attn<Bf16, false>(p, nt, s);
-  return f8 ? launch_attn<F16, true>(p, nt, s) : launch_attn<F16, false>(p, nt, s);
+  if (desc->dtype == SDVG_BF16) return f8 ? launch_attn<Bf16, true>(p, tile, s) : launch_attn<Bf16, false>(p, tile, s);
+  return f8 ? launch_attn<F16, true>(p, tile, s) : launch_attn<F16, false>(p, tile, s);
 }

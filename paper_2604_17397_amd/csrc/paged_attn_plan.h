@@ -19,7 +19,7 @@ namespace sdvg {
 namespace paged {
 
 constexpr int kKeyTile = 32;   // keys a wave takes per step
-constexpr int kMinChunk = 4;   // key tiles: one per wave of a workgroup
+constexpr int kMinChunk = 4;   // key tiles of an item at least: one per wave
 
 // What a request asks for.
 struct Request {
@@ -51,12 +51,20 @@ SDVG_PAGED_HD int64_t work_of(const Request &q) { return static_cast<int64_t>(q.
 // Key tiles per item at most: total = the sum of work_of over all requests, row_tiles that of theirs, target the items that fill
 // the chip once (<= 0: no split). With few row tiles the items are made to be at most `target`, so that all run at once and
 // end together; every row tile may add one by rounding up. With many row tiles that would leave some items much
-// longer than others: then they are made kFiner times shorter, and the chip fills up again as they end.
-constexpr int kFiner = 2;
+// longer than others: then they are made shorter, kFiner rounds of them, and the chip fills up again as they end; but not shorter
+// than kRoundChunk (what comes before and after the keys takes as long as some 10 key tiles) unless the chip is not filled once.
+constexpr int kFiner = 3, kRoundChunk = 32;
+SDVG_PAGED_HD int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 SDVG_PAGED_HD int32_t chunk_of(int64_t total, int64_t row_tiles, int32_t target) {
   if (target <= 0) return INT32_MAX;
-  const int64_t items = 4 * row_tiles <= target ? target - row_tiles : static_cast<int64_t>(kFiner) * target;
-  const int64_t c = (total + items - 1) / items;
+  int64_t c;
+  if (4 * row_tiles <= target) {
+    c = ceil_div(total, target - row_tiles);
+  } else {
+    const int64_t once = ceil_div(total, target), finer = ceil_div(total, static_cast<int64_t>(kFiner) * target);
+    const int64_t least = once < kRoundChunk ? once : kRoundChunk;
+    c = finer > least ? finer : least;
+  }
   return c > kMinChunk ? static_cast<int32_t>(c < INT32_MAX ? c : INT32_MAX) : kMinChunk;
 }
 // Items per row tile.
