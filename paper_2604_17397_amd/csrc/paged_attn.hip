@@ -245,8 +245,9 @@ __global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(Attn
   const char *k_head = static_cast<const char *>(p.k) + head * p.head_stride * kBytes,
              *v_head = static_cast<const char *>(p.v) + head * p.head_stride * kBytes;
   // One step's worth of K and V on the way from memory, and where it lies. Loads are issued a step ahead: K's when the
-  // scores of the step before are done, V's when its values have been transposed, the pages of the step after those then. A wave
-  // waits for memory only where the loads of a whole step take longer than a step.
+  // scores of the step before are done, V's when its values have been transposed; page numbers two steps ahead, at the start of a
+  // step. Loads come back in the order in which they are issued: page numbers that were asked for behind K and V could not be
+  // used before both had arrived, and every step took a whole trip to memory.
   struct Place {
     int32_t page;      // -1: not there
     uint32_t token;    // in its page, of the first of the 8 keys
@@ -273,11 +274,17 @@ __global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(Attn
 #pragma unroll
     for (int j = 0; j < 8; ++j) vf[j] = __builtin_nontemporal_load(reinterpret_cast<const chunk *>(row + j * p.token_stride * kBytes));
   };
-  Place k_next, v_next;  // of the step after the one whose loads are under way
+  Place k_next, v_next;  // of the next step
   // One step; kMore: another one follows.
   const auto step = [&](int tile, int32_t v_page, auto more) {
     constexpr bool kMore = decltype(more)::value;
     const int key0 = tile * pg::kKeyTile;
+    Place k_after, v_after;
+    if constexpr (kMore) {
+      const int after = tile + 2 * kKeyWaves < end ? tile + 2 * kKeyWaves : tile;
+      k_after = place_of(after * 4 + (col >> 2));
+      v_after = place_of(after * 4 + quad);
+    }
     // keys of this lane's block of 8 that are there
     int there = f.q.len - (key0 + 8 * quad);
     there = v_page < 0 ? 0 : there < 0 ? 0 : there > 8 ? 8 : there;
@@ -353,9 +360,8 @@ __global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(Attn
       if constexpr (kMore) {
         if (e == 3) {
           load_v(v_next);
-          const int block = tile + 2 * kKeyWaves < end ? (tile + 2 * kKeyWaves) * 4 : key0 / 8;
-          k_next = place_of(block + (col >> 2));
-          v_next = place_of(block + quad);
+          k_next = k_after;
+          v_next = v_after;
         }
       }
 #pragma unroll
