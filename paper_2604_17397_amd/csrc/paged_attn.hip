@@ -132,7 +132,7 @@ __device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readl
 // Found by every wave for itself: lane i looks at request 64 b + i. Batches of 64 requests at a time.
 struct Found {
   pg::Request q;
-  int32_t request, tile, piece, pieces, slot;   // row tile of the request; slot of its first piece
+  int32_t request, tile, piece, pieces, slot, chunk;   // row tile of the request; slot of its first piece; key tiles of a piece
 };
 template <int kRowTile>
 __device__ __forceinline__ pg::Request load_request(const AttnParams &p, int r) {
@@ -171,7 +171,8 @@ __device__ __forceinline__ bool find(const AttnParams &p, int x, Found &f) {
       f.request = b + src;
       f.pieces = get(pieces);
       const int i = get(at), slot0 = slots_before + get(slots_upto - slots);
-      f.tile = kItems ? i / f.pieces : i;
+      f.chunk = chunk;
+      f.tile = !kItems ? i : f.q.row_tiles > 1 ? static_cast<uint32_t>(i) / static_cast<uint32_t>(f.pieces) : 0;
       f.piece = kItems ? i - f.tile * f.pieces : 0;
       f.slot = slot0 + f.tile * f.pieces;
       return true;
@@ -239,8 +240,9 @@ __global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(Attn
     for (int d = 0; d < 8; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  const int begin = f.q.first_tile + pg::piece_begin(f.q.tiles, f.piece, f.pieces);
-  const int end = f.q.first_tile + pg::piece_begin(f.q.tiles, f.piece + 1, f.pieces);
+  const int before = f.piece * f.chunk;   // (0 in a request of one piece, whatever the chunk is)
+  const int begin = f.q.first_tile + before;
+  const int end = f.q.first_tile + (f.q.tiles - before < f.chunk ? f.q.tiles : before + f.chunk);
   const int32_t *table = p.table + f.request * p.table_stride;
   const char *k_head = static_cast<const char *>(p.k) + head * p.head_stride * kBytes,
              *v_head = static_cast<const char *>(p.v) + head * p.head_stride * kBytes;

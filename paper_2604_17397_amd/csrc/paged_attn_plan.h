@@ -54,26 +54,25 @@ SDVG_PAGED_HD int64_t work_of(const Request &q) { return static_cast<int64_t>(q.
 // longer than others: then they are made shorter, kFiner rounds of them, and the chip fills up again as they end; but not shorter
 // than kRoundChunk (what comes before and after the keys takes as long as some 10 key tiles) unless the chip is not filled once.
 constexpr int kFiner = 3, kRoundChunk = 32;
-SDVG_PAGED_HD int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+SDVG_PAGED_HD int64_t ceil_div(int64_t a, int32_t b) {
+  if (a <= INT32_MAX) return (static_cast<uint32_t>(a) + static_cast<uint32_t>(b) - 1) / static_cast<uint32_t>(b);  // (the shorter division)
+  return (a + b - 1) / b;
+}
 SDVG_PAGED_HD int32_t chunk_of(int64_t total, int64_t row_tiles, int32_t target) {
   if (target <= 0) return INT32_MAX;
   int64_t c;
   if (4 * row_tiles <= target) {
-    c = ceil_div(total, target - row_tiles);
+    c = ceil_div(total, target - static_cast<int32_t>(row_tiles));
   } else {
-    const int64_t once = ceil_div(total, target), finer = ceil_div(total, static_cast<int64_t>(kFiner) * target);
+    const int64_t once = ceil_div(total, target), finer = ceil_div(once, kFiner);
     const int64_t least = once < kRoundChunk ? once : kRoundChunk;
     c = finer > least ? finer : least;
   }
   return c > kMinChunk ? static_cast<int32_t>(c < INT32_MAX ? c : INT32_MAX) : kMinChunk;
 }
-// Items per row tile.
+// Items per row tile, each of `chunk` key tiles but the last.
 SDVG_PAGED_HD int32_t pieces_of(const Request &q, int32_t chunk) {
-  return q.tiles > chunk ? static_cast<int32_t>((static_cast<int64_t>(q.tiles) + chunk - 1) / chunk) : 1;
-}
-// First key tile of piece i of n, counted from the request's first: even shares.
-SDVG_PAGED_HD int32_t piece_begin(int32_t tiles, int32_t i, int32_t n) {
-  return static_cast<int32_t>(static_cast<int64_t>(tiles) * i / n);
+  return q.tiles > chunk ? static_cast<int32_t>((static_cast<uint32_t>(q.tiles) + static_cast<uint32_t>(chunk) - 1) / static_cast<uint32_t>(chunk)) : 1;
 }
 
 // Bounds for the launch, from what the host knows, with most = kFiner * target >= total / chunk. Items: most full chunks, and one

@@ -61,11 +61,7 @@ static void one(int R, int longest, int most_new, int group, int row_tile, int w
       slots += int64_t{q[r].row_tiles} * n;
       groups += q[r].row_tiles;
     }
-    CHECK(n >= 1 && pg::piece_begin(q[r].tiles, 0, n) == 0 && pg::piece_begin(q[r].tiles, n, n) == q[r].tiles);
-    for (int i = 0; i < n; ++i) {
-      const int share = pg::piece_begin(q[r].tiles, i + 1, n) - pg::piece_begin(q[r].tiles, i, n);
-      CHECK(share >= (n > 1 ? 1 : 0) && share <= chunk);
-    }
+    CHECK(n >= 1 && int64_t{n} * chunk >= q[r].tiles && (n == 1 || int64_t{n - 1} * chunk < q[r].tiles));
   }
   if (4 * row_tiles <= target) CHECK(items <= target);
   CHECK(row_tiles <= pg::max_row_tiles(R, tokens, group, row_tile));
