@@ -368,7 +368,7 @@ typedef struct {
 } sdvg_rope_desc;
 
 /* Rows [n_tokens][n_heads][128] that are read at in and written at out (which may be in itself, with the same strides;
- * otherwise they must not overlap). 16-byte aligned; strides in elements, multiples of 16 bytes, those of dimensions of size 1
+ * otherwise they must not overlap). 16-byte aligned; strides in elements, multiples of 16 bytes below 2^30, those of dimensions of size 1
  * are not looked at. */
 typedef struct {
   const void *in; /* device */
@@ -390,7 +390,7 @@ int sdvg_rope_positions(const sdvg_rope_desc *rope, const sdvg_rows *x, const sd
  * negative or past the pools are not written. Slots that are written must differ (two rows of one slot: either may win, in parts).
  *   rope      nullable. K is rotated on its way (v is not); a 16-bit cache then holds what sdvg_rope_positions would give.
  *   q         nullable, needs rope: rows that are rotated to q->out in the same launch.
- *   SDVG_E4M3: stored = round(x / scale), clamped to +-448 first (NaN stays NaN); x is not rounded to `dtype` after
+ *   SDVG_E4M3: stored = round(x * (1 / scale)) in fp32, clamped to +-448 first (NaN stays NaN); x is not rounded to `dtype` after
  *             the rotation.
  * k->out and v->out are not looked at. The sources must not overlap the pools (SDVG_ERR_RANGE). n_tokens < 2^26; 0 is a no-op.
  * Asynchronous on `stream`.

@@ -17,12 +17,13 @@ inline bool disjoint(const void *x, int64_t x_bytes, const void *y, int64_t y_by
   return a >= b + static_cast<uintptr_t>(y_bytes) || b >= a + static_cast<uintptr_t>(x_bytes);
 }
 
-// One stride in elements of `size` bytes over rows of 128: status of its check. Strides of dimensions of one entry are free.
-inline int check_stride(int64_t n, int64_t stride, int size) {
+// One stride in elements of `size` bytes over rows of 128, below `most`: status of its check. Strides of dimensions of one
+// entry are free.
+inline int check_stride(int64_t n, int64_t stride, int size, int64_t most = int64_t{1} << 30) {
   if (n <= 1) return SDVG_OK;
   if (stride < 128) return SDVG_ERR_SHAPE;
   if ((stride * size) & 15) return SDVG_ERR_ALIGN;
-  return stride >= (int64_t{1} << 40) ? SDVG_ERR_UNSUPPORTED : SDVG_OK;
+  return stride >= most ? SDVG_ERR_UNSUPPORTED : SDVG_OK;
 }
 
 // Elements from the first to one past the last of [n0][n1][128].

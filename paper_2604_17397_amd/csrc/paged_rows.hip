@@ -16,20 +16,23 @@ typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
 
 constexpr int kThreads = 256;
-constexpr int kUnits = 8;             // a row's 128 elements in units of two groups of 8 (the two halves of 8 pairs, or neighbours)
+constexpr int kUnits = 8;             // threads per row, each with two groups of 8 elements
+constexpr int kPass = kThreads / kUnits, kUnroll = 2;  // rows that a workgroup takes at a time, and how many times
+constexpr int64_t kMaxTokens = 1 << 26;  // a grid holds fewer than 2^32 threads, a workgroup has 1 or 4 tokens
 constexpr float kE4m3Max = 448.0f;
 
 struct RowsArg {
   const void *in;
   void *out;
-  int64_t in_ts, in_hs, out_ts, out_hs;
+  int64_t in_ts, in_hs, out_ts, out_hs;  // elements, below 2^30 (those of dimensions that are stepped over)
+  sdvg::FastDiv heads;
 };
 
 struct RowsParams {
-  RowsArg t[3];               // rotated rows | rows that are stored in k (or a second rotated tensor) | rows that are stored in v
-  uint32_t first1, first2, n_rows;  // rows per token: those of t[0] come first, then t[1] from first1 on, t[2] from first2 on
+  RowsArg t[3];               // rotated rows | rows that are stored in k (or a second rotated tensor) | rows that are stored in v; heads.d 0: none
   uint32_t n_tokens;
   const int32_t *positions;   // null: nothing is rotated
   const double *freqs;
@@ -40,66 +43,73 @@ struct RowsParams {
   sdvg::FastDiv page;
   int64_t page_stride, token_stride, head_stride;
   const float *scale[2];      // of k and v per head, or null
-  sdvg::FastDiv rows;         // by n_rows
 };
 
-// Eight elements as floats and back. E: element type.
+// Eight elements as they come from memory (raw), as floats, and back.
+template <bool kStream, typename V>
+__device__ __forceinline__ void put(void *p, V v) {
+  if (kStream)
+    __builtin_nontemporal_store(v, static_cast<V *>(p));
+  else
+    *static_cast<V *>(p) = v;
+}
 struct Bf16 {
+  typedef u32x4 raw;
   static constexpr int kBytes = 2;
-  static __device__ __forceinline__ void load(const void *p, float *x) {
-    const u32x4 v = *static_cast<const u32x4 *>(p);
+  static __device__ __forceinline__ raw fetch(const void *p) { return *static_cast<const raw *>(p); }
+  static __device__ __forceinline__ void widen(raw v, float *x) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       x[2 * i] = __uint_as_float(v[i] << 16);
       x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
     }
   }
+  template <bool kStream>
   static __device__ __forceinline__ void store(void *p, const float *x) {
     u32x4 v;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const f32x2 f = {x[2 * i], x[2 * i + 1]};
-      const bf16x2 b = __builtin_convertvector(f, bf16x2);
-      unsigned int w;
-      __builtin_memcpy(&w, &b, 4);
-      v[i] = w;
+      v[i] = __builtin_bit_cast(unsigned int, __builtin_convertvector(f, bf16x2));
     }
-    *static_cast<u32x4 *>(p) = v;
+    put<kStream>(p, v);
   }
 };
 struct F16 {
+  typedef __attribute__((ext_vector_type(8))) _Float16 raw;
   static constexpr int kBytes = 2;
-  typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-  static __device__ __forceinline__ void load(const void *p, float *x) {
-    const f16x8 v = *static_cast<const f16x8 *>(p);
+  static __device__ __forceinline__ raw fetch(const void *p) { return *static_cast<const raw *>(p); }
+  static __device__ __forceinline__ void widen(raw v, float *x) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = static_cast<float>(v[i]);
   }
+  template <bool kStream>
   static __device__ __forceinline__ void store(void *p, const float *x) {
-    f16x8 v;
+    raw v;
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = static_cast<_Float16>(x[i]);
-    *static_cast<f16x8 *>(p) = v;
+    put<kStream>(p, v);
   }
 };
 struct F32 {
+  struct raw {
+    f32x4 v[2];
+  };
   static constexpr int kBytes = 4;
-  typedef __attribute__((ext_vector_type(4))) float f32x4;
-  static __device__ __forceinline__ void load(const void *p, float *x) {
-    const f32x4 a = static_cast<const f32x4 *>(p)[0], b = static_cast<const f32x4 *>(p)[1];
+  static __device__ __forceinline__ raw fetch(const void *p) { return raw{{static_cast<const f32x4 *>(p)[0], static_cast<const f32x4 *>(p)[1]}}; }
+  static __device__ __forceinline__ void widen(raw v, float *x) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = a[i];
-      x[4 + i] = b[i];
-    }
+    for (int i = 0; i < 8; ++i) x[i] = v.v[i >> 2][i & 3];
   }
+  template <bool kStream>
   static __device__ __forceinline__ void store(void *p, const float *x) {
-    static_cast<f32x4 *>(p)[0] = f32x4{x[0], x[1], x[2], x[3]};
-    static_cast<f32x4 *>(p)[1] = f32x4{x[4], x[5], x[6], x[7]};
+    put<kStream>(p, f32x4{x[0], x[1], x[2], x[3]});
+    put<kStream>(static_cast<f32x4 *>(p) + 1, f32x4{x[4], x[5], x[6], x[7]});
   }
 };
 struct E4m3 {
   static constexpr int kBytes = 1;
+  template <bool kStream>
   static __device__ __forceinline__ void store(void *p, const float *x) {
     float y[8];
 #pragma unroll
@@ -110,7 +120,7 @@ struct E4m3 {
     int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false);
     lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
     hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], hi, true);
-    *static_cast<u32x2 *>(p) = u32x2{static_cast<unsigned int>(lo), static_cast<unsigned int>(hi)};
+    put<kStream>(p, u32x2{static_cast<unsigned int>(lo), static_cast<unsigned int>(hi)});
   }
 };
 
@@ -129,63 +139,102 @@ __device__ __forceinline__ void turn(int position, double freq, float gain, floa
   if (n >= 2) s = -s;
 }
 
-// T: type of the rows, C: type of the cache (T where none is written). A workgroup has kTok tokens; 8 threads share a row.
-template <typename T, typename C, bool kHalf, int kTok>
+__device__ __forceinline__ void turn_pair(float &re, float &im, float c, float s) {
+  const float a = re, b = im;
+  re = __fmaf_rn(a, c, -__fmul_rn(b, s));
+  im = __fmaf_rn(a, s, __fmul_rn(b, c));
+}
+// 8 pairs of which `re` and `im` are the halves; 4 pairs of neighbours.
+__device__ __forceinline__ void turn8(float *re, float *im, const float *c, const float *s) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) turn_pair(re[k], im[k], c[k], s[k]);
+}
+__device__ __forceinline__ void turn4(float *x, const float *c, const float *s) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) turn_pair(x[2 * k], x[2 * k + 1], c[k], s[k]);
+}
+
+// T: type of the rows, C: type of the cache (T where none is written). A workgroup has kTok tokens of one of the tensors
+// (blockIdx.y, so that everything about it is scalar); 8 threads share a row. A thread's kUnroll rows are all asked for before
+// the angles are computed or the rows before them are turned.
+// Bound by HBM from some thousand rows on, with the vector units close behind (130 instructions per 32 bytes in and out).
+template <typename T, typename C, bool kHalf, int kTok, bool kStream>
 __global__ __launch_bounds__(kThreads) void paged_rows_kernel(RowsParams p) {
   __shared__ float cs[kTok][64], sn[kTok][64];
   const uint32_t first = blockIdx.x * kTok;
   const uint32_t n_tok = p.n_tokens - first < kTok ? p.n_tokens - first : kTok;
-  if (p.positions) {
+  const int which = blockIdx.y;
+  const RowsArg a = which == 0 ? p.t[0] : which == 1 ? p.t[1] : p.t[2];
+  const bool rotate = p.positions && which < 2, store = p.slots && which > 0;
+  const int u = threadIdx.x & (kUnits - 1);
+  // The thread's two groups of 8 elements: those of pairs 8u .. 8u + 7 in the half layout, otherwise the u-th of both halves, so
+  // that the 8 threads of a row touch whole lines with every access (a nontemporal store of parts of one is slow).
+  const int units = rotate ? p.rotary_units : 0, c0 = kHalf && u >= units ? u + units : u, c1 = kHalf && u < units ? u + units : u + 8;
+  const int g0 = 8 * c0, g1 = 8 * c1;
+  const char *src = static_cast<const char *>(a.in) + static_cast<int64_t>(first) * a.in_ts * T::kBytes;
+  char *out = static_cast<char *>(a.out) + (store ? 0 : static_cast<int64_t>(first) * a.out_ts * T::kBytes);
+  const uint32_t n_rows = n_tok * a.heads.d;
+
+  typename T::raw x[kUnroll][2];
+  const auto load = [&](uint32_t base) {
+#pragma unroll
+    for (int j = 0; j < kUnroll; ++j) {
+      const uint32_t i = base + j * kPass;
+      if (i >= n_rows) continue;
+      const uint32_t t = kTok == 1 ? 0 : a.heads.div(i), head = i - t * a.heads.d;
+      const char *row = src + static_cast<uint64_t>(t) * (static_cast<uint32_t>(a.in_ts) * T::kBytes) +
+                        static_cast<uint64_t>(head) * (static_cast<uint32_t>(a.in_hs) * T::kBytes);
+      x[j][0] = T::fetch(row + g0 * T::kBytes);
+      x[j][1] = T::fetch(row + g1 * T::kBytes);
+    }
+  };
+  load(threadIdx.x / kUnits);
+  if (rotate) {
     for (uint32_t i = threadIdx.x; i < kTok * 64; i += kThreads) {
       const uint32_t t = i >> 6, pair = i & 63;
       if (t < n_tok && pair < 8u * p.rotary_units) turn(p.positions[first + t], p.freqs[pair], p.gain, cs[t][pair], sn[t][pair]);
     }
     __syncthreads();
   }
-  const int u = threadIdx.x & (kUnits - 1);
-  for (uint32_t i = threadIdx.x / kUnits; i < n_tok * p.n_rows; i += kThreads / kUnits) {
-    const uint32_t t = p.rows.div(i), row = i - t * p.n_rows;
-    const int which = row >= p.first2 ? 2 : row >= p.first1 ? 1 : 0;
-    const uint32_t head = row - (which == 2 ? p.first2 : which == 1 ? p.first1 : 0);
-    const RowsArg &a = p.t[which];
-    const bool rotate = p.positions && which < 2 && u < p.rotary_units, store = p.slots && which > 0;
-    // the unit's two groups of 8 elements: pairs 8u .. 8u + 7 where it is rotated
-    const int g0 = kHalf && u < p.rotary_units ? 8 * u : 16 * u;
-    const int g1 = kHalf && u < p.rotary_units ? 8 * (u + p.rotary_units) : 16 * u + 8;
-    char *dst;
-    if (store) {
-      const int64_t slot = p.slots[first + t];
-      if (slot < 0 || slot >= p.n_slots) continue;
-      const uint32_t page = p.page.div(static_cast<uint32_t>(slot)), place = static_cast<uint32_t>(slot) - page * p.page.d;
-      dst = static_cast<char *>(a.out) + (page * p.page_stride + place * p.token_stride + head * p.head_stride) * C::kBytes;
-    } else {
-      dst = static_cast<char *>(a.out) + (static_cast<int64_t>(first + t) * a.out_ts + head * a.out_hs) * T::kBytes;
-    }
-    const char *src = static_cast<const char *>(a.in) + (static_cast<int64_t>(first + t) * a.in_ts + head * a.in_hs) * T::kBytes;
-    float x[16];
-    T::load(src + g0 * T::kBytes, x);
-    T::load(src + g1 * T::kBytes, x + 8);
-    if (rotate) {
-      const float *c = &cs[t][8 * u], *s = &sn[t][8 * u];
+  for (uint32_t base = threadIdx.x / kUnits; base < n_rows; base += kPass * kUnroll) {
+    if (base != threadIdx.x / kUnits) load(base);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float &re = kHalf ? x[j] : x[2 * j], &im = kHalf ? x[8 + j] : x[2 * j + 1];
-        const float a0 = re, b0 = im;
-        re = __fmaf_rn(a0, c[j], -__fmul_rn(b0, s[j]));
-        im = __fmaf_rn(a0, s[j], __fmul_rn(b0, c[j]));
+    for (int j = 0; j < kUnroll; ++j) {
+      const uint32_t i = base + j * kPass;
+      if (i >= n_rows) continue;
+      const uint32_t t = kTok == 1 ? 0 : a.heads.div(i), head = i - t * a.heads.d;
+      float y[16];
+      T::widen(x[j][0], y);
+      T::widen(x[j][1], y + 8);
+      if (kHalf) {
+        if (u < units) turn8(y, y + 8, &cs[t][8 * u], &sn[t][8 * u]);
+      } else {
+        if (c0 < 2 * units) turn4(y, &cs[t][4 * c0], &sn[t][4 * c0]);
+        if (c1 < 2 * units) turn4(y + 8, &cs[t][4 * c1], &sn[t][4 * c1]);
       }
-    }
-    if (store) {
-      if (p.scale[which - 1]) {
-        const float scale = p.scale[which - 1][head];
+      if (store) {
+        const int64_t slot = p.slots[first + t];
+        if (slot < 0 || slot >= p.n_slots) continue;
+        const uint32_t s32 = static_cast<uint32_t>(slot), page = p.page.div(s32), place = s32 - page * p.page.d;
+        char *row = out + (page * p.page_stride + place * p.token_stride + head * p.head_stride) * C::kBytes;
+        if constexpr (C::kBytes == 1) {
+          const float *scale = which == 1 ? p.scale[0] : p.scale[1];
+          if (scale) {
+            const float d = 1.0f / scale[head];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) x[j] = x[j] / scale;
+            for (int k = 0; k < 16; ++k) y[k] *= d;
+          }
+        }
+        constexpr bool kWhole = kStream && C::kBytes == 2;
+        C::template store<kWhole>(row + g0 * C::kBytes, y);
+        C::template store<kWhole>(row + g1 * C::kBytes, y + 8);
+      } else {
+        char *row = out + static_cast<uint64_t>(t) * (static_cast<uint32_t>(a.out_ts) * T::kBytes) +
+                    static_cast<uint64_t>(head) * (static_cast<uint32_t>(a.out_hs) * T::kBytes);
+        constexpr bool kWhole = kStream && T::kBytes == 2;
+        T::template store<kWhole>(row + g0 * T::kBytes, y);
+        T::template store<kWhole>(row + g1 * T::kBytes, y + 8);
       }
-      C::store(dst + g0 * C::kBytes, x);
-      C::store(dst + g1 * C::kBytes, x + 8);
-    } else {
-      T::store(dst + g0 * T::kBytes, x);
-      T::store(dst + g1 * T::kBytes, x + 8);
     }
   }
 }
@@ -214,37 +263,31 @@ int check_rows(const sdvg_rows *r, int64_t n_tokens, int size, bool out, RowsArg
   if (out && n_tokens > 0 && r->in == r->out &&
       ((n_tokens > 1 && r->in_token_stride != r->out_token_stride) || (r->n_heads > 1 && r->in_head_stride != r->out_head_stride)))
     return SDVG_ERR_RANGE;
-  a = RowsArg{r->in, r->out, r->in_token_stride, r->in_head_stride, r->out_token_stride, r->out_head_stride};
+  if (r->n_heads > (1 << 20)) return SDVG_ERR_UNSUPPORTED;
+  const auto step = [](int64_t n, int64_t stride) { return n > 1 ? stride : 0; };
+  a = RowsArg{r->in, r->out, step(n_tokens, r->in_token_stride), step(r->n_heads, r->in_head_stride), step(n_tokens, r->out_token_stride),
+              step(r->n_heads, r->out_head_stride), sdvg::FastDiv::of(r->n_heads)};
   return SDVG_OK;
 }
 
+template <typename T, typename C, bool kHalf, int kTok, bool kStream>
+int launch_rows(const RowsParams &p, hipStream_t s) {
+  hipLaunchKernelGGL((paged_rows_kernel<T, C, kHalf, kTok, kStream>),
+                     dim3((p.n_tokens + kTok - 1) / kTok, p.t[2].heads.d ? 3 : p.t[1].heads.d ? 2 : 1), dim3(kThreads), 0, s, p);
+  SDVG_HIP_CHECK(hipGetLastError());
+  return SDVG_OK;
+}
 template <typename T, typename C, bool kHalf>
 int launch_rows(const RowsParams &p, hipStream_t s) {
   // Few tokens: a workgroup each, so that more compute units work on them. Many: 4, which fills the computation of the
-  // angles (64 per token) with all threads.
-  if (p.n_tokens < 1024) {
-    hipLaunchKernelGGL((paged_rows_kernel<T, C, kHalf, 1>), dim3(p.n_tokens), dim3(kThreads), 0, s, p);
-  } else {
-    hipLaunchKernelGGL((paged_rows_kernel<T, C, kHalf, 4>), dim3((p.n_tokens + 3) / 4), dim3(kThreads), 0, s, p);
-  }
-  SDVG_HIP_CHECK(hipGetLastError());
-  return SDVG_OK;
+  // angles (64 per token) with all threads. Stores as in the pass with tables: ordinary ones up to 4 MiB.
+  const int64_t rows = static_cast<int64_t>(p.n_tokens) * (p.t[0].heads.d + p.t[1].heads.d + p.t[2].heads.d);
+  if (p.n_tokens < 1024) return launch_rows<T, C, kHalf, 1, false>(p, s);
+  return rows * 128 * T::kBytes <= (4 << 20) ? launch_rows<T, C, kHalf, 4, false>(p, s) : launch_rows<T, C, kHalf, 4, true>(p, s);
 }
 template <typename T, typename C>
 int launch_rows(const RowsParams &p, bool half, hipStream_t s) {
   return half ? launch_rows<T, C, true>(p, s) : launch_rows<T, C, false>(p, s);
-}
-
-// Rows per token and tokens, checked against what the kernel counts in 32 bits.
-int set_rows(RowsParams &p, int64_t h0, int64_t h1, int64_t h2, int64_t n_tokens) {
-  const int64_t per_token = h0 + h1 + h2;
-  if (per_token > (1 << 24) || n_tokens >= (1 << 26)) return SDVG_ERR_UNSUPPORTED;  // (a grid holds fewer than 2^32 threads)
-  p.first1 = static_cast<uint32_t>(h0);
-  p.first2 = static_cast<uint32_t>(h0 + h1);
-  p.n_rows = static_cast<uint32_t>(per_token);
-  p.n_tokens = static_cast<uint32_t>(n_tokens);
-  p.rows = sdvg::FastDiv::of(p.n_rows);
-  return SDVG_OK;
 }
 
 void set_rope(RowsParams &p, const sdvg_rope_desc &r) {
@@ -273,7 +316,7 @@ int check_paged_kv(const sdvg_paged_kv *c) {
     int64_t n, stride;
   } d[3] = {{c->n_pages, c->page_stride}, {c->page_tokens, c->token_stride}, {c->n_kv_heads, c->head_stride}};
   for (const Dim &x : d) {
-    const int st = check_stride(x.n, x.stride, element_bytes(c->dtype));
+    const int st = check_stride(x.n, x.stride, element_bytes(c->dtype), int64_t{1} << 40);  // (a pool may be most of the memory)
     if (st != SDVG_OK) return st;
   }
   for (int i = 0; i < 2; ++i)
@@ -303,14 +346,15 @@ extern "C" int sdvg_rope_positions(const sdvg_rope_desc *rope, const sdvg_rows *
                                    int32_t head_dim, int32_t dtype, void *stream) {
   if (!rope || !x) return SDVG_ERR_NULL;
   if (n_tokens < 0) return SDVG_ERR_SHAPE;
+  if (n_tokens >= kMaxTokens) return SDVG_ERR_UNSUPPORTED;
   if (head_dim != 128 || (dtype != SDVG_BF16 && dtype != SDVG_F16 && dtype != SDVG_F32)) return SDVG_ERR_UNSUPPORTED;
   const int size = sdvg::element_bytes(dtype);
   RowsParams p{};
   int st = check_rope(rope, n_tokens);
   if (st == SDVG_OK) st = check_rows(x, n_tokens, size, true, p.t[0]);
   if (st == SDVG_OK && y) st = check_rows(y, n_tokens, size, true, p.t[1]);
-  if (st == SDVG_OK) st = set_rows(p, x->n_heads, y ? y->n_heads : 0, 0, n_tokens);
   if (st != SDVG_OK || n_tokens == 0) return st;
+  p.n_tokens = static_cast<uint32_t>(n_tokens);
   set_rope(p, *rope);
   const bool half = rope->layout == SDVG_ROPE_HALF;
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -326,7 +370,7 @@ extern "C" int sdvg_paged_commit(const sdvg_paged_kv *cache, const sdvg_rows *k,
   int st = sdvg::check_paged_kv(cache);
   if (st != SDVG_OK) return st;
   if (n_tokens < 0 || k->n_heads != cache->n_kv_heads || v->n_heads != cache->n_kv_heads) return SDVG_ERR_SHAPE;
-  if (dtype != SDVG_BF16 && dtype != SDVG_F16) return SDVG_ERR_UNSUPPORTED;
+  if (n_tokens >= kMaxTokens || (dtype != SDVG_BF16 && dtype != SDVG_F16)) return SDVG_ERR_UNSUPPORTED;
   if (cache->dtype != dtype && cache->dtype != SDVG_E4M3) return SDVG_ERR_UNSUPPORTED;
   if (q && !rope) return SDVG_ERR_NULL;
   if (n_tokens > 0 && !slots) return SDVG_ERR_NULL;
@@ -336,9 +380,8 @@ extern "C" int sdvg_paged_commit(const sdvg_paged_kv *cache, const sdvg_rows *k,
   if (st == SDVG_OK && q) st = check_rows(q, n_tokens, 2, true, p.t[0]);
   if (st == SDVG_OK) st = check_rows(k, n_tokens, 2, false, p.t[1]);
   if (st == SDVG_OK) st = check_rows(v, n_tokens, 2, false, p.t[2]);
-  if (st == SDVG_OK) st = set_rows(p, q ? q->n_heads : 0, cache->n_kv_heads, cache->n_kv_heads, n_tokens);
-  if (st != SDVG_OK) return st;
-  if (n_tokens == 0) return SDVG_OK;
+  if (st != SDVG_OK || n_tokens == 0) return st;
+  p.n_tokens = static_cast<uint32_t>(n_tokens);
   const int64_t pool = sdvg::paged_pool_bytes(*cache);
   for (const sdvg_rows *r : {k, v}) {
     const int64_t span = sdvg::rows_span(n_tokens, r->in_token_stride, r->n_heads, r->in_head_stride) * 2;
