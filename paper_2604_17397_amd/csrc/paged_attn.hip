@@ -42,17 +42,27 @@ constexpr int kPad = 132;               // floats per row of O in LDS
 constexpr float kSlack = 8.0f;          // powers of two by which a probability may pass 1
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+// What a workgroup needs first, apart from the other arguments: these dwords are preloaded into registers at launch (build.py).
+#define FIRST_ARGS                                                                                                    \
+  const int32_t *__restrict__ q_start, const int32_t *__restrict__ kv_lens, int32_t n_requests, int32_t n_tokens,     \
+      int32_t group, int32_t window, int32_t target, int32_t capacity, uint32_t heads_d, uint32_t heads_m, uint32_t heads_s
+struct First {
+  const int32_t *q_start, *kv_lens;
+  int32_t n_requests, n_tokens, group, window, target;
+  int32_t capacity;                   // keys a row of the table can name
+  sdvg::FastDiv by_heads;             // workgroups -> items
+};
+
 struct AttnParams {
   const void *q, *k, *v;
   void *out;
   float *lse;
   const float *k_scale, *v_scale;
-  const int32_t *table, *q_start, *kv_lens;
+  const int32_t *table;
   float *part_o, *part_ml;            // partial results: O [slot][key head][row][128], (m, l) [slot][key head][row][2]
   int64_t q_ts, q_hs, o_ts, o_hs, page_stride, token_stride, head_stride, table_stride;
-  int64_t capacity;                   // keys a row of the table can name
-  int32_t n_requests, n_tokens, n_heads, n_kv_heads, group, n_pages, table_width, window, target;
-  sdvg::FastDiv by_group, by_page, by_heads;  // rows -> tokens; blocks of 8 keys -> pages; workgroups -> items
+  int32_t n_heads, n_kv_heads, group, n_pages, table_width, window;
+  sdvg::FastDiv by_group, by_page;    // rows -> tokens; blocks of 8 keys -> pages
   float scale_log2e;
 };
 
@@ -135,13 +145,13 @@ struct Found {
   int32_t request, tile, piece, pieces, slot, chunk;   // row tile of the request; slot of its first piece; key tiles of a piece
 };
 template <int kRowTile>
-__device__ __forceinline__ pg::Request load_request(const AttnParams &p, int r) {
+__device__ __forceinline__ pg::Request load_request(const First &p, int r) {
   if (r >= p.n_requests) return pg::Request{0, 0, 0, 0, 0, 0};
   return pg::request_of(p.q_start[r], p.q_start[r + 1], p.kv_lens[r], p.n_tokens, p.group, kRowTile, p.window, p.capacity);
 }
 // Number `x` among the items (kItems) or among the split row tiles.
 template <int kRowTile, bool kItems>
-__device__ __forceinline__ bool find(const AttnParams &p, int x, Found &f) {
+__device__ __forceinline__ bool find(const First &p, int x, Found &f) {
   const int lane = threadIdx.x & 63;
   const pg::Request mine0 = load_request<kRowTile>(p, lane);
   int32_t chunk = INT32_MAX;
@@ -185,7 +195,7 @@ __device__ __forceinline__ bool find(const AttnParams &p, int x, Found &f) {
 
 // T: type of q, of P and of the output. kF8: the cache holds e4m3 numbers.
 template <typename T, bool kF8, int NT, int RS>
-__global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(AttnParams p) {
+__global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(FIRST_ARGS, AttnParams p) {
   constexpr int kRowTile = row_tile(NT, RS), kWaves = kKeyWaves * RS, kThreads = 64 * kWaves;
   constexpr int kDims = 128 * kRows * RS / kThreads;   // per thread where the workgroup finishes rows
   constexpr int kBytes = kF8 ? 1 : 2;
@@ -193,8 +203,9 @@ __global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(Attn
   __shared__ float ml_s[kWaves][kRows][2];
   Found f;
   // the key heads of an item are neighbours: together they read whole rows of the cache's tokens
-  const int item = p.by_heads.div(blockIdx.x), head = blockIdx.x - item * p.n_kv_heads;
-  if (!find<kRowTile, true>(p, item, f)) return;
+  const First first{q_start, kv_lens, n_requests, n_tokens, group, window, target, capacity, {heads_d, heads_m, heads_s}};
+  const int item = first.by_heads.div(blockIdx.x), head = blockIdx.x - item * heads_d;
+  if (!find<kRowTile, true>(first, item, f)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
   const int rows = f.q.n * p.group - f.tile * kRowTile;   // rows of this tile, those past kRowTile included
   const int row0 = wave / kKeyWaves * (NT * kRows);       // this wave's first
@@ -446,13 +457,14 @@ __global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(Attn
 // Joins the pieces of the rows of a split row tile. 32 threads have a row's dims; the 8 sets of them in a workgroup have
 // a row each where the pieces are few, and share the pieces of one row where they are many.
 template <typename T, bool kF8, int NT, int RS>
-__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(AttnParams p) {
+__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(FIRST_ARGS, AttnParams p) {
   constexpr int kRowTile = row_tile(NT, RS), kSets = kJoinThreads / 32;
   __shared__ f32x4 o_s[kSets][32];
   __shared__ float ml_s[kSets][2];
   Found f;
-  const int index = p.by_heads.div(blockIdx.x), head = blockIdx.x - index * p.n_kv_heads;
-  if (!find<kRowTile, false>(p, index, f)) return;
+  const First head_args{q_start, kv_lens, n_requests, n_tokens, group, window, target, capacity, {heads_d, heads_m, heads_s}};
+  const int index = head_args.by_heads.div(blockIdx.x), head = blockIdx.x - index * heads_d;
+  if (!find<kRowTile, false>(head_args, index, f)) return;
   const int left = f.q.n * p.group - f.tile * kRowTile, rows = left < kRowTile ? left : kRowTile;
   const int64_t step = static_cast<int64_t>(p.n_kv_heads) * kRowTile;   // rows between two pieces
   const int d4 = threadIdx.x & 31, set = threadIdx.x >> 5;
@@ -546,32 +558,34 @@ int check_attn(const sdvg_paged_attn_desc *d, const sdvg_paged_kv *c) {
   return SDVG_OK;
 }
 
+#define FIRST(f) \
+  f.q_start, f.kv_lens, f.n_requests, f.n_tokens, f.group, f.window, f.target, f.capacity, f.by_heads.d, f.by_heads.m, f.by_heads.s
 template <typename T, bool kF8, int NT, int RS>
-int launch_attn(const AttnParams &p, hipStream_t s) {
+int launch_attn(const First &f, const AttnParams &p, hipStream_t s) {
   constexpr int kRowTile = row_tile(NT, RS), kThreads = 64 * kKeyWaves * RS;
-  const int64_t tiles = pg::max_row_tiles(p.n_requests, p.n_tokens, p.group, kRowTile);
-  const int64_t items = pg::max_items(tiles, p.target);
+  const int64_t tiles = pg::max_row_tiles(f.n_requests, f.n_tokens, f.group, kRowTile);
+  const int64_t items = pg::max_items(tiles, f.target);
   if (items * p.n_kv_heads >= (1 << 23)) return SDVG_ERR_UNSUPPORTED;  // (a grid holds fewer than 2^32 threads)
-  hipLaunchKernelGGL((paged_attn_kernel<T, kF8, NT, RS>), dim3(static_cast<uint32_t>(items * p.n_kv_heads)), dim3(kThreads), 0, s, p);
+  hipLaunchKernelGGL((paged_attn_kernel<T, kF8, NT, RS>), dim3(static_cast<uint32_t>(items * p.n_kv_heads)), dim3(kThreads), 0, s, FIRST(f), p);
   SDVG_HIP_CHECK(hipGetLastError());
-  if (p.target > 0) {
+  if (f.target > 0) {
     // Workgroups per row tile: one for every row of an average request's where that are few (then the pieces are many, and
     // shared), otherwise one for every 8 rows. A workgroup takes more rows where there are more.
-    const int64_t groups = pg::max_groups(tiles, p.target) * p.n_kv_heads;
-    int64_t rows = (static_cast<int64_t>(p.n_tokens) + p.n_requests - 1) / p.n_requests * p.group;
+    const int64_t groups = pg::max_groups(tiles, f.target) * p.n_kv_heads;
+    int64_t rows = (static_cast<int64_t>(f.n_tokens) + f.n_requests - 1) / f.n_requests * f.group;
     rows = rows < kRowTile ? rows : kRowTile;
     if (groups * rows > 1024) rows = (rows + 7) / 8;
     hipLaunchKernelGGL((paged_join_kernel<T, kF8, NT, RS>), dim3(static_cast<uint32_t>(groups), static_cast<uint32_t>(rows)),
-                       dim3(kJoinThreads), 0, s, p);
+                       dim3(kJoinThreads), 0, s, FIRST(f), p);
     SDVG_HIP_CHECK(hipGetLastError());
   }
   return SDVG_OK;
 }
 template <typename T, bool kF8>
-int launch_attn(const AttnParams &p, int row_tile, hipStream_t s) {
-  return row_tile == 16   ? launch_attn<T, kF8, 1, 1>(p, s)
-         : row_tile == 32 ? launch_attn<T, kF8, 2, 1>(p, s)
-                          : launch_attn<T, kF8, 2, 2>(p, s);
+int launch_attn(const First &f, const AttnParams &p, int row_tile, hipStream_t s) {
+  return row_tile == 16   ? launch_attn<T, kF8, 1, 1>(f, p, s)
+         : row_tile == 32 ? launch_attn<T, kF8, 2, 1>(f, p, s)
+                          : launch_attn<T, kF8, 2, 2>(f, p, s);
 }
 
 }  // namespace
@@ -615,8 +629,6 @@ extern "C" int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_page
   p.k_scale = cache->k_scale;
   p.v_scale = cache->v_scale;
   p.table = block_table;
-  p.q_start = q_start;
-  p.kv_lens = kv_lens;
   p.q_ts = desc->q_token_stride;
   p.q_hs = desc->q_head_stride;
   p.o_ts = desc->o_token_stride;
@@ -625,10 +637,8 @@ extern "C" int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_page
   p.token_stride = cache->token_stride;
   p.head_stride = cache->head_stride;
   p.table_stride = desc->table_stride;
-  p.capacity = int64_t{desc->table_width} * cache->page_tokens;
-  if (p.capacity > INT32_MAX - 2 * pg::kKeyTile) p.capacity = INT32_MAX - 2 * pg::kKeyTile;  // (more than any pool holds)
-  p.n_requests = desc->n_requests;
-  p.n_tokens = desc->n_tokens;
+  int64_t capacity = int64_t{desc->table_width} * cache->page_tokens;
+  if (capacity > INT32_MAX - 2 * pg::kKeyTile) capacity = INT32_MAX - 2 * pg::kKeyTile;  // (more than any pool holds)
   p.n_heads = desc->n_heads;
   p.n_kv_heads = cache->n_kv_heads;
   p.group = desc->n_heads / cache->n_kv_heads;
@@ -636,17 +646,18 @@ extern "C" int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_page
   p.table_width = desc->table_width;
   p.window = desc->window;
   p.by_group = sdvg::FastDiv::of(p.group);
-  p.by_heads = sdvg::FastDiv::of(p.n_kv_heads);
   p.by_page = sdvg::FastDiv::of(cache->page_tokens / 8);
   p.scale_log2e = (desc->scale == 0.f ? 1.0f / sqrtf(128.0f) : desc->scale) * kLog2e;
-  const int tile = row_tile_of(p.n_requests, p.n_tokens, p.group), target = target_of(n_cu, p.n_kv_heads, tile);
+  First f{q_start, kv_lens, desc->n_requests, desc->n_tokens, p.group, p.window, 0, static_cast<int32_t>(capacity),
+          sdvg::FastDiv::of(p.n_kv_heads)};
+  const int tile = row_tile_of(f.n_requests, f.n_tokens, p.group), target = target_of(n_cu, p.n_kv_heads, tile);
   if (workspace && workspace_bytes >= workspace_of(target, p.n_kv_heads, tile)) {
-    p.target = target;
+    f.target = target;
     p.part_o = static_cast<float *>(workspace);
     p.part_ml = p.part_o + pg::max_slots(target) * p.n_kv_heads * tile * 128;
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool f8 = cache->dtype == SDVG_E4M3;
-  if (desc->dtype == SDVG_BF16) return f8 ? launch_attn<Bf16, true>(p, tile, s) : launch_attn<Bf16, false>(p, tile, s);
-  return f8 ? launch_attn<F16, true>(p, tile, s) : launch_attn<F16, false>(p, tile, s);
+  if (desc->dtype == SDVG_BF16) return f8 ? launch_attn<Bf16, true>(f, p, tile, s) : launch_attn<Bf16, false>(f, p, tile, s);
+  return f8 ? launch_attn<F16, true>(f, p, tile, s) : launch_attn<F16, false>(f, p, tile, s);
 }
