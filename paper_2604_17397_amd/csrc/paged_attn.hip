@@ -564,11 +564,11 @@ template <typename T, bool kF8, int NT, int RS>
 int launch_attn(const First &f, const AttnParams &p, hipStream_t s) {
   constexpr int kRowTile = row_tile(NT, RS), kThreads = 64 * kKeyWaves * RS;
   const int64_t tiles = pg::max_row_tiles(f.n_requests, f.n_tokens, f.group, kRowTile);
-  const int64_t items = pg::max_items(tiles, f.target);
+  const int64_t items = pg::max_items(tiles, f.target, f.capacity);
   if (items * p.n_kv_heads >= (1 << 23)) return SDVG_ERR_UNSUPPORTED;  // (a grid holds fewer than 2^32 threads)
   hipLaunchKernelGGL((paged_attn_kernel<T, kF8, NT, RS>), dim3(static_cast<uint32_t>(items * p.n_kv_heads)), dim3(kThreads), 0, s, FIRST(f), p);
   SDVG_HIP_CHECK(hipGetLastError());
-  if (f.target > 0) {
+  if (f.target > 0 && pg::max_pieces(f.capacity) > 1) {
     // Workgroups per row tile: one for every row of an average request's where that are few (then the pieces are many, and
     // shared), otherwise one for every 8 rows. A workgroup takes more rows where there are more.
     const int64_t groups = pg::max_groups(tiles, f.target) * p.n_kv_heads;

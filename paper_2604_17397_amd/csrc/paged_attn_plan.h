@@ -76,14 +76,21 @@ SDVG_PAGED_HD int32_t pieces_of(const Request &q, int32_t chunk) {
 }
 
 // Bounds for the launch, from what the host knows, with most = kFiner * target >= total / chunk. Items: most full chunks, and one
-// more per row tile. Slots: a split row tile of t > chunk tiles has ceil(t / chunk) < 2 t / chunk pieces. Groups (split row tiles): t >
-// chunk each.
+// more per row tile; no more than `target` where the row tiles are few; and none of a row tile below kMinChunk key tiles of what a row of
+// the block table can name (`capacity` keys). Slots: a split row tile of t > chunk tiles has ceil(t / chunk) < 2 t / chunk pieces. Groups
+// (split row tiles): t > chunk each.
 SDVG_PAGED_HD int64_t max_row_tiles(int64_t n_requests, int64_t n_tokens, int32_t group, int32_t row_tile) {
   const int64_t rows = n_tokens * group;
   const int64_t bound = rows / row_tile + n_requests;
   return bound < rows ? bound : rows;
 }
-SDVG_PAGED_HD int64_t max_items(int64_t row_tiles, int32_t target) { return row_tiles + (target > 0 ? kFiner * static_cast<int64_t>(target) : 0); }
+SDVG_PAGED_HD int64_t max_pieces(int64_t capacity) { return ceil_div(ceil_div(capacity, kKeyTile) + 1, kMinChunk); }  // (+ 1: a window may begin inside a tile)
+SDVG_PAGED_HD int64_t max_items(int64_t row_tiles, int32_t target, int64_t capacity) {
+  if (target <= 0) return row_tiles;
+  const int64_t by_chunk = 4 * row_tiles <= target ? target : row_tiles + kFiner * static_cast<int64_t>(target);
+  const int64_t by_keys = row_tiles * max_pieces(capacity);
+  return by_chunk < by_keys ? by_chunk : by_keys;
+}
 SDVG_PAGED_HD int64_t max_groups(int64_t row_tiles, int32_t target) { return row_tiles < kFiner * static_cast<int64_t>(target) ? row_tiles : kFiner * static_cast<int64_t>(target); }
 SDVG_PAGED_HD int64_t max_slots(int32_t target) { return 2 * kFiner * static_cast<int64_t>(target); }
 

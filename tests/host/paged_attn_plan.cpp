@@ -65,7 +65,9 @@ static void one(int R, int longest, int most_new, int group, int row_tile, int w
   }
   if (4 * row_tiles <= target) CHECK(items <= target);
   CHECK(row_tiles <= pg::max_row_tiles(R, tokens, group, row_tile));
-  CHECK(items <= pg::max_items(pg::max_row_tiles(R, tokens, group, row_tile), target));
+  const int64_t bound = pg::max_row_tiles(R, tokens, group, row_tile);
+  CHECK(items <= pg::max_items(bound, target, capacity));
+  if (pg::max_pieces(capacity) == 1) CHECK(groups == 0);
   CHECK(slots <= pg::max_slots(target > 0 ? target : 0));
   CHECK(groups <= (target > 0 ? pg::max_groups(row_tiles, target) : 0));
 }
@@ -81,6 +83,7 @@ int main() {
             for (int target : targets) {
               one(R, longest, 1, group, row_tile, window, target, INT32_MAX - 64);
               one(R, longest, 9, group, row_tile, window, target, n % 3 ? INT32_MAX - 64 : longest / 2 + 8);
+              one(R, longest, 2, group, row_tile, window, target, (longest + 9) / 8 * 8);
               ++n;
             }
   // out of range: clamped
