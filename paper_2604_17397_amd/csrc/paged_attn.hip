@@ -53,17 +53,26 @@ struct First {
   sdvg::FastDiv by_heads;             // workgroups -> items
 };
 
+// What both kernels need of the output. (A launch takes 0.3 us longer per 100 bytes of arguments.)
+struct OutParams {
+  void *out;
+  float *lse, *part_o, *part_ml;      // partial results: O [slot][key head][row][128], (m, l) [slot][key head][row][2]
+  const float *v_scale;
+  uint32_t o_ts, o_hs;                // elements, below 2^30
+  int32_t n_heads;
+  sdvg::FastDiv by_group;             // rows -> tokens
+};
+
 struct AttnParams {
   const void *q, *k, *v;
-  void *out;
-  float *lse;
-  const float *k_scale, *v_scale;
+  const float *k_scale;
   const int32_t *table;
-  float *part_o, *part_ml;            // partial results: O [slot][key head][row][128], (m, l) [slot][key head][row][2]
-  int64_t q_ts, q_hs, o_ts, o_hs, page_stride, token_stride, head_stride, table_stride;
-  int32_t n_heads, n_kv_heads, group, n_pages, table_width, window;
-  sdvg::FastDiv by_group, by_page;    // rows -> tokens; blocks of 8 keys -> pages
+  int64_t page_stride, token_stride, head_stride;
+  uint32_t q_ts, q_hs;                // elements, below 2^30
+  int32_t table_stride, table_width, n_pages;
   float scale_log2e;
+  sdvg::FastDiv by_page;              // blocks of 8 keys -> pages
+  OutParams to;
 };
 
 // Rows of a workgroup: NT tiles of 16 per wave, RS sets of 4 waves with different rows and the same keys (they share K and V
@@ -207,7 +216,7 @@ __global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(FIRS
   const int item = first.by_heads.div(blockIdx.x), head = blockIdx.x - item * heads_d;
   if (!find<kRowTile, true>(first, item, f)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
-  const int rows = f.q.n * p.group - f.tile * kRowTile;   // rows of this tile, those past kRowTile included
+  const int rows = f.q.n * group - f.tile * kRowTile;   // rows of this tile, those past kRowTile included
   const int row0 = wave / kKeyWaves * (NT * kRows);       // this wave's first
 
   // the query rows of this lane: column col of every tile of 16
@@ -216,15 +225,15 @@ __global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(FIRS
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int row = row0 + t * kRows + col;
-    const uint32_t all = f.tile * kRowTile + row, i = p.by_group.div(all), h = all - i * p.group;
+    const uint32_t all = f.tile * kRowTile + row, i = p.to.by_group.div(all), h = all - i * group;
     sees[t] = from[t] = 0;
 #pragma unroll
     for (int s = 0; s < 4; ++s) qf[t][s] = u32x4{0, 0, 0, 0};
     if (row < rows) {
       sees[t] = f.q.len - f.q.n + static_cast<int>(i) + 1;
-      from[t] = p.window > 0 && sees[t] > p.window ? sees[t] - p.window : 0;
+      from[t] = window > 0 && sees[t] > window ? sees[t] - window : 0;
       const uint16_t *src = static_cast<const uint16_t *>(p.q) + (f.q.row0 + static_cast<int64_t>(i)) * p.q_ts +
-                            (static_cast<int64_t>(head) * p.group + h) * p.q_hs;
+                            (static_cast<int64_t>(head) * group + h) * p.q_hs;
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
         // dims of product s in this lane: as K's load has them (below)
@@ -235,10 +244,10 @@ __global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(FIRS
   }
   // tiles in which every row of the workgroup sees every key
   const int last_row = rows < kRowTile ? rows - 1 : kRowTile - 1;
-  const int first_i = static_cast<int>(p.by_group.div(f.tile * kRowTile)),
-            last_i = static_cast<int>(p.by_group.div(f.tile * kRowTile + last_row));
+  const int first_i = static_cast<int>(p.to.by_group.div(f.tile * kRowTile)),
+            last_i = static_cast<int>(p.to.by_group.div(f.tile * kRowTile + last_row));
   const int all_sees = f.q.len - f.q.n + first_i + 1, last_sees = f.q.len - f.q.n + last_i + 1;
-  const int all_from = p.window > 0 && last_sees > p.window ? last_sees - p.window : 0;
+  const int all_from = window > 0 && last_sees > window ? last_sees - window : 0;
 
   const float scale = p.scale_log2e * (kF8 && p.k_scale ? p.k_scale[head] : 1.0f);
   f32x4 o[NT][8];
@@ -254,7 +263,7 @@ __global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(FIRS
   const int before = f.piece * f.chunk;   // (0 in a request of one piece, whatever the chunk is)
   const int begin = f.q.first_tile + before;
   const int end = f.q.first_tile + (f.q.tiles - before < f.chunk ? f.q.tiles : before + f.chunk);
-  const int32_t *table = p.table + f.request * p.table_stride;
+  const int32_t *table = p.table + static_cast<int64_t>(f.request) * p.table_stride;
   const char *k_head = static_cast<const char *>(p.k) + head * p.head_stride * kBytes,
              *v_head = static_cast<const char *>(p.v) + head * p.head_stride * kBytes;
   // One step's worth of K and V on the way from memory, and where it lies. Loads are issued a step ahead: K's when the
@@ -401,7 +410,7 @@ __global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(FIRS
   }
 
   // The waves' results of a tile of 16 rows meet in LDS.
-  const float v_scale = kF8 && p.v_scale ? p.v_scale[head] : 1.0f;
+  const float v_scale = kF8 && p.to.v_scale ? p.to.v_scale[head] : 1.0f;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     if (t * kRows >= rows) break;
@@ -437,27 +446,27 @@ __global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(FIRS
         acc[j] += weight * *reinterpret_cast<const f32x4 *>(&o_s[set * kKeyWaves + w][c][d0 + 4 * j]);
     }
     if (f.pieces > 1) {
-      const int64_t at = (static_cast<int64_t>(f.slot + f.piece) * p.n_kv_heads + head) * kRowTile + row;
+      const int64_t at = (static_cast<int64_t>(f.slot + f.piece) * heads_d + head) * kRowTile + row;
 #pragma unroll
-      for (int j = 0; j < kDims / 4; ++j) reinterpret_cast<f32x4 *>(p.part_o + at * 128 + d0)[j] = acc[j];
-      if (d0 == 0) *reinterpret_cast<f32x2 *>(p.part_ml + at * 2) = f32x2{top, total};
+      for (int j = 0; j < kDims / 4; ++j) reinterpret_cast<f32x4 *>(p.to.part_o + at * 128 + d0)[j] = acc[j];
+      if (d0 == 0) *reinterpret_cast<f32x2 *>(p.to.part_ml + at * 2) = f32x2{top, total};
       continue;
     }
-    const uint32_t all = f.tile * kRowTile + row, i = p.by_group.div(all), h = all - i * p.group;
-    const int64_t token = f.q.row0 + static_cast<int64_t>(i), q_head = static_cast<int64_t>(head) * p.group + h;
+    const uint32_t all = f.tile * kRowTile + row, i = p.to.by_group.div(all), h = all - i * group;
+    const int64_t token = f.q.row0 + static_cast<int64_t>(i), q_head = static_cast<int64_t>(head) * group + h;
     const float norm = top == -INFINITY ? 0.f : v_scale / total;   // (sum 0 only without a key)
-    uint16_t *dst = static_cast<uint16_t *>(p.out) + token * p.o_ts + q_head * p.o_hs + d0;
+    uint16_t *dst = static_cast<uint16_t *>(p.to.out) + token * p.to.o_ts + q_head * p.to.o_hs + d0;
 #pragma unroll
     for (int j = 0; j < kDims / 4; ++j)
       reinterpret_cast<u32x2 *>(dst)[j] = u32x2{T::pack(acc[j][0] * norm, acc[j][1] * norm), T::pack(acc[j][2] * norm, acc[j][3] * norm)};
-    if (p.lse && d0 == 0) p.lse[token * p.n_heads + q_head] = top == -INFINITY ? -INFINITY : (top + log2f(total)) * kLn2;
+    if (p.to.lse && d0 == 0) p.to.lse[token * p.to.n_heads + q_head] = top == -INFINITY ? -INFINITY : (top + log2f(total)) * kLn2;
   }
 }
 
 // Joins the pieces of the rows of a split row tile. 32 threads have a row's dims; the 8 sets of them in a workgroup have
 // a row each where the pieces are few, and share the pieces of one row where they are many.
 template <typename T, bool kF8, int NT, int RS>
-__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(FIRST_ARGS, AttnParams p) {
+__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(FIRST_ARGS, OutParams p) {
   constexpr int kRowTile = row_tile(NT, RS), kSets = kJoinThreads / 32;
   __shared__ f32x4 o_s[kSets][32];
   __shared__ float ml_s[kSets][2];
@@ -465,13 +474,13 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(FIRST_ARGS, At
   const First head_args{q_start, kv_lens, n_requests, n_tokens, group, window, target, capacity, {heads_d, heads_m, heads_s}};
   const int index = head_args.by_heads.div(blockIdx.x), head = blockIdx.x - index * heads_d;
   if (!find<kRowTile, false>(head_args, index, f)) return;
-  const int left = f.q.n * p.group - f.tile * kRowTile, rows = left < kRowTile ? left : kRowTile;
-  const int64_t step = static_cast<int64_t>(p.n_kv_heads) * kRowTile;   // rows between two pieces
+  const int left = f.q.n * group - f.tile * kRowTile, rows = left < kRowTile ? left : kRowTile;
+  const int64_t step = static_cast<int64_t>(heads_d) * kRowTile;   // rows between two pieces
   const int d4 = threadIdx.x & 31, set = threadIdx.x >> 5;
   const bool shared = f.pieces > 2 * kSets;
   const int first = shared ? blockIdx.y : blockIdx.y * kSets + set, rows_step = shared ? gridDim.y : gridDim.y * kSets;
   for (int row = first; row < rows; row += rows_step) {
-    const int64_t at = (static_cast<int64_t>(f.slot) * p.n_kv_heads + head) * kRowTile + row;
+    const int64_t at = (static_cast<int64_t>(f.slot) * heads_d + head) * kRowTile + row;
     float top = -INFINITY, total = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
@@ -503,8 +512,8 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(FIRST_ARGS, At
         acc += weight * o_s[w][d4];
       }
     }
-    const uint32_t all = f.tile * kRowTile + row, i = p.by_group.div(all), h = all - i * p.group;
-    const int64_t token = f.q.row0 + static_cast<int64_t>(i), q_head = static_cast<int64_t>(head) * p.group + h;
+    const uint32_t all = f.tile * kRowTile + row, i = p.by_group.div(all), h = all - i * group;
+    const int64_t token = f.q.row0 + static_cast<int64_t>(i), q_head = static_cast<int64_t>(head) * group + h;
     acc *= top == -INFINITY ? 0.f : (kF8 && p.v_scale ? p.v_scale[head] : 1.0f) / total;
     const u32x2 w = {T::pack(acc[0], acc[1]), T::pack(acc[2], acc[3])};
     *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(p.out) + token * p.o_ts + q_head * p.o_hs + 4 * d4) = w;
@@ -554,6 +563,7 @@ int check_attn(const sdvg_paged_attn_desc *d, const sdvg_paged_kv *c) {
     return SDVG_ERR_SHAPE;
   if (c->n_kv_heads > 65535 || int64_t{d->n_tokens} * d->n_heads > INT32_MAX) return SDVG_ERR_UNSUPPORTED;
   if (d->n_requests > 1 && d->table_stride < d->table_width) return SDVG_ERR_SHAPE;
+  if (d->n_requests > 1 && d->table_stride > INT32_MAX) return SDVG_ERR_UNSUPPORTED;
   if (!(d->scale >= 0.f) || !isfinite(d->scale)) return SDVG_ERR_RANGE;
   return SDVG_OK;
 }
@@ -565,18 +575,18 @@ int launch_attn(const First &f, const AttnParams &p, hipStream_t s) {
   constexpr int kRowTile = row_tile(NT, RS), kThreads = 64 * kKeyWaves * RS;
   const int64_t tiles = pg::max_row_tiles(f.n_requests, f.n_tokens, f.group, kRowTile);
   const int64_t items = pg::max_items(tiles, f.target, f.capacity);
-  if (items * p.n_kv_heads >= (1 << 23)) return SDVG_ERR_UNSUPPORTED;  // (a grid holds fewer than 2^32 threads)
-  hipLaunchKernelGGL((paged_attn_kernel<T, kF8, NT, RS>), dim3(static_cast<uint32_t>(items * p.n_kv_heads)), dim3(kThreads), 0, s, FIRST(f), p);
+  if (items * f.by_heads.d >= (1 << 23)) return SDVG_ERR_UNSUPPORTED;  // (a grid holds fewer than 2^32 threads)
+  hipLaunchKernelGGL((paged_attn_kernel<T, kF8, NT, RS>), dim3(static_cast<uint32_t>(items * f.by_heads.d)), dim3(kThreads), 0, s, FIRST(f), p);
   SDVG_HIP_CHECK(hipGetLastError());
   if (f.target > 0 && pg::max_pieces(f.capacity) > 1) {
     // Workgroups per row tile: one for every row of an average request's where that are few (then the pieces are many, and
     // shared), otherwise one for every 8 rows. A workgroup takes more rows where there are more.
-    const int64_t groups = pg::max_groups(tiles, f.target) * p.n_kv_heads;
+    const int64_t groups = pg::max_groups(tiles, f.target) * f.by_heads.d;
     int64_t rows = (static_cast<int64_t>(f.n_tokens) + f.n_requests - 1) / f.n_requests * f.group;
     rows = rows < kRowTile ? rows : kRowTile;
     if (groups * rows > 1024) rows = (rows + 7) / 8;
     hipLaunchKernelGGL((paged_join_kernel<T, kF8, NT, RS>), dim3(static_cast<uint32_t>(groups), static_cast<uint32_t>(rows)),
-                       dim3(kJoinThreads), 0, s, FIRST(f), p);
+                       dim3(kJoinThreads), 0, s, FIRST(f), p.to);
     SDVG_HIP_CHECK(hipGetLastError());
   }
   return SDVG_OK;
@@ -620,41 +630,33 @@ extern "C" int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_page
     return SDVG_ERR_RANGE;
   int n_cu = 0;
   if ((st = compute_units(n_cu)) != SDVG_OK) return st;
+  int64_t capacity = int64_t{desc->table_width} * cache->page_tokens;
+  if (capacity > INT32_MAX - 2 * pg::kKeyTile) capacity = INT32_MAX - 2 * pg::kKeyTile;  // (more than any pool holds)
+  const int32_t n_kv = cache->n_kv_heads, group = desc->n_heads / n_kv;
+  First f{q_start, kv_lens, desc->n_requests, desc->n_tokens, group, desc->window, 0, static_cast<int32_t>(capacity), sdvg::FastDiv::of(n_kv)};
   AttnParams p{};
   p.q = q;
   p.k = cache->k;
   p.v = cache->v;
-  p.out = out;
-  p.lse = lse;
   p.k_scale = cache->k_scale;
-  p.v_scale = cache->v_scale;
   p.table = block_table;
-  p.q_ts = desc->q_token_stride;
-  p.q_hs = desc->q_head_stride;
-  p.o_ts = desc->o_token_stride;
-  p.o_hs = desc->o_head_stride;
   p.page_stride = cache->page_stride;
   p.token_stride = cache->token_stride;
   p.head_stride = cache->head_stride;
-  p.table_stride = desc->table_stride;
-  int64_t capacity = int64_t{desc->table_width} * cache->page_tokens;
-  if (capacity > INT32_MAX - 2 * pg::kKeyTile) capacity = INT32_MAX - 2 * pg::kKeyTile;  // (more than any pool holds)
-  p.n_heads = desc->n_heads;
-  p.n_kv_heads = cache->n_kv_heads;
-  p.group = desc->n_heads / cache->n_kv_heads;
-  p.n_pages = cache->n_pages;
+  p.q_ts = static_cast<uint32_t>(desc->q_token_stride);
+  p.q_hs = static_cast<uint32_t>(desc->q_head_stride);
+  p.table_stride = desc->n_requests > 1 ? static_cast<int32_t>(desc->table_stride) : 0;
   p.table_width = desc->table_width;
-  p.window = desc->window;
-  p.by_group = sdvg::FastDiv::of(p.group);
-  p.by_page = sdvg::FastDiv::of(cache->page_tokens / 8);
+  p.n_pages = cache->n_pages;
   p.scale_log2e = (desc->scale == 0.f ? 1.0f / sqrtf(128.0f) : desc->scale) * kLog2e;
-  First f{q_start, kv_lens, desc->n_requests, desc->n_tokens, p.group, p.window, 0, static_cast<int32_t>(capacity),
-          sdvg::FastDiv::of(p.n_kv_heads)};
-  const int tile = row_tile_of(f.n_requests, f.n_tokens, p.group), target = target_of(n_cu, p.n_kv_heads, tile);
-  if (workspace && workspace_bytes >= workspace_of(target, p.n_kv_heads, tile)) {
+  p.by_page = sdvg::FastDiv::of(cache->page_tokens / 8);
+  p.to = OutParams{out, lse, nullptr, nullptr, cache->v_scale, static_cast<uint32_t>(desc->o_token_stride),
+                   static_cast<uint32_t>(desc->o_head_stride), desc->n_heads, sdvg::FastDiv::of(group)};
+  const int tile = row_tile_of(f.n_requests, f.n_tokens, group), target = target_of(n_cu, n_kv, tile);
+  if (workspace && workspace_bytes >= workspace_of(target, n_kv, tile)) {
     f.target = target;
-    p.part_o = static_cast<float *>(workspace);
-    p.part_ml = p.part_o + pg::max_slots(target) * p.n_kv_heads * tile * 128;
+    p.to.part_o = static_cast<float *>(workspace);
+    p.to.part_ml = p.to.part_o + pg::max_slots(target) * n_kv * tile * 128;
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool f8 = cache->dtype == SDVG_E4M3;

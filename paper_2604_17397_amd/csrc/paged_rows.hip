@@ -27,7 +27,7 @@ constexpr float kE4m3Max = 448.0f;
 struct RowsArg {
   const void *in;
   void *out;
-  int64_t in_ts, in_hs, out_ts, out_hs;  // elements, below 2^30 (those of dimensions that are stepped over)
+  uint32_t in_ts, in_hs, out_ts, out_hs;  // elements, below 2^30
   sdvg::FastDiv heads;
 };
 
@@ -182,8 +182,8 @@ __global__ __launch_bounds__(kThreads) void paged_rows_kernel(RowsParams p) {
       const uint32_t i = base + j * kPass;
       if (i >= n_rows) continue;
       const uint32_t t = kTok == 1 ? 0 : a.heads.div(i), head = i - t * a.heads.d;
-      const char *row = src + static_cast<uint64_t>(t) * (static_cast<uint32_t>(a.in_ts) * T::kBytes) +
-                        static_cast<uint64_t>(head) * (static_cast<uint32_t>(a.in_hs) * T::kBytes);
+      const char *row = src + static_cast<uint64_t>(t) * (a.in_ts * T::kBytes) +
+                        static_cast<uint64_t>(head) * (a.in_hs * T::kBytes);
       x[j][0] = T::fetch(row + g0 * T::kBytes);
       x[j][1] = T::fetch(row + g1 * T::kBytes);
     }
@@ -229,8 +229,8 @@ __global__ __launch_bounds__(kThreads) void paged_rows_kernel(RowsParams p) {
         C::template store<kWhole>(row + g0 * C::kBytes, y);
         C::template store<kWhole>(row + g1 * C::kBytes, y + 8);
       } else {
-        char *row = out + static_cast<uint64_t>(t) * (static_cast<uint32_t>(a.out_ts) * T::kBytes) +
-                    static_cast<uint64_t>(head) * (static_cast<uint32_t>(a.out_hs) * T::kBytes);
+        char *row = out + static_cast<uint64_t>(t) * (a.out_ts * T::kBytes) +
+                    static_cast<uint64_t>(head) * (a.out_hs * T::kBytes);
         constexpr bool kWhole = kStream && T::kBytes == 2;
         T::template store<kWhole>(row + g0 * T::kBytes, y);
         T::template store<kWhole>(row + g1 * T::kBytes, y + 8);
@@ -264,7 +264,7 @@ int check_rows(const sdvg_rows *r, int64_t n_tokens, int size, bool out, RowsArg
       ((n_tokens > 1 && r->in_token_stride != r->out_token_stride) || (r->n_heads > 1 && r->in_head_stride != r->out_head_stride)))
     return SDVG_ERR_RANGE;
   if (r->n_heads > (1 << 20)) return SDVG_ERR_UNSUPPORTED;
-  const auto step = [](int64_t n, int64_t stride) { return n > 1 ? stride : 0; };
+  const auto step = [](int64_t n, int64_t stride) { return n > 1 ? static_cast<uint32_t>(stride) : 0u; };  // (free where nothing is stepped over)
   a = RowsArg{r->in, r->out, step(n_tokens, r->in_token_stride), step(r->n_heads, r->in_head_stride), step(n_tokens, r->out_token_stride),
               step(r->n_heads, r->out_head_stride), sdvg::FastDiv::of(r->n_heads)};
   return SDVG_OK;
