@@ -174,12 +174,21 @@ __device__ __forceinline__ bool find(const First &p, int x, Found &f) {
     }
     chunk = pg::chunk_of(total, row_tiles, p.target);
   }
+  // items: the full pieces of all requests come before all others
+  int n_full = 0;
+  if (kItems && p.target > 0)
+    for (int b = 0; b < p.n_requests; b += 64) {
+      const pg::Request q = b ? load_request<kRowTile>(p, b + lane) : mine0;
+      n_full += wave_total(q.row_tiles * pg::full_pieces(q, chunk));
+    }
+  const bool among_full = kItems && x < n_full;
+  if (kItems && !among_full) x -= n_full;
   int before = 0, slots_before = 0;
   for (int b = 0; b < p.n_requests; b += 64) {
     const pg::Request q = b ? load_request<kRowTile>(p, b + lane) : mine0;
-    const int32_t pieces = pg::pieces_of(q, chunk);
+    const int32_t full = pg::full_pieces(q, chunk), pieces = pg::pieces_of(q, chunk, full);
     const int32_t slots = pieces > 1 ? q.row_tiles * pieces : 0;
-    const int32_t mine = kItems ? q.row_tiles * pieces : pieces > 1 ? q.row_tiles : 0;
+    const int32_t mine = q.row_tiles * (!kItems ? pieces > 1 : among_full ? full : pieces - full);
     const int upto = scan(mine), slots_upto = scan(slots);  // inclusive
     const int at = x - before - (upto - mine);
     const uint64_t hit = __ballot(at >= 0 && at < mine);
@@ -189,10 +198,10 @@ __device__ __forceinline__ bool find(const First &p, int x, Found &f) {
       f.q = pg::Request{get(q.row0), get(q.n), get(q.len), get(q.first_tile), get(q.tiles), get(q.row_tiles)};
       f.request = b + src;
       f.pieces = get(pieces);
-      const int i = get(at), slot0 = slots_before + get(slots_upto - slots);
+      const int i = get(at), n = get(full), slot0 = slots_before + get(slots_upto - slots);
       f.chunk = chunk;
-      f.tile = !kItems ? i : f.q.row_tiles > 1 ? static_cast<uint32_t>(i) / static_cast<uint32_t>(f.pieces) : 0;
-      f.piece = kItems ? i - f.tile * f.pieces : 0;
+      f.tile = among_full && f.q.row_tiles > 1 ? static_cast<uint32_t>(i) / static_cast<uint32_t>(n) : among_full ? 0 : i;
+      f.piece = among_full ? i - f.tile * n : n;
       f.slot = slot0 + f.tile * f.pieces;
       return true;
     }
@@ -260,7 +269,7 @@ __global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(FIRS
     for (int d = 0; d < 8; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  const int before = f.piece * f.chunk;   // (0 in a request of one piece, whatever the chunk is)
+  const int before = f.piece ? f.piece * f.chunk : 0;
   const int begin = f.q.first_tile + before;
   const int end = f.q.first_tile + (f.q.tiles - before < f.chunk ? f.q.tiles : before + f.chunk);
   const int32_t *table = p.table + static_cast<int64_t>(f.request) * p.table_stride;

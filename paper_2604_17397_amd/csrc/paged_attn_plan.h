@@ -70,9 +70,13 @@ SDVG_PAGED_HD int32_t chunk_of(int64_t total, int64_t row_tiles, int32_t target)
   }
   return c > kMinChunk ? static_cast<int32_t>(c < INT32_MAX ? c : INT32_MAX) : kMinChunk;
 }
-// Items per row tile, each of `chunk` key tiles but the last.
-SDVG_PAGED_HD int32_t pieces_of(const Request &q, int32_t chunk) {
-  return q.tiles > chunk ? static_cast<int32_t>((static_cast<uint32_t>(q.tiles) + static_cast<uint32_t>(chunk) - 1) / static_cast<uint32_t>(chunk)) : 1;
+// Pieces per row tile: `full` ones of `chunk` key tiles, and one of what is left (of everything where there are no keys). The
+// full ones of all requests are started first, so that short ones are left for the end, when the chip runs empty.
+SDVG_PAGED_HD int32_t full_pieces(const Request &q, int32_t chunk) {
+  return q.tiles >= chunk ? static_cast<int32_t>(static_cast<uint32_t>(q.tiles) / static_cast<uint32_t>(chunk)) : 0;
+}
+SDVG_PAGED_HD int32_t pieces_of(const Request &q, int32_t chunk, int32_t full) {
+  return full + (full == 0 || q.tiles > full * chunk ? 1 : 0);
 }
 
 // Bounds for the launch, from what the host knows, with most = kFiner * target >= total / chunk. Items: most full chunks, and one

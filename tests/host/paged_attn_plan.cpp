@@ -54,7 +54,8 @@ static void one(int R, int longest, int most_new, int group, int row_tile, int w
   for (const pg::Request &x : q) all_row_tiles += x.row_tiles;
   const int32_t chunk = pg::chunk_of(total, all_row_tiles, target);
   for (int r = 0; r < R; ++r) {
-    const int n = pg::pieces_of(q[r], chunk);
+    const int full = pg::full_pieces(q[r], chunk), n = pg::pieces_of(q[r], chunk, full);
+    CHECK(int64_t{full} * chunk <= q[r].tiles && (n == full || n == full + 1) && (n > full || int64_t{full} * chunk == q[r].tiles));
     row_tiles += q[r].row_tiles;
     items += int64_t{q[r].row_tiles} * n;
     if (n > 1) {
