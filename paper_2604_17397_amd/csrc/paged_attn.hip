@@ -50,7 +50,7 @@ struct First {
   const int32_t *q_start, *kv_lens;
   int32_t n_requests, n_tokens, group, window, target;
   int32_t capacity;                   // keys a row of the table can name
-  sdvg::FastDiv by_heads;             // workgroups -> items
+  sdvg::FastDiv by_heads;             // workgroups -> items, by (sets of) key heads
 };
 
 // What both kernels need of the output. (A launch takes 0.3 us longer per 100 bytes of arguments.)
@@ -75,9 +75,10 @@ struct AttnParams {
   OutParams to;
 };
 
-// Rows of a workgroup: NT tiles of 16 per wave, RS sets of 4 waves with different rows and the same keys (they share K and V
-// through the caches). Two waves per SIMD are what the registers leave room for.
-constexpr int kKeyWaves = 4;
+// A workgroup is 4 RS waves with NT tiles of 16 rows each. RS = 2: two sets of 4 waves have different rows and the same keys (they
+// share K and V through the caches). HS = 2: two sets of 2 waves have the same rows of neighbouring key heads, whose rows of K and
+// V are neighbours in a cache with tokens ahead of heads; read together, they keep more of each visit to a memory channel.
+// Two waves per SIMD are what the registers leave room for.
 constexpr int row_tile(int nt, int rs) { return kRows * nt * rs; }
 constexpr int per_unit(int row_tile) { return row_tile == 64 ? 1 : 2; }  // workgroups per compute unit
 
@@ -159,7 +160,7 @@ __device__ __forceinline__ pg::Request load_request(const First &p, int r) {
   return pg::request_of(p.q_start[r], p.q_start[r + 1], p.kv_lens[r], p.n_tokens, p.group, kRowTile, p.window, p.capacity);
 }
 // Number `x` among the items (kItems) or among the split row tiles.
-template <int kRowTile, bool kItems>
+template <int kRowTile, int kKeyWaves, bool kItems>
 __device__ __forceinline__ bool find(const First &p, int x, Found &f) {
   const int lane = threadIdx.x & 63;
   const pg::Request mine0 = load_request<kRowTile>(p, lane);
@@ -172,7 +173,7 @@ __device__ __forceinline__ bool find(const First &p, int x, Found &f) {
       row_tiles += wave_total(q.row_tiles);
       total += wave_total(static_cast<int>(w & 0xffff)) + (static_cast<int64_t>(wave_total(static_cast<int>(w >> 16))) << 16);
     }
-    chunk = pg::chunk_of(total, row_tiles, p.target);
+    chunk = pg::chunk_of(total, row_tiles, p.target, kKeyWaves);
   }
   // items: the full pieces of all requests come before all others
   int n_full = 0;
@@ -212,21 +213,23 @@ __device__ __forceinline__ bool find(const First &p, int x, Found &f) {
 }
 
 // T: type of q, of P and of the output. kF8: the cache holds e4m3 numbers.
-template <typename T, bool kF8, int NT, int RS>
-__global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(FIRST_ARGS, AttnParams p) {
-  constexpr int kRowTile = row_tile(NT, RS), kWaves = kKeyWaves * RS, kThreads = 64 * kWaves;
-  constexpr int kDims = 128 * kRows * RS / kThreads;   // per thread where the workgroup finishes rows
+template <typename T, bool kF8, int NT, int RS, int HS>
+__global__ __launch_bounds__(256 * RS, 2) void paged_attn_kernel(FIRST_ARGS, AttnParams p) {
+  static_assert(RS == 1 || HS == 1, "a set of waves has other rows or another head");
+  constexpr int kRowTile = row_tile(NT, RS), kWaves = 4 * RS, kThreads = 64 * kWaves, kKeyWaves = 4 / HS;
+  constexpr int kDims = 128 * kRows * RS * HS / kThreads;   // per thread where the workgroup finishes rows
   constexpr int kBytes = kF8 ? 1 : 2;
   __shared__ float o_s[kWaves][kRows][kPad];
   __shared__ float ml_s[kWaves][kRows][2];
   Found f;
   // the key heads of an item are neighbours: together they read whole rows of the cache's tokens
   const First first{q_start, kv_lens, n_requests, n_tokens, group, window, target, capacity, {heads_d, heads_m, heads_s}};
-  const int item = first.by_heads.div(blockIdx.x), head = blockIdx.x - item * heads_d;
-  if (!find<kRowTile, true>(first, item, f)) return;
+  const int item = first.by_heads.div(blockIdx.x), head0 = (blockIdx.x - item * heads_d) * HS, n_kv_heads = heads_d * HS;
+  if (!find<kRowTile, kKeyWaves, true>(first, item, f)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
+  const int head = head0 + (HS > 1 ? wave / kKeyWaves : 0);
   const int rows = f.q.n * group - f.tile * kRowTile;   // rows of this tile, those past kRowTile included
-  const int row0 = wave / kKeyWaves * (NT * kRows);       // this wave's first
+  const int row0 = RS > 1 ? wave / kKeyWaves * (NT * kRows) : 0;   // this wave's first
 
   // the query rows of this lane: column col of every tile of 16
   u32x4 qf[NT][4];
@@ -419,7 +422,6 @@ __global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(FIRS
   }
 
   // The waves' results of a tile of 16 rows meet in LDS.
-  const float v_scale = kF8 && p.to.v_scale ? p.to.v_scale[head] : 1.0f;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     if (t * kRows >= rows) break;
@@ -438,7 +440,7 @@ __global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(FIRS
     __syncthreads();
     constexpr int kPerRow = 128 / kDims;
     const int r = threadIdx.x / kPerRow, d0 = threadIdx.x % kPerRow * kDims, set = r / kRows, c = r % kRows;
-    const int row = set * (NT * kRows) + t * kRows + c;
+    const int row = (RS > 1 ? set * (NT * kRows) : 0) + t * kRows + c, of_head = head0 + (HS > 1 ? set : 0);
     if (row >= rows) continue;   // (all waves come to the barriers: `rows` is the workgroup's)
     const float(*const ml)[kRows][2] = ml_s + set * kKeyWaves;
     float top = ml[0][c][0], total = 0.f;
@@ -455,15 +457,15 @@ __global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(FIRS
         acc[j] += weight * *reinterpret_cast<const f32x4 *>(&o_s[set * kKeyWaves + w][c][d0 + 4 * j]);
     }
     if (f.pieces > 1) {
-      const int64_t at = (static_cast<int64_t>(f.slot + f.piece) * heads_d + head) * kRowTile + row;
+      const int64_t at = (static_cast<int64_t>(f.slot + f.piece) * n_kv_heads + of_head) * kRowTile + row;
 #pragma unroll
       for (int j = 0; j < kDims / 4; ++j) reinterpret_cast<f32x4 *>(p.to.part_o + at * 128 + d0)[j] = acc[j];
       if (d0 == 0) *reinterpret_cast<f32x2 *>(p.to.part_ml + at * 2) = f32x2{top, total};
       continue;
     }
     const uint32_t all = f.tile * kRowTile + row, i = p.to.by_group.div(all), h = all - i * group;
-    const int64_t token = f.q.row0 + static_cast<int64_t>(i), q_head = static_cast<int64_t>(head) * group + h;
-    const float norm = top == -INFINITY ? 0.f : v_scale / total;   // (sum 0 only without a key)
+    const int64_t token = f.q.row0 + static_cast<int64_t>(i), q_head = static_cast<int64_t>(of_head) * group + h;
+    const float norm = top == -INFINITY ? 0.f : (kF8 && p.to.v_scale ? p.to.v_scale[of_head] : 1.0f) / total;   // (sum 0 only without a key)
     uint16_t *dst = static_cast<uint16_t *>(p.to.out) + token * p.to.o_ts + q_head * p.to.o_hs + d0;
 #pragma unroll
     for (int j = 0; j < kDims / 4; ++j)
@@ -474,7 +476,7 @@ __global__ __launch_bounds__(64 * kKeyWaves * RS, 2) void paged_attn_kernel(FIRS
 
 // Joins the pieces of the rows of a split row tile. 32 threads have a row's dims; the 8 sets of them in a workgroup have
 // a row each where the pieces are few, and share the pieces of one row where they are many.
-template <typename T, bool kF8, int NT, int RS>
+template <typename T, bool kF8, int NT, int RS, int HS>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(FIRST_ARGS, OutParams p) {
   constexpr int kRowTile = row_tile(NT, RS), kSets = kJoinThreads / 32;
   __shared__ f32x4 o_s[kSets][32];
@@ -482,7 +484,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(FIRST_ARGS, Ou
   Found f;
   const First head_args{q_start, kv_lens, n_requests, n_tokens, group, window, target, capacity, {heads_d, heads_m, heads_s}};
   const int index = head_args.by_heads.div(blockIdx.x), head = blockIdx.x - index * heads_d;
-  if (!find<kRowTile, false>(head_args, index, f)) return;
+  if (!find<kRowTile, 4 / HS, false>(head_args, index, f)) return;
   const int left = f.q.n * group - f.tile * kRowTile, rows = left < kRowTile ? left : kRowTile;
   const int64_t step = static_cast<int64_t>(heads_d) * kRowTile;   // rows between two pieces
   const int d4 = threadIdx.x & 31, set = threadIdx.x >> 5;
@@ -550,9 +552,17 @@ int row_tile_of(int64_t n_requests, int64_t n_tokens, int group) {
   return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
 }
 
-// Items per key head that fill the chip once.
-int target_of(int n_cu, int n_kv_heads, int row_tile) {
-  const int t = per_unit(row_tile) * n_cu / n_kv_heads;
+// Sets of heads per workgroup (HS): where the rows of neighbouring heads are neighbours. us, 1 and 2: one request of 131071 keys x 8
+// heads, 16 bit 95.5 and 90.2, ragged 207 and 197, 32 rows e4m3 40.3 and 38.5; a cache with heads ahead of tokens 50.7 and 53.1 (e4m3).
+// 32 rows in 16 bits would spill registers.
+int head_sets(const sdvg_paged_kv &c, int row_tile) {
+  const bool fits = row_tile == 16 || (row_tile == 32 && c.dtype == SDVG_E4M3);
+  return fits && c.n_kv_heads % 2 == 0 && c.head_stride < c.token_stride ? 2 : 1;
+}
+
+// Items per (set of) key heads that fill the chip once.
+int target_of(int n_cu, const sdvg_paged_kv &c, int row_tile) {
+  const int t = per_unit(row_tile) * n_cu * head_sets(c, row_tile) / c.n_kv_heads;
   return t > 1 ? t : 1;
 }
 
@@ -579,32 +589,37 @@ int check_attn(const sdvg_paged_attn_desc *d, const sdvg_paged_kv *c) {
 
 #define FIRST(f) \
   f.q_start, f.kv_lens, f.n_requests, f.n_tokens, f.group, f.window, f.target, f.capacity, f.by_heads.d, f.by_heads.m, f.by_heads.s
-template <typename T, bool kF8, int NT, int RS>
-int launch_attn(const First &f, const AttnParams &p, hipStream_t s) {
-  constexpr int kRowTile = row_tile(NT, RS), kThreads = 64 * kKeyWaves * RS;
+template <typename T, bool kF8, int NT, int RS, int HS>
+int launch_attn(First f, const AttnParams &p, hipStream_t s) {
+  constexpr int kRowTile = row_tile(NT, RS), kThreads = 256 * RS;
   const int64_t tiles = pg::max_row_tiles(f.n_requests, f.n_tokens, f.group, kRowTile);
-  const int64_t items = pg::max_items(tiles, f.target, f.capacity);
+  const int64_t items = pg::max_items(tiles, f.target, f.capacity, 4 / HS);
   if (items * f.by_heads.d >= (1 << 23)) return SDVG_ERR_UNSUPPORTED;  // (a grid holds fewer than 2^32 threads)
-  hipLaunchKernelGGL((paged_attn_kernel<T, kF8, NT, RS>), dim3(static_cast<uint32_t>(items * f.by_heads.d)), dim3(kThreads), 0, s, FIRST(f), p);
+  hipLaunchKernelGGL((paged_attn_kernel<T, kF8, NT, RS, HS>), dim3(static_cast<uint32_t>(items * f.by_heads.d)), dim3(kThreads), 0, s, FIRST(f), p);
   SDVG_HIP_CHECK(hipGetLastError());
-  if (f.target > 0 && pg::max_pieces(f.capacity) > 1) {
+  if (f.target > 0 && pg::max_pieces(f.capacity, 4 / HS) > 1) {
     // Workgroups per row tile: one for every row of an average request's where that are few (then the pieces are many, and
     // shared), otherwise one for every 8 rows. A workgroup takes more rows where there are more.
+    f.by_heads = sdvg::FastDiv::of(f.by_heads.d * HS);
     const int64_t groups = pg::max_groups(tiles, f.target) * f.by_heads.d;
     int64_t rows = (static_cast<int64_t>(f.n_tokens) + f.n_requests - 1) / f.n_requests * f.group;
     rows = rows < kRowTile ? rows : kRowTile;
     if (groups * rows > 1024) rows = (rows + 7) / 8;
-    hipLaunchKernelGGL((paged_join_kernel<T, kF8, NT, RS>), dim3(static_cast<uint32_t>(groups), static_cast<uint32_t>(rows)),
+    hipLaunchKernelGGL((paged_join_kernel<T, kF8, NT, RS, HS>), dim3(static_cast<uint32_t>(groups), static_cast<uint32_t>(rows)),
                        dim3(kJoinThreads), 0, s, FIRST(f), p.to);
     SDVG_HIP_CHECK(hipGetLastError());
   }
   return SDVG_OK;
 }
 template <typename T, bool kF8>
-int launch_attn(const First &f, const AttnParams &p, int row_tile, hipStream_t s) {
-  return row_tile == 16   ? launch_attn<T, kF8, 1, 1>(f, p, s)
-         : row_tile == 32 ? launch_attn<T, kF8, 2, 1>(f, p, s)
-                          : launch_attn<T, kF8, 2, 2>(f, p, s);
+int launch_attn(const First &f, const AttnParams &p, int row_tile, int sets, hipStream_t s) {
+  if (row_tile == 64) return launch_attn<T, kF8, 2, 2, 1>(f, p, s);
+  if (sets == 2) {
+    if constexpr (kF8)
+      if (row_tile == 32) return launch_attn<T, kF8, 2, 1, 2>(f, p, s);
+    return launch_attn<T, kF8, 1, 1, 2>(f, p, s);
+  }
+  return row_tile == 16 ? launch_attn<T, kF8, 1, 1, 1>(f, p, s) : launch_attn<T, kF8, 2, 1, 1>(f, p, s);
 }
 
 }  // namespace
@@ -615,7 +630,7 @@ extern "C" int64_t sdvg_paged_attn_workspace_bytes(const sdvg_paged_attn_desc *d
   if (desc->n_requests == 0 || desc->n_tokens == 0) return 0;
   if ((st = compute_units(n_cu)) != SDVG_OK) return st;
   const int tile = row_tile_of(desc->n_requests, desc->n_tokens, desc->n_heads / cache->n_kv_heads);
-  return workspace_of(target_of(n_cu, cache->n_kv_heads, tile), cache->n_kv_heads, tile);
+  return workspace_of(target_of(n_cu, *cache, tile), cache->n_kv_heads, tile);
 }
 
 extern "C" int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_paged_kv *cache, const void *q,
@@ -642,7 +657,7 @@ extern "C" int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_page
   int64_t capacity = int64_t{desc->table_width} * cache->page_tokens;
   if (capacity > INT32_MAX - 2 * pg::kKeyTile) capacity = INT32_MAX - 2 * pg::kKeyTile;  // (more than any pool holds)
   const int32_t n_kv = cache->n_kv_heads, group = desc->n_heads / n_kv;
-  First f{q_start, kv_lens, desc->n_requests, desc->n_tokens, group, desc->window, 0, static_cast<int32_t>(capacity), sdvg::FastDiv::of(n_kv)};
+  First f{q_start, kv_lens, desc->n_requests, desc->n_tokens, group, desc->window, 0, static_cast<int32_t>(capacity), {}};
   AttnParams p{};
   p.q = q;
   p.k = cache->k;
@@ -661,7 +676,8 @@ extern "C" int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_page
   p.by_page = sdvg::FastDiv::of(cache->page_tokens / 8);
   p.to = OutParams{out, lse, nullptr, nullptr, cache->v_scale, static_cast<uint32_t>(desc->o_token_stride),
                    static_cast<uint32_t>(desc->o_head_stride), desc->n_heads, sdvg::FastDiv::of(group)};
-  const int tile = row_tile_of(f.n_requests, f.n_tokens, group), target = target_of(n_cu, n_kv, tile);
+  const int tile = row_tile_of(f.n_requests, f.n_tokens, group), target = target_of(n_cu, *cache, tile), sets = head_sets(*cache, tile);
+  f.by_heads = sdvg::FastDiv::of(n_kv / sets);
   if (workspace && workspace_bytes >= workspace_of(target, n_kv, tile)) {
     f.target = target;
     p.to.part_o = static_cast<float *>(workspace);
@@ -669,6 +685,6 @@ extern "C" int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_page
   }
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool f8 = cache->dtype == SDVG_E4M3;
-  if (desc->dtype == SDVG_BF16) return f8 ? launch_attn<Bf16, true>(f, p, tile, s) : launch_attn<Bf16, false>(f, p, tile, s);
-  return f8 ? launch_attn<F16, true>(f, p, tile, s) : launch_attn<F16, false>(f, p, tile, s);
+  if (desc->dtype == SDVG_BF16) return f8 ? launch_attn<Bf16, true>(f, p, tile, sets, s) : launch_attn<Bf16, false>(f, p, tile, sets, s);
+  return f8 ? launch_attn<F16, true>(f, p, tile, sets, s) : launch_attn<F16, false>(f, p, tile, sets, s);
 }

@@ -19,7 +19,6 @@ namespace sdvg {
 namespace paged {
 
 constexpr int kKeyTile = 32;   // keys a wave takes per step
-constexpr int kMinChunk = 4;   // key tiles of an item at least: one per wave
 
 // What a request asks for.
 struct Request {
@@ -49,7 +48,7 @@ SDVG_PAGED_HD Request request_of(int32_t start, int32_t end, int32_t len, int32_
 SDVG_PAGED_HD int64_t work_of(const Request &q) { return static_cast<int64_t>(q.row_tiles) * (q.tiles > 1 ? q.tiles : 1); }
 
 // Key tiles per item at most: total = the sum of work_of over all requests, row_tiles that of theirs, target the items that fill
-// the chip once (<= 0: no split). With few row tiles the items are made to be at most `target`, so that all run at once and
+// the chip once (<= 0: no split), key_waves the waves that share an item's key tiles, which have one each at least. With few row tiles the items are made to be at most `target`, so that all run at once and
 // end together; every row tile may add one by rounding up. With many row tiles that would leave some items much
 // longer than others: then they are made shorter, kFiner rounds of them, and the chip fills up again as they end; but not shorter
 // than kRoundChunk (what comes before and after the keys takes as long as some 10 key tiles) unless the chip is not filled once.
@@ -58,7 +57,7 @@ SDVG_PAGED_HD int64_t ceil_div(int64_t a, int32_t b) {
   if (a <= INT32_MAX) return (static_cast<uint32_t>(a) + static_cast<uint32_t>(b) - 1) / static_cast<uint32_t>(b);  // (the shorter division)
   return (a + b - 1) / b;
 }
-SDVG_PAGED_HD int32_t chunk_of(int64_t total, int64_t row_tiles, int32_t target) {
+SDVG_PAGED_HD int32_t chunk_of(int64_t total, int64_t row_tiles, int32_t target, int32_t key_waves) {
   if (target <= 0) return INT32_MAX;
   int64_t c;
   if (4 * row_tiles <= target) {
@@ -68,7 +67,7 @@ SDVG_PAGED_HD int32_t chunk_of(int64_t total, int64_t row_tiles, int32_t target)
     const int64_t least = once < kRoundChunk ? once : kRoundChunk;
     c = finer > least ? finer : least;
   }
-  return c > kMinChunk ? static_cast<int32_t>(c < INT32_MAX ? c : INT32_MAX) : kMinChunk;
+  return c > key_waves ? static_cast<int32_t>(c < INT32_MAX ? c : INT32_MAX) : key_waves;
 }
 // Pieces per row tile: `full` ones of `chunk` key tiles, and one of what is left (of everything where there are no keys). The
 // full ones of all requests are started first, so that short ones are left for the end, when the chip runs empty.
@@ -80,7 +79,7 @@ SDVG_PAGED_HD int32_t pieces_of(const Request &q, int32_t chunk, int32_t full) {
 }
 
 // Bounds for the launch, from what the host knows, with most = kFiner * target >= total / chunk. Items: most full chunks, and one
-// more per row tile; no more than `target` where the row tiles are few; and none of a row tile below kMinChunk key tiles of what a row of
+// more per row tile; no more than `target` where the row tiles are few; and none of a row tile below key_waves key tiles of what a row of
 // the block table can name (`capacity` keys). Slots: a split row tile of t > chunk tiles has ceil(t / chunk) < 2 t / chunk pieces. Groups
 // (split row tiles): t > chunk each.
 SDVG_PAGED_HD int64_t max_row_tiles(int64_t n_requests, int64_t n_tokens, int32_t group, int32_t row_tile) {
@@ -88,11 +87,11 @@ SDVG_PAGED_HD int64_t max_row_tiles(int64_t n_requests, int64_t n_tokens, int32_
   const int64_t bound = rows / row_tile + n_requests;
   return bound < rows ? bound : rows;
 }
-SDVG_PAGED_HD int64_t max_pieces(int64_t capacity) { return ceil_div(ceil_div(capacity, kKeyTile) + 1, kMinChunk); }  // (+ 1: a window may begin inside a tile)
-SDVG_PAGED_HD int64_t max_items(int64_t row_tiles, int32_t target, int64_t capacity) {
+SDVG_PAGED_HD int64_t max_pieces(int64_t capacity, int32_t key_waves) { return ceil_div(ceil_div(capacity, kKeyTile) + 1, key_waves); }  // (+ 1: a window may begin inside a tile)
+SDVG_PAGED_HD int64_t max_items(int64_t row_tiles, int32_t target, int64_t capacity, int32_t key_waves) {
   if (target <= 0) return row_tiles;
   const int64_t by_chunk = 4 * row_tiles <= target ? target : row_tiles + kFiner * static_cast<int64_t>(target);
-  const int64_t by_keys = row_tiles * max_pieces(capacity);
+  const int64_t by_keys = row_tiles * max_pieces(capacity, key_waves);
   return by_chunk < by_keys ? by_chunk : by_keys;
 }
 SDVG_PAGED_HD int64_t max_groups(int64_t row_tiles, int32_t target) { return row_tiles < kFiner * static_cast<int64_t>(target) ? row_tiles : kFiner * static_cast<int64_t>(target); }

@@ -25,7 +25,7 @@ static uint32_t rnd() {
     }                                                                                        \
   } while (0)
 
-static void one(int R, int longest, int most_new, int group, int row_tile, int window, int target, int64_t capacity) {
+static void one(int R, int longest, int most_new, int group, int row_tile, int window, int target, int64_t capacity, int key_waves) {
   std::vector<int32_t> start(R + 1), len(R);
   int tokens = 0;
   for (int r = 0; r < R; ++r) {
@@ -52,7 +52,7 @@ static void one(int R, int longest, int most_new, int group, int row_tile, int w
   }
   int64_t items = 0, slots = 0, groups = 0, row_tiles = 0, all_row_tiles = 0;
   for (const pg::Request &x : q) all_row_tiles += x.row_tiles;
-  const int32_t chunk = pg::chunk_of(total, all_row_tiles, target);
+  const int32_t chunk = pg::chunk_of(total, all_row_tiles, target, key_waves);
   for (int r = 0; r < R; ++r) {
     const int full = pg::full_pieces(q[r], chunk), n = pg::pieces_of(q[r], chunk, full);
     CHECK(int64_t{full} * chunk <= q[r].tiles && (n == full || n == full + 1) && (n > full || int64_t{full} * chunk == q[r].tiles));
@@ -67,8 +67,8 @@ static void one(int R, int longest, int most_new, int group, int row_tile, int w
   if (4 * row_tiles <= target) CHECK(items <= target);
   CHECK(row_tiles <= pg::max_row_tiles(R, tokens, group, row_tile));
   const int64_t bound = pg::max_row_tiles(R, tokens, group, row_tile);
-  CHECK(items <= pg::max_items(bound, target, capacity));
-  if (pg::max_pieces(capacity) == 1) CHECK(groups == 0);
+  CHECK(items <= pg::max_items(bound, target, capacity, key_waves));
+  if (pg::max_pieces(capacity, key_waves) == 1) CHECK(groups == 0);
   CHECK(slots <= pg::max_slots(target > 0 ? target : 0));
   CHECK(groups <= (target > 0 ? pg::max_groups(row_tiles, target) : 0));
 }
@@ -82,9 +82,9 @@ int main() {
         for (int row_tile : rows)
           for (int window : windows)
             for (int target : targets) {
-              one(R, longest, 1, group, row_tile, window, target, INT32_MAX - 64);
-              one(R, longest, 9, group, row_tile, window, target, n % 3 ? INT32_MAX - 64 : longest / 2 + 8);
-              one(R, longest, 2, group, row_tile, window, target, (longest + 9) / 8 * 8);
+              one(R, longest, 1, group, row_tile, window, target, INT32_MAX - 64, 4);
+              one(R, longest, 9, group, row_tile, window, target, n % 3 ? INT32_MAX - 64 : longest / 2 + 8, 1 << n % 3);
+              one(R, longest, 2, group, row_tile, window, target, (longest + 9) / 8 * 8, 2);
               ++n;
             }
   // out of range: clamped
