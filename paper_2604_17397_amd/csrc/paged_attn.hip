@@ -75,12 +75,12 @@ struct AttnParams {
   OutParams to;
 };
 
-// A workgroup is 4 RS waves with NT tiles of 16 rows each. RS = 2: two sets of 4 waves have different rows and the same keys (they
-// share K and V through the caches). HS = 2: two sets of 2 waves have the same rows of neighbouring key heads, whose rows of K and
-// V are neighbours in a cache with tokens ahead of heads; read together, they keep more of each visit to a memory channel.
-// Two waves per SIMD are what the registers leave room for.
-constexpr int row_tile(int nt, int rs) { return kRows * nt * rs; }
-constexpr int per_unit(int row_tile) { return row_tile == 64 ? 1 : 2; }  // workgroups per compute unit
+// A workgroup is 4 waves with NT tiles of 16 rows each. HS = 2: two sets of 2 waves have the same rows of neighbouring key heads, whose
+// rows of K and V are neighbours in a cache with tokens ahead of heads; read together, they keep more of each visit to a
+// memory channel. Two waves per SIMD are what the registers leave room for. (64 rows in two sets of 4 waves with the same keys were
+// slower than two workgroups of 32: one request of 131071 keys, 40 to 64 rows, e4m3 101 us and 91.)
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kPerUnit = 2;             // workgroups per compute unit
 
 // ---- the two 16-bit types
 struct Bf16 {
@@ -201,8 +201,22 @@ __device__ __forceinline__ bool find(const First &p, int x, Found &f) {
       f.pieces = get(pieces);
       const int i = get(at), n = get(full), slot0 = slots_before + get(slots_upto - slots);
       f.chunk = chunk;
-      f.tile = among_full && f.q.row_tiles > 1 ? static_cast<uint32_t>(i) / static_cast<uint32_t>(n) : among_full ? 0 : i;
-      f.piece = among_full ? i - f.tile * n : n;
+      // The row tiles of a piece follow each other where workgroups that read the same keys then are on the same XCD (they are
+      // dealt out to 8 in turn): 64 rows x 131071 keys x 8 heads, 16 bit, 166 us with the pieces of a row tile in a row, 136 so;
+      // with 4 sets of heads (e4m3) 92 and 97.
+      if (!among_full) {
+        f.tile = i;
+        f.piece = kItems ? n : 0;
+      } else if (f.q.row_tiles == 1) {
+        f.tile = 0;
+        f.piece = i;
+      } else if (p.by_heads.d % 8 == 0) {
+        f.piece = static_cast<uint32_t>(i) / static_cast<uint32_t>(f.q.row_tiles);
+        f.tile = i - f.piece * f.q.row_tiles;
+      } else {
+        f.tile = static_cast<uint32_t>(i) / static_cast<uint32_t>(n);
+        f.piece = i - f.tile * n;
+      }
       f.slot = slot0 + f.tile * f.pieces;
       return true;
     }
@@ -213,11 +227,10 @@ __device__ __forceinline__ bool find(const First &p, int x, Found &f) {
 }
 
 // T: type of q, of P and of the output. kF8: the cache holds e4m3 numbers.
-template <typename T, bool kF8, int NT, int RS, int HS>
-__global__ __launch_bounds__(256 * RS, 2) void paged_attn_kernel(FIRST_ARGS, AttnParams p) {
-  static_assert(RS == 1 || HS == 1, "a set of waves has other rows or another head");
-  constexpr int kRowTile = row_tile(NT, RS), kWaves = 4 * RS, kThreads = 64 * kWaves, kKeyWaves = 4 / HS;
-  constexpr int kDims = 128 * kRows * RS * HS / kThreads;   // per thread where the workgroup finishes rows
+template <typename T, bool kF8, int NT, int HS>
+__global__ __launch_bounds__(kThreads, kPerUnit) void paged_attn_kernel(FIRST_ARGS, AttnParams p) {
+  constexpr int kRowTile = kRows * NT, kKeyWaves = kWaves / HS;
+  constexpr int kDims = 128 * kRows * HS / kThreads;   // per thread where the workgroup finishes rows
   constexpr int kBytes = kF8 ? 1 : 2;
   __shared__ float o_s[kWaves][kRows][kPad];
   __shared__ float ml_s[kWaves][kRows][2];
@@ -227,16 +240,15 @@ __global__ __launch_bounds__(256 * RS, 2) void paged_attn_kernel(FIRST_ARGS, Att
   const int item = first.by_heads.div(blockIdx.x), head0 = (blockIdx.x - item * heads_d) * HS, n_kv_heads = heads_d * HS;
   if (!find<kRowTile, kKeyWaves, true>(first, item, f)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
-  const int head = head0 + (HS > 1 ? wave / kKeyWaves : 0);
+  const int head = head0 + (HS > 1 ? __builtin_amdgcn_readfirstlane(wave / kKeyWaves) : 0);   // (one for the wave: its addresses stay scalar)
   const int rows = f.q.n * group - f.tile * kRowTile;   // rows of this tile, those past kRowTile included
-  const int row0 = RS > 1 ? wave / kKeyWaves * (NT * kRows) : 0;   // this wave's first
 
   // the query rows of this lane: column col of every tile of 16
   u32x4 qf[NT][4];
   int32_t sees[NT], from[NT];   // keys from[..] <= j < sees[..]
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const int row = row0 + t * kRows + col;
+    const int row = t * kRows + col;
     const uint32_t all = f.tile * kRowTile + row, i = p.to.by_group.div(all), h = all - i * group;
     sees[t] = from[t] = 0;
 #pragma unroll
@@ -405,7 +417,7 @@ __global__ __launch_bounds__(256 * RS, 2) void paged_attn_kernel(FIRST_ARGS, Att
     }
   };
   int tile = begin + wave % kKeyWaves;
-  if (tile < end && row0 < rows) {
+  if (tile < end) {
     const Place k_at = place_of(tile * 4 + (col >> 2)), v_at = place_of(tile * 4 + quad);
     const int next = tile + kKeyWaves < end ? tile + kKeyWaves : tile;
     k_next = place_of(next * 4 + (col >> 2));
@@ -440,7 +452,7 @@ __global__ __launch_bounds__(256 * RS, 2) void paged_attn_kernel(FIRST_ARGS, Att
     __syncthreads();
     constexpr int kPerRow = 128 / kDims;
     const int r = threadIdx.x / kPerRow, d0 = threadIdx.x % kPerRow * kDims, set = r / kRows, c = r % kRows;
-    const int row = (RS > 1 ? set * (NT * kRows) : 0) + t * kRows + c, of_head = head0 + (HS > 1 ? set : 0);
+    const int row = t * kRows + c, of_head = head0 + (HS > 1 ? set : 0);
     if (row >= rows) continue;   // (all waves come to the barriers: `rows` is the workgroup's)
     const float(*const ml)[kRows][2] = ml_s + set * kKeyWaves;
     float top = ml[0][c][0], total = 0.f;
@@ -476,15 +488,15 @@ __global__ __launch_bounds__(256 * RS, 2) void paged_attn_kernel(FIRST_ARGS, Att
 
 // Joins the pieces of the rows of a split row tile. 32 threads have a row's dims; the 8 sets of them in a workgroup have
 // a row each where the pieces are few, and share the pieces of one row where they are many.
-template <typename T, bool kF8, int NT, int RS, int HS>
+template <typename T, bool kF8, int NT, int HS>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(FIRST_ARGS, OutParams p) {
-  constexpr int kRowTile = row_tile(NT, RS), kSets = kJoinThreads / 32;
+  constexpr int kRowTile = kRows * NT, kSets = kJoinThreads / 32;
   __shared__ f32x4 o_s[kSets][32];
   __shared__ float ml_s[kSets][2];
   Found f;
   const First head_args{q_start, kv_lens, n_requests, n_tokens, group, window, target, capacity, {heads_d, heads_m, heads_s}};
   const int index = head_args.by_heads.div(blockIdx.x), head = blockIdx.x - index * heads_d;
-  if (!find<kRowTile, 4 / HS, false>(head_args, index, f)) return;
+  if (!find<kRowTile, kWaves / HS, false>(head_args, index, f)) return;
   const int left = f.q.n * group - f.tile * kRowTile, rows = left < kRowTile ? left : kRowTile;
   const int64_t step = static_cast<int64_t>(heads_d) * kRowTile;   // rows between two pieces
   const int d4 = threadIdx.x & 31, set = threadIdx.x >> 5;
@@ -546,23 +558,23 @@ int compute_units(int &n) {
   return SDVG_OK;
 }
 
-// Rows per workgroup by the average request, so that K and V are read once per key head as a rule.
+// Rows per workgroup by the average request.
 int row_tile_of(int64_t n_requests, int64_t n_tokens, int group) {
   const int64_t rows = (n_tokens + n_requests - 1) / n_requests * group;
-  return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  return rows <= 16 ? 16 : 32;
 }
 
 // Sets of heads per workgroup (HS): where the rows of neighbouring heads are neighbours. us, 1 and 2: one request of 131071 keys x 8
 // heads, 16 bit 95.5 and 90.2, ragged 207 and 197, 32 rows e4m3 40.3 and 38.5; a cache with heads ahead of tokens 50.7 and 53.1 (e4m3).
 // 32 rows in 16 bits would spill registers.
 int head_sets(const sdvg_paged_kv &c, int row_tile) {
-  const bool fits = row_tile == 16 || (row_tile == 32 && c.dtype == SDVG_E4M3);
+  const bool fits = row_tile == 16 || c.dtype == SDVG_E4M3;
   return fits && c.n_kv_heads % 2 == 0 && c.head_stride < c.token_stride ? 2 : 1;
 }
 
 // Items per (set of) key heads that fill the chip once.
 int target_of(int n_cu, const sdvg_paged_kv &c, int row_tile) {
-  const int t = per_unit(row_tile) * n_cu * head_sets(c, row_tile) / c.n_kv_heads;
+  const int t = kPerUnit * n_cu * head_sets(c, row_tile) / c.n_kv_heads;
   return t > 1 ? t : 1;
 }
 
@@ -589,15 +601,15 @@ int check_attn(const sdvg_paged_attn_desc *d, const sdvg_paged_kv *c) {
 
 #define FIRST(f) \
   f.q_start, f.kv_lens, f.n_requests, f.n_tokens, f.group, f.window, f.target, f.capacity, f.by_heads.d, f.by_heads.m, f.by_heads.s
-template <typename T, bool kF8, int NT, int RS, int HS>
+template <typename T, bool kF8, int NT, int HS>
 int launch_attn(First f, const AttnParams &p, hipStream_t s) {
-  constexpr int kRowTile = row_tile(NT, RS), kThreads = 256 * RS;
+  constexpr int kRowTile = kRows * NT, kKeyWaves = kWaves / HS;
   const int64_t tiles = pg::max_row_tiles(f.n_requests, f.n_tokens, f.group, kRowTile);
-  const int64_t items = pg::max_items(tiles, f.target, f.capacity, 4 / HS);
+  const int64_t items = pg::max_items(tiles, f.target, f.capacity, kKeyWaves);
   if (items * f.by_heads.d >= (1 << 23)) return SDVG_ERR_UNSUPPORTED;  // (a grid holds fewer than 2^32 threads)
-  hipLaunchKernelGGL((paged_attn_kernel<T, kF8, NT, RS, HS>), dim3(static_cast<uint32_t>(items * f.by_heads.d)), dim3(kThreads), 0, s, FIRST(f), p);
+  hipLaunchKernelGGL((paged_attn_kernel<T, kF8, NT, HS>), dim3(static_cast<uint32_t>(items * f.by_heads.d)), dim3(kThreads), 0, s, FIRST(f), p);
   SDVG_HIP_CHECK(hipGetLastError());
-  if (f.target > 0 && pg::max_pieces(f.capacity, 4 / HS) > 1) {
+  if (f.target > 0 && pg::max_pieces(f.capacity, kKeyWaves) > 1) {
     // Workgroups per row tile: one for every row of an average request's where that are few (then the pieces are many, and
     // shared), otherwise one for every 8 rows. A workgroup takes more rows where there are more.
     f.by_heads = sdvg::FastDiv::of(f.by_heads.d * HS);
@@ -605,7 +617,7 @@ int launch_attn(First f, const AttnParams &p, hipStream_t s) {
     int64_t rows = (static_cast<int64_t>(f.n_tokens) + f.n_requests - 1) / f.n_requests * f.group;
     rows = rows < kRowTile ? rows : kRowTile;
     if (groups * rows > 1024) rows = (rows + 7) / 8;
-    hipLaunchKernelGGL((paged_join_kernel<T, kF8, NT, RS, HS>), dim3(static_cast<uint32_t>(groups), static_cast<uint32_t>(rows)),
+    hipLaunchKernelGGL((paged_join_kernel<T, kF8, NT, HS>), dim3(static_cast<uint32_t>(groups), static_cast<uint32_t>(rows)),
                        dim3(kJoinThreads), 0, s, FIRST(f), p.to);
     SDVG_HIP_CHECK(hipGetLastError());
   }
@@ -613,13 +625,12 @@ int launch_attn(First f, const AttnParams &p, hipStream_t s) {
 }
 template <typename T, bool kF8>
 int launch_attn(const First &f, const AttnParams &p, int row_tile, int sets, hipStream_t s) {
-  if (row_tile == 64) return launch_attn<T, kF8, 2, 2, 1>(f, p, s);
   if (sets == 2) {
     if constexpr (kF8)
-      if (row_tile == 32) return launch_attn<T, kF8, 2, 1, 2>(f, p, s);
-    return launch_attn<T, kF8, 1, 1, 2>(f, p, s);
+      if (row_tile == 32) return launch_attn<T, kF8, 2, 2>(f, p, s);
+    return launch_attn<T, kF8, 1, 2>(f, p, s);
   }
-  return row_tile == 16 ? launch_attn<T, kF8, 1, 1, 1>(f, p, s) : launch_attn<T, kF8, 2, 1, 1>(f, p, s);
+  return row_tile == 16 ? launch_attn<T, kF8, 1, 1>(f, p, s) : launch_attn<T, kF8, 2, 1>(f, p, s);
 }
 
 }  // namespace
