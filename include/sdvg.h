@@ -329,7 +329,7 @@ typedef struct {
  * A token without a page (free_pages ran out, the table is too narrow, the entry is negative) has slot -1; rows t
  * behind the last token have slot -1 and position 0. held_out[r] is the number of pages the request holds now and
  * *next_free_out = *next_free + all pages asked for: more than n_free says by how many they ran out.
- * Negative lengths count as 0. New tokens past max_tokens have pages, but no row: q_start, kv_lens,
+ * Negative lengths, held pages and cursors count as 0. New tokens past max_tokens have pages, but no row: q_start, kv_lens,
  * positions and slots count them as not there.
  *   held     device [n_requests], or NULL: every page a request needs is in its row of the table already, none is taken
  *            (free_pages, next_free, held_out and next_free_out are then not used and may be NULL).
@@ -413,10 +413,12 @@ int sdvg_paged_commit(const sdvg_paged_kv *cache, const sdvg_rows *k, const sdvg
  *             out = 0 and lse = -infinity. Numbers out of range in q_start and kv_lens are clamped.
  *   workspace device, nullable, 16-byte aligned: with at least sdvg_paged_attn_workspace_bytes(desc, cache) bytes the keys of long
  *             requests are split over workgroups and the pieces joined by a second small launch; without, every
- *             request's keys are one workgroup's per key head and tile of rows. Scratch: overlapping calls need their own.
+ *             request's keys are one workgroup's per key head and tile of rows. A workspace that is too small is ignored; one
+ *             request of many tokens needs the most of all with as many heads. Scratch: overlapping calls need their own.
  *   Arithmetic: products on the matrix cores with fp32 accumulation, fp32 softmax statistics and sums; probabilities are
  *   rounded to `dtype` before the product with V (their sum is not, so that lse has 32 bits), e4m3 numbers are exact in it. What
- *   lies in the cache behind a request's last key may be anything; keys that any row of a request sees must be finite.
+ *   lies in the cache outside of the keys that a row of the request sees (behind the last one, ahead of the first one's
+ *   window) may be anything, and pages that hold nothing else need not be there; keys that any row of a request sees must be finite.
  *   Made for few new tokens per request (1 .. some 16); longer ones are right, but read the keys once per 64 rows.
  * scale as in sdvg_attn_desc. n_requests and n_tokens may be 0 (no-op). Asynchronous on `stream`; launches kernels only.
  */

@@ -20,4 +20,4 @@ extern "C" const char *sdvg_status_string(int status) {
 
 extern "C" int sdvg_last_device_error(void) { return sdvg::g_last_device_error; }
 
-extern "C" int sdvg_version(void) { return 100; }
+extern "C" int sdvg_version(void) { return 200; }

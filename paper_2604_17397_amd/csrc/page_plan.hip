@@ -77,7 +77,7 @@ __global__ __launch_bounds__(kThreads) void page_plan_kernel(PlanParams p) {
   }
   tokens = tokens < a.max_tokens ? tokens : a.max_tokens;  // those that have rows
 
-  const int64_t next = a.held && a.next_free ? *a.next_free : 0;
+  const int64_t next = a.held && a.next_free && *a.next_free > 0 ? *a.next_free : 0;
   if (writer && first == 0 && threadIdx.x == 0) a.q_start[0] = 0;
   const int last = first + p.per_group < a.n_requests ? first + p.per_group : a.n_requests;
   for (int r = first; r < last; ++r) {
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(kThreads) void page_plan_kernel(PlanParams p) {
     const auto page_at = [&](int64_t j) -> int32_t {
       if (j < q.held) return j < a.table_width ? row[j] : -1;
       const int64_t at = base + (j - q.held);
-      return j < q.need && at >= 0 && at < a.n_free ? a.free_pages[at] : -1;
+      return j < q.need && at < a.n_free ? a.free_pages[at] : -1;
     };
     if (writer) {
       for (int64_t j = q.held + threadIdx.x; j < q.need; j += kThreads) row[j] = page_at(j);
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(kThreads) void page_plan_kernel(PlanParams p) {
         const int64_t len = q.cached + q.fresh;
         a.kv_lens[r] = static_cast<int32_t>(len < INT32_MAX ? len : INT32_MAX);
         if (a.held) {
-          int64_t left = base < 0 ? 0 : a.n_free - base;  // pages the list still has for this request
+          int64_t left = a.n_free - base;  // pages the list still has for this request
           left = left < 0 ? 0 : left < q.take ? left : q.take;
           a.held_out[r] = static_cast<int32_t>(q.held + left);
         }

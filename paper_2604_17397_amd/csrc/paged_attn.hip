@@ -271,6 +271,7 @@ __global__ __launch_bounds__(kThreads, kPerUnit) void paged_attn_kernel(FIRST_AR
   const int first_i = static_cast<int>(p.to.by_group.div(f.tile * kRowTile)),
             last_i = static_cast<int>(p.to.by_group.div(f.tile * kRowTile + last_row));
   const int all_sees = f.q.len - f.q.n + first_i + 1, last_sees = f.q.len - f.q.n + last_i + 1;
+  const int seen_from = window > 0 && all_sees - first_i > window ? all_sees - first_i - window : 0;   // by the request's first token
   const int all_from = window > 0 && last_sees > window ? last_sees - window : 0;
 
   const float scale = p.scale_log2e * (kF8 && p.k_scale ? p.k_scale[head] : 1.0f);
@@ -331,10 +332,11 @@ __global__ __launch_bounds__(kThreads, kPerUnit) void paged_attn_kernel(FIRST_AR
       k_after = place_of(after * 4 + (col >> 2));
       v_after = place_of(after * 4 + quad);
     }
-    // keys of this lane's block of 8 that are there
-    int there = f.q.len - (key0 + 8 * quad);
-    there = v_page < 0 ? 0 : there < 0 ? 0 : there > 8 ? 8 : there;
-    const bool gaps = __any(there < 8), masked = gaps || key0 + pg::kKeyTile > all_sees || key0 < all_from;
+    // keys of this lane's block of 8 that a row of the request may see: below .. upto
+    const int block0 = key0 + 8 * quad, below = seen_from - block0;
+    int upto = f.q.len - block0;
+    upto = v_page < 0 ? 0 : upto < 0 ? 0 : upto > 8 ? 8 : upto;
+    const bool gaps = __any(upto < 8 || below > 0), masked = gaps || key0 + pg::kKeyTile > all_sees || key0 < all_from;
     u32x4 pf[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -358,8 +360,8 @@ __global__ __launch_bounds__(kThreads, kPerUnit) void paged_attn_kernel(FIRST_AR
       if (masked) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int key = key0 + 8 * quad + e;
-          x[e] = e < there && key < sees[t] && key >= from[t] ? x[e] : -INFINITY;
+          const int key = block0 + e;
+          x[e] = e < upto && key < sees[t] && key >= from[t] ? x[e] : -INFINITY;
         }
       }
       const float high = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
@@ -380,11 +382,11 @@ __global__ __launch_bounds__(kThreads, kPerUnit) void paged_attn_kernel(FIRST_AR
         l[t] += a + b;
       }
     }
-    // V of keys that are not there is cleared (0 times anything but a number is no 0)
+    // V of keys that nobody sees is cleared (0 times anything but a number is no 0)
     if (gaps) {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (j >= there) vf[j] = chunk{};
+        if (j >= upto || j < below) vf[j] = chunk{};
     }
     // V^T: dim 2e + h of keys 2c, 2c + 1 from dword e of both
 #pragma unroll
@@ -592,7 +594,7 @@ int check_attn(const sdvg_paged_attn_desc *d, const sdvg_paged_kv *c) {
   if (d->n_requests < 0 || d->n_tokens < 0 || d->n_heads < 1 || d->n_heads % c->n_kv_heads != 0 || d->table_width < 1 ||
       d->window < 0)
     return SDVG_ERR_SHAPE;
-  if (c->n_kv_heads > 65535 || int64_t{d->n_tokens} * d->n_heads > INT32_MAX) return SDVG_ERR_UNSUPPORTED;
+  if (c->n_kv_heads > 65535 || int64_t{d->n_tokens} * d->n_heads > INT32_MAX - 64) return SDVG_ERR_UNSUPPORTED;
   if (d->n_requests > 1 && d->table_stride < d->table_width) return SDVG_ERR_SHAPE;
   if (d->n_requests > 1 && d->table_stride > INT32_MAX) return SDVG_ERR_UNSUPPORTED;
   if (!(d->scale >= 0.f) || !isfinite(d->scale)) return SDVG_ERR_RANGE;

@@ -75,6 +75,8 @@ def test_narrow_table_missing_pages_and_negative_lengths():
     check([3, 8, -5], [6, 1, 3], np.array([[-1, 6], [3, -1], [2, 2]]), 8, 12)          # a page that is missing
     check([-7, 4], [-2, 3], np.array([[1], [2]]), 8, 4, [-3, 1], [5], 0)
     check([2**31 - 3], [2], np.array([[1]]), 8, 2)                                      # far past the table
+    want = check([9, 4], [9, 6], np.array([[3, 8, -1], [4, -1, -1]]), 8, 15, [9, 1], [5, 6], None)   # more held than the table has
+    assert want["held"].tolist() == [9, 2]
 
 
 def test_tokens_past_the_room_have_no_row():

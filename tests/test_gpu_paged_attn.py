@@ -211,6 +211,81 @@ def test_numbers_out_of_range_are_clamped():
     assert (none == 7).all()
 
 
+@pytest.mark.parametrize("kind,cache", [("bf16", None), ("f16", "e4m3")])
+@pytest.mark.parametrize("window", [1, 37, 64, 500])
+def test_what_lies_ahead_of_the_window_may_be_anything(kind, cache, window):
+    """A rolling cache: pages ahead of the first token's window are gone, and the rest of the page it begins in is no number."""
+    requests = [(700, 3), (41, 2), (2000, 1), (1111, 8)]
+    c = Case(requests, 6, 2, 16, kind, cache)
+    want = c.check(window=window).clone()
+    poison = torch.tensor(float("nan"), device="cuda").to(c.k.dtype)
+    for r, (n, new) in enumerate(requests):
+        first = max(0, n - new + 1 - window)
+        for j in range(first // 16 * 16, first):
+            for t in (c.k, c.v):
+                raw = t.view(torch.uint8 if cache else torch.int16)
+                raw[c.table[r, j // 16], j % 16] = poison.view(torch.uint8 if cache else torch.int16)
+        c.table[r, :first // 16] = torch.tensor([-1, 2**31 - 1], dtype=torch.int32, device="cuda").repeat(400)[:first // 16]
+    import paper_2604_17397_amd as P
+    for ws in (None, torch.empty(P.paged_attn_workspace_bytes(c.q, c.handle(), c.table), dtype=torch.uint8, device="cuda")):
+        got = P.paged_attn(c.q, c.handle(), c.table, c.q_start, c.kv_lens, window=window, workspace=ws)
+        torch.cuda.synchronize()
+        if ws is not None:
+            assert torch.equal(got, want)
+        assert not torch.isnan(got).any()
+
+
+def test_pools_past_32_bits():
+    """Offsets of pages, heads and slots beyond 2^32 bytes and 2^31 elements: token-major and head-major pools of 5 GiB."""
+    import paper_2604_17397_amd as P
+    H, page = 8, 16
+    pages = (5 << 30) // (page * H * 256)
+    for how in ("token", "head"):
+        shape = (pages, page, H, 128) if how == "token" else (H, pages, page, 128)
+        pools = [torch.empty(shape, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        k, v = pools if how == "token" else [t.permute(1, 2, 0, 3) for t in pools]
+        c = P.PagedKV(k, v)
+        n = 200
+        table = i32([[pages - 1 - 7 * i for i in range(13)]])
+        x, y = (torch.randn((n, H, 128), device="cuda").bfloat16() for _ in range(2))
+        j = torch.arange(n, device="cuda")
+        slots = table[0].long()[j // page] * page + j % page
+        P.paged_commit(c, x, y, slots)
+        torch.cuda.synchronize()
+        assert torch.equal(k[table[0].long()[j // page], j % page], x) and torch.equal(v[table[0].long()[j // page], j % page], y)
+        q = torch.randn((1, H, 128), device="cuda").bfloat16()
+        got = P.paged_attn(q, c, table, i32([0, 1]), i32([n])).double()
+        torch.cuda.synchronize()
+        for h in range(H):
+            p = torch.softmax(x[:, h].double() @ q[0, h].double() / math.sqrt(128), 0)
+            assert ((got[0, h] - p @ y[:, h].double()).abs() <= 2.0**-7 * (p @ y[:, h].double().abs())).all()
+        del pools, k, v, c
+        torch.cuda.empty_cache()
+
+
+def test_two_streams_at_once_and_strided_output():
+    """Calls that overlap, each with a workspace of its own, and rows ahead of the first request's left as they are."""
+    import paper_2604_17397_amd as P
+    cases = [Case([(30000, 1), (5, 1)], 8, 2, 16, seed=s) for s in (1, 2)]
+    want = [c.check().clone() for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    outs = [torch.full((c.n_tokens + 1, 12, 128), 3.0, dtype=torch.bfloat16, device="cuda") for c in cases]
+    ws = [torch.empty(P.paged_attn_workspace_bytes(c.q, c.handle(), c.table), dtype=torch.uint8, device="cuda") for c in cases]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, s, o, w in zip(cases, streams, outs, ws):
+            P.paged_attn(c.q, c.handle(), c.table, c.q_start, c.kv_lens, out=o[1:, 2:10], workspace=w, stream=s)
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        assert torch.equal(o[1:, 2:10], w) and (o[0] == 3).all() and (o[:, :2] == 3).all() and (o[:, 10:] == 3).all()
+    c = cases[0]
+    q = torch.cat([c.q[:1] * 0 + 7, c.q])
+    out = torch.full_like(q, 3.0)
+    P.paged_attn(q, c.handle(), c.table, c.q_start + 1, c.kv_lens, out=out, workspace=ws[0])
+    torch.cuda.synchronize()
+    assert torch.equal(out[1:], want[0]) and (out[0] == 3).all()
+
+
 def test_split_and_whole_agree_and_repeat():
     """With and without the split the same result up to rounding; the same bits every time."""
     c = Case([(9000, 1), (100, 1), (20000, 1)], 10, 2, 16, "f16")

@@ -57,7 +57,7 @@ def strided(t, how):
     return t
 
 
-@pytest.mark.parametrize("n,H,Hy", [(1, 1, 0), (1, 40, 8), (3, 5, 1), (257, 12, 12), (1031, 3, 2), (4099, 1, 0)])
+@pytest.mark.parametrize("n,H,Hy", [(1, 1, 0), (1, 40, 8), (3, 5, 1), (257, 12, 12), (1031, 3, 2), (4099, 1, 0), (1026, 40, 70)])
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
 @pytest.mark.parametrize("rot,kind,how", [(128, "bf16", "plain"), (16, "bf16", "wide"), (48, "f16", "head"), (96, "f32", "wide"),
                                           (112, "f32", "plain")])
@@ -112,7 +112,7 @@ def test_rope_positions_and_the_pass_with_tables_agree():
     assert ((a - b).abs() <= 2.0**-7 * a.abs() + 2.0**-20).all() and (a != b).float().mean() < 1e-3
 
 
-@pytest.mark.parametrize("n,H,Hq,P_", [(1, 1, 1, 8), (1, 8, 40, 16), (70, 3, 9, 24), (1030, 2, 4, 64)])
+@pytest.mark.parametrize("n,H,Hq,P_", [(1, 1, 1, 8), (1, 8, 40, 16), (70, 3, 9, 24), (1030, 2, 4, 64), (1025, 20, 33, 16)])
 @pytest.mark.parametrize("kind,cache,rot,layout", [("bf16", "bf16", 128, "half"), ("f16", "f16", 64, "interleaved"),
                                                    ("bf16", "e4m3", 96, "half"), ("f16", "e4m3", 0, "half"), ("bf16", "bf16", 0, "half")])
 @pytest.mark.parametrize("pool", ["token", "head", "padded"])
