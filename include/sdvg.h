@@ -413,14 +413,17 @@ int sdvg_paged_commit(const sdvg_paged_kv *cache, const sdvg_rows *k, const sdvg
  *             out = 0 and lse = -infinity. Numbers out of range in q_start and kv_lens are clamped.
  *   workspace device, nullable, 16-byte aligned: with at least sdvg_paged_attn_workspace_bytes(desc, cache) bytes the keys of long
  *             requests are split over workgroups and the pieces joined by a second small launch; without, every
- *             request's keys are one workgroup's per key head and tile of rows. A workspace that is too small is ignored; one
- *             request of many tokens needs the most of all with as many heads. Scratch: overlapping calls need their own.
+ *             request's keys are one workgroup's per key head and tile of rows. A workspace that is too small is ignored. The
+ *             need may grow or shrink with n_requests and n_tokens: one that serves several shapes has the largest of their
+ *             sizes. Scratch: overlapping calls need their own.
  *   Arithmetic: products on the matrix cores with fp32 accumulation, fp32 softmax statistics and sums; probabilities are
  *   rounded to `dtype` before the product with V (their sum is not, so that lse has 32 bits), e4m3 numbers are exact in it. What
  *   lies in the cache outside of the keys that a row of the request sees (behind the last one, ahead of the first one's
  *   window) may be anything, and pages that hold nothing else need not be there; keys that any row of a request sees must be finite.
- *   Made for few new tokens per request (1 .. some 16); longer ones are right, but read the keys once per 64 rows.
- * scale as in sdvg_attn_desc. n_requests and n_tokens may be 0 (no-op). Asynchronous on `stream`; launches kernels only.
+ *   Made for few new tokens per request (1 .. some 16); longer ones are right, but read the keys once per 32 rows
+ *   (tokens x query heads of a group).
+ * scale as in sdvg_attn_desc. n_requests and n_tokens may be 0 (no-op); n_tokens * n_heads < 2^31 - 64. Asynchronous on `stream`;
+ * launches kernels only.
  */
 typedef struct {
   int32_t n_requests, n_tokens, n_heads, head_dim; /* n_heads: a multiple of the cache's; head_dim must be 128 */

@@ -157,7 +157,9 @@ __device__ __forceinline__ void turn4(float *x, const float *c, const float *s) 
 // T: type of the rows, C: type of the cache (T where none is written). A workgroup has kTok tokens of one of the tensors
 // (blockIdx.y, so that everything about it is scalar); 8 threads share a row. A thread's kUnroll rows are all asked for before
 // the angles are computed or the rows before them are turned.
-// Bound by HBM from some thousand rows on, with the vector units close behind (130 instructions per 32 bytes in and out).
+// Bound by HBM from some thousand rows on: 40 + 40 heads x 4680 tokens, bf16, 31.5 us = 6.1 TB/s; 6007 tokens into e4m3 pages, q of 32
+// heads beside k and v of 8, 23 us = 5.9 TB/s. Few tokens: 3 us, a launch and two trips to memory. One row at a time per thread with
+// the tensor looked up per row, accesses of 16 bytes 16 apart: 44.8 and 30.9 us.
 template <typename T, typename C, bool kHalf, int kTok, bool kStream>
 __global__ __launch_bounds__(kThreads) void paged_rows_kernel(RowsParams p) {
   __shared__ float cs[kTok][64], sn[kTok][64];
@@ -280,7 +282,9 @@ int launch_rows(const RowsParams &p, hipStream_t s) {
 template <typename T, typename C, bool kHalf>
 int launch_rows(const RowsParams &p, hipStream_t s) {
   // Few tokens: a workgroup each, so that more compute units work on them. Many: 4, which fills the computation of the
-  // angles (64 per token) with all threads. Stores as in the pass with tables: ordinary ones up to 4 MiB.
+  // angles (64 per token) with all threads. Stores as in the pass with tables: ordinary ones up to 4 MiB,
+  // which the next kernel finds in the caches. Beyond, 40 + 40 heads x 4680 tokens called in a row 32 us, with ordinary stores 38
+  // (what the last call left to be written back meets the next one's reads); the commit of 6007 tokens 22.6 and 23.8.
   const int64_t rows = static_cast<int64_t>(p.n_tokens) * (p.t[0].heads.d + p.t[1].heads.d + p.t[2].heads.d);
   if (p.n_tokens < 1024) return launch_rows<T, C, kHalf, 1, false>(p, s);
   return rows * 128 * T::kBytes <= (4 << 20) ? launch_rows<T, C, kHalf, 4, false>(p, s) : launch_rows<T, C, kHalf, 4, true>(p, s);
