@@ -15,7 +15,7 @@
 //     registers with 32 v_perm; product d of 8 then has rows 8 m + d of O^T.
 // Pages hold multiples of 8 tokens, so such a block of 8 keys lies on one page.
 //
-// us (kernel and join), TB/s of K and V: one request of 131071 keys, 40 query and 8 key heads, bf16 84 + 6, 6.0 (a read of
+// us (kernel and join), TB/s of K and V: one request of 131071 keys, 40 query and 8 key heads, bf16 81.5 + 5, 6.6 (a read of
 // contiguous memory reaches 6.1 to 6.3, with nontemporal loads 6.9 to 7.1; without its arithmetic the kernel takes as long);
 // 96 requests of 16 to 16384 keys, f16 189 + 6, 5.7; 24 requests with up to 8 new tokens of 40 heads, window 4096, e4m3 33 + 5, 3.1 (a
 // third is what comes before and after a workgroup's keys, and the second row tile of a request reads them again); one
@@ -583,7 +583,7 @@ int head_sets(const sdvg_paged_kv &c, int row_tile) {
   return fits && c.n_kv_heads % 2 == 0 && c.head_stride < c.token_stride ? 2 : 1;
 }
 
-// Items per (set of) key heads that fill the chip once.
+// Items per (set of) key heads that fill the chip, kPerUnit workgroups per unit.
 int target_of(int n_cu, const sdvg_paged_kv &c, int row_tile) {
   const int t = kPerUnit * n_cu * head_sets(c, row_tile) / c.n_kv_heads;
   return t > 1 ? t : 1;

@@ -48,11 +48,18 @@ SDVG_PAGED_HD Request request_of(int32_t start, int32_t end, int32_t len, int32_
 SDVG_PAGED_HD int64_t work_of(const Request &q) { return static_cast<int64_t>(q.row_tiles) * (q.tiles > 1 ? q.tiles : 1); }
 
 // Key tiles per item at most: total = the sum of work_of over all requests, row_tiles that of theirs, target the items that fill
-// the chip once (<= 0: no split), key_waves the waves that share an item's key tiles, which have one each at least. With few row tiles the items are made to be at most `target`, so that all run at once and
-// end together; every row tile may add one by rounding up. With many row tiles that would leave some items much
-// longer than others: then they are made shorter, kFiner rounds of them, and the chip fills up again as they end; but not shorter
-// than kRoundChunk (what comes before and after the keys takes as long as some 10 key tiles) unless the chip is not filled once.
-constexpr int kFiner = 3, kRoundChunk = 32;
+// the chip with two workgroups per compute unit (<= 0: no split), key_waves the waves that share an item's key tiles, which have
+// one each at least.
+// Few row tiles: the items are made to fit the chip, so that all run at once and end together; every row tile may add one by rounding
+// up. One workgroup per unit is enough for HBM where that rounding is small (up to a quarter of the units: 131071 keys 87 us, with two
+// 90; 24 requests x 8 heads x 2000 keys, which is more, 38 and 37).
+// Many row tiles: fitting would leave some items much longer than others, so they are made shorter, kFiner rounds of them, and the
+// chip fills up again as they end; but not shorter than kRoundChunk (what comes before and after the keys takes as long as some
+// 10 key tiles), unless the row tiles alone leave over a third of the units without work. us with that least and without: 64 requests x
+// 8 heads x 500 keys 25.0, 27.8, x 16 to 1000 keys 32.3, 31.1; 24 x 8, 30 rows, 936 keys 22.8, 28.1, 16 to 4000 keys 51, 53; but 40 x
+// 8 x 2000 keys 66, 54.
+// Requests of kWhole key tiles on average are not split: 64 x 8 x 120 keys 6.9 us, split 12.2; 250 keys 12.9, 18.4.
+constexpr int kFiner = 3, kRoundChunk = 32, kWhole = 8;
 SDVG_PAGED_HD int64_t ceil_div(int64_t a, int32_t b) {
   if (a <= INT32_MAX) return (static_cast<uint32_t>(a) + static_cast<uint32_t>(b) - 1) / static_cast<uint32_t>(b);  // (the shorter division)
   return (a + b - 1) / b;
@@ -61,12 +68,14 @@ SDVG_PAGED_HD int32_t chunk_of(int64_t total, int64_t row_tiles, int32_t target,
   if (target <= 0) return INT32_MAX;
   int64_t c;
   if (4 * row_tiles <= target) {
-    c = ceil_div(total, target - static_cast<int32_t>(row_tiles));
+    const int32_t slots = 8 * row_tiles <= target && target > 1 ? target / 2 : target;
+    c = ceil_div(total, slots - static_cast<int32_t>(row_tiles));
   } else {
     const int64_t once = ceil_div(total, target), finer = ceil_div(once, kFiner);
-    const int64_t least = once < kRoundChunk ? once : kRoundChunk;
+    const int64_t least = once < kRoundChunk && 3 * row_tiles < target ? once : kRoundChunk;
     c = finer > least ? finer : least;
   }
+  if (total <= kWhole * row_tiles && c < kWhole) c = kWhole;
   return c > key_waves ? static_cast<int32_t>(c < INT32_MAX ? c : INT32_MAX) : key_waves;
 }
 // Pieces per row tile: `full` ones of `chunk` key tiles, and one of what is left (of everything where there are no keys). The
@@ -80,14 +89,14 @@ SDVG_PAGED_HD int32_t pieces_of(const Request &q, int32_t chunk, int32_t full) {
 
 // Bounds for the launch, from what the host knows, with most = kFiner * target >= total / chunk. Items: most full chunks, and one
 // more per row tile; no more than `target` where the row tiles are few; and none of a row tile below key_waves key tiles of what a row of
-// the block table can name (`capacity` keys). Slots: a split row tile of t > chunk tiles has ceil(t / chunk) < 2 t / chunk pieces. Groups
+// the block table can name (`capacity` keys; one item where these are kWhole tiles). Slots: a split row tile of t > chunk tiles has ceil(t / chunk) < 2 t / chunk pieces. Groups
 // (split row tiles): t > chunk each.
 SDVG_PAGED_HD int64_t max_row_tiles(int64_t n_requests, int64_t n_tokens, int32_t group, int32_t row_tile) {
   const int64_t rows = n_tokens * group;
   const int64_t bound = rows / row_tile + n_requests;
   return bound < rows ? bound : rows;
 }
-SDVG_PAGED_HD int64_t max_pieces(int64_t capacity, int32_t key_waves) { return ceil_div(ceil_div(capacity, kKeyTile) + 1, key_waves); }  // (+ 1: a window may begin inside a tile)
+SDVG_PAGED_HD int64_t max_pieces(int64_t capacity, int32_t key_waves) { return ceil_div(capacity, kKeyTile) <= kWhole ? 1 : ceil_div(ceil_div(capacity, kKeyTile) + 1, key_waves); }  // (+ 1: a window may begin inside a tile)
 SDVG_PAGED_HD int64_t max_items(int64_t row_tiles, int32_t target, int64_t capacity, int32_t key_waves) {
   if (target <= 0) return row_tiles;
   const int64_t by_chunk = 4 * row_tiles <= target ? target : row_tiles + kFiner * static_cast<int64_t>(target);
