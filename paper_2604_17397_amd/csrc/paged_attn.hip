@@ -15,11 +15,11 @@
 //     registers with 32 v_perm; product d of 8 then has rows 8 m + d of O^T.
 // Pages hold multiples of 8 tokens, so such a block of 8 keys lies on one page.
 //
-// us (kernel and join), TB/s of K and V: one request of 131071 keys, 40 query and 8 key heads, bf16 81.5 + 5, 6.6 (a read of
+// us (kernel and join), TB/s of K and V: one request of 131071 keys, 40 query and 8 key heads, bf16 82 + 6, 6.6 (a read of
 // contiguous memory reaches 6.1 to 6.3, with nontemporal loads 6.9 to 7.1; without its arithmetic the kernel takes as long);
 // 96 requests of 16 to 16384 keys, f16 189 + 6, 5.7; 24 requests with up to 8 new tokens of 40 heads, window 4096, e4m3 33 + 5, 3.1 (a
 // third is what comes before and after a workgroup's keys, and the second row tile of a request reads them again); one
-// request of 936 keys, 12 heads 5.6 + 4, a chain of latencies: lengths 0.7, page numbers and q 0.6, K and V 1.3, one step 0.5, merge and
+// request of 936 keys, 12 heads 5.6 + 3 to 4, a chain of latencies: lengths 0.7, page numbers and q 0.6, K and V 1.3, one step 0.5, merge and
 // store 0.7, and the launch itself.
 #include <math.h>
 
@@ -511,7 +511,9 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(FIRST_ARGS, Ou
   const int left = f.q.n * group - f.tile * kRowTile, rows = left < kRowTile ? left : kRowTile;
   const int64_t step = static_cast<int64_t>(heads_d) * kRowTile;   // rows between two pieces
   const int d4 = threadIdx.x & 31, set = threadIdx.x >> 5;
-  const bool shared = f.pieces > 2 * kSets;
+  // (a row of its own costs a set a trip to memory for every 4 pieces, and one for each of the rest: one request of 12 heads, 936 keys,
+  // 15 pieces, 10.6 us, shared 8.9; 24 requests x 5 pieces 22.0, shared 22.6)
+  const bool shared = f.pieces > (rows <= static_cast<int>(gridDim.y) ? 5 : 2 * kSets);
   const int first = shared ? blockIdx.y : blockIdx.y * kSets + set, rows_step = shared ? gridDim.y : gridDim.y * kSets;
   for (int row = first; row < rows; row += rows_step) {
     const int64_t at = (static_cast<int64_t>(f.slot) * heads_d + head) * kRowTile + row;
