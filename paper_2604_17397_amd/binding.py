@@ -572,6 +572,13 @@ class PagePlan:
         self.slots = torch.zeros(max_tokens, dtype=torch.int64, device=device)
 
 
+def _int32(name, v):
+    v = int(v)
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError("%s must fit 32 bits" % name)
+    return v
+
+
 def _int_array(name, t, n, dtype=torch.int32):
     if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
         raise ValueError("%s must be a dense %s tensor of %d elements" % (name, str(dtype)[6:], n))
@@ -586,7 +593,11 @@ def page_plan(cached, new_tokens, block_table, page_tokens, free_pages=None, hel
     if out is None:
         if max_tokens is None:
             raise ValueError("page_plan needs max_tokens or out")
-        out = PagePlan(cached.shape[0], max_tokens, cached.device)
+        if stream is None:
+            out = PagePlan(cached.shape[0], max_tokens, cached.device)
+        else:
+            with torch.cuda.stream(stream):   # (its zeros must not come behind the plan)
+                out = PagePlan(cached.shape[0], max_tokens, cached.device)
     elif max_tokens is not None and max_tokens != out.slots.shape[0]:
         raise ValueError("out holds another number of tokens than max_tokens")
     r = (_NATIVE or _native()).page_plan(cached, new_tokens, block_table, page_tokens, free_pages, held, next_free, out.q_start,
@@ -615,7 +626,7 @@ def page_plan(cached, new_tokens, block_table, page_tokens, free_pages=None, hel
 
     def p(t):
         return None if t is None or t.numel() == 0 else t.data_ptr()
-    a = sdvg_page_plan_args(n, int(page_tokens), block_table.shape[1], 0 if free_pages is None else free_pages.shape[0],
+    a = sdvg_page_plan_args(n, _int32("page_tokens", page_tokens), block_table.shape[1], 0 if free_pages is None else free_pages.shape[0],
                             block_table.stride(0) if n > 1 else block_table.shape[1], out.slots.shape[0],
                             p(cached), p(new_tokens), p(free_pages),
                             # (without requests an empty `held` has no address, and still says that pages may be taken)
@@ -788,7 +799,7 @@ def _paged_attn_desc(q, cache, block_table, out, scale, window):
         raise ValueError("block_table must be int32 [requests, pages] with unit stride along the pages")
     _check_rows("out", out, q)
     n = block_table.shape[0]
-    return sdvg_paged_attn_desc(n, q.shape[0], q.shape[1], q.shape[2], block_table.shape[1], int(window),
+    return sdvg_paged_attn_desc(n, q.shape[0], q.shape[1], q.shape[2], block_table.shape[1], _int32("window", window),
                                 block_table.stride(0), q.stride(0), q.stride(1), out.stride(0), out.stride(1),
                                 0.0 if scale is None else float(scale), _ROW_TYPES[q.dtype])
 

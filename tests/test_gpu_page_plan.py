@@ -118,3 +118,23 @@ def test_steps_in_a_graph_take_pages_one_after_the_other():
             assert np.array_equal(table.cpu().numpy(), want_table), rep
             assert np.array_equal(plan.slots.cpu().numpy(), w["slots"]) and np.array_equal(plan.positions.cpu().numpy(), w["positions"])
             torch.zeros(1000, device="cuda").sum().item()       # eager work between the replays
+
+
+def test_new_plan_on_another_stream_than_the_busy_current_one():
+    import paper_2604_17397_amd as S
+    cached, new, table = np.array([5, 31, 0]), np.array([1, 4, 17]), np.array([[3, 4, 9], [7, 1, 8], [2, 0, -1]])
+    want = plan_oracle(cached, new, table, 16, 24, None, (), 0)
+    args = [i32(cached), i32(new), i32(table)]
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    torch.cuda._sleep(20_000_000)   # some ms of the current stream's time
+    plan = S.page_plan(*args, 16, max_tokens=24, stream=s)
+    torch.cuda.synchronize()
+    for name in ("q_start", "kv_lens", "positions", "slots"):
+        assert np.array_equal(getattr(plan, name).cpu().numpy(), want[name]), name
+
+
+def test_numbers_beyond_32_bits_are_refused():
+    import paper_2604_17397_amd as S
+    with pytest.raises(ValueError, match="32 bits"):
+        S.page_plan(i32([1]), i32([1]), i32([[0]]), 2**32 + 16, max_tokens=1)
