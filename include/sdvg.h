@@ -422,8 +422,8 @@ int sdvg_paged_commit(const sdvg_paged_kv *cache, const sdvg_rows *k, const sdvg
  *   window) may be anything, and pages that hold nothing else need not be there; keys that any row of a request sees must be finite.
  *   Made for few new tokens per request (1 .. some 16); longer ones are right, but read the keys once per 32 rows
  *   (tokens x query heads of a group).
- * scale as in sdvg_attn_desc. n_requests and n_tokens may be 0 (no-op); n_tokens * n_heads < 2^31 - 64. Asynchronous on `stream`;
- * launches kernels only.
+ * scale as in sdvg_attn_desc. n_requests and n_tokens may be 0 (no-op); n_tokens * n_heads < 2^31 - 64, and the
+ * tiles of 16 or 32 rows times the key heads below some 2^23 (SDVG_ERR_UNSUPPORTED). Asynchronous on `stream`; launches kernels only.
  */
 typedef struct {
   int32_t n_requests, n_tokens, n_heads, head_dim; /* n_heads: a multiple of the cache's; head_dim must be 128 */

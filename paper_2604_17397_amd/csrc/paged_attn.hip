@@ -224,7 +224,8 @@ __device__ __forceinline__ bool find(const First &p, int x, Found &f) {
         f.piece = i - f.tile * n;
       }
       f.slot = slot0 + f.tile * f.pieces;
-      return true;
+      // (always so, unless q_start decreases so far that sums leave 32 bits: the workspace is not left even then)
+      return f.pieces == 1 || (f.slot >= 0 && f.slot <= pg::max_slots(p.target) - f.pieces);
     }
     before += __builtin_amdgcn_readlane(upto, 63);
     slots_before += __builtin_amdgcn_readlane(slots_upto, 63);

@@ -329,3 +329,20 @@ def test_graph_with_other_lengths():
             g.replay()
             torch.cuda.synchronize()
             assert torch.equal(out, want), (a, b, d)
+
+
+def test_window_beyond_32_bits_is_refused():
+    import paper_2604_17397_amd as P
+    cache = P.PagedKV(*[torch.zeros((1, 16, 1, 128), device="cuda").bfloat16() for _ in range(2)])
+    q = torch.zeros((1, 1, 128), device="cuda").bfloat16()
+    with pytest.raises(ValueError, match="32 bits"):
+        P.paged_attn(q, cache, i32([[0]]), i32([0, 1]), i32([1]), window=2**32 + 5)
+
+
+@pytest.mark.parametrize("kv_heads", [1, 2])
+@pytest.mark.parametrize("lengths", [[256], [257], [8 * 32] * 5, [1] * 70 + [3000], [255, 256, 257, 1000], [9 * 32] * 40, [64] * 300])
+def test_around_the_shortest_request_that_is_split(lengths, kv_heads):
+    """Tables as wide as the longest request needs: up to 256 keys no request is split and nothing joined."""
+    c = Case([(n, 1) for n in lengths], 2 * kv_heads, kv_heads, 16, seed=len(lengths))
+    c.table = c.table[:, :-1].contiguous()
+    c.check()
