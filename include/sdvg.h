@@ -379,7 +379,7 @@ typedef struct {
 
 /*
  * Rotates x and, in the same launch, y (nullable: e.g. q and k of a layer), both of n_tokens tokens and of type `dtype`
- * (SDVG_BF16, SDVG_F16, SDVG_F32). n_tokens < 2^26; 0 is a no-op. Asynchronous on `stream`.
+ * (SDVG_BF16, SDVG_F16, SDVG_F32). n_tokens < 2^26 - 3; 0 is a no-op. Asynchronous on `stream`.
  */
 int sdvg_rope_positions(const sdvg_rope_desc *rope, const sdvg_rows *x, const sdvg_rows *y, int64_t n_tokens,
                         int32_t head_dim, int32_t dtype, void *stream);
@@ -392,7 +392,7 @@ int sdvg_rope_positions(const sdvg_rope_desc *rope, const sdvg_rows *x, const sd
  *   q         nullable, needs rope: rows that are rotated to q->out in the same launch.
  *   SDVG_E4M3: stored = round(x * (1 / scale)) in fp32, clamped to +-448 first (NaN stays NaN); x is not rounded to `dtype` after
  *             the rotation.
- * k->out and v->out are not looked at. The sources must not overlap the pools (SDVG_ERR_RANGE). n_tokens < 2^26; 0 is a no-op.
+ * k->out and v->out are not looked at. The sources must not overlap the pools (SDVG_ERR_RANGE). n_tokens < 2^26 - 3; 0 is a no-op.
  * Asynchronous on `stream`.
  */
 int sdvg_paged_commit(const sdvg_paged_kv *cache, const sdvg_rows *k, const sdvg_rows *v, const int64_t *slots,

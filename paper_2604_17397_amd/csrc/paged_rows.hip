@@ -21,7 +21,7 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 constexpr int kThreads = 256;
 constexpr int kUnits = 8;             // threads per row, each with two groups of 8 elements
 constexpr int kPass = kThreads / kUnits, kUnroll = 2;  // rows that a workgroup takes at a time, and how many times
-constexpr int64_t kMaxTokens = 1 << 26;  // a grid holds fewer than 2^32 threads, a workgroup has 1 or 4 tokens
+constexpr int64_t kMaxTokens = (1 << 26) - 3;  // a grid holds fewer than 2^32 threads, a workgroup has 1 or 4 tokens
 constexpr float kE4m3Max = 448.0f;
 
 struct RowsArg {

@@ -95,7 +95,7 @@ def test_rope_positions_rejects_bad_arguments(b):
     for kw, want in ROWS_BAD + OUT_BAD:
         assert call(x=rows(b, **kw)) == want, kw
         assert call(y=rows(b, **kw)) == want, kw
-    assert call(n=-1) == -2 and call(d=64) == -5 and call(dtype=3) == -5 and call(dtype=9) == -5 and call(n=1 << 26) == -5
+    assert call(n=-1) == -2 and call(d=64) == -5 and call(dtype=3) == -5 and call(dtype=9) == -5 and call(n=1 << 26) == -5 and call(n=(1 << 26) - 3) == -5
     assert call(n=0) == 0 and call(n=0, x=rows(b, in_=None, out=None)) == 0
     assert b.lib().sdvg_rope_positions(None, ref(rows(b)), None, 4, 128, 0, None) == -1
     assert b.lib().sdvg_rope_positions(ref(rope_desc(b)), None, None, 4, 128, 0, None) == -1
@@ -133,7 +133,7 @@ def test_paged_commit_rejects_bad_arguments(b):
     for kw, want in ROWS_BAD + OUT_BAD:
         assert call(rope=rope_desc(b), q=rows(b, **kw)) == want, kw
     assert call(q=rows(b)) == -1                                        # q without a rotation
-    assert call(slots=None) == -1 and call(slots=FAKE + 4) == -4 and call(n=-1) == -2 and call(n=1 << 26) == -5
+    assert call(slots=None) == -1 and call(slots=FAKE + 4) == -4 and call(n=-1) == -2 and call(n=1 << 26) == -5 and call(n=(1 << 26) - 3) == -5
     assert call(dtype=1) == -5 and call(dtype=2) == -5                  # fp32 rows; half rows into a bfloat16 cache
     assert call(k=rows(b, n_heads=3)) == -2
     assert call(v=rows(b, in_=(FAKE << 4) + 4096)) == -3                # v inside the pool of k
