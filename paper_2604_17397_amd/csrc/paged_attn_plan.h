@@ -55,11 +55,13 @@ SDVG_PAGED_HD int64_t work_of(const Request &q) { return static_cast<int64_t>(q.
 // 90; 24 requests x 8 heads x 2000 keys, which is more, 38 and 37).
 // Many row tiles: fitting would leave some items much longer than others, so they are made shorter, kFiner rounds of them, and the
 // chip fills up again as they end; but not shorter than kRoundChunk (what comes before and after the keys takes as long as some
-// 10 key tiles), unless the row tiles alone leave over a third of the units without work. us with that least and without: 64 requests x
-// 8 heads x 500 keys 25.0, 27.8, x 16 to 1000 keys 32.3, 31.1; 24 x 8, 30 rows, 936 keys 22.8, 28.1, 16 to 4000 keys 51, 53; but 40 x
-// 8 x 2000 keys 66, 54.
+// 10 key tiles) unless the chip is not filled once, and not shorter than kFilledChunk unless the row tiles alone leave over a third of
+// the units without work. us with kFilledChunk 24, without, and with 32: 64 requests x 8 heads x 500 keys 24.8, 28.4, 25.0; 32 x 8, 30
+// rows, 350 keys 13.9, 19.9, 13.9, lengths of 16 to 600 16.5, 24.0, 16.4; but 64 x 8 x 16 to 1400 keys 43.5, 37.2, 53.5 (54 batches of
+// one length 6 and 7 % faster than without, 54 of unlike lengths as fast, the worst cases 1.35, 1.6, 1.5 times the best of the three). With
+// fewer row tiles it loses: 40 x 8 x 2000 keys 66, 54.
 // Requests of kWhole key tiles on average are not split: 64 x 8 x 120 keys 6.9 us, split 12.2; 250 keys 12.9, 18.4.
-constexpr int kFiner = 3, kRoundChunk = 32, kWhole = 8;
+constexpr int kFiner = 3, kRoundChunk = 32, kFilledChunk = 24, kWhole = 8;
 SDVG_PAGED_HD int64_t ceil_div(int64_t a, int32_t b) {
   if (a <= INT32_MAX) return (static_cast<uint32_t>(a) + static_cast<uint32_t>(b) - 1) / static_cast<uint32_t>(b);  // (the shorter division)
   return (a + b - 1) / b;
@@ -72,7 +74,8 @@ SDVG_PAGED_HD int32_t chunk_of(int64_t total, int64_t row_tiles, int32_t target,
     c = ceil_div(total, slots - static_cast<int32_t>(row_tiles));
   } else {
     const int64_t once = ceil_div(total, target), finer = ceil_div(once, kFiner);
-    const int64_t least = once < kRoundChunk && 3 * row_tiles < target ? once : kRoundChunk;
+    const int64_t filled = once > kFilledChunk || 3 * row_tiles < target ? once : kFilledChunk;
+    const int64_t least = filled < kRoundChunk ? filled : kRoundChunk;
     c = finer > least ? finer : least;
   }
   if (total <= kWhole * row_tiles && c < kWhole) c = kWhole;
