@@ -346,3 +346,24 @@ def test_around_the_shortest_request_that_is_split(lengths, kv_heads):
     c = Case([(n, 1) for n in lengths], 2 * kv_heads, kv_heads, 16, seed=len(lengths))
     c.table = c.table[:, :-1].contiguous()
     c.check()
+
+
+@pytest.mark.parametrize("cache", [None, "e4m3"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_a_row_that_is_not_finite_stays_by_itself(cache, bad):
+    """A padded or broken token's q shares a tile with other rows; they do not see it."""
+    import paper_2604_17397_amd as P
+    c = Case([(700, 3), (65, 4), (3001, 8)], 10, 2, 16, cache=cache)
+    ws = torch.empty(P.paged_attn_workspace_bytes(c.q, c.handle(), c.table), dtype=torch.uint8, device="cuda")
+    args = c.handle(), c.table, c.q_start, c.kv_lens
+    good = P.paged_attn(c.q, *args, workspace=ws)
+    broken = c.q.clone()
+    broken[1], broken[8] = bad, bad
+    got = P.paged_attn(broken, *args, workspace=ws)
+    want, size, _ = c.want()
+    rest = [t for t in range(c.n_tokens) if t not in (1, 8)]
+    # the maximum that a row is shifted by may be raised at another step than without them: each result holds the bound
+    h = HALF_STEP["bf16"]
+    for x in (good, got):
+        excess = ((x.double() - want).abs() - ((h + 2.0**-12) * size + h * want.abs()))[rest]
+        assert not torch.isnan(excess).any() and excess.max().item() <= 0
