@@ -5,6 +5,7 @@ here and there is no fallback: a missing library raises. The most frequent calls
 the extension module _native.so (csrc/host/native.cpp), which makes the same checks in C++ and
 leaves every call it does not recognise as valid to the Python code here, which also works alone.
 """
+import contextlib
 import ctypes
 import importlib.util
 import math
@@ -209,6 +210,26 @@ def _ptr(t):
     return ctypes.c_void_p(t.data_ptr()) if t is not None else None
 
 
+def _memory_of(stream, device):
+    """Context in which new tensors come from the memory of `stream`, a torch stream or anything with a cuda_stream."""
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+    return torch.cuda.stream(stream)
+
+
+def _empty(shape, dtype, device, stream):
+    """A new tensor for a call on `stream` (None: the current one) to write. It comes from that stream's memory: a block that
+    the allocator has for the current stream may still be written by work that is queued there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with _memory_of(stream, device):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _empty_like(t, stream):
+    return _empty(t.shape, t.dtype, t.device, stream)
+
+
 def _check_dev(*tensors):
     for t in tensors:
         if t is not None and not t.is_cuda:
@@ -280,6 +301,8 @@ def block_attn(q, k_cache, v_cache, k_blk, v_blk, cache_len, out=None, scale=Non
     """sdvg_block_attn: q, k_blk, v_blk [tokens, heads, 128]; k_cache, v_cache one layer's
     [>= cache_len, heads, 128] (may be None when cache_len == 0). `scale=None` passes 0, which the
     library reads as 1/sqrt(head_dim). `out` defaults to a new tensor; pass out=q for in place. Returns out."""
+    if out is None and stream is not None:
+        out = _empty_like(q, stream)
     r = (_NATIVE or _native()).block_attn(q, k_cache, v_cache, k_blk, v_blk, cache_len, out, scale,
                                          None if stream is None else stream.cuda_stream, False)
     if r is not None:
@@ -288,7 +311,7 @@ def block_attn(q, k_cache, v_cache, k_blk, v_blk, cache_len, out=None, scale=Non
         return r
     cache_len = int(cache_len)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _empty_like(q, stream)
     d = _attn_desc(q, k_cache, v_cache, k_blk, v_blk, cache_len, out, scale)
     st = lib().sdvg_block_attn(ctypes.byref(d), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_blk),
                                _ptr(v_blk), cache_len, _ptr(out), _stream_ptr(stream))
@@ -300,6 +323,8 @@ def block_attn(q, k_cache, v_cache, k_blk, v_blk, cache_len, out=None, scale=Non
 def block_attn_commit(q, k_cache, v_cache, k_blk, v_blk, cache_len, out=None, scale=None, stream=None):
     """sdvg_block_attn_commit: block_attn for one layer that also copies k_blk / v_blk into tokens
     [cache_len, cache_len + n_blk) of k_cache / v_cache (which must be long enough). Returns out."""
+    if out is None and stream is not None:
+        out = _empty_like(q, stream)
     r = (_NATIVE or _native()).block_attn(q, k_cache, v_cache, k_blk, v_blk, cache_len, out, scale,
                                          None if stream is None else stream.cuda_stream, True)
     if r is not None:
@@ -308,7 +333,7 @@ def block_attn_commit(q, k_cache, v_cache, k_blk, v_blk, cache_len, out=None, sc
         return r
     cache_len = int(cache_len)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _empty_like(q, stream)
     if k_cache is None or v_cache is None:
         raise ValueError("the fused commit needs the layer's cache tensors")
     d = _attn_desc(q, k_cache, v_cache, k_blk, v_blk, cache_len, out, scale)
@@ -356,6 +381,8 @@ def block_attn_batch(qs, k_caches, v_caches, k_blks, v_blks, cache_len, outs=Non
     cache_len == 0); every item must have the same shapes and strides. `workspace`: optional
     device tensor (any dtype) the library may use to split keys over workgroups, under the policy
     `split` ("never", "auto", "always"). Returns outs."""
+    if outs is None and stream is not None:
+        outs = [_empty_like(q, stream) for q in qs]
     if type(split) is str and split in _SPLIT:
         r = (_NATIVE or _native()).batch(qs, k_caches, v_caches, k_blks, v_blks, cache_len, outs, workspace,
                                         _SPLIT[split], scale, None if stream is None else stream.cuda_stream, _static)
@@ -370,7 +397,7 @@ def block_attn_batch(qs, k_caches, v_caches, k_blks, v_blks, cache_len, outs=Non
     if not (len(k_caches) == len(v_caches) == len(k_blks) == len(v_blks) == n):
         raise ValueError("every list needs one tensor per item")
     if outs is None:
-        outs = [torch.empty(q.shape, dtype=q.dtype, device=q.device) for q in qs]
+        outs = [_empty_like(q, stream) for q in qs]
     descs = [_attn_desc(qs[i], k_caches[i], v_caches[i], k_blks[i], v_blks[i], cache_len, outs[i], scale)
              for i in range(n)]
     if any(_desc_key(d) != _desc_key(descs[0]) for d in descs[1:]):
@@ -430,6 +457,8 @@ def _check_tables(cos, sin, n_tokens, device):
 def rope(x, cos, sin, out=None, stream=None):
     """sdvg_rope: rotary embedding of bf16 rows x [tokens, heads, 128] by the angle tables cos, sin
     float32 [tokens, 64]. out defaults to a new tensor; pass out=x for in place."""
+    if out is None and stream is not None:
+        out = _empty_like(x, stream)
     r = (_NATIVE or _native()).rope(x, cos, sin, out, None if stream is None else stream.cuda_stream)
     if r is not None:
         if type(r) is int:
@@ -439,7 +468,7 @@ def rope(x, cos, sin, out=None, stream=None):
     if x.dtype != torch.bfloat16 or x.dim() != 3 or x.shape[2] != 128 or x.stride(2) != 1:
         raise ValueError("x must be bfloat16 [tokens, heads, 128] with unit dim stride")
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _empty_like(x, stream)
     elif out.shape != x.shape or out.dtype != x.dtype or out.stride(2) != 1 or out.device != x.device:
         raise ValueError("out must match x")
     _check_tables(cos, sin, x.shape[0], x.device)
@@ -538,8 +567,8 @@ def worst_frame_route_batch(frame_scores, tau, block_idx=None, first_block_idx=0
     n_blocks, n_frames = frame_scores.shape
     if block_idx is not None and (block_idx.dtype != torch.int32 or block_idx.numel() != n_blocks):
         raise ValueError("block_idx must be int32 [n_blocks]")
-    dec = torch.empty(n_blocks, dtype=torch.int32, device=frame_scores.device)
-    qb = torch.empty(n_blocks, dtype=torch.float32, device=frame_scores.device)
+    dec = _empty(n_blocks, torch.int32, frame_scores.device, stream)
+    qb = _empty(n_blocks, torch.float32, frame_scores.device, stream)
     st = fn(_ptr(frame_scores), n_blocks, n_frames, float(tau), _ptr(block_idx), int(first_block_idx),
             _ptr(dec), _ptr(qb), _stream_ptr(stream))
     if st != 0:
@@ -596,7 +625,7 @@ def page_plan(cached, new_tokens, block_table, page_tokens, free_pages=None, hel
         if stream is None:
             out = PagePlan(cached.shape[0], max_tokens, cached.device)
         else:
-            with torch.cuda.stream(stream):   # (its zeros must not come behind the plan)
+            with _memory_of(stream, cached.device):   # (its zeros must not come behind the plan)
                 out = PagePlan(cached.shape[0], max_tokens, cached.device)
     elif max_tokens is not None and max_tokens != out.slots.shape[0]:
         raise ValueError("out holds another number of tokens than max_tokens")
@@ -700,6 +729,9 @@ def rope_positions(x, positions, freqs, y=None, layout="half", gain=1.0, out=Non
     number of heads) in the same launch, at int32 positions [tokens] with float64 freqs [rotary_dim / 2] (rope_frequencies).
     layout "half" pairs elements p and p + rotary_dim / 2, "interleaved" 2p and 2p + 1. out / y_out default to new tensors;
     pass the input for in place. Returns out, or (out, y_out) with y."""
+    if stream is not None:
+        out = _empty_like(x, stream) if out is None else out
+        y_out = _empty_like(y, stream) if y is not None and y_out is None else y_out
     if type(layout) is str and layout in _LAYOUT:
         r = (_NATIVE or _native()).rope_positions(x, positions, freqs, y, _LAYOUT[layout], gain, out, y_out,
                                                  None if stream is None else stream.cuda_stream)
@@ -716,10 +748,10 @@ def rope_positions(x, positions, freqs, y=None, layout="half", gain=1.0, out=Non
         if y.dtype != x.dtype or y.shape[0] != x.shape[0]:
             raise ValueError("y must have x's tokens and dtype")
     rope = _rope_desc(positions, freqs, layout, gain, x.shape[0])
-    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    out = _empty_like(x, stream) if out is None else out
     _check_rows("out", out, x)
     if y is not None:
-        y_out = torch.empty(y.shape, dtype=y.dtype, device=y.device) if y_out is None else y_out
+        y_out = _empty_like(y, stream) if y_out is None else y_out
         _check_rows("y_out", y_out, y)
     st = lib().sdvg_rope_positions(ctypes.byref(rope), ctypes.byref(_rows(x, out)),
                                    None if y is None else ctypes.byref(_rows(y, y_out)), x.shape[0], 128,
@@ -757,6 +789,8 @@ def paged_commit(cache, k, v, slots, positions=None, freqs=None, q=None, q_out=N
     """sdvg_paged_commit: rows k, v [tokens, kv_heads, 128] of bfloat16 or float16 into the int64 slots [tokens] of a PagedKV;
     a negative slot writes nothing. With positions and freqs (as for rope_positions) K is rotated on its way, and so is
     q [tokens, heads, 128] into q_out (default: a new tensor; pass q for in place). Returns q_out, or None without q."""
+    if stream is not None and q is not None and q_out is None:
+        q_out = _empty_like(q, stream)
     if type(layout) is str and layout in _LAYOUT:
         r = (_NATIVE or _native()).paged_commit(cache.c, cache.k, k, v, slots, positions, freqs, q, q_out, _LAYOUT[layout], gain,
                                                None if stream is None else stream.cuda_stream)
@@ -781,7 +815,7 @@ def paged_commit(cache, k, v, slots, positions=None, freqs=None, q=None, q_out=N
         _check_rows("q", q)
         if q.dtype != k.dtype or q.shape[0] != k.shape[0]:
             raise ValueError("q must have k's tokens and dtype")
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+        q_out = _empty_like(q, stream) if q_out is None else q_out
         _check_rows("q_out", q_out, q)
     st = lib().sdvg_paged_commit(ctypes.byref(cache.c), ctypes.byref(_rows(k, None)), ctypes.byref(_rows(v, None)),
                                  _ptr(slots), k.shape[0], _ROW_TYPES[k.dtype], None if rope is None else ctypes.byref(rope),
@@ -820,6 +854,8 @@ def paged_attn(q, cache, block_table, q_start, kv_lens, out=None, lse=None, scal
     them. `window` > 0: every token sees the last `window` keys only. `lse`: optional float32 [tokens, heads] for the log of the sums.
     `workspace`: optional device tensor of paged_attn_workspace_bytes, with which the keys of long requests are split
     over the chip. `scale=None` is 1/sqrt(128). out defaults to a new tensor; pass out=q for in place. Returns out."""
+    if out is None and stream is not None:
+        out = _empty_like(q, stream)
     r = (_NATIVE or _native()).paged_attn(q, cache.c, cache.k, block_table, q_start, kv_lens, out, lse, scale, window, workspace,
                                          None if stream is None else stream.cuda_stream)
     if r is not None:
@@ -828,7 +864,7 @@ def paged_attn(q, cache, block_table, q_start, kv_lens, out=None, lse=None, scal
         return r
     _check_here(q, cache.k, block_table, q_start, kv_lens, out, lse, workspace)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _empty_like(q, stream)
     d = _paged_attn_desc(q, cache, block_table, out, scale, window)
     _int_array("q_start", q_start, d.n_requests + 1)
     _int_array("kv_lens", kv_lens, d.n_requests)
@@ -849,8 +885,9 @@ def probe_mfma(iters=20000, stream=None, changing=False):
     measurement kernel. Returns (flops, cycles) with cycles a device uint64 tensor (as int64)
     holding wave 0's shader clocks once it has run."""
     dev = torch.device("cuda", torch.cuda.current_device())
-    out = torch.empty(256 * 256, dtype=torch.float32, device=dev)
-    cycles = torch.zeros(1, dtype=torch.int64, device=dev)
+    out = _empty(256 * 256, torch.float32, dev, stream)
+    with contextlib.nullcontext() if stream is None else _memory_of(stream, dev):
+        cycles = torch.zeros(1, dtype=torch.int64, device=dev)
     flops = ctypes.c_double(0.0)
     name = "sdvg_probe_mfma_changing" if changing else "sdvg_probe_mfma"
     st = getattr(lib(), name)(_ptr(out), out.numel(), _ptr(cycles), int(iters), ctypes.byref(flops),

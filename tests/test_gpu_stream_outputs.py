@@ -1,0 +1,57 @@
+"""Calls with stream= and no output while the current stream still has work queued on a block that it has given back: the
+result is not that block, and is that of a call on the current stream."""
+import pytest
+import torch
+
+from paged_util import i32
+
+pytestmark = pytest.mark.gpu
+
+
+def rows(n, heads, seed=0):
+    torch.manual_seed(seed)
+    return torch.randn((n, heads, 128), device="cuda").bfloat16()
+
+
+def calls():
+    import paper_2604_17397_amd as P
+    q, kc, vc, kb, vb = rows(70, 4), rows(200, 4, 1), rows(200, 4, 2), rows(70, 4, 3), rows(70, 4, 4)
+    cos, sin = torch.rand((70, 64), device="cuda"), torch.rand((70, 64), device="cuda")
+    freqs, _ = P.rope_frequencies(128)
+    pos, slots = i32(range(70)), torch.arange(70, device="cuda")
+    pools = [torch.randn((9, 16, 4, 128), device="cuda").bfloat16() for _ in range(2)]
+    cache = P.PagedKV(*pools)
+    table, start, lens = i32([[3, 4, 2, 1, 0, 8]]), i32([0, 70]), i32([90])
+    scores = torch.randn((5000, 12), device="cuda")
+    return {
+        "block_attn": lambda **kw: P.block_attn(q, kc, vc, kb, vb, 100, **kw),
+        "block_attn_commit": lambda **kw: P.block_attn_commit(q, kc, vc, kb, vb, 100, **kw),
+        "block_attn_batch": lambda **kw: P.block_attn_batch([q, q], [kc, kc], [vc, vc], [kb, kb], [vb, vb], 100, **kw),
+        "rope": lambda **kw: P.rope(q, cos, sin, **kw),
+        "worst_frame_route_batch": lambda **kw: P.worst_frame_route_batch(scores, 0.1, **kw),
+        "rope_positions": lambda **kw: P.rope_positions(q, pos, freqs, y=kb, **kw),
+        "paged_commit": lambda **kw: P.paged_commit(cache, kb, vb, slots, positions=pos, freqs=freqs, q=q, **kw),
+        "paged_attn": lambda **kw: P.paged_attn(q, cache, table, start, lens, **kw),
+    }
+
+
+@pytest.mark.parametrize("name", ["block_attn", "block_attn_commit", "block_attn_batch", "rope", "worst_frame_route_batch",
+                                  "rope_positions", "paged_commit", "paged_attn"])
+def test_given_back_block_of_a_busy_stream(name):
+    call = calls()[name]
+
+    def listed(r):
+        return [r] if torch.is_tensor(r) else list(r)
+    want = [t.clone() for t in listed(call())]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)       # some ms of the current stream's time, and behind it writes to blocks as large as the outputs
+    junk = [torch.empty(t.shape, dtype=t.dtype, device="cuda") for t in want]
+    for t in junk:
+        t.fill_(77)
+    given_back = {t.data_ptr() for t in junk}
+    del junk, t
+    got = listed(call(stream=side))
+    assert not given_back & {t.data_ptr() for t in got}
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, w) for g, w in zip(got, want))
