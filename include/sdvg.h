@@ -417,7 +417,8 @@ int sdvg_paged_commit(const sdvg_paged_kv *cache, const sdvg_rows *k, const sdvg
  *             need may grow or shrink with n_requests and n_tokens: one that serves several shapes has the largest of their
  *             sizes. Scratch: overlapping calls need their own.
  *   Arithmetic: products on the matrix cores with fp32 accumulation, fp32 softmax statistics and sums; probabilities are
- *   rounded to `dtype` before the product with V (their sum is not, so that lse has 32 bits), e4m3 numbers are exact in it. What
+ *   rounded to `dtype` before the product with V (their sum is not, so that lse has 32 bits; fp16 ones below 2^-27 of the
+ *   largest, which it has no 11 bits for, to steps of 2^-37 of that), e4m3 numbers are exact in it. What
  *   lies in the cache outside of the keys that a row of the request sees (behind the last one, ahead of the first one's
  *   window) may be anything, and pages that hold nothing else need not be there; keys that any row of a request sees must be finite.
  *   Made for few new tokens per request (1 .. some 16); longer ones are right, but read the keys once per 32 rows
