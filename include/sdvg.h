@@ -410,7 +410,8 @@ int sdvg_paged_commit(const sdvg_paged_kv *cache, const sdvg_rows *k, const sdvg
  *   block_table  device int32 [n_requests][table_width]; q_start device int32 [n_requests + 1], not decreasing;
  *             kv_lens device int32 [n_requests], kv_lens[r] >= n: all as sdvg_page_plan leaves them.
  *             Keys on a page whose number is negative or not below n_pages, or past the table, count as not there. A row without any key gets
- *             out = 0 and lse = -infinity. Numbers out of range in q_start and kv_lens are clamped.
+ *             out = 0 and lse = -infinity. A row whose scores are NaN gets NaN in both, and no other row sees it. Numbers
+ *             out of range in q_start and kv_lens are clamped.
  *   workspace device, nullable, 16-byte aligned: with at least sdvg_paged_attn_workspace_bytes(desc, cache) bytes the keys of long
  *             requests are split over workgroups and the pieces joined by a second small launch; without, every
  *             request's keys are one workgroup's per key head and tile of rows. A workspace that is too small is ignored. The

@@ -494,12 +494,13 @@ __global__ __launch_bounds__(kThreads, kPerUnit) void paged_attn_kernel(FIRST_AR
     }
     const uint32_t all = f.tile * kRowTile + row, i = p.to.by_group.div(all), h = all - i * group;
     const int64_t token = f.q.row0 + static_cast<int64_t>(i), q_head = static_cast<int64_t>(of_head) * group + h;
-    const float norm = top == -INFINITY ? 0.f : T::kUnit * (kF8 && p.to.v_scale ? p.to.v_scale[of_head] : 1.0f) / total;   // (sum 0 only without a key)
+    // (the sum is 0 only without a key. A row whose scores are NaN has no maximum either, but a sum of NaN, which out and lse get)
+    const float norm = total == 0.f ? 0.f : T::kUnit * (kF8 && p.to.v_scale ? p.to.v_scale[of_head] : 1.0f) / total;
     uint16_t *dst = static_cast<uint16_t *>(p.to.out) + token * p.to.o_ts + q_head * p.to.o_hs + d0;
 #pragma unroll
     for (int j = 0; j < kDims / 4; ++j)
       reinterpret_cast<u32x2 *>(dst)[j] = u32x2{T::pack(acc[j][0] * norm, acc[j][1] * norm), T::pack(acc[j][2] * norm, acc[j][3] * norm)};
-    if (p.to.lse && d0 == 0) p.to.lse[token * p.to.n_heads + q_head] = top == -INFINITY ? -INFINITY : (top + log2f(total)) * kLn2;
+    if (p.to.lse && d0 == 0) p.to.lse[token * p.to.n_heads + q_head] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
   }
 }
 
@@ -556,10 +557,10 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(FIRST_ARGS, Ou
     }
     const uint32_t all = f.tile * kRowTile + row, i = p.by_group.div(all), h = all - i * group;
     const int64_t token = f.q.row0 + static_cast<int64_t>(i), q_head = static_cast<int64_t>(head) * group + h;
-    acc *= top == -INFINITY ? 0.f : T::kUnit * (kF8 && p.v_scale ? p.v_scale[head] : 1.0f) / total;
+    acc *= total == 0.f ? 0.f : T::kUnit * (kF8 && p.v_scale ? p.v_scale[head] : 1.0f) / total;
     const u32x2 w = {T::pack(acc[0], acc[1]), T::pack(acc[2], acc[3])};
     *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(p.out) + token * p.o_ts + q_head * p.o_hs + 4 * d4) = w;
-    if (p.lse && d4 == 0) p.lse[token * p.n_heads + q_head] = top == -INFINITY ? -INFINITY : (top + log2f(total)) * kLn2;
+    if (p.lse && d4 == 0) p.lse[token * p.n_heads + q_head] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
   }
 }
 
