@@ -392,7 +392,7 @@ int sdvg_rope_positions(const sdvg_rope_desc *rope, const sdvg_rows *x, const sd
  *   q         nullable, needs rope: rows that are rotated to q->out in the same launch.
  *   SDVG_E4M3: stored = round(x * (1 / scale)) in fp32, clamped to +-448 first (NaN stays NaN); x is not rounded to `dtype` after
  *             the rotation.
- * k->out and v->out are not looked at. The sources must not overlap the pools (SDVG_ERR_RANGE). n_tokens < 2^26 - 3; 0 is a no-op.
+ * k->out and v->out are not looked at. The sources and q->out must not overlap the pools (SDVG_ERR_RANGE). n_tokens < 2^26 - 3; 0 is a no-op.
  * Asynchronous on `stream`.
  */
 int sdvg_paged_commit(const sdvg_paged_kv *cache, const sdvg_rows *k, const sdvg_rows *v, const int64_t *slots,

@@ -387,10 +387,13 @@ extern "C" int sdvg_paged_commit(const sdvg_paged_kv *cache, const sdvg_rows *k,
   if (st != SDVG_OK || n_tokens == 0) return st;
   p.n_tokens = static_cast<uint32_t>(n_tokens);
   const int64_t pool = sdvg::paged_pool_bytes(*cache);
-  for (const sdvg_rows *r : {k, v}) {
-    const int64_t span = sdvg::rows_span(n_tokens, r->in_token_stride, r->n_heads, r->in_head_stride) * 2;
-    if (!sdvg::disjoint(r->in, span, cache->k, pool) || !sdvg::disjoint(r->in, span, cache->v, pool)) return SDVG_ERR_RANGE;
-  }
+  const auto apart = [&](const void *rows, int32_t heads, int64_t token_stride, int64_t head_stride) {
+    const int64_t span = sdvg::rows_span(n_tokens, token_stride, heads, head_stride) * 2;
+    return sdvg::disjoint(rows, span, cache->k, pool) && sdvg::disjoint(rows, span, cache->v, pool);
+  };
+  for (const sdvg_rows *r : {k, v, q})
+    if (r && !apart(r->in, r->n_heads, r->in_token_stride, r->in_head_stride)) return SDVG_ERR_RANGE;
+  if (q && !apart(q->out, q->n_heads, q->out_token_stride, q->out_head_stride)) return SDVG_ERR_RANGE;
   if (rope) set_rope(p, *rope);
   p.t[1].out = cache->k;
   p.t[2].out = cache->v;
