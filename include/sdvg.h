@@ -368,7 +368,7 @@ typedef struct {
 } sdvg_rope_desc;
 
 /* Rows [n_tokens][n_heads][128] that are read at in and written at out (which may be in itself, with the same strides;
- * otherwise they must not overlap). 16-byte aligned; strides in elements, multiples of 16 bytes below 2^30, those of dimensions of size 1
+ * otherwise they must not overlap, nor other rows of the call; an equal start is refused, SDVG_ERR_RANGE). 16-byte aligned; strides in elements, multiples of 16 bytes below 2^30, those of dimensions of size 1
  * are not looked at. */
 typedef struct {
   const void *in; /* device */

@@ -251,6 +251,9 @@ int check_rope(const sdvg_rope_desc *r, int64_t n_tokens) {
   return SDVG_OK;
 }
 
+// Whether rows that one tensor of a launch is written to are, by their start (see below), what another is read from or written to.
+bool meet(const sdvg_rows &written, const void *in, const void *out) { return written.out == in || written.out == out; }
+
 // Checks a set of rows (`out`: whether they are written at r->out) and fills its argument.
 int check_rows(const sdvg_rows *r, int64_t n_tokens, int size, bool out, RowsArg &a) {
   if (r->n_heads < 1) return SDVG_ERR_SHAPE;
@@ -358,6 +361,7 @@ extern "C" int sdvg_rope_positions(const sdvg_rope_desc *rope, const sdvg_rows *
   if (st == SDVG_OK) st = check_rows(x, n_tokens, size, true, p.t[0]);
   if (st == SDVG_OK && y) st = check_rows(y, n_tokens, size, true, p.t[1]);
   if (st != SDVG_OK || n_tokens == 0) return st;
+  if (y && (meet(*x, y->in, y->out) || meet(*y, x->in, nullptr))) return SDVG_ERR_RANGE;
   p.n_tokens = static_cast<uint32_t>(n_tokens);
   set_rope(p, *rope);
   const bool half = rope->layout == SDVG_ROPE_HALF;
@@ -393,7 +397,7 @@ extern "C" int sdvg_paged_commit(const sdvg_paged_kv *cache, const sdvg_rows *k,
   };
   for (const sdvg_rows *r : {k, v, q})
     if (r && !apart(r->in, r->n_heads, r->in_token_stride, r->in_head_stride)) return SDVG_ERR_RANGE;
-  if (q && !apart(q->out, q->n_heads, q->out_token_stride, q->out_head_stride)) return SDVG_ERR_RANGE;
+  if (q && (!apart(q->out, q->n_heads, q->out_token_stride, q->out_head_stride) || meet(*q, k->in, v->in))) return SDVG_ERR_RANGE;
   if (rope) set_rope(p, *rope);
   p.t[1].out = cache->k;
   p.t[2].out = cache->v;
