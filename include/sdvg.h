@@ -415,8 +415,8 @@ int sdvg_paged_commit(const sdvg_paged_kv *cache, const sdvg_rows *k, const sdvg
  *   workspace device, nullable, 16-byte aligned: with at least sdvg_paged_attn_workspace_bytes(desc, cache) bytes the keys of long
  *             requests are split over workgroups and the pieces joined by a second small launch; without, every
  *             request's keys are one workgroup's per key head and tile of rows. A workspace that is too small is ignored. The
- *             need may grow or shrink with n_requests and n_tokens: one that serves several shapes has the largest of their
- *             sizes. Scratch: overlapping calls need their own.
+ *             need may grow or shrink with n_requests, n_tokens and table_width: one that serves several shapes has the largest of
+ *             their sizes. It is 0 where a row of the table names too few keys to be split (256). Scratch: overlapping calls need their own.
  *   Arithmetic: products on the matrix cores with fp32 accumulation, fp32 softmax statistics and sums; probabilities are
  *   rounded to `dtype` before the product with V (their sum is not, so that lse has 32 bits; fp16 ones below 2^-27 of the
  *   largest, which it has no 11 bits for, to steps of 2^-37 of that), e4m3 numbers are exact in it. What

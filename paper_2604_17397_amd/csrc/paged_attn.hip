@@ -592,9 +592,16 @@ int head_sets(const sdvg_paged_kv &c, int row_tile) {
   return fits && c.n_kv_heads % 2 == 0 && c.head_stride < c.token_stride ? 2 : 1;
 }
 
-// Items per (set of) key heads that fill the chip, kPerUnit workgroups per unit.
-int target_of(int n_cu, const sdvg_paged_kv &c, int row_tile) {
-  const int t = kPerUnit * n_cu * head_sets(c, row_tile) / c.n_kv_heads;
+// Keys that a row of the block table can name.
+int32_t capacity_of(const sdvg_paged_attn_desc &d, const sdvg_paged_kv &c) {
+  const int64_t most = INT32_MAX - 2 * pg::kKeyTile, keys = int64_t{d.table_width} * c.page_tokens;
+  return static_cast<int32_t>(keys < most ? keys : most);   // (more than any pool holds)
+}
+
+// Items per (set of) key heads that fill the chip, kPerUnit workgroups per unit; 0 where no request can be split.
+int target_of(int n_cu, const sdvg_paged_attn_desc &d, const sdvg_paged_kv &c, int row_tile) {
+  const int sets = head_sets(c, row_tile), t = kPerUnit * n_cu * sets / c.n_kv_heads;
+  if (pg::max_pieces(capacity_of(d, c), kWaves / sets) <= 1) return 0;
   return t > 1 ? t : 1;
 }
 
@@ -629,7 +636,7 @@ int launch_attn(First f, const AttnParams &p, hipStream_t s) {
   if (items * f.by_heads.d >= (1 << 23)) return SDVG_ERR_UNSUPPORTED;  // (a grid holds fewer than 2^32 threads)
   hipLaunchKernelGGL((paged_attn_kernel<T, kF8, NT, HS>), dim3(static_cast<uint32_t>(items * f.by_heads.d)), dim3(kThreads), 0, s, FIRST(f), p);
   SDVG_HIP_CHECK(hipGetLastError());
-  if (f.target > 0 && pg::max_pieces(f.capacity, kKeyWaves) > 1) {
+  if (f.target > 0) {
     // Workgroups per row tile: one for every row of an average request's where that are few (then the pieces are many, and
     // shared), otherwise one for every 8 rows. A workgroup takes more rows where there are more.
     f.by_heads = sdvg::FastDiv::of(f.by_heads.d * HS);
@@ -661,7 +668,7 @@ extern "C" int64_t sdvg_paged_attn_workspace_bytes(const sdvg_paged_attn_desc *d
   if (desc->n_requests == 0 || desc->n_tokens == 0) return 0;
   if ((st = compute_units(n_cu)) != SDVG_OK) return st;
   const int tile = row_tile_of(desc->n_requests, desc->n_tokens, desc->n_heads / cache->n_kv_heads);
-  return workspace_of(target_of(n_cu, *cache, tile), cache->n_kv_heads, tile);
+  return workspace_of(target_of(n_cu, *desc, *cache, tile), cache->n_kv_heads, tile);
 }
 
 extern "C" int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_paged_kv *cache, const void *q,
@@ -685,10 +692,8 @@ extern "C" int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_page
     return SDVG_ERR_RANGE;
   int n_cu = 0;
   if ((st = compute_units(n_cu)) != SDVG_OK) return st;
-  int64_t capacity = int64_t{desc->table_width} * cache->page_tokens;
-  if (capacity > INT32_MAX - 2 * pg::kKeyTile) capacity = INT32_MAX - 2 * pg::kKeyTile;  // (more than any pool holds)
   const int32_t n_kv = cache->n_kv_heads, group = desc->n_heads / n_kv;
-  First f{q_start, kv_lens, desc->n_requests, desc->n_tokens, group, desc->window, 0, static_cast<int32_t>(capacity), {}};
+  First f{q_start, kv_lens, desc->n_requests, desc->n_tokens, group, desc->window, 0, capacity_of(*desc, *cache), {}};
   AttnParams p{};
   p.q = q;
   p.k = cache->k;
@@ -707,9 +712,9 @@ extern "C" int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_page
   p.by_page = sdvg::FastDiv::of(cache->page_tokens / 8);
   p.to = OutParams{out, lse, nullptr, nullptr, cache->v_scale, static_cast<uint32_t>(desc->o_token_stride),
                    static_cast<uint32_t>(desc->o_head_stride), desc->n_heads, sdvg::FastDiv::of(group)};
-  const int tile = row_tile_of(f.n_requests, f.n_tokens, group), target = target_of(n_cu, *cache, tile), sets = head_sets(*cache, tile);
+  const int tile = row_tile_of(f.n_requests, f.n_tokens, group), target = target_of(n_cu, *desc, *cache, tile), sets = head_sets(*cache, tile);
   f.by_heads = sdvg::FastDiv::of(n_kv / sets);
-  if (workspace && workspace_bytes >= workspace_of(target, n_kv, tile)) {
+  if (target > 0 && workspace && workspace_bytes >= workspace_of(target, n_kv, tile)) {
     f.target = target;
     p.to.part_o = static_cast<float *>(workspace);
     p.to.part_ml = p.to.part_o + pg::max_slots(target) * n_kv * tile * 128;
