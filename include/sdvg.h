@@ -353,8 +353,8 @@ int sdvg_page_plan(const sdvg_page_plan_args *args, void *stream);
  * Rotary embedding by positions. For pair p < rotary_dim / 2 of every row's vector, at angle = position * freqs[p],
  *     (a, b) -> (a c - b s, a s + b c),   c = gain * cos(angle), s = gain * sin(angle),
  * where (a, b) are elements (p, p + rotary_dim / 2) in SDVG_ROPE_HALF and (2p, 2p + 1) in SDVG_ROPE_INTERLEAVED; elements from
- * rotary_dim on are copied. The angle is a product in 64 bits taken modulo one turn before anything is rounded to
- * 32, so positions up to 2^31 keep full accuracy; the rest is fp32, the result rounded once. Scaling for contexts
+ * rotary_dim on are copied. The angle is taken modulo one turn in 64 bits and what their roundings leave, before
+ * anything is rounded to 32, so all positions keep full accuracy; the rest is fp32, the result rounded once. Scaling for contexts
  * longer than the original one is in freqs and gain (the Python package's rope_frequencies makes them).
  *   positions device int32 [n_tokens], 4-byte aligned, of either sign; freqs device double [rotary_dim / 2], 8-byte aligned,
  *   in radians per position. rotary_dim: a multiple of 16, at most 128.

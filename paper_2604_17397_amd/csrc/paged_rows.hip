@@ -2,7 +2,7 @@
 // the way. One kernel does both: for every token the rows of up to three tensors (q rotated, k rotated and / or
 // stored, v stored).
 //
-// Angles: turns = position * freq / (2 pi) in 64 bits, of which only the distance r to the nearest quarter turn
+// Angles: turns = position * freq / (2 pi) in 64 bits and a rest, of which only the distance r to the nearest quarter turn
 // (|r| <= 1/8) is rounded to 32; sine and cosine of r are exchanged and negated by the quarter. A position of 2^20 times a
 // frequency near 1 has 17 bits before the point: in 32 bits 7 would be left behind it.
 // A token's 64 sines and cosines are computed once by 64 threads and kept in LDS for all of its rows; with a thread per 16-byte
@@ -124,12 +124,15 @@ struct E4m3 {
   }
 };
 
-// gain * cos and gain * sin of position * freq.
+// gain * cos and gain * sin of position * freq. 1 / (2 pi) has a second number behind its 53 bits, and both products keep what their
+// rounding leaves (fma): with products rounded to 64 bits alone an angle near 2^31 was 7e-7 off, 12 steps of fp32, now 1e-15 whatever
+// the position. (No difference in the times below.)
 __device__ __forceinline__ void turn(int position, double freq, float gain, float &c, float &s) {
-  constexpr double kTurnsPerRadian = 0.15915494309189533577;
-  const double quarters = 4.0 * (position * (freq * kTurnsPerRadian));
-  const double q = rint(quarters);
-  const float r = static_cast<float>(0.5 * (quarters - q));  // of half a turn, |r| <= 1/4
+  constexpr double kTurnsPerRadian = 0.15915494309189535, kTurnsRest = -9.839338337591243e-18;
+  const double p = position, per = freq * kTurnsPerRadian, per_rest = fma(freq, kTurnsPerRadian, -per) + freq * kTurnsRest;
+  const double turns = p * per, rest = fma(p, per, -turns) + p * per_rest;
+  const double q = rint(4.0 * turns);
+  const float r = static_cast<float>(0.5 * (4.0 * turns - q) + 2.0 * rest);  // of half a turn, |r| <= 1/4
   float sr, cr;
   sincospif(r, &sr, &cr);
   const int n = static_cast<int>(q - 4.0 * floor(0.25 * q));  // quarter 0 .. 3
