@@ -586,7 +586,8 @@ int row_tile_of(int64_t n_requests, int64_t n_tokens, int group) {
 
 // Sets of heads per workgroup (HS): where the rows of neighbouring heads are neighbours. us, 1 and 2: one request of 131071 keys x 8
 // heads, 16 bit 95.5 and 90.2, ragged 207 and 197, 32 rows e4m3 40.3 and 38.5; a cache with heads ahead of tokens 50.7 and 53.1 (e4m3).
-// 32 rows in 16 bits would spill registers.
+// 32 rows in 16 bits are not built: 24 requests of up to 8 new tokens 60.2 against 61.8, but 255 of the 256 registers, and a change of the
+// loop that made it spill gave wrong results. (A test holds all instances to no spilled register.)
 int head_sets(const sdvg_paged_kv &c, int row_tile) {
   const bool fits = row_tile == 16 || c.dtype == SDVG_E4M3;
   return fits && c.n_kv_heads % 2 == 0 && c.head_stride < c.token_stride ? 2 : 1;
