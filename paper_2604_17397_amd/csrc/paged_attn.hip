@@ -192,16 +192,16 @@ __device__ __forceinline__ bool find(const First &p, int x, Found &f) {
   if (kItems && p.target > 0)
     for (int b = 0; b < p.n_requests; b += 64) {
       const pg::Request q = b ? load_request<kRowTile>(p, b + lane) : mine0;
-      n_full += wave_total(q.row_tiles * pg::full_pieces(q, chunk));
+      n_full += wave_total(pg::numbers_of(q, pg::full_pieces(q, chunk), 0, pg::kFull));
     }
-  const bool among_full = kItems && x < n_full;
-  if (kItems && !among_full) x -= n_full;
+  const pg::Range range = !kItems ? pg::kSplit : x < n_full ? pg::kFull : pg::kRest;
+  if (range == pg::kRest) x -= n_full;
   int before = 0, slots_before = 0;
   for (int b = 0; b < p.n_requests; b += 64) {
     const pg::Request q = b ? load_request<kRowTile>(p, b + lane) : mine0;
     const int32_t full = pg::full_pieces(q, chunk), pieces = pg::pieces_of(q, chunk, full);
-    const int32_t slots = pieces > 1 ? q.row_tiles * pieces : 0;
-    const int32_t mine = q.row_tiles * (!kItems ? pieces > 1 : among_full ? full : pieces - full);
+    const int32_t slots = pg::slots_of(q, pieces);
+    const int32_t mine = pg::numbers_of(q, full, pieces, range);
     const int upto = scan(mine), slots_upto = scan(slots);  // inclusive
     const int at = x - before - (upto - mine);
     const uint64_t hit = __ballot(at >= 0 && at < mine);
@@ -211,25 +211,11 @@ __device__ __forceinline__ bool find(const First &p, int x, Found &f) {
       f.q = pg::Request{get(q.row0), get(q.n), get(q.len), get(q.first_tile), get(q.tiles), get(q.row_tiles)};
       f.request = b + src;
       f.pieces = get(pieces);
-      const int i = get(at), n = get(full), slot0 = slots_before + get(slots_upto - slots);
+      const pg::Place at_x = pg::place_of(f.q, get(at), get(full), range, p.by_heads.d);
+      f.tile = at_x.tile;
+      f.piece = at_x.piece;
       f.chunk = chunk;
-      // The row tiles of a piece follow each other where workgroups that read the same keys then are on the same XCD (they are
-      // dealt out to 8 in turn): 64 rows x 131071 keys x 8 heads, 16 bit, 166 us with the pieces of a row tile in a row, 136 so;
-      // with 4 sets of heads (e4m3) 92 and 97.
-      if (!among_full) {
-        f.tile = i;
-        f.piece = kItems ? n : 0;
-      } else if (f.q.row_tiles == 1) {
-        f.tile = 0;
-        f.piece = i;
-      } else if (p.by_heads.d % 8 == 0) {
-        f.piece = static_cast<uint32_t>(i) / static_cast<uint32_t>(f.q.row_tiles);
-        f.tile = i - f.piece * f.q.row_tiles;
-      } else {
-        f.tile = static_cast<uint32_t>(i) / static_cast<uint32_t>(n);
-        f.piece = i - f.tile * n;
-      }
-      f.slot = slot0 + f.tile * f.pieces;
+      f.slot = pg::first_slot(slots_before + get(slots_upto - slots), f.tile, f.pieces);
       // (always so, unless q_start decreases so far that sums leave 32 bits: the workspace is not left even then)
       return f.pieces == 1 || (f.slot >= 0 && f.slot <= pg::max_slots(p.target) - f.pieces);
     }
@@ -298,9 +284,8 @@ __global__ __launch_bounds__(kThreads, kPerUnit) void paged_attn_kernel(FIRST_AR
     for (int d = 0; d < 8; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  const int before = f.piece ? f.piece * f.chunk : 0;
-  const int begin = f.q.first_tile + before;
-  const int end = f.q.first_tile + (f.q.tiles - before < f.chunk ? f.q.tiles : before + f.chunk);
+  const pg::KeyTiles keys = pg::key_tiles_of(f.q, f.piece, f.chunk);
+  const int begin = keys.begin, end = keys.end;
   const int32_t *table = p.table + static_cast<int64_t>(f.request) * p.table_stride;
   const char *k_head = static_cast<const char *>(p.k) + head * p.head_stride * kBytes,
              *v_head = static_cast<const char *>(p.v) + head * p.head_stride * kBytes;

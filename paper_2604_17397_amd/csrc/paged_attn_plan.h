@@ -90,6 +90,40 @@ SDVG_PAGED_HD int32_t pieces_of(const Request &q, int32_t chunk, int32_t full) {
   return full + (full == 0 || q.tiles > full * chunk ? 1 : 0);
 }
 
+// Items are numbered through all requests, first the full pieces of every request (kFull), then the others (kRest); the join numbers
+// the split row tiles (kSplit). How many of a number range a request of `pieces` pieces per row tile, `full` full ones among them, has:
+enum Range { kFull, kRest, kSplit };
+SDVG_PAGED_HD int32_t numbers_of(const Request &q, int32_t full, int32_t pieces, Range range) {
+  return q.row_tiles * (range == kFull ? full : range == kRest ? pieces - full : pieces > 1);
+}
+// Row tile and piece of number i of a request's own. The row tiles of a full piece follow each other where workgroups that read the same
+// keys then are on the same XCD (they are dealt out to 8 in turn), which is where the (sets of) key heads are a multiple of 8: 64 rows x 131071 keys x
+// 8 heads, 16 bit, 166 us with the pieces of a row tile in a row, 136 so; with 4 sets of heads (e4m3) 92 and 97.
+struct Place {
+  int32_t tile, piece;
+};
+SDVG_PAGED_HD Place place_of(const Request &q, int32_t i, int32_t full, Range range, uint32_t head_sets) {
+  if (range != kFull) return Place{i, range == kRest ? full : 0};
+  if (q.row_tiles == 1) return Place{0, i};
+  if (head_sets % 8 == 0) {
+    const int32_t piece = static_cast<uint32_t>(i) / static_cast<uint32_t>(q.row_tiles);
+    return Place{i - piece * q.row_tiles, piece};
+  }
+  const int32_t tile = static_cast<uint32_t>(i) / static_cast<uint32_t>(full);
+  return Place{tile, i - tile * full};
+}
+// Slot of a piece's partial result: slot0 is the number of slots of the requests before.
+SDVG_PAGED_HD int32_t slots_of(const Request &q, int32_t pieces) { return pieces > 1 ? q.row_tiles * pieces : 0; }
+SDVG_PAGED_HD int32_t first_slot(int32_t slot0, int32_t tile, int32_t pieces) { return slot0 + tile * pieces; }
+// Key tiles begin .. end - 1 of a piece.
+struct KeyTiles {
+  int32_t begin, end;
+};
+SDVG_PAGED_HD KeyTiles key_tiles_of(const Request &q, int32_t piece, int32_t chunk) {
+  const int32_t before = piece ? piece * chunk : 0;
+  return KeyTiles{q.first_tile + before, q.first_tile + (q.tiles - before < chunk ? q.tiles : before + chunk)};
+}
+
 // Bounds for the launch, from what the host knows, with most = kFiner * target >= total / chunk. Items: most full chunks, and one
 // more per row tile; no more than `target` where the row tiles are few; and none of a row tile below key_waves key tiles of what a row of
 // the block table can name (`capacity` keys; one item where these are kWhole tiles). Slots: a split row tile of t > chunk tiles has ceil(t / chunk) < 2 t / chunk pieces. Groups
