@@ -417,9 +417,9 @@ int sdvg_paged_commit(const sdvg_paged_kv *cache, const sdvg_rows *k, const sdvg
  *             request's keys are one workgroup's per key head and tile of rows. A workspace that is too small is ignored. The
  *             need may grow or shrink with n_requests, n_tokens and table_width: one that serves several shapes has the largest of
  *             their sizes. It is 0 where a row of the table names too few keys to be split (256). Scratch: overlapping calls need their own.
- *   Arithmetic: products on the matrix cores with fp32 accumulation, fp32 softmax statistics and sums; probabilities are
- *   rounded to `dtype` before the product with V (their sum is not, so that lse has 32 bits; fp16 ones below 2^-27 of the
- *   largest, which it has no 11 bits for, to steps of 2^-37 of that), e4m3 numbers are exact in it. What
+ *   Arithmetic: products on the matrix cores with fp32 accumulation, fp32 softmax statistics and sums; a probability goes into
+ *   the product with V as two numbers of `dtype` that together have 16 (bf16) or 22 bits (fp16 down to 2^-16 of the largest one
+ *   of the keys that a wave takes, below that in steps of 2^-37 of it), and whole into the sum; e4m3 numbers are exact in it. What
  *   lies in the cache outside of the keys that a row of the request sees (behind the last one, ahead of the first one's
  *   window) may be anything, and pages that hold nothing else need not be there; keys that any row of a request sees must be finite.
  *   Made for few new tokens per request (1 .. some 16); longer ones are right, but read the keys once per 32 rows

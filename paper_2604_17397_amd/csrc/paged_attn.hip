@@ -89,11 +89,15 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kPerUnit = 2;             // workgroups per compute unit
 
 // ---- the two 16-bit types
-// A probability is held as 2^kShift p, p <= 2^kSlack being relative to the running maximum, in the sum as in the product with V.
-// bf16 has the range of fp32 and needs no shift. fp16 has 11 bits from 2^-14 to 65504: with p between 2^13 and 2^15 at the
-// largest key those down to 2^-27 of it, 18.7 nats, are rounded to 11 bits, and a smaller one is off by 2^-38 of it at most (many small
-// ones beside one large one whose V is small, an attention sink, are what the result then consists of). The maximum is raised more often
-// by it, which costs nothing that shows: 96 requests 196.6 us with and without, one of 131071 keys 89.0, verification 61.7.
+// A probability is held as 2^kShift p, p <= 2^kSlack being relative to the running maximum, in the sum as in the product with V. For
+// the product it is the sum of two 16-bit numbers, the rounded one and what that rounding leaves, each with its own matrix product:
+// rounded once, it was the larger part of the result's error (bf16 2.0e-3 to 2.4e-3 rms, now the 1.65e-3 of the result's own rounding; fp16
+// 2.6e-4 and 2.1e-4). us without and with the rest: one request of 131071 keys 87.0, 87.2, 96 requests 196.8, 197.0, 64 x 936 keys 47.8,
+// 48.0, one of 936 keys 9.8, 9.8, verification 38.9, 38.8 (16 bits 61.9, 61.3).
+// bf16 then has 16 bits and the range of fp32. fp16 has steps of 2^-24 at the least: with 2^13 p, p <= 4, both numbers together have 22 bits
+// from 2^-16 of the largest probability down, and a smaller one is off by 2^-38 of the largest at most (many small ones beside one
+// large one whose V is small, an attention sink, are what the result then consists of). The maximum is raised more often by it,
+// which costs nothing that shows: 96 requests 196.6 us with and without.
 struct Bf16 {
   static constexpr float kSlack = 8.0f, kShift = 0.0f, kUnit = 1.0f;   // kUnit = 2^-kShift
   static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
@@ -103,6 +107,8 @@ struct Bf16 {
     const f32x2 f = {x, y};
     return __builtin_bit_cast(unsigned, __builtin_convertvector(f, bf16x2));
   }
+  static __device__ __forceinline__ float first(unsigned w) { return __uint_as_float(w << 16); }
+  static __device__ __forceinline__ float second(unsigned w) { return __uint_as_float(w & 0xffff0000u); }
   // elements 2i, 2i + 1 of a dword of four e4m3 numbers (exact in 16 bits)
   static __device__ __forceinline__ unsigned lo8(unsigned w) {
     return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false));
@@ -120,6 +126,8 @@ struct F16 {
     const f16x2 h = {static_cast<_Float16>(x), static_cast<_Float16>(y)};
     return __builtin_bit_cast(unsigned, h);
   }
+  static __device__ __forceinline__ float first(unsigned w) { return static_cast<float>(__builtin_bit_cast(f16x2, w)[0]); }
+  static __device__ __forceinline__ float second(unsigned w) { return static_cast<float>(__builtin_bit_cast(f16x2, w)[1]); }
   static __device__ __forceinline__ unsigned lo8(unsigned w) {
     return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false));
   }
@@ -337,7 +345,7 @@ __global__ __launch_bounds__(kThreads, kPerUnit) void paged_attn_kernel(FIRST_AR
     int upto = f.q.len - block0;
     upto = v_page < 0 ? 0 : upto < 0 ? 0 : upto > 8 ? 8 : upto;
     const bool gaps = __any(upto < 8 || below > 0), masked = gaps || key0 + pg::kKeyTile > all_sees || key0 < all_from;
-    u32x4 pf[NT];
+    u32x4 pf[NT], rest[NT];   // probabilities in 16 bits, and what is left of them
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
@@ -379,6 +387,7 @@ __global__ __launch_bounds__(kThreads, kPerUnit) void paged_attn_kernel(FIRST_AR
       for (int c = 0; c < 4; ++c) {
         const float a = exp2_of(x[2 * c] - base), b = exp2_of(x[2 * c + 1] - base);
         pf[t][c] = T::pack(a, b);
+        rest[t][c] = T::pack(a - T::first(pf[t][c]), b - T::second(pf[t][c]));
         l[t] += a + b;
       }
     }
@@ -391,6 +400,8 @@ __global__ __launch_bounds__(kThreads, kPerUnit) void paged_attn_kernel(FIRST_AR
     // V^T: dim 2e + h of keys 2c, 2c + 1 from dword e of both
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
+      // (where registers are short nothing moves ahead of its turn: with all of V^T on the way 13 would be spilled, so it takes 229)
+      if constexpr (NT == 2 && !kF8) __builtin_amdgcn_sched_barrier(0);
       unsigned w[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -415,7 +426,7 @@ __global__ __launch_bounds__(kThreads, kPerUnit) void paged_attn_kernel(FIRST_AR
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) o[t][2 * e + h] = T::mfma(vt[h], pf[t], o[t][2 * e + h]);
+        for (int t = 0; t < NT; ++t) o[t][2 * e + h] = T::mfma(vt[h], pf[t], T::mfma(vt[h], rest[t], o[t][2 * e + h]));
     }
   };
   int tile = begin + wave % kKeyWaves;
