@@ -587,9 +587,10 @@ def _check_here(*tensors):
 
 
 class PagePlan:
-    """What page_plan computes, in device tensors of its own that every plan of up to this size may reuse: q_start
-    int32 [requests + 1], kv_lens and held int32 [requests], positions int32 and slots int64 [max_tokens], next_free
-    int32 [1] (held and next_free are written only by plans that take pages)."""
+    """What page_plan computes, in device tensors of its own that every plan of as many requests may reuse (max_tokens is the most
+    new tokens that have rows): q_start int32 [requests + 1], kv_lens and held int32 [requests], positions int32 and slots
+    int64 [max_tokens], next_free int32 [1] (held and next_free are written only by plans that take pages). Cleared on the
+    current stream."""
 
     def __init__(self, n_requests, max_tokens, device="cuda"):
         n_requests, max_tokens = int(n_requests), int(max_tokens)

@@ -17,9 +17,9 @@
 //
 // us (kernel and join), TB/s of K and V: one request of 131071 keys, 40 query and 8 key heads, bf16 82 + 6, 6.6 (a read of
 // contiguous memory reaches 6.1 to 6.3, with nontemporal loads 6.9 to 7.1; without its arithmetic the kernel takes as long);
-// 96 requests of 16 to 16384 keys, f16 189 + 6, 5.7; 24 requests with up to 8 new tokens of 40 heads, window 4096, e4m3 33 + 5, 3.1 (a
-// third is what comes before and after a workgroup's keys, and the second row tile of a request reads them again); one
-// request of 936 keys, 12 heads 5.6 + 3 to 4, a chain of latencies: lengths 0.7, page numbers and q 0.6, K and V 1.3, one step 0.5, merge and
+// 96 requests of 16 to 16384 keys, f16 190 + 7, 5.9; 24 requests with up to 8 new tokens of 40 heads, window 4096, e4m3 33 + 5, 3.1 (452
+// workgroups in one round, which lasts as long as the longest, 24 key tiles; second row tiles of 3 to 8 rows read 22 % of the keys again); one
+// request of 936 keys, 12 heads 5.9 + 3 to 4, a chain of latencies: lengths 0.7, page numbers and q 0.6, K and V 1.3, one step 0.5, merge and
 // store 0.7, and the launch itself.
 #include <math.h>
 
@@ -582,8 +582,8 @@ int row_tile_of(int64_t n_requests, int64_t n_tokens, int group) {
 
 // Sets of heads per workgroup (HS): where the rows of neighbouring heads are neighbours. us, 1 and 2: one request of 131071 keys x 8
 // heads, 16 bit 95.5 and 90.2, ragged 207 and 197, 32 rows e4m3 40.3 and 38.5; a cache with heads ahead of tokens 50.7 and 53.1 (e4m3).
-// 32 rows in 16 bits are not built: 24 requests of up to 8 new tokens 60.2 against 61.8, but 255 of the 256 registers, and a change of the
-// loop that made it spill gave wrong results. (A test holds all instances to no spilled register.)
+// 32 rows in 16 bits are not built: 24 requests of up to 8 new tokens 60.2 against 61.8 (P rounded once), but with 255 of the 256 registers,
+// and a form of the loop with two steps on their way, which spilled, gave wrong results. (A test holds all instances to no spilled register.)
 int head_sets(const sdvg_paged_kv &c, int row_tile) {
   const bool fits = row_tile == 16 || c.dtype == SDVG_E4M3;
   return fits && c.n_kv_heads % 2 == 0 && c.head_stride < c.token_stride ? 2 : 1;

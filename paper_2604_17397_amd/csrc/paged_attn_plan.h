@@ -55,11 +55,11 @@ SDVG_PAGED_HD int64_t work_of(const Request &q) { return static_cast<int64_t>(q.
 // 90; 24 requests x 8 heads x 2000 keys, which is more, 38 and 37).
 // Many row tiles: fitting would leave some items much longer than others, so they are made shorter, kFiner rounds of them, and the
 // chip fills up again as they end; but not shorter than kRoundChunk (what comes before and after the keys takes as long as some
-// 10 key tiles) unless the chip is not filled once, and not shorter than kFilledChunk unless the row tiles alone leave over a third of
-// the units without work. us with kFilledChunk 24, without, and with 32: 64 requests x 8 heads x 500 keys 24.8, 28.4, 25.0; 32 x 8, 30
-// rows, 350 keys 13.9, 19.9, 13.9, lengths of 16 to 600 16.5, 24.0, 16.4; but 64 x 8 x 16 to 1400 keys 43.5, 37.2, 53.5 (54 batches of
-// one length 6 and 7 % faster than without, 54 of unlike lengths as fast, the worst cases 1.35, 1.6, 1.5 times the best of the three). With
-// fewer row tiles it loses: 40 x 8 x 2000 keys 66, 54.
+// 10 key tiles) unless the chip is not filled once, and not shorter than kFilledChunk where the row tiles alone give two thirds of the
+// units a workgroup. us with kFilledChunk 24, without, and with 32: 64 requests x 8 heads x 500 keys 25.6, 28.3, 25.6; 32 x 8, 30
+// rows, 350 keys 14.2, 20.5, 14.4, lengths of 16 to 500 15.0, 22.4, 15.0; but 64 x 8 x 936 keys 44.9, 43.5, 41.8 and 16 to 1400 keys 43.4, 37.5,
+// 54.2. Over 128 batches of one length 3 % better than without, over 128 of unlike lengths 1 %, the worst 1.4 times the best way of all that
+// were tried, without 2.1 (profiles/paged_attn_cut_sweep.txt, with the other constants). With fewer row tiles it loses: 40 x 8 x 2000 keys 66, 54.
 // Requests of kWhole key tiles on average are not split: 64 x 8 x 120 keys 6.9 us, split 12.2; 250 keys 12.9, 18.4.
 constexpr int kFiner = 3, kRoundChunk = 32, kFilledChunk = 24, kWhole = 8;
 SDVG_PAGED_HD int64_t ceil_div(int64_t a, int32_t b) {
@@ -91,14 +91,14 @@ SDVG_PAGED_HD int32_t pieces_of(const Request &q, int32_t chunk, int32_t full) {
 }
 
 // Items are numbered through all requests, first the full pieces of every request (kFull), then the others (kRest); the join numbers
-// the split row tiles (kSplit). How many of a number range a request of `pieces` pieces per row tile, `full` full ones among them, has:
+// the split row tiles (kSplit). How many of a range are a request's, which has `pieces` pieces per row tile, `full` full ones among them:
 enum Range { kFull, kRest, kSplit };
 SDVG_PAGED_HD int32_t numbers_of(const Request &q, int32_t full, int32_t pieces, Range range) {
   return q.row_tiles * (range == kFull ? full : range == kRest ? pieces - full : pieces > 1);
 }
-// Row tile and piece of number i of a request's own. The row tiles of a full piece follow each other where workgroups that read the same
-// keys then are on the same XCD (they are dealt out to 8 in turn), which is where the (sets of) key heads are a multiple of 8: 64 rows x 131071 keys x
-// 8 heads, 16 bit, 166 us with the pieces of a row tile in a row, 136 so; with 4 sets of heads (e4m3) 92 and 97.
+// Row tile and piece of number i of a request's own. The row tiles of a full piece follow each other where workgroups that read
+// the same keys then are on the same XCD (they are dealt out to 8 in turn): where the (sets of) key heads are a multiple of 8. 64 rows x
+// 131071 keys x 8 heads, 16 bit, 166 us with the pieces of a row tile in a row, 136 so; with 4 sets of heads (e4m3) 92 and 97.
 struct Place {
   int32_t tile, piece;
 };

@@ -287,8 +287,8 @@ int launch_rows(const RowsParams &p, hipStream_t s) {
 }
 template <typename T, typename C, bool kHalf>
 int launch_rows(const RowsParams &p, hipStream_t s) {
-  // Few tokens: a workgroup each, so that more compute units work on them. Many: 4, which fills the computation of the
-  // angles (64 per token) with all threads. Stores as in the pass with tables: ordinary ones up to 4 MiB,
+  // Few tokens: a workgroup each, so that more compute units work on them, and ordinary stores, however many heads they have. Many: 4, which
+  // fills the computation of the angles (64 per token) with all threads, and stores as in the pass with tables: ordinary ones up to 4 MiB,
   // which the next kernel finds in the caches. Beyond, 40 + 40 heads x 4680 tokens called in a row 32 us, with ordinary stores 38
   // (what the last call left to be written back meets the next one's reads); the commit of 6007 tokens 22.6 and 23.8.
   const int64_t rows = static_cast<int64_t>(p.n_tokens) * (p.t[0].heads.d + p.t[1].heads.d + p.t[2].heads.d);
