@@ -301,8 +301,6 @@ def block_attn(q, k_cache, v_cache, k_blk, v_blk, cache_len, out=None, scale=Non
     """sdvg_block_attn: q, k_blk, v_blk [tokens, heads, 128]; k_cache, v_cache one layer's
     [>= cache_len, heads, 128] (may be None when cache_len == 0). `scale=None` passes 0, which the
     library reads as 1/sqrt(head_dim). `out` defaults to a new tensor; pass out=q for in place. Returns out."""
-    if out is None and stream is not None:
-        out = _empty_like(q, stream)
     r = (_NATIVE or _native()).block_attn(q, k_cache, v_cache, k_blk, v_blk, cache_len, out, scale,
                                          None if stream is None else stream.cuda_stream, False)
     if r is not None:
@@ -323,8 +321,6 @@ def block_attn(q, k_cache, v_cache, k_blk, v_blk, cache_len, out=None, scale=Non
 def block_attn_commit(q, k_cache, v_cache, k_blk, v_blk, cache_len, out=None, scale=None, stream=None):
     """sdvg_block_attn_commit: block_attn for one layer that also copies k_blk / v_blk into tokens
     [cache_len, cache_len + n_blk) of k_cache / v_cache (which must be long enough). Returns out."""
-    if out is None and stream is not None:
-        out = _empty_like(q, stream)
     r = (_NATIVE or _native()).block_attn(q, k_cache, v_cache, k_blk, v_blk, cache_len, out, scale,
                                          None if stream is None else stream.cuda_stream, True)
     if r is not None:
@@ -381,8 +377,6 @@ def block_attn_batch(qs, k_caches, v_caches, k_blks, v_blks, cache_len, outs=Non
     cache_len == 0); every item must have the same shapes and strides. `workspace`: optional
     device tensor (any dtype) the library may use to split keys over workgroups, under the policy
     `split` ("never", "auto", "always"). Returns outs."""
-    if outs is None and stream is not None:
-        outs = [_empty_like(q, stream) for q in qs]
     if type(split) is str and split in _SPLIT:
         r = (_NATIVE or _native()).batch(qs, k_caches, v_caches, k_blks, v_blks, cache_len, outs, workspace,
                                         _SPLIT[split], scale, None if stream is None else stream.cuda_stream, _static)
@@ -457,8 +451,6 @@ def _check_tables(cos, sin, n_tokens, device):
 def rope(x, cos, sin, out=None, stream=None):
     """sdvg_rope: rotary embedding of bf16 rows x [tokens, heads, 128] by the angle tables cos, sin
     float32 [tokens, 64]. out defaults to a new tensor; pass out=x for in place."""
-    if out is None and stream is not None:
-        out = _empty_like(x, stream)
     r = (_NATIVE or _native()).rope(x, cos, sin, out, None if stream is None else stream.cuda_stream)
     if r is not None:
         if type(r) is int:
@@ -730,9 +722,6 @@ def rope_positions(x, positions, freqs, y=None, layout="half", gain=1.0, out=Non
     number of heads) in the same launch, at int32 positions [tokens] with float64 freqs [rotary_dim / 2] (rope_frequencies).
     layout "half" pairs elements p and p + rotary_dim / 2, "interleaved" 2p and 2p + 1. out / y_out default to new tensors;
     pass the input for in place. Returns out, or (out, y_out) with y."""
-    if stream is not None:
-        out = _empty_like(x, stream) if out is None else out
-        y_out = _empty_like(y, stream) if y is not None and y_out is None else y_out
     if type(layout) is str and layout in _LAYOUT:
         r = (_NATIVE or _native()).rope_positions(x, positions, freqs, y, _LAYOUT[layout], gain, out, y_out,
                                                  None if stream is None else stream.cuda_stream)
@@ -790,8 +779,6 @@ def paged_commit(cache, k, v, slots, positions=None, freqs=None, q=None, q_out=N
     """sdvg_paged_commit: rows k, v [tokens, kv_heads, 128] of bfloat16 or float16 into the int64 slots [tokens] of a PagedKV;
     a negative slot writes nothing. With positions and freqs (as for rope_positions) K is rotated on its way, and so is
     q [tokens, heads, 128] into q_out (default: a new tensor; pass q for in place). Returns q_out, or None without q."""
-    if stream is not None and q is not None and q_out is None:
-        q_out = _empty_like(q, stream)
     if type(layout) is str and layout in _LAYOUT:
         r = (_NATIVE or _native()).paged_commit(cache.c, cache.k, k, v, slots, positions, freqs, q, q_out, _LAYOUT[layout], gain,
                                                None if stream is None else stream.cuda_stream)
@@ -855,8 +842,6 @@ def paged_attn(q, cache, block_table, q_start, kv_lens, out=None, lse=None, scal
     them. `window` > 0: every token sees the last `window` keys only. `lse`: optional float32 [tokens, heads] for the log of the sums.
     `workspace`: optional device tensor of paged_attn_workspace_bytes, with which the keys of long requests are split
     over the chip. `scale=None` is 1/sqrt(128). out defaults to a new tensor; pass out=q for in place. Returns out."""
-    if out is None and stream is not None:
-        out = _empty_like(q, stream)
     r = (_NATIVE or _native()).paged_attn(q, cache.c, cache.k, block_table, q_start, kv_lens, out, lse, scale, window, workspace,
                                          None if stream is None else stream.cuda_stream)
     if r is not None:

@@ -11,8 +11,12 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/core/Stream.h>
+#include <c10/core/impl/DeviceGuardImplInterface.h>
 
 #include <string.h>
+
+#include <optional>
 
 #include "sdvg.h"
 
@@ -103,9 +107,28 @@ bool stream_ptr(PyObject *o, void *&s) {
   return true;
 }
 
-// The output tensor: the one given if it matches `like`, a new one for None; undefined if neither.
-at::Tensor output(PyObject *o, const at::Tensor &like) {
+// Makes `stream` a device's current one for as long as this lives, unless the call names none (`given` is None): 0.1 us of the host's time,
+// 8 in Python.
+struct StreamGuard {
+  std::optional<c10::Stream> before;
+  StreamGuard(PyObject *given, const at::Device &device, void *stream) {
+    if (given == Py_None) return;
+    // (a stream that torch did not make has its pointer for an id, and one that it made is the same to the allocator by its pointer)
+    before = c10::impl::getDeviceGuardImpl(device.type())
+                 ->exchangeStream(c10::Stream(c10::Stream::UNSAFE, device, reinterpret_cast<c10::StreamId>(stream)));
+  }
+  ~StreamGuard() {
+    if (before) c10::impl::getDeviceGuardImpl(before->device_type())->exchangeStream(*before);
+  }
+  StreamGuard(const StreamGuard &) = delete;
+  StreamGuard &operator=(const StreamGuard &) = delete;
+};
+
+// The output tensor: the one given if it matches `like`, a new one for None; undefined if neither. A new one comes from the memory of
+// the call's stream, as in binding.py.
+at::Tensor output(PyObject *o, const at::Tensor &like, PyObject *given_stream, void *stream) {
   if (o == Py_None) {
+    const StreamGuard guard(given_stream, like.device(), stream);
     at::Tensor out = at::empty(like.sizes(), at::TensorOptions().dtype(like.scalar_type()).device(like.device()));
     return out.unsafeGetTensorImpl()->is_python_dispatch() ? at::Tensor() : out;
   }
@@ -174,7 +197,7 @@ PyObject *block_attn_impl(PyObject *const *a, Py_ssize_t n) {
   if (commit && (!it.kc || cache_len + it.kb->size(0) > it.kc->size(0))) PYTHON_TAKES_OVER;
   void *stream;
   if (!stream_ptr(a[8], stream)) PYTHON_TAKES_OVER;
-  const at::Tensor out = output(a[6], *it.q);
+  const at::Tensor out = output(a[6], *it.q, a[8], stream);
   if (!out.defined()) PYTHON_TAKES_OVER;
   const sdvg_attn_desc d = attn_desc(it, out, scale);
   void *const qp = it.q->data_ptr(), *const kcp = it.kc ? it.kc->data_ptr() : nullptr,
@@ -224,7 +247,7 @@ PyObject *batch_impl(PyObject *const *a, Py_ssize_t n_args) {
   for (Py_ssize_t i = 0; i < n; ++i) {
     PyObject *given = own_outs ? Py_None : entry(a[6], i);
     if (!given || (given == Py_None && !own_outs)) PYTHON_TAKES_OVER;
-    outs[i] = output(given, *items[i].q);
+    outs[i] = output(given, *items[i].q, a[10], stream);
     if (!outs[i].defined()) PYTHON_TAKES_OVER;
     const sdvg_attn_desc di = attn_desc(items[i], outs[i], scale);
     if (i == 0)
@@ -360,7 +383,7 @@ PyObject *rope_impl(PyObject *const *a, Py_ssize_t n) {
       PYTHON_TAKES_OVER;
   void *stream;
   if (!stream_ptr(a[4], stream)) PYTHON_TAKES_OVER;
-  const at::Tensor out = output(a[3], *x);
+  const at::Tensor out = output(a[3], *x, a[4], stream);
   if (!out.defined()) PYTHON_TAKES_OVER;
   void *const xp = x->data_ptr(), *const op = out.data_ptr();
   const float *const cp = static_cast<const float *>(cos->data_ptr()), *const sp = static_cast<const float *>(sin->data_ptr());
@@ -517,7 +540,7 @@ PyObject *rope_positions_impl(PyObject *const *a, Py_ssize_t n_args) {
   if (two ? (!y || y->scalar_type() != x->scalar_type() || y->size(0) != x->size(0)) : a[7] != Py_None) PYTHON_TAKES_OVER;
   sdvg_rope_desc rope;
   if (!rope_of(a[1], a[2], a[4], a[5], x->size(0), device, rope)) PYTHON_TAKES_OVER;
-  const at::Tensor out = output(a[6], *x), y_out = two ? output(a[7], *y) : at::Tensor();
+  const at::Tensor out = output(a[6], *x, a[8], stream), y_out = two ? output(a[7], *y, a[8], stream) : at::Tensor();
   if (!out.defined() || (two && !y_out.defined())) PYTHON_TAKES_OVER;
   const sdvg_rows rx = rows_of(*x, &out), ry = two ? rows_of(*y, &y_out) : sdvg_rows{};
   const int64_t n = x->size(0);
@@ -554,7 +577,7 @@ PyObject *paged_commit_impl(PyObject *const *a, Py_ssize_t n_args) {
   if (turn && !rope_of(a[5], a[6], a[9], a[10], n, device, rope)) PYTHON_TAKES_OVER;
   const at::Tensor *q = with_q ? rows_tensor(a[7], device) : nullptr;
   if (with_q && (!q || q->size(0) != n || q->scalar_type() != k->scalar_type())) PYTHON_TAKES_OVER;
-  const at::Tensor q_out = with_q ? output(a[8], *q) : at::Tensor();
+  const at::Tensor q_out = with_q ? output(a[8], *q, a[11], stream) : at::Tensor();
   if (with_q && !q_out.defined()) PYTHON_TAKES_OVER;
   const sdvg_rows rk = rows_of(*k, nullptr), rv = rows_of(*v, nullptr), rq = with_q ? rows_of(*q, &q_out) : sdvg_rows{};
   const int64_t *const sp = static_cast<const int64_t *>(slots->data_ptr());
@@ -586,7 +609,7 @@ PyObject *paged_attn_impl(PyObject *const *a, Py_ssize_t n_args) {
                           lse->size(1) != q->size(1) || !lse->is_contiguous() || lse->get_device() != device))
     PYTHON_TAKES_OVER;
   if (a[10] != Py_None && (!ws || !ws->is_contiguous() || ws->get_device() != device)) PYTHON_TAKES_OVER;
-  const at::Tensor out = output(a[6], *q);
+  const at::Tensor out = output(a[6], *q, a[11], stream);
   if (!out.defined()) PYTHON_TAKES_OVER;
   const sdvg_paged_attn_desc d{static_cast<int32_t>(n), static_cast<int32_t>(q->size(0)), static_cast<int32_t>(q->size(1)), 128,
                                static_cast<int32_t>(table->size(1)), static_cast<int32_t>(window), table->stride(0), q->stride(0),

@@ -37,8 +37,13 @@ def calls():
 
 @pytest.mark.parametrize("name", ["block_attn", "block_attn_commit", "block_attn_batch", "rope", "worst_frame_route_batch",
                                   "rope_positions", "paged_commit", "paged_attn"])
-def test_given_back_block_of_a_busy_stream(name):
+@pytest.mark.parametrize("native", [True, False])
+def test_given_back_block_of_a_busy_stream(monkeypatch, name, native):
+    import paper_2604_17397_amd as P
     call = calls()[name]
+    P.lib()
+    if not native:
+        monkeypatch.setattr(P.binding, "_NATIVE", P.binding._PythonOnly)
 
     def listed(r):
         return [r] if torch.is_tensor(r) else list(r)
@@ -55,3 +60,29 @@ def test_given_back_block_of_a_busy_stream(name):
     assert not given_back & {t.data_ptr() for t in got}
     torch.cuda.synchronize()
     assert all(torch.equal(g, w) for g, w in zip(got, want))
+    assert torch.cuda.current_stream() == torch.cuda.default_stream()
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_result_that_is_dropped_while_its_stream_is_busy(monkeypatch, native):
+    """The memory of a result that nobody keeps goes back to the call's stream, not to the current one, which could hand it out
+    before the call has run."""
+    import paper_2604_17397_amd as P
+    P.lib()
+    if not native:
+        monkeypatch.setattr(P.binding, "_NATIVE", P.binding._PythonOnly)
+    x, cos, sin = rows(70, 4), torch.rand((70, 64), device="cuda"), torch.rand((70, 64), device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+    at = P.rope(x, cos, sin, stream=side).data_ptr()
+    y = [torch.full((70, 4, 128), 5.0, device="cuda", dtype=torch.bfloat16) for _ in range(4)]
+    assert at not in [t.data_ptr() for t in y]
+    torch.cuda.synchronize()
+    assert all((t == 5).all() for t in y)
+    with torch.cuda.stream(side):       # one pool, however the stream is named
+        again = P.rope(x, cos, sin).data_ptr()
+        named = P.rope(x, cos, sin, stream=side).data_ptr()
+    assert at == again == named
+    torch.cuda.synchronize()
