@@ -4,6 +4,9 @@ PyTorch tensors supply device memory (`data_ptr()`) and the HIP stream; nothing 
 here and there is no fallback: a missing library raises. The most frequent calls are marshalled by
 the extension module _native.so (csrc/host/native.cpp), which makes the same checks in C++ and
 leaves every call it does not recognise as valid to the Python code here, which also works alone.
+
+A result that a call with stream= makes for itself belongs to that stream, its memory too: another stream waits for
+that one before it reads the result, and names itself with record_stream if it still reads when the result is dropped.
 """
 import contextlib
 import ctypes

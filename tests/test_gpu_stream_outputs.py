@@ -86,3 +86,29 @@ def test_result_that_is_dropped_while_its_stream_is_busy(monkeypatch, native):
         named = P.rope(x, cos, sin, stream=side).data_ptr()
     assert at == again == named
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_captured_call_that_names_the_capturing_stream(monkeypatch, native):
+    import paper_2604_17397_amd as P
+    P.lib()
+    if not native:
+        monkeypatch.setattr(P.binding, "_NATIVE", P.binding._PythonOnly)
+    x, cos, sin = rows(70, 4), torch.rand((70, 64), device="cuda"), torch.rand((70, 64), device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        P.rope(x, cos, sin, stream=side)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            first = P.rope(x, cos, sin, stream=side)
+            second = P.rope(first, cos, sin, stream=side)
+        for seed in range(4):
+            x.copy_(rows(70, 4, seed))
+            torch.cuda.synchronize()
+            junk = [torch.full_like(x, 3.0) for _ in range(8)]      # eager work between the replays
+            want = P.rope(x, cos, sin)
+            want2 = P.rope(want, cos, sin)
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(first, want) and torch.equal(second, want2) and all((t == 3).all() for t in junk)
