@@ -2,7 +2,7 @@
 with a small value is, whose weight the sum has and the product with V must not lose.
 
 Bounds as in the attention's other tests. fp16 has 11 bits down to 2^-14 and steps of 2^-24 below; the kernel keeps the largest
-probability of a wave between 2^13 and 2^15, so those down to 2^-27 of it (18.7 nats) are rounded once to 11 bits and a smaller one is
+probability of a wave between 2^13 and 2^15, so those down to 2^-27 of it (18.7 nats) keep 11 bits at least and a smaller one is
 off by 2^-38 of it at most. In the ragged cases such ones are off by 2^-38 n |v| together, below the 2^-12 A that is allowed for the scores (A
 is about n e^(-17 + 1/2) |v| = 2^-23.8 n |v| there, and the scores, of one product each, are exact to 2^-24)."""
 import pytest
