@@ -136,7 +136,7 @@ def _prepare_prefix(case, gen, st):
     if own:
         import paper_2604_17397_amd as package
         st["handle"] = package.PagedKV(st["kc"], st["vc"], st["k_scale"], st["v_scale"])
-        n = package.paged_prefix_attn_workspace_bytes(st["q"], st["handle"], table, R, case["groups"], window=case["window"])
+        n = package.paged_prefix_attn_workspace_bytes(st["q"], st["handle"], table, case["groups"])
         st["workspace"] = torch.empty(n, dtype=torch.uint8, device="cuda")
 
 
