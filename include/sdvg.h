@@ -442,6 +442,29 @@ int sdvg_paged_attn(const sdvg_paged_attn_desc *desc, const sdvg_paged_kv *cache
 int64_t sdvg_paged_attn_workspace_bytes(const sdvg_paged_attn_desc *desc, const sdvg_paged_kv *cache);
 
 /*
+ * sdvg_paged_attn where groups of requests share their first keys, as continuations of one prompt do: the same result (sums in
+ * another order), but the shared keys are read once for all rows of a group. Requests group_start[g] .. group_start[g + 1] - 1 are group g;
+ * the rows of the block table of a group's requests list the same pages for its first prefix_lens[g] keys (where these end inside a page,
+ * pages with the same first keys), which are read through the row of its first request. Everything else is as
+ * sdvg_paged_attn has it: kv_lens count the shared keys, positions go through them, requests keep tables, slots and lengths as
+ * sdvg_page_plan leaves them.
+ *   group_start device int32 [n_groups + 1], not decreasing, or NULL: one group (n_groups == 1) of all requests. Requests outside of
+ *             all groups share nothing. prefix_lens device int32 [n_groups]; 0 (or less): the group shares nothing.
+ *             prefix_lens[g] <= kv_lens[r] - n for every request r of the group that has new tokens: no new token is part of the
+ *             prefix. (A row at a position inside it still sees no key behind its own, but with a window it misses those ahead of
+ *             prefix_lens[g] + 1 - window.) All keys of a prefix that lie between those that its rows see must be finite.
+ *   n_groups  >= 0; with 0 the call is sdvg_paged_attn.
+ *   workspace as in sdvg_paged_attn, of sdvg_paged_prefix_attn_workspace_bytes(desc, cache, n_groups) bytes; without one, or with one that is
+ *             too small, the call is sdvg_paged_attn with that workspace. A need of 0 means that there is nothing to do.
+ * Made for many rows per group (its requests' tokens x the query heads of a key head): every 64 or 128 of them read the shared keys again.
+ * Every workgroup looks through all groups and requests. Up to three launches; asynchronous on `stream`.
+ */
+int sdvg_paged_prefix_attn(const sdvg_paged_attn_desc *desc, const sdvg_paged_kv *cache, const void *q, const int32_t *block_table,
+                           const int32_t *q_start, const int32_t *kv_lens, int32_t n_groups, const int32_t *group_start,
+                           const int32_t *prefix_lens, void *out, float *lse, void *workspace, int64_t workspace_bytes, void *stream);
+int64_t sdvg_paged_prefix_attn_workspace_bytes(const sdvg_paged_attn_desc *desc, const sdvg_paged_kv *cache, int32_t n_groups);
+
+/*
  * Measurement aid (no passage of the paper: it exists so that a benchmark can report what the
  * matrix cores of the chip it runs on deliver, next to the attention kernel's rate). Launches
  * 256 workgroups of 4 waves (one wave per SIMD of the chip); every wave issues iters x 16 v_mfma_f32_32x32x16_bf16 from

@@ -28,6 +28,8 @@ from .binding import (  # noqa: F401
     paged_commit,
     paged_attn,
     paged_attn_workspace_bytes,
+    paged_prefix_attn,
+    paged_prefix_attn_workspace_bytes,
     probe_mfma,
     lib,
     status_string,

@@ -150,6 +150,10 @@ def lib():
         L.sdvg_paged_attn.argtypes = [pa, pc, vp, vp, vp, vp, vp, vp, vp, i64, vp]
         L.sdvg_paged_attn_workspace_bytes.restype = ctypes.c_int64
         L.sdvg_paged_attn_workspace_bytes.argtypes = [pa, pc]
+        L.sdvg_paged_prefix_attn.restype = ctypes.c_int
+        L.sdvg_paged_prefix_attn.argtypes = [pa, pc, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, i64, vp]
+        L.sdvg_paged_prefix_attn_workspace_bytes.restype = ctypes.c_int64
+        L.sdvg_paged_prefix_attn_workspace_bytes.argtypes = [pa, pc, i32]
         L.sdvg_probe_mfma.restype = ctypes.c_int
         L.sdvg_probe_mfma.argtypes = [vp, i64, vp, i32, ctypes.POINTER(ctypes.c_double), vp]
         L.sdvg_probe_mfma_changing.restype = ctypes.c_int
@@ -167,7 +171,7 @@ def lib():
 class _PythonOnly:
     """Stands in for the marshalling module where it has not been built: Python handles every call."""
     block_attn = rope = route = batch = commit = rollback = snapshot = staticmethod(lambda *args: None)
-    page_plan = rope_positions = paged_commit = paged_attn = staticmethod(lambda *args: None)
+    page_plan = rope_positions = paged_commit = paged_attn = paged_prefix_attn = staticmethod(lambda *args: None)
 
 
 _NATIVE = None
@@ -190,7 +194,7 @@ def _bind_native(L):
              (L.sdvg_block_attn, L.sdvg_block_attn_commit, L.sdvg_rope, L.sdvg_worst_frame_route, L.sdvg_avg_frame_route,
               L.sdvg_block_attn_batch, L.sdvg_block_attn_batch_static, L.sdvg_kv_commit, L.sdvg_kv_commit_rope,
               L.sdvg_kv_rollback, L.sdvg_buffer_snapshot, L.sdvg_page_plan, L.sdvg_rope_positions, L.sdvg_paged_commit,
-              L.sdvg_paged_attn)]
+              L.sdvg_paged_attn, L.sdvg_paged_prefix_attn)]
     module.init(*entry, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, np.float32, sdvg_kv_cache, sdvg_paged_kv)
     _NATIVE = module
 
@@ -839,6 +843,21 @@ def paged_attn_workspace_bytes(q, cache, block_table):
     return int(n)
 
 
+def _attn_args(q, cache, block_table, q_start, kv_lens, out, lse, scale, window, workspace, stream):
+    """Checks what paged_attn and paged_prefix_attn have in common; the descriptor and the output."""
+    _check_here(q, cache.k, block_table, q_start, kv_lens, out, lse, workspace)
+    if out is None:
+        out = _empty_like(q, stream)
+    d = _paged_attn_desc(q, cache, block_table, out, scale, window)
+    _int_array("q_start", q_start, d.n_requests + 1)
+    _int_array("kv_lens", kv_lens, d.n_requests)
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous()):
+        raise ValueError("lse must be dense float32 [tokens, heads]")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return d, out
+
+
 def paged_attn(q, cache, block_table, q_start, kv_lens, out=None, lse=None, scale=None, window=0, workspace=None, stream=None):
     """sdvg_paged_attn: attention of the new tokens q [tokens, heads, 128] of several requests over their pages in a PagedKV.
     block_table int32 [requests, pages], q_start int32 [requests + 1] and kv_lens int32 [requests] as page_plan leaves
@@ -851,21 +870,56 @@ def paged_attn(q, cache, block_table, q_start, kv_lens, out=None, lse=None, scal
         if type(r) is int:
             raise SdvgError(r, "sdvg_paged_attn")
         return r
-    _check_here(q, cache.k, block_table, q_start, kv_lens, out, lse, workspace)
-    if out is None:
-        out = _empty_like(q, stream)
-    d = _paged_attn_desc(q, cache, block_table, out, scale, window)
-    _int_array("q_start", q_start, d.n_requests + 1)
-    _int_array("kv_lens", kv_lens, d.n_requests)
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous()):
-        raise ValueError("lse must be dense float32 [tokens, heads]")
-    if workspace is not None and not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous")
+    d, out = _attn_args(q, cache, block_table, q_start, kv_lens, out, lse, scale, window, workspace, stream)
     st = lib().sdvg_paged_attn(ctypes.byref(d), ctypes.byref(cache.c), _ptr(q), _ptr(block_table), _ptr(q_start), _ptr(kv_lens),
                                _ptr(out), _ptr(lse), _ptr(workspace),
                                0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_ptr(stream))
     if st != 0:
         raise SdvgError(st, "sdvg_paged_attn")
+    return out
+
+
+def _n_groups(prefix_lens, group_start):
+    n = prefix_lens.shape[0] if prefix_lens.dim() == 1 else -1
+    _int_array("prefix_lens", prefix_lens, n)
+    if group_start is not None:
+        _int_array("group_start", group_start, n + 1)
+    elif n > 1:
+        raise ValueError("several prefixes need group_start")
+    return n
+
+
+def paged_prefix_attn_workspace_bytes(q, cache, block_table, n_groups=1):
+    """sdvg_paged_prefix_attn_workspace_bytes for the shapes of these tensors and a number of groups."""
+    _check_here(q, cache.k, block_table)
+    d, n_groups = _paged_attn_desc(q, cache, block_table, q, None, 0), _int32("n_groups", n_groups)
+    n = lib().sdvg_paged_prefix_attn_workspace_bytes(ctypes.byref(d), ctypes.byref(cache.c), n_groups)
+    if n < 0:
+        raise SdvgError(n, "sdvg_paged_prefix_attn_workspace_bytes")
+    return int(n)
+
+
+def paged_prefix_attn(q, cache, block_table, q_start, kv_lens, prefix_lens, group_start=None, out=None, lse=None, scale=None,
+                      window=0, workspace=None, stream=None):
+    """sdvg_paged_prefix_attn: paged_attn where the requests of a group share their first keys, which are then read once for the
+    group. prefix_lens int32 [groups]: shared keys, which the rows of block_table of a group's requests name alike; group_start int32
+    [groups + 1]: first request of every group and the end of the last one (None: one group of all requests). kv_lens and
+    positions count the shared keys, and no new token lies among them. `workspace`: device tensor of
+    paged_prefix_attn_workspace_bytes; without it the call is paged_attn. Everything else as in paged_attn. Returns out."""
+    r = (_NATIVE or _native()).paged_prefix_attn(q, cache.c, cache.k, block_table, q_start, kv_lens, out, lse, scale, window, workspace,
+                                                None if stream is None else stream.cuda_stream, prefix_lens, group_start)
+    if r is not None:
+        if type(r) is int:
+            raise SdvgError(r, "sdvg_paged_prefix_attn")
+        return r
+    _check_here(q, prefix_lens, group_start)
+    n_groups = _n_groups(prefix_lens, group_start)
+    d, out = _attn_args(q, cache, block_table, q_start, kv_lens, out, lse, scale, window, workspace, stream)
+    st = lib().sdvg_paged_prefix_attn(ctypes.byref(d), ctypes.byref(cache.c), _ptr(q), _ptr(block_table), _ptr(q_start), _ptr(kv_lens),
+                                      n_groups, _ptr(group_start), _ptr(prefix_lens), _ptr(out), _ptr(lse), _ptr(workspace),
+                                      0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+    if st != 0:
+        raise SdvgError(st, "sdvg_paged_prefix_attn")
     return out
 
 

@@ -22,7 +22,7 @@ HIPCC_FLAGS = [
 ]
 # Sources compiled with a kernel's first dwords of arguments (14 at most) preloaded into scalar registers: worth 0.3 us
 # of a launch where the arguments are what a short kernel waits for. The routers lose 0.2 us by it.
-PRELOADED = {"block_attn_rows32.hip", "rope.hip", "paged_attn.hip"}
+PRELOADED = {"block_attn_rows32.hip", "rope.hip", "paged_attn.hip", "paged_prefix.hip"}
 PRELOAD_FLAGS = ["-mllvm", "-amdgpu-kernarg-preload-count=16"]
 
 

@@ -46,6 +46,8 @@ using paged_commit_fn = int (*)(const sdvg_paged_kv *, const sdvg_rows *, const 
                                 const sdvg_rope_desc *, const sdvg_rows *, void *);
 using paged_attn_fn = int (*)(const sdvg_paged_attn_desc *, const sdvg_paged_kv *, const void *, const int32_t *, const int32_t *,
                               const int32_t *, void *, float *, void *, int64_t, void *);
+using paged_prefix_attn_fn = int (*)(const sdvg_paged_attn_desc *, const sdvg_paged_kv *, const void *, const int32_t *, const int32_t *,
+                                     const int32_t *, int32_t, const int32_t *, const int32_t *, void *, float *, void *, int64_t, void *);
 
 // Entry points of the libsdvg that binding.py has loaded, and torch's current-stream functions.
 struct Api {
@@ -63,6 +65,7 @@ struct Api {
   rope_positions_fn rope_positions = nullptr;
   paged_commit_fn paged_commit = nullptr;
   paged_attn_fn paged_attn = nullptr;
+  paged_prefix_attn_fn paged_prefix_attn = nullptr;
   PyObject *get_device = nullptr, *get_raw_stream = nullptr, *float32 = nullptr, *cache_type = nullptr, *paged_type = nullptr;
 } api;
 
@@ -589,8 +592,10 @@ PyObject *paged_commit_impl(PyObject *const *a, Py_ssize_t n_args) {
 }
 
 // (q, cache.c, cache.k, block_table, q_start, kv_lens, out, lse, scale, window, workspace, stream)
+// (kPrefix: of groups that share their first keys; two arguments more, prefix_lens and group_start)
+template <bool kPrefix>
 PyObject *paged_attn_impl(PyObject *const *a, Py_ssize_t n_args) {
-  if (n_args != 12) PYTHON_TAKES_OVER;
+  if (n_args != (kPrefix ? 14 : 12)) PYTHON_TAKES_OVER;
   int64_t device, window;
   void *stream;
   double scale;
@@ -609,6 +614,17 @@ PyObject *paged_attn_impl(PyObject *const *a, Py_ssize_t n_args) {
                           lse->size(1) != q->size(1) || !lse->is_contiguous() || lse->get_device() != device))
     PYTHON_TAKES_OVER;
   if (a[10] != Py_None && (!ws || !ws->is_contiguous() || ws->get_device() != device)) PYTHON_TAKES_OVER;
+  const int32_t *group_p = nullptr, *prefix_p = nullptr;
+  int64_t n_groups = 0;
+  if constexpr (kPrefix) {
+    const at::Tensor *lens_t = gpu_tensor(a[12]);
+    if (!lens_t || lens_t->dim() != 1) PYTHON_TAKES_OVER;
+    n_groups = lens_t->size(0);
+    const at::Tensor *prefix = array(a[12], at::kInt, n_groups, device), *starts_t = a[13] == Py_None ? nullptr : array(a[13], at::kInt, n_groups + 1, device);
+    if (!prefix || n_groups > INT32_MAX - 1 || (!starts_t && (a[13] != Py_None || n_groups > 1))) PYTHON_TAKES_OVER;
+    prefix_p = static_cast<const int32_t *>(prefix->data_ptr());
+    if (starts_t) group_p = static_cast<const int32_t *>(starts_t->data_ptr());
+  }
   const at::Tensor out = output(a[6], *q, a[11], stream);
   if (!out.defined()) PYTHON_TAKES_OVER;
   const sdvg_paged_attn_desc d{static_cast<int32_t>(n), static_cast<int32_t>(q->size(0)), static_cast<int32_t>(q->size(1)), 128,
@@ -622,7 +638,10 @@ PyObject *paged_attn_impl(PyObject *const *a, Py_ssize_t n_args) {
   const int64_t w_bytes = ws ? static_cast<int64_t>(ws->nbytes()) : 0;
   int status;
   Py_BEGIN_ALLOW_THREADS
-  status = api.paged_attn(&d, cache.c, qp, tp, sp, lp, op, ep, wp, w_bytes, stream);
+  if constexpr (kPrefix)
+    status = api.paged_prefix_attn(&d, cache.c, qp, tp, sp, lp, static_cast<int32_t>(n_groups), group_p, prefix_p, op, ep, wp, w_bytes, stream);
+  else
+    status = api.paged_attn(&d, cache.c, qp, tp, sp, lp, op, ep, wp, w_bytes, stream);
   Py_END_ALLOW_THREADS
   return result(status, a[6], out);
 }
@@ -640,13 +659,13 @@ PyObject *guarded(PyObject *, PyObject *const *args, Py_ssize_t n) {
 }
 
 // (addresses of attn, attn_commit, rope, route_min, route_mean, batch, batch_static, commit, commit_rope, rollback,
-// snapshot, page_plan, rope_positions, paged_commit, paged_attn; torch._C._cuda_getDevice,
+// snapshot, page_plan, rope_positions, paged_commit, paged_attn, paged_prefix_attn; torch._C._cuda_getDevice,
 // torch._C._cuda_getCurrentRawStream, numpy.float32, the ctypes classes of the cache and of the paged cache)
 PyObject *init(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  constexpr int kEntries = 15;
+  constexpr int kEntries = 16;
   int64_t p[kEntries];
   if (n != kEntries + 5) {
-    PyErr_SetString(PyExc_TypeError, "init takes 20 arguments");
+    PyErr_SetString(PyExc_TypeError, "init takes 21 arguments");
     return nullptr;
   }
   for (int i = 0; i < kEntries; ++i)
@@ -660,7 +679,7 @@ PyObject *init(PyObject *, PyObject *const *a, Py_ssize_t n) {
             reinterpret_cast<batch_static_fn>(p[6]), reinterpret_cast<commit_fn>(p[7]),  reinterpret_cast<commit_rope_fn>(p[8]),
             reinterpret_cast<rollback_fn>(p[9]), reinterpret_cast<snapshot_fn>(p[10]),   reinterpret_cast<page_plan_fn>(p[11]),
             reinterpret_cast<rope_positions_fn>(p[12]), reinterpret_cast<paged_commit_fn>(p[13]),
-            reinterpret_cast<paged_attn_fn>(p[14]), a[15], a[16], a[17], a[18], a[19]};
+            reinterpret_cast<paged_attn_fn>(p[14]), reinterpret_cast<paged_prefix_attn_fn>(p[15]), a[16], a[17], a[18], a[19], a[20]};
   Py_RETURN_NONE;
 }
 
@@ -671,7 +690,8 @@ PyMethodDef methods[] = {METHOD("init", init), METHOD("block_attn", guarded<bloc
                          METHOD("batch", guarded<batch_impl>), METHOD("commit", guarded<commit_impl>),
                          METHOD("rollback", guarded<rollback_impl>), METHOD("snapshot", guarded<snapshot_impl>),
                          METHOD("page_plan", guarded<page_plan_impl>), METHOD("rope_positions", guarded<rope_positions_impl>),
-                         METHOD("paged_commit", guarded<paged_commit_impl>), METHOD("paged_attn", guarded<paged_attn_impl>),
+                         METHOD("paged_commit", guarded<paged_commit_impl>), METHOD("paged_attn", guarded<paged_attn_impl<false>>),
+                         METHOD("paged_prefix_attn", guarded<paged_attn_impl<true>>),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", "Argument marshalling of libsdvg's most frequent calls.",
                           -1, methods, nullptr, nullptr, nullptr, nullptr};

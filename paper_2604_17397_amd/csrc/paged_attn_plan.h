@@ -26,19 +26,22 @@ struct Request {
   int32_t len;                  // keys of the last token: positions 0 .. len - 1
   int32_t first_tile, tiles;    // key tiles that any of its rows sees
   int32_t row_tiles;
+  int32_t from;                 // keys ahead of this one are another launch's (a prefix that several requests share)
 };
 SDVG_PAGED_HD int32_t clamp(int32_t x, int32_t lo, int32_t hi) { return x < lo ? lo : x > hi ? hi : x; }
 
 // start, end: q_start[r], q_start[r + 1]; capacity: keys that a row of the block table can name.
 SDVG_PAGED_HD Request request_of(int32_t start, int32_t end, int32_t len, int32_t n_tokens, int32_t group, int32_t row_tile,
-                                 int32_t window, int64_t capacity) {
+                                 int32_t window, int64_t capacity, int32_t prefix = 0) {
   Request q;
   q.row0 = clamp(start, 0, n_tokens);
   q.n = clamp(end, q.row0, n_tokens) - q.row0;
   q.len = len > 0 ? len : 0;
   const int64_t first = static_cast<int64_t>(q.len) - q.n + 1 - window;  // of the first token's window
-  const int32_t lo = window > 0 && first > 0 ? static_cast<int32_t>(first) : 0;
   const int32_t hi = q.len < capacity ? q.len : static_cast<int32_t>(capacity);
+  int32_t lo = window > 0 && first > 0 ? static_cast<int32_t>(first) : 0;
+  q.from = prefix > 0 ? prefix : 0;
+  lo = lo > q.from ? lo : q.from;
   q.first_tile = lo / kKeyTile;
   q.tiles = hi > lo ? static_cast<int32_t>((static_cast<int64_t>(hi) + kKeyTile - 1) / kKeyTile) - q.first_tile : 0;
   q.row_tiles = static_cast<int32_t>((static_cast<int64_t>(q.n) * group + row_tile - 1) / row_tile);
@@ -93,8 +96,9 @@ SDVG_PAGED_HD int32_t pieces_of(const Request &q, int32_t chunk, int32_t full) {
 // Items are numbered through all requests, first the full pieces of every request (kFull), then the others (kRest); the join numbers
 // the split row tiles (kSplit). How many of a range are a request's, which has `pieces` pieces per row tile, `full` full ones among them:
 enum Range { kFull, kRest, kSplit };
-SDVG_PAGED_HD int32_t numbers_of(const Request &q, int32_t full, int32_t pieces, Range range) {
-  return q.row_tiles * (range == kFull ? full : range == kRest ? pieces - full : pieces > 1);
+// (`join`: a row tile is joined, and has slots, even where its own keys are one piece.)
+SDVG_PAGED_HD int32_t numbers_of(const Request &q, int32_t full, int32_t pieces, Range range, bool join = false) {
+  return q.row_tiles * (range == kFull ? full : range == kRest ? pieces - full : join || pieces > 1);
 }
 // Row tile and piece of number i of a request's own. The row tiles of a full piece follow each other where workgroups that read
 // the same keys then are on the same XCD (they are dealt out to 8 in turn): where the (sets of) key heads are a multiple of 8. 64 rows x
@@ -113,7 +117,7 @@ SDVG_PAGED_HD Place place_of(const Request &q, int32_t i, int32_t full, Range ra
   return Place{tile, i - tile * full};
 }
 // Slot of a piece's partial result: slot0 is the number of slots of the requests before.
-SDVG_PAGED_HD int32_t slots_of(const Request &q, int32_t pieces) { return pieces > 1 ? q.row_tiles * pieces : 0; }
+SDVG_PAGED_HD int32_t slots_of(const Request &q, int32_t pieces, bool join = false) { return join || pieces > 1 ? q.row_tiles * pieces : 0; }
 SDVG_PAGED_HD int32_t first_slot(int32_t slot0, int32_t tile, int32_t pieces) { return slot0 + tile * pieces; }
 // Key tiles begin .. end - 1 of a piece.
 struct KeyTiles {

@@ -1,0 +1,81 @@
+// How the keys that groups of requests share are cut into workgroups: integer arithmetic on the groups' rows and keys, which the
+// kernels do on the device and a host test repeats. (The requests' own keys are cut as paged_attn_plan.h says.)
+//
+// The rows of a group that share a key head (the new tokens of all its requests x the query heads of a key head) are cut into tiles
+// of row_tile rows, the shared keys into pieces of `chunk` key tiles at most. Every item (row tile, piece) leaves a partial
+// result in a numbered slot; a row tile's are consecutive.
+#pragma once
+#include "paged_attn_plan.h"
+
+namespace sdvg {
+namespace paged {
+
+constexpr int kSharedTile = 64;   // keys that a workgroup has in LDS at a time
+
+struct SharedKeys {
+  int32_t request0, requests;     // the group's
+  int32_t token0, tokens;         // their new tokens, which are neighbours
+  int32_t lo, hi;                 // keys lo .. hi - 1 are shared and may be seen
+  int32_t first_tile, tiles;      // key tiles that hold them
+  int32_t row_tiles;
+};
+// start, end: the group's first request and the next group's; token0, token1: q_start of the two; n: shared keys.
+// (No new token lies among the shared keys, so with a window none sees one ahead of n + 1 - window.)
+SDVG_PAGED_HD SharedKeys shared_of(int32_t start, int32_t end, int32_t token0, int32_t token1, int32_t n, int32_t n_tokens, int32_t group,
+                                   int32_t row_tile, int32_t window, int64_t capacity) {
+  SharedKeys s;
+  s.request0 = start;
+  s.requests = end - start;
+  s.token0 = clamp(token0, 0, n_tokens);
+  s.tokens = clamp(token1, s.token0, n_tokens) - s.token0;
+  const int64_t first = static_cast<int64_t>(n) + 1 - window;
+  s.lo = window > 0 && first > 0 ? static_cast<int32_t>(first) : 0;
+  s.hi = n < capacity ? n : static_cast<int32_t>(capacity);
+  s.first_tile = s.lo / kSharedTile;
+  s.tiles = s.hi > s.lo && s.tokens > 0 ? (s.hi + kSharedTile - 1) / kSharedTile - s.first_tile : 0;
+  s.row_tiles = s.tiles > 0 ? static_cast<int32_t>((static_cast<int64_t>(s.tokens) * group + row_tile - 1) / row_tile) : 0;
+  return s;
+}
+SDVG_PAGED_HD int64_t work_of(const SharedKeys &s) { return static_cast<int64_t>(s.row_tiles) * s.tiles; }
+
+// Key tiles per item at most: total = the sum of work_of over all groups, row_tiles that of theirs, target the items that fill the chip.
+// Where the row tiles are few, the items are made to fit the chip once; rounding up adds one per row tile at most.
+constexpr int kSharedRounds = 2, kSharedLeast = 8;
+SDVG_PAGED_HD int32_t shared_chunk(int64_t total, int64_t row_tiles, int32_t target) {
+  int64_t c;
+  if (2 * row_tiles <= target) {
+    c = ceil_div(total, target - static_cast<int32_t>(row_tiles));
+  } else {
+    c = ceil_div(total, kSharedRounds * target);
+    if (c < kSharedLeast) c = kSharedLeast;
+  }
+  return c < 1 ? 1 : c < INT32_MAX ? static_cast<int32_t>(c) : INT32_MAX;
+}
+SDVG_PAGED_HD int32_t shared_pieces(const SharedKeys &s, int32_t chunk) {
+  return s.tiles > 0 ? static_cast<int32_t>((static_cast<uint32_t>(s.tiles) + static_cast<uint32_t>(chunk) - 1) / static_cast<uint32_t>(chunk)) : 0;
+}
+// Item i of a group: the row tiles of a piece follow each other, so that workgroups that read the same keys run at the same time. Its
+// slot is slot0 (of the groups before) + tile * pieces + piece.
+SDVG_PAGED_HD Place shared_place(const SharedKeys &s, int32_t i) {
+  const int32_t piece = static_cast<uint32_t>(i) / static_cast<uint32_t>(s.row_tiles);
+  return Place{i - piece * s.row_tiles, piece};
+}
+SDVG_PAGED_HD KeyTiles shared_tiles_of(const SharedKeys &s, int32_t piece, int32_t chunk) {
+  const int32_t before = piece ? piece * chunk : 0;
+  return KeyTiles{s.first_tile + before, s.first_tile + (s.tiles - before < chunk ? s.tiles : before + chunk)};
+}
+
+// Bounds for the launch from what the host knows: row tiles, and items (and slots). total / chunk <= target - row_tiles, or
+// kSharedRounds * target; and one more per row tile.
+SDVG_PAGED_HD int64_t max_shared_row_tiles(int64_t n_groups, int64_t n_tokens, int32_t group, int32_t row_tile) {
+  const int64_t rows = n_tokens * group, bound = rows / row_tile + n_groups;
+  return bound < rows ? bound : rows;
+}
+SDVG_PAGED_HD int64_t max_shared_items(int64_t row_tiles, int32_t target, int64_t capacity) {
+  const int64_t by_chunk = 2 * row_tiles <= target ? target : row_tiles + kSharedRounds * static_cast<int64_t>(target);
+  const int64_t by_keys = row_tiles * ceil_div(capacity, kSharedTile);
+  return by_chunk < by_keys ? by_chunk : by_keys;
+}
+
+}  // namespace paged
+}  // namespace sdvg

@@ -52,10 +52,10 @@ def main():
     rt = subprocess.run([clang, "-print-file-name=libclang_rt.asan-x86_64.so"], stdout=subprocess.PIPE,
                         text=True).stdout.strip()
     env = dict(base, SDVG_LIBRARY=lib, LD_PRELOAD=rt)
-    rc |= run([sys.executable, "-m", "pytest", "-x", "-q", "tests/test_abi.py", "tests/test_paged_abi.py"], env)
+    rc |= run([sys.executable, "-m", "pytest", "-x", "-q", "tests/test_abi.py", "tests/test_paged_abi.py", "tests/test_paged_prefix_host.py"], env)
     # (3) the host programs over the kernels' index headers
     for name in ("attn_index_replay", "attn_groups_replay", "attn_rows32_replay", "attn_rows32_halves", "attn_split_check",
-                 "row_map_check", "paged_attn_plan"):
+                 "row_map_check", "paged_attn_plan", "paged_prefix_items"):
         exe = os.path.join(tmp, name + "_san")
         rc |= run(["g++", "-O1", "-g", "-std=c++17", "-fopenmp", "-fsanitize=address,undefined", "-fno-omit-frame-pointer",
                    "-I", os.path.join(ROOT, "paper_2604_17397_amd", "csrc"), "-I", os.path.join(ROOT, "include"),
