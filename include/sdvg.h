@@ -465,6 +465,47 @@ int sdvg_paged_prefix_attn(const sdvg_paged_attn_desc *desc, const sdvg_paged_kv
 int64_t sdvg_paged_prefix_attn_workspace_bytes(const sdvg_paged_attn_desc *desc, const sdvg_paged_kv *cache, int32_t n_groups);
 
 /*
+ * ---- Drawing tokens ---------------------------------------------------------------------------
+ * One token per row of logits, from a random number that the caller gives: the last call of a step whose rows are the next tokens
+ * of many requests, or of many continuations of one prompt. With t = temperature, M the row's largest logit and w_i = exp((logit_i - M) / t):
+ *   the tokens in order, larger logits first, of equal ones the lower index;
+ *   top-k: the first top_k of them;
+ *   top-p: the shortest prefix of those whose weight is at least top_p times theirs (at least one token);
+ *   min-p: of these the ones with w_i >= min_p;
+ *   tokens[r] = the lowest index i for which the sum of the kept weights up to i is more than u[r] times their total.
+ * logprob[r] is the natural logarithm of its weight over that total. Weights and sums are held in 64 bits, a weight at most 2^-35
+ * of itself off; one below 2^-63 of the largest counts as 0 where there is a filter. The same call gives the same tokens, and so does a row alone
+ * or among others, but where u or top_p lie as near to a border as that.
+ *   logits    device [n_rows][vocab] of type dtype (SDVG_F32, SDVG_BF16, SDVG_F16), row_stride elements apart (not looked at for one row),
+ *             aligned to their own size. -infinity: the token is never drawn; -0 is 0; +infinity is more than all numbers. A row that has a NaN, or
+ *             nothing but -infinity, gets token -1 and a logprob of NaN.
+ *   u         device float [n_rows], in [0, 1); other numbers are clamped, NaN is 0.
+ *   temperature, top_k, top_p, min_p  device float / int32 / float / float [n_rows], nullable: then all rows have all_temperature, all_top_k,
+ *             all_top_p, all_min_p. temperature <= 0 (or NaN): the token with the largest logit, the lowest index of several, logprob 0. top_k <= 0
+ *             or >= vocab, top_p >= 1 (or NaN) and min_p <= 0 (or NaN) are off; min_p > 1 is 1.
+ *   tokens    device int32 [n_rows]; logprob device float [n_rows], nullable. They must not overlap the inputs or each other (SDVG_ERR_RANGE).
+ *   workspace device, 16-byte aligned, of at least sdvg_sample_tokens_workspace_bytes(n_rows, vocab) bytes (SDVG_ERR_RANGE if it is
+ *             smaller). Scratch: overlapping calls need their own.
+ * 1 <= vocab <= 2^20; n_rows slices of 8192 tokens below some 2^23 (SDVG_ERR_UNSUPPORTED); n_rows may be 0. Two launches, three with any
+ * filter; asynchronous on `stream`.
+ */
+typedef struct {
+  const void *logits;                        /* device */
+  const float *u, *temperature;              /* device */
+  const int32_t *top_k;                      /* device */
+  const float *top_p, *min_p;                /* device */
+  float all_temperature;
+  int32_t all_top_k;
+  float all_top_p, all_min_p;
+  int32_t *tokens;                           /* device */
+  float *logprob;                            /* device */
+  int64_t row_stride;
+  int32_t n_rows, vocab, dtype;
+} sdvg_sample_args;
+int sdvg_sample_tokens(const sdvg_sample_args *args, void *workspace, int64_t workspace_bytes, void *stream);
+int64_t sdvg_sample_tokens_workspace_bytes(int32_t n_rows, int32_t vocab);
+
+/*
  * Measurement aid (no passage of the paper: it exists so that a benchmark can report what the
  * matrix cores of the chip it runs on deliver, next to the attention kernel's rate). Launches
  * 256 workgroups of 4 waves (one wave per SIMD of the chip); every wave issues iters x 16 v_mfma_f32_32x32x16_bf16 from

@@ -30,6 +30,8 @@ from .binding import (  # noqa: F401
     paged_attn_workspace_bytes,
     paged_prefix_attn,
     paged_prefix_attn_workspace_bytes,
+    sample_tokens,
+    sample_tokens_workspace_bytes,
     probe_mfma,
     lib,
     status_string,

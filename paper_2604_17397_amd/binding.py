@@ -91,6 +91,14 @@ class sdvg_page_plan_args(ctypes.Structure):
                 ("held_out", ctypes.c_void_p), ("next_free_out", ctypes.c_void_p), ("slots", ctypes.c_void_p)]
 
 
+class sdvg_sample_args(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("u", ctypes.c_void_p), ("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p),
+                ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p), ("all_temperature", ctypes.c_float),
+                ("all_top_k", ctypes.c_int32), ("all_top_p", ctypes.c_float), ("all_min_p", ctypes.c_float),
+                ("tokens", ctypes.c_void_p), ("logprob", ctypes.c_void_p), ("row_stride", ctypes.c_int64),
+                ("n_rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
 _LIB = None
 
 
@@ -154,6 +162,10 @@ def lib():
         L.sdvg_paged_prefix_attn.argtypes = [pa, pc, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, i64, vp]
         L.sdvg_paged_prefix_attn_workspace_bytes.restype = ctypes.c_int64
         L.sdvg_paged_prefix_attn_workspace_bytes.argtypes = [pa, pc, i32]
+        L.sdvg_sample_tokens.restype = ctypes.c_int
+        L.sdvg_sample_tokens.argtypes = [ctypes.POINTER(sdvg_sample_args), vp, i64, vp]
+        L.sdvg_sample_tokens_workspace_bytes.restype = ctypes.c_int64
+        L.sdvg_sample_tokens_workspace_bytes.argtypes = [i32, i32]
         L.sdvg_probe_mfma.restype = ctypes.c_int
         L.sdvg_probe_mfma.argtypes = [vp, i64, vp, i32, ctypes.POINTER(ctypes.c_double), vp]
         L.sdvg_probe_mfma_changing.restype = ctypes.c_int
@@ -171,7 +183,7 @@ def lib():
 class _PythonOnly:
     """Stands in for the marshalling module where it has not been built: Python handles every call."""
     block_attn = rope = route = batch = commit = rollback = snapshot = staticmethod(lambda *args: None)
-    page_plan = rope_positions = paged_commit = paged_attn = paged_prefix_attn = staticmethod(lambda *args: None)
+    page_plan = rope_positions = paged_commit = paged_attn = paged_prefix_attn = sample_tokens = staticmethod(lambda *args: None)
 
 
 _NATIVE = None
@@ -194,7 +206,7 @@ def _bind_native(L):
              (L.sdvg_block_attn, L.sdvg_block_attn_commit, L.sdvg_rope, L.sdvg_worst_frame_route, L.sdvg_avg_frame_route,
               L.sdvg_block_attn_batch, L.sdvg_block_attn_batch_static, L.sdvg_kv_commit, L.sdvg_kv_commit_rope,
               L.sdvg_kv_rollback, L.sdvg_buffer_snapshot, L.sdvg_page_plan, L.sdvg_rope_positions, L.sdvg_paged_commit,
-              L.sdvg_paged_attn, L.sdvg_paged_prefix_attn)]
+              L.sdvg_paged_attn, L.sdvg_paged_prefix_attn, L.sdvg_sample_tokens)]
     module.init(*entry, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, np.float32, sdvg_kv_cache, sdvg_paged_kv)
     _NATIVE = module
 
@@ -920,6 +932,64 @@ def paged_prefix_attn(q, cache, block_table, q_start, kv_lens, prefix_lens, grou
                                       0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_ptr(stream))
     if st != 0:
         raise SdvgError(st, "sdvg_paged_prefix_attn")
+    return out
+
+
+def sample_tokens_workspace_bytes(n_rows, vocab):
+    """sdvg_sample_tokens_workspace_bytes: for logits [n_rows, vocab] of any type."""
+    n_rows, vocab = _int32("n_rows", n_rows), _int32("vocab", vocab)
+    n = lib().sdvg_sample_tokens_workspace_bytes(n_rows, vocab)
+    if n < 0:
+        raise SdvgError(n, "sdvg_sample_tokens_workspace_bytes")
+    return int(n)
+
+
+def _setting(name, x, dtype, n, off):
+    """A setting of sample_tokens: one per row, as an array, or one number for all (None: off)."""
+    if isinstance(x, torch.Tensor):
+        if x.dtype != dtype or x.shape != (n,) or not x.is_contiguous():
+            raise ValueError("%s must be a number or dense %s [rows]" % (name, str(dtype)[6:]))
+        return x, off
+    return None, off if x is None else _int32(name, x) if dtype == torch.int32 else float(x)
+
+
+def sample_tokens(logits, u, temperature=1.0, top_k=None, top_p=None, min_p=None, out=None, logprob=None, workspace=None, stream=None):
+    """sdvg_sample_tokens: a token for every row of logits [rows, vocab] (float32, bfloat16 or float16), from the random numbers u
+    float32 [rows] in [0, 1). temperature, top_p, min_p (float32) and top_k (int32): an array [rows] each, or a number for all rows, or
+    None (off); temperature 0 takes the largest logit. `logprob`: optional float32 [rows] for the log of the drawn token's probability among
+    the kept ones. `workspace`: device tensor of sample_tokens_workspace_bytes; None makes one for the call. out defaults to a new
+    int32 tensor [rows]. Returns out."""
+    r = (_NATIVE or _native()).sample_tokens(logits, u, temperature, top_k, top_p, min_p, out, logprob, workspace,
+                                            None if stream is None else stream.cuda_stream)
+    if r is not None:
+        if type(r) is int:
+            raise SdvgError(r, "sdvg_sample_tokens")
+        return r
+    arrays = [x for x in (temperature, top_k, top_p, min_p) if isinstance(x, torch.Tensor)]
+    _check_here(logits, u, out, logprob, workspace, *arrays)
+    if logits.dtype not in _ROW_TYPES or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be float32, bfloat16 or float16 [rows, vocab] with unit stride along the vocabulary")
+    n, vocab = logits.shape
+    if u.dtype != torch.float32 or u.shape != (n,) or not u.is_contiguous():
+        raise ValueError("u must be dense float32 [rows]")
+    (t, all_t), (k, all_k) = _setting("temperature", temperature, torch.float32, n, 1.0), _setting("top_k", top_k, torch.int32, n, 0)
+    (p, all_p), (m, all_m) = _setting("top_p", top_p, torch.float32, n, 1.0), _setting("min_p", min_p, torch.float32, n, 0.0)
+    if out is not None and (out.dtype != torch.int32 or out.shape != (n,) or not out.is_contiguous()):
+        raise ValueError("out must be dense int32 [rows]")
+    if logprob is not None and (logprob.dtype != torch.float32 or logprob.shape != (n,) or not logprob.is_contiguous()):
+        raise ValueError("logprob must be dense float32 [rows]")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    if workspace is None:
+        workspace = _empty((sample_tokens_workspace_bytes(n, vocab),), torch.uint8, logits.device, stream)
+    if out is None:
+        out = _empty((n,), torch.int32, logits.device, stream)
+    a = sdvg_sample_args(logits.data_ptr(), u.data_ptr(), t.data_ptr() if t is not None else None, k.data_ptr() if k is not None else None,
+                         p.data_ptr() if p is not None else None, m.data_ptr() if m is not None else None, all_t, all_k, all_p, all_m,
+                         out.data_ptr(), logprob.data_ptr() if logprob is not None else None, logits.stride(0), n, vocab, _ROW_TYPES[logits.dtype])
+    st = lib().sdvg_sample_tokens(ctypes.byref(a), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+    if st != 0:
+        raise SdvgError(st, "sdvg_sample_tokens")
     return out
 
 

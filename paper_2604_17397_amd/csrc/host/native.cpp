@@ -48,6 +48,7 @@ using paged_attn_fn = int (*)(const sdvg_paged_attn_desc *, const sdvg_paged_kv 
                               const int32_t *, void *, float *, void *, int64_t, void *);
 using paged_prefix_attn_fn = int (*)(const sdvg_paged_attn_desc *, const sdvg_paged_kv *, const void *, const int32_t *, const int32_t *,
                                      const int32_t *, int32_t, const int32_t *, const int32_t *, void *, float *, void *, int64_t, void *);
+using sample_tokens_fn = int (*)(const sdvg_sample_args *, void *, int64_t, void *);
 
 // Entry points of the libsdvg that binding.py has loaded, and torch's current-stream functions.
 struct Api {
@@ -66,6 +67,7 @@ struct Api {
   paged_commit_fn paged_commit = nullptr;
   paged_attn_fn paged_attn = nullptr;
   paged_prefix_attn_fn paged_prefix_attn = nullptr;
+  sample_tokens_fn sample_tokens = nullptr;
   PyObject *get_device = nullptr, *get_raw_stream = nullptr, *float32 = nullptr, *cache_type = nullptr, *paged_type = nullptr;
 } api;
 
@@ -646,6 +648,74 @@ PyObject *paged_attn_impl(PyObject *const *a, Py_ssize_t n_args) {
   return result(status, a[6], out);
 }
 
+// A setting of sample_tokens: an array [n] or a number for all rows (None: `all` stays as it is).
+bool setting(PyObject *o, int64_t n, int64_t device, const float *&p, float &all) {
+  if (o == Py_None) return true;
+  if (PyFloat_CheckExact(o)) {
+    all = static_cast<float>(PyFloat_AS_DOUBLE(o));
+    return true;
+  }
+  const at::Tensor *t = array(o, at::kFloat, n, device);
+  if (t) p = static_cast<const float *>(t->data_ptr());
+  return t;
+}
+bool setting(PyObject *o, int64_t n, int64_t device, const int32_t *&p, int32_t &all) {
+  if (o == Py_None) return true;
+  int64_t v;
+  if (PyLong_CheckExact(o)) {
+    if (!integer(o, v) || v != static_cast<int32_t>(v)) return false;
+    all = static_cast<int32_t>(v);
+    return true;
+  }
+  return optional_array(o, n, device, p);
+}
+
+// (logits, u, temperature, top_k, top_p, min_p, out, logprob, workspace, stream) -> out, a negative status, or None
+PyObject *sample_tokens_impl(PyObject *const *a, Py_ssize_t n_args) {
+  if (n_args != 10) PYTHON_TAKES_OVER;
+  int64_t device;
+  void *stream;
+  if (!launch_place(a[9], device, stream)) PYTHON_TAKES_OVER;
+  const at::Tensor *x = gpu_tensor(a[0]), *ws = gpu_tensor(a[8]);
+  if (!x || x->dim() != 2 || x->get_device() != device || type_of(*x) < 0 || x->size(0) < 1 || x->size(0) > INT32_MAX || x->size(1) < 1 ||
+      x->size(1) > INT32_MAX || (x->size(1) > 1 && x->stride(1) != 1) || !ws || !ws->is_contiguous() || ws->get_device() != device)
+    PYTHON_TAKES_OVER;
+  const int64_t n = x->size(0);
+  sdvg_sample_args s{};
+  s.all_temperature = s.all_top_p = 1.0f;
+  const at::Tensor *u = array(a[1], at::kFloat, n, device);
+  if (!u || !setting(a[2], n, device, s.temperature, s.all_temperature) || !setting(a[3], n, device, s.top_k, s.all_top_k) ||
+      !setting(a[4], n, device, s.top_p, s.all_top_p) || !setting(a[5], n, device, s.min_p, s.all_min_p))
+    PYTHON_TAKES_OVER;
+  const at::Tensor *lp = a[7] == Py_None ? nullptr : array(a[7], at::kFloat, n, device);
+  if (a[7] != Py_None && !lp) PYTHON_TAKES_OVER;
+  at::Tensor out;
+  if (a[6] == Py_None) {
+    const StreamGuard guard(a[9], x->device(), stream);
+    out = at::empty({n}, at::TensorOptions().dtype(at::kInt).device(x->device()));
+    if (out.unsafeGetTensorImpl()->is_python_dispatch()) PYTHON_TAKES_OVER;
+  } else {
+    const at::Tensor *t = array(a[6], at::kInt, n, device);
+    if (!t) PYTHON_TAKES_OVER;
+    out = *t;
+  }
+  s.logits = x->data_ptr();
+  s.u = static_cast<const float *>(u->data_ptr());
+  s.tokens = static_cast<int32_t *>(out.data_ptr());
+  s.logprob = lp ? static_cast<float *>(lp->data_ptr()) : nullptr;
+  s.row_stride = x->stride(0);
+  s.n_rows = static_cast<int32_t>(n);
+  s.vocab = static_cast<int32_t>(x->size(1));
+  s.dtype = type_of(*x);
+  void *const wp = ws->data_ptr();
+  const int64_t w_bytes = static_cast<int64_t>(ws->nbytes());
+  int status;
+  Py_BEGIN_ALLOW_THREADS
+  status = api.sample_tokens(&s, wp, w_bytes, stream);
+  Py_END_ALLOW_THREADS
+  return result(status, a[6], out);
+}
+
 // Anything torch throws (a tensor without storage, ...) happens before the launch: Python repeats
 // the call and reports it its own way.
 template <PyObject *(*F)(PyObject *const *, Py_ssize_t)>
@@ -659,13 +729,13 @@ PyObject *guarded(PyObject *, PyObject *const *args, Py_ssize_t n) {
 }
 
 // (addresses of attn, attn_commit, rope, route_min, route_mean, batch, batch_static, commit, commit_rope, rollback,
-// snapshot, page_plan, rope_positions, paged_commit, paged_attn, paged_prefix_attn; torch._C._cuda_getDevice,
+// snapshot, page_plan, rope_positions, paged_commit, paged_attn, paged_prefix_attn, sample_tokens; torch._C._cuda_getDevice,
 // torch._C._cuda_getCurrentRawStream, numpy.float32, the ctypes classes of the cache and of the paged cache)
 PyObject *init(PyObject *, PyObject *const *a, Py_ssize_t n) {
-  constexpr int kEntries = 16;
+  constexpr int kEntries = 17;
   int64_t p[kEntries];
   if (n != kEntries + 5) {
-    PyErr_SetString(PyExc_TypeError, "init takes 21 arguments");
+    PyErr_SetString(PyExc_TypeError, "init takes 22 arguments");
     return nullptr;
   }
   for (int i = 0; i < kEntries; ++i)
@@ -679,7 +749,8 @@ PyObject *init(PyObject *, PyObject *const *a, Py_ssize_t n) {
             reinterpret_cast<batch_static_fn>(p[6]), reinterpret_cast<commit_fn>(p[7]),  reinterpret_cast<commit_rope_fn>(p[8]),
             reinterpret_cast<rollback_fn>(p[9]), reinterpret_cast<snapshot_fn>(p[10]),   reinterpret_cast<page_plan_fn>(p[11]),
             reinterpret_cast<rope_positions_fn>(p[12]), reinterpret_cast<paged_commit_fn>(p[13]),
-            reinterpret_cast<paged_attn_fn>(p[14]), reinterpret_cast<paged_prefix_attn_fn>(p[15]), a[16], a[17], a[18], a[19], a[20]};
+            reinterpret_cast<paged_attn_fn>(p[14]), reinterpret_cast<paged_prefix_attn_fn>(p[15]),
+            reinterpret_cast<sample_tokens_fn>(p[16]), a[17], a[18], a[19], a[20], a[21]};
   Py_RETURN_NONE;
 }
 
@@ -691,7 +762,7 @@ PyMethodDef methods[] = {METHOD("init", init), METHOD("block_attn", guarded<bloc
                          METHOD("rollback", guarded<rollback_impl>), METHOD("snapshot", guarded<snapshot_impl>),
                          METHOD("page_plan", guarded<page_plan_impl>), METHOD("rope_positions", guarded<rope_positions_impl>),
                          METHOD("paged_commit", guarded<paged_commit_impl>), METHOD("paged_attn", guarded<paged_attn_impl<false>>),
-                         METHOD("paged_prefix_attn", guarded<paged_attn_impl<true>>),
+                         METHOD("paged_prefix_attn", guarded<paged_attn_impl<true>>), METHOD("sample_tokens", guarded<sample_tokens_impl>),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", "Argument marshalling of libsdvg's most frequent calls.",
                           -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -52,7 +52,7 @@ def main():
     rt = subprocess.run([clang, "-print-file-name=libclang_rt.asan-x86_64.so"], stdout=subprocess.PIPE,
                         text=True).stdout.strip()
     env = dict(base, SDVG_LIBRARY=lib, LD_PRELOAD=rt)
-    rc |= run([sys.executable, "-m", "pytest", "-x", "-q", "tests/test_abi.py", "tests/test_paged_abi.py", "tests/test_paged_prefix_host.py"], env)
+    rc |= run([sys.executable, "-m", "pytest", "-x", "-q", "tests/test_abi.py", "tests/test_paged_abi.py", "tests/test_paged_prefix_host.py", "tests/test_sample_host.py"], env)
     # (3) the host programs over the kernels' index headers
     for name in ("attn_index_replay", "attn_groups_replay", "attn_rows32_replay", "attn_rows32_halves", "attn_split_check",
                  "row_map_check", "paged_attn_plan", "paged_prefix_items"):

@@ -1,0 +1,315 @@
+"""sdvg_sample_tokens against its definition in 64 bits: the same tokens, and log-probabilities that have the weights' rounding (2^-35 of
+each, so of their total) and that of the result to 32 bits, 2^-24 of the value."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from sample_util import draw
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def check(x, u, temperature=1.0, top_k=None, top_p=None, min_p=None, **kw):
+    """x [rows, vocab] on the GPU; settings as numbers or lists, one per row."""
+    import paper_2604_17397_amd as P
+    n = x.shape[0]
+    u = torch.tensor(u, dtype=torch.float32, device="cuda")
+
+    def arg(v, dtype):
+        return torch.tensor(v, dtype=dtype, device="cuda") if isinstance(v, list) else v
+
+    def of(v, r, off):
+        return off if v is None else v[r] if isinstance(v, list) else v
+    lp = torch.full((n,), 77.0, device="cuda")
+    got = P.sample_tokens(x, u, arg(temperature, torch.float32), arg(top_k, torch.int32), arg(top_p, torch.float32),
+                          arg(min_p, torch.float32), logprob=lp, **kw)
+    torch.cuda.synchronize()
+    host, f = x.double().cpu().numpy(), np.float32
+    for r in range(n):
+        token, want = draw(host[r], u[r].item(), float(f(of(temperature, r, 1.0))), of(top_k, r, 0), float(f(of(top_p, r, 1.0))),
+                           float(f(of(min_p, r, 0.0))))
+        assert got[r].item() == token, (r, got[r].item(), token)
+        if math.isnan(want):
+            assert math.isnan(lp[r].item())
+        else:
+            assert abs(lp[r].item() - want) <= 2.0**-24 * abs(want) * (1 + 2.0**-20) + 2.0**-34, (r, lp[r].item(), want)
+    return got
+
+
+def rows(n, vocab, kind, seed=1, steep=1.2, spread=0.5):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    u = torch.rand((n, vocab), generator=gen, device="cuda")
+    x = -steep * torch.log1p(u * vocab) + spread * torch.randn((n, vocab), generator=gen, device="cuda") + 8
+    return x.to(DT[kind]), torch.rand(n, generator=gen, device="cuda").tolist()
+
+
+FILTERS = {
+    "none": {}, "k": dict(top_k=40), "p": dict(top_p=0.9), "m": dict(min_p=0.05), "k one": dict(top_k=1), "p low": dict(top_p=0.01),
+    "all": dict(top_k=300, top_p=0.95, min_p=0.001), "k p": dict(top_k=900, top_p=0.5), "p m": dict(top_p=0.999, min_p=0.0001),
+    "wide": dict(top_p=0.99999), "cold": dict(temperature=0.1, top_p=0.9), "hot": dict(temperature=30.0, top_k=5000, top_p=0.97, min_p=0.3),
+    "greedy": dict(temperature=0.0, top_k=5),
+}
+
+
+@pytest.mark.parametrize("kind", list(DT))
+@pytest.mark.parametrize("filters", list(FILTERS))
+@pytest.mark.parametrize("n,vocab", [(3, 1), (5, 2), (9, 7), (4, 8), (4, 9), (7, 1000), (2, 2041), (3, 2048), (3, 2049), (5, 8191), (1, 32000),
+                                     (70, 4099), (2, 100003), (1, 262144)])
+def test_sizes_types_and_filters(kind, filters, n, vocab):
+    x, u = rows(n, vocab, kind, seed=vocab)
+    check(x, u, **FILTERS[filters])
+
+
+@pytest.mark.parametrize("kind", list(DT))
+def test_settings_of_every_row(kind):
+    n, vocab = 120, 5003
+    x, u = rows(n, vocab, kind, seed=5)
+    rng = np.random.default_rng(3)
+    f = lambda lo, hi: [float(np.float32(v)) for v in rng.uniform(lo, hi, n)]  # noqa: E731
+    t, p, m = f(0.3, 2.0), f(0.1, 1.1), f(-0.02, 0.05)
+    k = [int(v) for v in rng.integers(-3, 6000, n)]
+    for r in range(0, n, 7):
+        t[r] = 0.0
+    for r in range(1, n, 5):
+        p[r], k[r] = 1.0, 0
+    for r in range(1, n, 10):
+        m[r] = 0.0
+    check(x, u, t, k, p, m)
+    check(x, u, t, 50, p, None)
+    check(x, u, 0.7, k, 0.8, m)
+
+
+def test_odd_settings():
+    x, _ = rows(12, 3000, "f32", seed=9)
+    u = [0.3] * 12
+    nan, inf = math.nan, math.inf
+    want = check(x, u)
+    for kw in [dict(top_k=0), dict(top_k=-5), dict(top_k=3000), dict(top_k=2**31 - 1), dict(top_p=1.0), dict(top_p=inf), dict(min_p=0.0),
+               dict(min_p=-inf), dict(top_k=[-2**31] * 12), dict(top_p=[2.0] * 12, min_p=[-1.0] * 12)]:
+        assert torch.equal(check(x, u, **kw), want)
+    import paper_2604_17397_amd as P
+    ut = torch.tensor(u, device="cuda")
+    for kw in [dict(top_p=nan), dict(min_p=nan), dict(top_p=torch.full((12,), nan, device="cuda"))]:
+        assert torch.equal(P.sample_tokens(x, ut, **kw), want)
+    best = x.argmax(1).int()
+    for kw in [dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=nan), dict(temperature=-inf)]:
+        assert torch.equal(P.sample_tokens(x, ut, **kw), best)
+    for kw in [dict(top_p=0.0), dict(top_p=-1.0), dict(min_p=1.0), dict(min_p=7.0), dict(top_k=1), dict(temperature=1e-40), dict(temperature=1e-4, top_p=0.5)]:
+        assert torch.equal(P.sample_tokens(x, ut, **kw), best), kw
+    check(x, u, temperature=1e30)
+    check(x, u, temperature=1e30, top_k=17)
+
+
+@pytest.mark.parametrize("u", [0.0, -0.0, 2.0**-24, 0.5, 1 - 2.0**-24])
+def test_ends_of_the_random_numbers(u):
+    for kind in DT:
+        x, _ = rows(6, 9001, kind, seed=2)
+        for filters in FILTERS.values():
+            check(x, [u] * 6, **filters)
+    import paper_2604_17397_amd as P
+    x, _ = rows(3, 50, "f32")
+    for bad, same in [(math.nan, 0.0), (-3.0, 0.0), (1.0, 1 - 2.0**-24), (math.inf, 1 - 2.0**-24)]:
+        a, b = (P.sample_tokens(x, torch.full((3,), v, device="cuda"), top_p=0.9) for v in (bad, same))
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("kind", list(DT))
+@pytest.mark.parametrize("n", [1, 4, 1000, 4096, 20000, 70001])
+def test_equal_logits(kind, n):
+    """All weights are the same: borders are exact, and the first ones by index are kept. 20000 of one weight are more than are listed."""
+    x = torch.full((6, n), 3.25, device="cuda").to(DT[kind])
+    u = [0.0, 0.25, 0.5, 0.75, 0.625, 1 - 2.0**-24]
+    for kw in [{}, dict(top_k=max(1, n // 2)), dict(top_p=0.5), dict(top_p=0.75, top_k=max(1, n - 1)), dict(min_p=1.0), dict(min_p=1.0, top_p=0.25),
+               dict(temperature=0.0), dict(temperature=7.0, top_p=0.5)]:
+        got = check(x, u, **kw)
+        if not kw:
+            assert got.tolist()[:3] == [0, n // 4, n // 2]
+
+
+@pytest.mark.parametrize("kind", list(DT))
+@pytest.mark.parametrize("steep,spread", [(0.0, 0.02), (0.9, 0.3), (0.0, 0.3)])
+def test_flat_rows(kind, steep, spread):
+    """Bins with more tokens than are listed, or sorted: the row is read again."""
+    for n, vocab in ((2, 262144), (3, 40000)):
+        x, u = rows(n, vocab, kind, seed=4, steep=steep, spread=spread)
+        for kw in [dict(top_p=0.5), dict(top_k=vocab // 3), dict(top_k=vocab // 2, top_p=0.7), dict(top_p=0.9999), dict(min_p=0.5, top_p=0.9),
+                   dict(top_k=vocab - 1, min_p=0.9), dict(top_p=0.3, temperature=0.05)]:
+            check(x, u, **kw)
+
+
+def test_few_values_and_ties_at_the_cuts():
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(1)
+    for levels in (2, 3, 17):
+        x = torch.randint(0, levels, (8, 30011), generator=gen, device="cuda").float() * 0.5
+        u = torch.rand(8, generator=gen, device="cuda").tolist()
+        for kw in [dict(top_k=1), dict(top_k=10000), dict(top_k=20000, top_p=0.875), dict(top_p=0.375), dict(min_p=0.5), dict(top_k=12345, min_p=0.1)]:
+            for kind in DT:
+                check(x.to(DT[kind]), u, **kw)
+
+
+@pytest.mark.parametrize("kind", list(DT))
+def test_numbers_that_are_not_ordinary(kind):
+    import paper_2604_17397_amd as P
+    inf, big = math.inf, torch.finfo(DT[kind]).max
+    vocab = 5000
+    x, u = rows(12, vocab, kind, seed=3)
+    x[0, :] = -inf                                  # nothing to draw
+    x[1, 77] = math.nan
+    x[2, 4000] = inf
+    x[3, [17, 3000]] = inf
+    x[4, :] = -inf
+    x[4, 4999] = -big                               # one token, the lowest number
+    x[5, :] = -big                                  # a mask of the type's lowest value, on everything
+    x[6, torch.arange(vocab, device="cuda") % 3 > 0] = -big
+    x[7, torch.arange(vocab, device="cuda") % 50 > 0] = -inf
+    x[8, 0], x[8, 1] = big, -big
+    x[9, :] = 0.0
+    x[9, ::2] = -0.0
+    x[10, :] = -inf
+    x[10, 0] = math.nan
+    x[11, :] = inf
+    for kw in FILTERS.values():
+        check(x, u, **kw)
+    got = P.sample_tokens(x, torch.tensor(u, device="cuda"), top_p=0.9)
+    assert got[[0, 1, 10]].tolist() == [-1] * 3 and got[2] == 4000 and got[4] == 4999
+
+
+@pytest.mark.parametrize("kind", list(DT))
+@pytest.mark.parametrize("at,pad", [(0, 0), (1, 5), (3, 8), (7, 1), (5, 2)])
+def test_rows_that_begin_anywhere(kind, at, pad):
+    """Slices of wider tensors: a row's first logit at any place of 16 bytes, other numbers around it."""
+    vocab, n = 4500, 6
+    wide = torch.full((n, vocab + at + pad), 60000.0, device="cuda").to(DT[kind])
+    x, u = rows(n, vocab, kind, seed=at)
+    wide[:, at:at + vocab] = x
+    for name in ("none", "all", "greedy", "wide", "m"):
+        check(wide[:, at:at + vocab], u, **FILTERS[name])
+    one = wide[2:3, at:at + vocab]
+    check(one, u[2:3], **FILTERS["all"])
+
+
+def test_given_outputs_workspaces_and_streams():
+    import paper_2604_17397_amd as P
+    x, u = rows(40, 20000, "bf16", seed=6)
+    kw = dict(top_k=500, top_p=0.9, min_p=0.001)
+    want = check(x, u, **kw)
+    ut = torch.tensor(u, device="cuda")
+    need = P.sample_tokens_workspace_bytes(40, 20000)
+    guarded = torch.full((need + 4096,), 201, dtype=torch.uint8, device="cuda")
+    out = torch.full((42,), 5, dtype=torch.int32, device="cuda")
+    assert P.sample_tokens(x, ut, out=out[1:41], workspace=guarded[16:16 + need], **kw).data_ptr() == out[1:].data_ptr()
+    torch.cuda.synchronize()
+    assert torch.equal(out[1:41], want) and out[0] == 5 and out[41] == 5 and (guarded[:16] == 201).all() and (guarded[16 + need:] == 201).all()
+    with pytest.raises(P.SdvgError):
+        P.sample_tokens(x, ut, workspace=guarded[:need - 16], **kw)
+    # two streams at once, each with a workspace of its own
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.zeros(40, dtype=torch.int32, device="cuda") for _ in streams]
+    ws = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(30):
+        for s, o, w in zip(streams, outs, ws):
+            P.sample_tokens(x, ut, out=o, workspace=w, stream=s, **kw)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = P.sample_tokens(x, ut, stream=side, **kw)          # a new output and a workspace of the call's own
+    side.synchronize()
+    assert torch.equal(got, want)
+    e = P.sample_tokens(x[:0], ut[:0], **kw)
+    assert e.shape == (0,) and e.dtype == torch.int32
+
+
+def test_graph_with_other_numbers():
+    """Two captured calls that share a workspace, replayed in turn with other logits, random numbers and settings in the arrays."""
+    import paper_2604_17397_amd as P
+    n, vocab = 16, 30000
+    x, _ = rows(n, vocab, "f16", seed=8)
+    ut = torch.zeros(n, device="cuda")
+    k, p, t = torch.full((n,), 100, dtype=torch.int32, device="cuda"), torch.full((n,), 0.9, device="cuda"), torch.ones(n, device="cuda")
+    lp = torch.zeros(n, device="cuda")
+    ws = torch.empty(P.sample_tokens_workspace_bytes(n, vocab), dtype=torch.uint8, device="cuda")
+    outs = [torch.zeros(n, dtype=torch.int32, device="cuda") for _ in range(2)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        def first():
+            P.sample_tokens(x, ut, t, k, p, out=outs[0], logprob=lp, workspace=ws)
+
+        def second():
+            P.sample_tokens(x, ut, t, out=outs[1], workspace=ws)
+        graphs = []
+        for call in (first, second):
+            call()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                call()
+            graphs.append(g)
+        for seed in range(4):
+            y, u = rows(n, vocab, "f16", seed=20 + seed, steep=0.3 * seed)
+            x.copy_(y)
+            ut.copy_(torch.tensor(u))
+            k.fill_([100, 0, 20000, 1][seed])
+            p.fill_([0.9, 0.99, 0.999, 1.0][seed])
+            t.fill_([1.0, 0.0, 2.0, 0.5][seed])
+            torch.cuda.synchronize()
+            for g, o in zip(graphs, outs):
+                o.fill_(-9)
+                g.replay()
+            torch.cuda.synchronize()
+            w0 = P.sample_tokens(x, ut, t, k, p)
+            w1 = P.sample_tokens(x, ut, t)
+            torch.cuda.synchronize()
+            assert torch.equal(outs[0], w0) and torch.equal(outs[1], w1), seed
+            tt = float(np.float32([1.0, 0.0, 2.0, 0.5][seed]))
+            host = x.double().cpu().numpy()
+            assert [draw(host[r], u_, tt, [100, 0, 20000, 1][seed], float(np.float32([0.9, 0.99, 0.999, 1.0][seed])))[0]
+                    for r, u_ in enumerate(ut.tolist())] == outs[0].tolist()
+
+
+def test_the_largest_vocabulary_and_many_rows():
+    x, u = rows(1, 1 << 20, "f32", seed=1)
+    for name in ("none", "all", "wide", "k"):
+        check(x, u, **FILTERS[name])
+    x, u = rows(3000, 33, "bf16", seed=1)
+    check(x, u, **FILTERS["all"])
+    import paper_2604_17397_amd as P
+    y = torch.randn((40000, 5), device="cuda")
+    ut = torch.rand(40000, device="cuda")
+    w = torch.softmax(y.double(), 1).cumsum(1)
+    got = P.sample_tokens(y, ut)
+    torch.cuda.synchronize()
+    near = ((w - ut.double()[:, None]).abs() < 1e-9).any(1)     # (as near to a border as that: either)
+    assert (got.long() == (w <= ut.double()[:, None] * w[:, -1:]).sum(1))[~near].all() and near.sum() < 3
+
+
+def test_the_same_alone_and_among_others():
+    import paper_2604_17397_amd as P
+    x, u = rows(300, 9000, "f32", seed=12)
+    ut = torch.tensor(u, device="cuda")
+    for kw in (dict(top_p=0.9), dict(), dict(top_k=77, min_p=0.01)):
+        lp = torch.empty(300, device="cuda")
+        got = P.sample_tokens(x, ut, logprob=lp, **kw)
+        for r in (0, 150, 299):
+            one = torch.empty(1, device="cuda")
+            assert torch.equal(P.sample_tokens(x[r:r + 1], ut[r:r + 1], logprob=one, **kw), got[r:r + 1]) and abs(one.item() - lp[r].item()) < 1e-6
+        for _ in range(3):
+            assert torch.equal(P.sample_tokens(x, ut, **kw), got)
+
+
+def test_frequencies():
+    """Over many random numbers the tokens come as often as their probabilities say."""
+    import paper_2604_17397_amd as P
+    x = torch.tensor([[1.0, 3.0, -math.inf, 2.0, 0.0, 2.5]], device="cuda").expand(65536, 6).contiguous()
+    u = (torch.arange(65536, device="cuda").float() + 0.5) / 65536
+    got = P.sample_tokens(x, u, temperature=0.8, top_k=4)
+    torch.cuda.synchronize()
+    w = torch.softmax(torch.tensor([1.0, 3.0, -math.inf, 2.0, -math.inf, 2.5], dtype=torch.float64) / 0.8, 0)
+    count = torch.bincount(got.long().cpu(), minlength=6).double()
+    assert ((count - 65536 * w).abs() <= 1).all()
