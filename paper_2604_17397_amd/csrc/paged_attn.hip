@@ -29,7 +29,9 @@ namespace {
 template <typename T, bool kF8, int NT, int HS>
 __global__ __launch_bounds__(kThreads, kPerUnit) void paged_attn_kernel(FIRST_ARGS, AttnParams p) {
   const First first{q_start, kv_lens, n_requests, n_tokens, group, window, target, capacity, {heads_d, heads_m, heads_s}};
-  attend<T, kF8, NT, HS, false>(first, p, Groups{});
+  __shared__ float o_s[kWaves][kRows][kPad];
+  __shared__ float ml_s[kWaves][kRows][2];
+  attend<T, kF8, NT, HS, false>(first, p, Groups{}, blockIdx.x, o_s, ml_s);
 }
 
 // Joins the pieces of the rows of a split row tile. 32 threads have a row's dims; the 8 sets of them in a workgroup have

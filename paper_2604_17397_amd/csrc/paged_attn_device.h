@@ -45,8 +45,10 @@ struct Groups {
   const int32_t *start, *lens;        // start nullable: one group of all requests
   int32_t n;
   int32_t max_slots, max_shared;      // slots of the requests' own keys, and of the shared ones
-  int32_t shared_target, row_tile;    // how the shared keys are cut (paged_prefix_plan.h)
-  float *part_o, *part_ml;            // their partial results: O [slot][key head][row_tile][128], (m, l) [slot][key head][row_tile][2]
+  int32_t shared_target;              // how the shared keys are cut (paged_prefix_plan.h)
+  int32_t shared_turns, own_turns;    // of blocks
+  sdvg::FastDiv by_heads;             // blocks of the shared keys -> items
+  float *part_o, *part_ml;            // their partial results: O [slot][key head][kSharedRows][128], (m, l) [slot][key head][kSharedRows][2]
 
   __device__ __forceinline__ int32_t first(int g, int32_t n_requests) const { return start ? start[g] : g ? n_requests : 0; }
   // the group that has request r, or -1
@@ -239,18 +241,18 @@ __device__ __forceinline__ bool find(const First &p, const Groups &gr, int x, Fo
 }
 
 // T: type of q, of P and of the output. kF8: the cache holds e4m3 numbers.
+// `block`: number among the workgroups of this kind. o_s, ml_s: LDS.
 template <typename T, bool kF8, int NT, int HS, bool kShared>
-__device__ __forceinline__ void attend(const First &first, const AttnParams &p, const Groups &gr) {
+__device__ __forceinline__ void attend(const First &first, const AttnParams &p, const Groups &gr, uint32_t block, float (*o_s)[kRows][kPad],
+                                       float (*ml_s)[kRows][2]) {
   constexpr int kRowTile = kRows * NT, kKeyWaves = kWaves / HS;
   constexpr int kDims = 128 * kRows * HS / kThreads;   // per thread where the workgroup finishes rows
   constexpr int kBytes = kF8 ? 1 : 2;
-  __shared__ float o_s[kWaves][kRows][kPad];
-  __shared__ float ml_s[kWaves][kRows][2];
   Found f;
   // the key heads of an item are neighbours: together they read whole rows of the cache's tokens
   const int group = first.group, window = first.window;
   const uint32_t heads_d = first.by_heads.d;
-  const int item = first.by_heads.div(blockIdx.x), head0 = (blockIdx.x - item * heads_d) * HS, n_kv_heads = heads_d * HS;
+  const int item = first.by_heads.div(block), head0 = (block - item * heads_d) * HS, n_kv_heads = heads_d * HS;
   if (!find<kRowTile, kKeyWaves, true, kShared>(first, gr, item, f)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
   const int head = head0 + (HS > 1 ? __builtin_amdgcn_readfirstlane(wave / kKeyWaves) : 0);   // (one for the wave: its addresses stay scalar)

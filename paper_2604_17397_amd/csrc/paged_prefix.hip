@@ -83,22 +83,24 @@ __device__ __forceinline__ void barrier_after_lds() {   // (loads may stay on th
 // ---- which part of the shared keys a workgroup has
 struct FoundShared {
   pg::SharedKeys q;
-  int32_t tile, piece, pieces, slot, chunk;   // row tile of the group; slot of its first piece; key tiles of a piece
+  pg::Place at;
+  pg::SharedPieces pieces;
+  int32_t slot, chunk;   // slot of the group's first piece; key tiles of a piece
 };
-__device__ __forceinline__ pg::SharedKeys load_group(const First &p, const Groups &gr, int row_tile, int g) {
+__device__ __forceinline__ pg::SharedKeys load_group(const First &p, const Groups &gr, int g) {
   if (g >= gr.n) return pg::SharedKeys{};
   const int32_t start = pg::clamp(gr.first(g, p.n_requests), 0, p.n_requests), end = pg::clamp(gr.first(g + 1, p.n_requests), start, p.n_requests);
   const int32_t n = gr.lens[g];
-  return pg::shared_of(start, end, p.q_start[start], p.q_start[end], n > 0 ? n : 0, p.n_tokens, p.group, row_tile, p.window, p.capacity);
+  return pg::shared_of(start, end, p.q_start[start], p.q_start[end], n > 0 ? n : 0, p.n_tokens, p.group, p.window, p.capacity);
 }
-// Item number x (kItems), or the slots of group x, of which `tile` and `piece` stay open.
+// Item number x (kItems), or the slots of group x.
 template <bool kItems>
-__device__ __forceinline__ bool find_shared(const First &p, const Groups &gr, int row_tile, int x, FoundShared &f) {
+__device__ __forceinline__ bool find_shared(const First &p, const Groups &gr, int x, FoundShared &f) {
   const int lane = threadIdx.x & 63;
-  const pg::SharedKeys mine0 = load_group(p, gr, row_tile, lane);
+  const pg::SharedKeys mine0 = load_group(p, gr, lane);
   int64_t total = 0, row_tiles = 0;
   for (int b = 0; b < gr.n; b += 64) {
-    const pg::SharedKeys q = b ? load_group(p, gr, row_tile, b + lane) : mine0;
+    const pg::SharedKeys q = b ? load_group(p, gr, b + lane) : mine0;
     const int64_t w = pg::work_of(q);
     row_tiles += wave_total(q.row_tiles);
     total += wave_total(static_cast<int>(w & 0xffff)) + (static_cast<int64_t>(wave_total(static_cast<int>(w >> 16))) << 16);
@@ -106,25 +108,19 @@ __device__ __forceinline__ bool find_shared(const First &p, const Groups &gr, in
   f.chunk = pg::shared_chunk(total, row_tiles, gr.shared_target);
   int before = 0;
   for (int b = 0; b < gr.n; b += 64) {
-    const pg::SharedKeys q = b ? load_group(p, gr, row_tile, b + lane) : mine0;
-    const int32_t pieces = pg::shared_pieces(q, f.chunk), mine = q.row_tiles * pieces;
+    const pg::SharedKeys q = b ? load_group(p, gr, b + lane) : mine0;
+    const pg::SharedPieces n = pg::shared_pieces(q, f.chunk);
+    const int32_t mine = pg::shared_items(q, n);
     const int upto = scan(mine), at = x - before - (upto - mine);
     const uint64_t hit = __ballot(kItems ? at >= 0 && at < mine : b + lane == x);
     if (hit) {
       const int src = __ffsll(static_cast<unsigned long long>(hit)) - 1;
       const auto get = [src](int v) { return __builtin_amdgcn_readlane(v, src); };
-      f.q = pg::SharedKeys{get(q.request0), get(q.requests), get(q.token0), get(q.tokens), get(q.lo), get(q.hi), get(q.first_tile), get(q.tiles), get(q.row_tiles)};
-      f.pieces = get(pieces);
-      const int32_t slot0 = before + get(upto - mine);
-      if constexpr (kItems) {
-        const pg::Place place = pg::shared_place(f.q, get(at));
-        f.tile = place.tile;
-        f.piece = place.piece;
-        f.slot = slot0 + f.tile * f.pieces;
-        return f.slot >= 0 && f.slot <= gr.max_shared - f.pieces;
-      }
-      f.slot = slot0;
-      return slot0 >= 0 && slot0 <= gr.max_shared - f.q.row_tiles * f.pieces;
+      f.q = pg::SharedKeys{get(q.request0), get(q.requests), get(q.token0), get(q.tokens), get(q.lo), get(q.hi), get(q.first_tile), get(q.tiles), get(q.row_tiles), get(q.half)};
+      f.pieces = pg::SharedPieces{get(n.whole), get(n.half)};
+      f.slot = before + get(upto - mine);
+      if constexpr (kItems) f.at = pg::shared_place(f.q, f.pieces, get(at));
+      return f.slot >= 0 && f.slot <= gr.max_shared - get(mine);
     }
     before += __builtin_amdgcn_readlane(upto, 63);
   }
@@ -147,17 +143,18 @@ __device__ __forceinline__ void seen_by(const First &p, const FoundShared &f, in
   from = p.window > 0 && sees > p.window ? sees - p.window : 0;
 }
 
-// RW: waves with 32 rows each; the 4 / RW sets of them have 64 / (4 / RW) keys of a tile each.
-template <typename T, bool kF8, int RW>
-__global__ __launch_bounds__(kSharedThreads, 2) void paged_shared_kernel(First first, Groups gr, AttnParams p) {
-  constexpr int kRowTile = 32 * RW, kSets = kSharedWaves / RW, kHalves = 2 / kSets, kBytes = kF8 ? 1 : 2;
-  __shared__ __attribute__((aligned(16))) char lds[4 * kTileBytes];   // K and V of two tiles
+// The shared keys of a row tile. Its waves have 32 rows each; where that leaves two of them without, two sets of two waves have the same rows
+// and half of every key tile each.
+template <typename T, bool kF8>
+__device__ __forceinline__ void attend_shared(const First &first, const Groups &gr, const AttnParams &p, uint32_t block, char *lds) {
+  constexpr int kRowTile = pg::kSharedRows, kBytes = kF8 ? 1 : 2;
   FoundShared f;
-  const int item = first.by_heads.div(blockIdx.x), head = blockIdx.x - item * first.by_heads.d;
-  if (!find_shared<true>(first, gr, kRowTile, item, f)) return;
+  const int item = gr.by_heads.div(block), head = block - item * gr.by_heads.d;
+  if (!find_shared<true>(first, gr, item, f)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, hh = lane >> 5;
-  const int rw = wave % RW, set = wave / RW;
-  const int left = f.q.tokens * first.group - f.tile * kRowTile, rows = left < kRowTile ? left : kRowTile;
+  const int left = f.q.tokens * first.group - f.at.tile * kRowTile, rows = left < kRowTile ? left : kRowTile;
+  const bool half = pg::is_half(f.q, f.at.tile);
+  const int rw = half ? wave & 1 : wave, set = wave >> 1;
   const int row = rw * 32 + col;
   const bool any_row = rw * 32 < rows;
 
@@ -167,7 +164,7 @@ __global__ __launch_bounds__(kSharedThreads, 2) void paged_shared_kernel(First f
   for (int s = 0; s < 8; ++s) qf[s] = u32x4{0, 0, 0, 0};
   int from = 0, sees = INT32_MAX;
   {
-    const uint32_t all = f.tile * kRowTile + (row < rows ? row : rows - 1), i = p.to.by_group.div(all), h = all - i * first.group;
+    const uint32_t all = f.at.tile * kRowTile + (row < rows ? row : rows - 1), i = p.to.by_group.div(all), h = all - i * first.group;
     int a, b;
     seen_by(first, f, f.q.token0 + static_cast<int>(i), a, b);
     if (row < rows) {
@@ -201,7 +198,14 @@ __global__ __launch_bounds__(kSharedThreads, 2) void paged_shared_kernel(First f
     hi = __builtin_amdgcn_readfirstlane(hi < f.q.hi ? hi : f.q.hi);
   }
 
-  const float scale = p.scale_log2e * (kF8 && p.k_scale ? p.k_scale[head] : 1.0f);
+  // (scores are compared ahead of their scale, which is positive then; -infinity times 0 would be no number)
+  float scale = p.scale_log2e * (kF8 && p.k_scale ? p.k_scale[head] : 1.0f);
+  if (scale < 0.f) {
+    scale = -scale;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) qf[s] ^= 0x80008000u;
+  }
+  scale = fmaxf(scale, 0x1p-126f);
   f32x16 o[4];
 #pragma unroll
   for (int d = 0; d < 4; ++d)
@@ -209,7 +213,7 @@ __global__ __launch_bounds__(kSharedThreads, 2) void paged_shared_kernel(First f
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
   float m = -INFINITY, l = 0.f;
 
-  const pg::KeyTiles keys = pg::shared_tiles_of(f.q, f.piece, f.chunk);
+  const pg::KeyTiles keys = pg::shared_tiles_of(f.q, f.at, f.chunk);
   const int begin = keys.begin > lo / pg::kSharedTile ? keys.begin : lo / pg::kSharedTile;
   const int last = hi > 0 ? (hi - 1) / pg::kSharedTile + 1 : 0, end = keys.end < last ? keys.end : last;
   const int32_t *table = p.table + static_cast<int64_t>(f.q.request0) * p.table_stride;
@@ -311,31 +315,26 @@ __global__ __launch_bounds__(kSharedThreads, 2) void paged_shared_kernel(First f
         }
         barrier_after_lds();
       }
-      if (any_row) {
-#pragma unroll
-        for (int half = 0; half < kHalves; ++half) {
-          const int kb = kSets == 2 ? set : half;
-          const char *const k_tile = lds + slot * (2 * kTileBytes), *const v_tile = k_tile + kTileBytes;
+      const char *const k_tile = lds + slot * (2 * kTileBytes), *const v_tile = k_tile + kTileBytes;
+      const auto take = [&](int kb) {   // 32 keys of the tile
           f32x16 s;
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
           for (int c = 0; c < 8; ++c) s = mfma32<T>(*reinterpret_cast<const u32x4 *>(k_tile + ai::k_read_offset(lane, c, kb)), qf[c], s);
-          float x[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) x[i] = s[i] * scale;
           const int first_key = key0 + 32 * kb;
           if (special || first_key + 32 > all_sees || first_key < all_from) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const int key = first_key + 8 * (i >> 2) + 4 * hh + (i & 3);
               const bool ok = ((valid >> (4 * kb + (i >> 2))) & 1) && key >= lo && key < hi && key >= from && key < sees;
-              x[i] = ok ? x[i] : -INFINITY;
+              s[i] = ok ? s[i] : -INFINITY;
             }
           }
-          float high = x[0];
+          float high = s[0];
 #pragma unroll
-          for (int i = 1; i < 16; ++i) high = fmaxf(high, x[i]);
+          for (int i = 1; i < 16; ++i) high = fmaxf(high, s[i]);
+          high *= scale;
           // m is raised only when some row's scores pass it by more than kSlack
           if (__any(high > m + T::kSlack)) {
             const float top = fmaxf(m, pair_max(high));
@@ -345,11 +344,11 @@ __global__ __launch_bounds__(kSharedThreads, 2) void paged_shared_kernel(First f
 #pragma unroll
             for (int d = 0; d < 4; ++d) o[d] *= keep;
           }
-          const float base = m == -INFINITY ? 0.f : m - T::kShift;
+          const float base = m == -INFINITY ? 0.f : T::kShift - m;
           u32x4 pf[2], rest[2];   // probabilities in 16 bits, and what is left of them
 #pragma unroll
           for (int c = 0; c < 8; ++c) {
-            const float a = exp2_of(x[2 * c] - base), b = exp2_of(x[2 * c + 1] - base);
+            const float a = exp2_of(fmaf(s[2 * c], scale, base)), b = exp2_of(fmaf(s[2 * c + 1], scale, base));
             const unsigned w = T::pack(a, b);
             pf[c >> 2][c & 3] = w;
             rest[c >> 2][c & 3] = T::pack(a - T::first(w), b - T::second(w));
@@ -365,7 +364,10 @@ __global__ __launch_bounds__(kSharedThreads, 2) void paged_shared_kernel(First f
               const u32x4 vt = {a2[0], a2[1], b2[0], b2[1]};
               o[d] = mfma32<T>(vt, pf[j], mfma32<T>(vt, rest[j], o[d]));
             }
-        }
+      };
+      if (any_row) {
+#pragma unroll 1
+        for (int kb = half ? set : 0; kb < (half ? set + 1 : 2); ++kb) take(kb);
       }
       valid = valid_next;
     }
@@ -373,9 +375,9 @@ __global__ __launch_bounds__(kSharedThreads, 2) void paged_shared_kernel(First f
 
   // the sets' results meet
   l = pair_sum(l) * T::kUnit;
-  if constexpr (kSets == 2) {
+  if (half) {
     __syncthreads();
-    float *const os = reinterpret_cast<float *>(lds) + rw * 64 * 64, *const ml = reinterpret_cast<float *>(lds) + RW * 64 * 64 + rw * 128;
+    float *const os = reinterpret_cast<float *>(lds) + rw * 64 * 64, *const ml = reinterpret_cast<float *>(lds) + 2 * 64 * 64 + rw * 128;
     if (set == 1) {
 #pragma unroll
       for (int d = 0; d < 4; ++d)
@@ -396,7 +398,7 @@ __global__ __launch_bounds__(kSharedThreads, 2) void paged_shared_kernel(First f
       for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * mine + os[(16 * d + i) * 64 + lane] * theirs;
   }
   if (row >= rows) return;
-  const int64_t at = (static_cast<int64_t>(f.slot + f.piece) * first.by_heads.d + head) * kRowTile + row;
+  const int64_t at = (static_cast<int64_t>(f.slot + f.at.tile * f.pieces.whole + f.at.piece) * gr.by_heads.d + head) * kRowTile + row;
   float *const dst = gr.part_o + at * 128 + 4 * hh;
 #pragma unroll
   for (int d = 0; d < 4; ++d)
@@ -406,38 +408,52 @@ __global__ __launch_bounds__(kSharedThreads, 2) void paged_shared_kernel(First f
   if (hh == 0) *reinterpret_cast<f32x2 *>(gr.part_ml + at * 2) = f32x2{m, l};
 }
 
-// The keys behind the shared ones.
+// Both kinds of workgroups: those that wait for memory and those that keep the matrix cores busy run side by side.
 template <typename T, bool kF8, int NT, int HS>
-__global__ __launch_bounds__(kThreads, kPerUnit) void paged_own_kernel(FIRST_ARGS, AttnParams p, Groups gr) {
+__global__ __launch_bounds__(kThreads, kPerUnit) void paged_prefix_kernel(FIRST_ARGS, Groups gr, AttnParams p) {
+  static_assert(kThreads == kSharedThreads && sizeof(float) * kWaves * kRows * (kPad + 2) <= 4 * kTileBytes, "LDS of both kinds");
+  __shared__ __attribute__((aligned(16))) char lds[4 * kTileBytes];   // K and V of two tiles
   const First first{q_start, kv_lens, n_requests, n_tokens, group, window, target, capacity, {heads_d, heads_m, heads_s}};
-  attend<T, kF8, NT, HS, true>(first, p, gr);
+  const pg::Turn turn = pg::turn_of(blockIdx.x, gr.shared_turns, gr.own_turns);
+  if (turn.shared) {
+    attend_shared<T, kF8>(first, gr, p, turn.block, lds);
+  } else {
+    float(*const o_s)[kRows][kPad] = reinterpret_cast<float(*)[kRows][kPad]>(lds);
+    attend<T, kF8, NT, HS, true>(first, p, gr, turn.block, o_s, reinterpret_cast<float(*)[kRows][2]>(o_s + kWaves));
+  }
 }
 
-// Joins the pieces of a request's own keys and those of its group's shared ones. 32 threads have a row's dims.
+// Joins the pieces of a request's own keys and those of its group's shared ones. 32 threads have a row's dims; `per` sets of them (1, 2, 4
+// or 8) share the pieces of a row.
 template <typename T, bool kF8, int NT, int HS>
-__global__ __launch_bounds__(kJoinThreads) void paged_shared_join_kernel(First first, OutParams p, Groups gr) {
-  constexpr int kRowTile = kRows * NT, kPerBlock = kJoinThreads / 32;
+__global__ __launch_bounds__(kJoinThreads) void paged_prefix_join_kernel(First first, OutParams p, Groups gr, int per) {
+  constexpr int kRowTile = kRows * NT, kSets = kJoinThreads / 32;
+  __shared__ f32x4 o_s[kSets][32];
+  __shared__ float ml_s[kSets][2];
   Found f;
   const int heads = first.by_heads.d, index = first.by_heads.div(blockIdx.x), head = blockIdx.x - index * heads;
   if (!find<kRowTile, kWaves / HS, false, true>(first, gr, index, f)) return;
   const int left = f.q.n * first.group - f.tile * kRowTile, rows = left < kRowTile ? left : kRowTile;
   FoundShared s{};
   const int g = gr.group_of(f.request, first.n_requests);
-  if (g >= 0) find_shared<false>(first, gr, gr.row_tile, g, s);
-  const int64_t own_step = static_cast<int64_t>(heads) * kRowTile, shared_step = static_cast<int64_t>(heads) * gr.row_tile;
-  const int d4 = threadIdx.x & 31;
-  for (int row = blockIdx.y * kPerBlock + (threadIdx.x >> 5); row < rows; row += gridDim.y * kPerBlock) {
+  if (g >= 0) find_shared<false>(first, gr, g, s);
+  const int64_t own_step = static_cast<int64_t>(heads) * kRowTile, shared_step = static_cast<int64_t>(heads) * pg::kSharedRows;
+  const int d4 = threadIdx.x & 31, set = threadIdx.x >> 5, sub = set % per, at_once = kSets / per;
+  for (int row0 = blockIdx.y * at_once; row0 < rows; row0 += gridDim.y * at_once) {   // (all threads come round as often)
+    const int row = row0 + set / per;
     const uint32_t all = f.tile * kRowTile + row, i = p.by_group.div(all), h = all - i * first.group;
     const int64_t own_at = (static_cast<int64_t>(f.slot) * heads + head) * kRowTile + row;
     // its number among the group's rows
     const int64_t among = (static_cast<int64_t>(f.q.row0) - s.q.token0) * first.group + all;
-    const bool in = among >= 0 && among < static_cast<int64_t>(s.q.tokens) * first.group;
-    const int tile = in ? static_cast<int>(among / gr.row_tile) : 0, shared = in && tile < s.q.row_tiles ? s.pieces : 0;
-    const int64_t shared_at = ((s.slot + static_cast<int64_t>(tile) * s.pieces) * heads + head) * gr.row_tile + (among - static_cast<int64_t>(tile) * gr.row_tile);
+    const bool in = row < rows && among >= 0 && among < static_cast<int64_t>(s.q.tokens) * first.group;
+    const int tile = in ? static_cast<int>(among / pg::kSharedRows) : 0;
+    const int shared = in && tile < s.q.row_tiles ? (pg::is_half(s.q, tile) ? s.pieces.half : s.pieces.whole) : 0;
+    const int64_t shared_at = ((s.slot + static_cast<int64_t>(tile) * s.pieces.whole) * heads + head) * pg::kSharedRows + (among - static_cast<int64_t>(tile) * pg::kSharedRows);
     float top = -INFINITY, total = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    const int pieces = row < rows ? f.pieces + shared : 0;
 #pragma unroll 4
-    for (int j = 0; j < f.pieces + shared; ++j) {
+    for (int j = sub; j < pieces; j += per) {
       const bool own = j < f.pieces;
       const int64_t at = own ? own_at + j * own_step : shared_at + (j - f.pieces) * shared_step;
       const f32x2 ml = *reinterpret_cast<const f32x2 *>((own ? p.part_ml : gr.part_ml) + at * 2);
@@ -448,6 +464,27 @@ __global__ __launch_bounds__(kJoinThreads) void paged_shared_join_kernel(First f
       total = total * keep + ml[1] * weight;
       acc = acc * keep + o * weight;
     }
+    if (per > 1) {
+      __syncthreads();
+      o_s[set][d4] = acc;
+      if (d4 == 0) {
+        ml_s[set][0] = top;
+        ml_s[set][1] = total;
+      }
+      __syncthreads();
+      if (sub == 0) {
+        for (int w = 1; w < per; ++w) top = fmaxf(top, ml_s[set + w][0]);
+        const float base = top == -INFINITY ? 0.f : top;
+        acc = f32x4{0.f, 0.f, 0.f, 0.f};
+        total = 0.f;
+        for (int w = 0; w < per; ++w) {
+          const float weight = exp2_of(ml_s[set + w][0] - base);
+          total += weight * ml_s[set + w][1];
+          acc += weight * o_s[set + w][d4];
+        }
+      }
+    }
+    if (sub != 0 || row >= rows) continue;
     const int64_t token = f.q.row0 + static_cast<int64_t>(i), q_head = static_cast<int64_t>(head) * first.group + h;
     acc *= total == 0.f ? 0.f : T::kUnit * (kF8 && p.v_scale ? p.v_scale[head] : 1.0f) / total;
     const u32x2 w = {T::pack(acc[0], acc[1]), T::pack(acc[2], acc[3])};
@@ -457,61 +494,53 @@ __global__ __launch_bounds__(kJoinThreads) void paged_shared_join_kernel(First f
 }
 
 // ---- host
-struct Layout {              // of the workspace, in rows of 128 + 2 floats
-  int own_tile, sets, target;
-  int shared_tile, shared_target;
-  int64_t own_slots, shared_slots, own_rows, shared_rows;
+struct Layout {              // of the launch, and of the workspace in rows of 128 + 2 floats
+  int own_tile, sets, target, shared_target;
+  int64_t own_items, own_slots, shared_slots, own_rows, shared_rows;
   int64_t bytes() const { return (own_rows + shared_rows) * (128 + 2) * 4; }
 };
-// Rows per workgroup of the shared keys by the average group: 128, or 64 where that is enough, whose keys then are shared by two sets of waves.
 Layout layout_of(int n_cu, const sdvg_paged_attn_desc &d, const sdvg_paged_kv &c, int32_t n_groups) {
   Layout w;
   const int group = d.n_heads / c.n_kv_heads;
   w.own_tile = row_tile_of(d.n_requests, d.n_tokens, group);
   w.sets = head_sets(c, w.own_tile);
   w.target = target_of(n_cu, d, c, w.own_tile);
-  w.shared_tile = (int64_t{d.n_tokens} + n_groups - 1) / n_groups * group <= 64 ? 64 : 128;
   w.shared_target = 2 * n_cu / c.n_kv_heads > 1 ? 2 * n_cu / c.n_kv_heads : 1;
-  w.own_slots = pg::max_slots(w.target) + pg::max_row_tiles(d.n_requests, d.n_tokens, group, w.own_tile);
-  w.shared_slots = pg::max_shared_items(pg::max_shared_row_tiles(n_groups, d.n_tokens, group, w.shared_tile), w.shared_target, capacity_of(d, c));
+  const int64_t tiles = pg::max_row_tiles(d.n_requests, d.n_tokens, group, w.own_tile);
+  w.own_items = pg::max_items(tiles, w.target, capacity_of(d, c), kWaves / w.sets);
+  w.own_slots = pg::max_slots(w.target) + tiles;
+  w.shared_slots = pg::max_shared_items(pg::max_shared_row_tiles(n_groups, d.n_tokens, group), w.shared_target, capacity_of(d, c));
   w.own_rows = w.own_slots * c.n_kv_heads * w.own_tile;
-  w.shared_rows = w.shared_slots * c.n_kv_heads * w.shared_tile;
+  w.shared_rows = w.shared_slots * c.n_kv_heads * pg::kSharedRows;
   return w;
 }
 
 template <typename T, bool kF8, int NT, int HS>
-int launch_own(First f, const AttnParams &p, const Groups &gr, hipStream_t s) {
-  constexpr int kRowTile = kRows * NT, kKeyWaves = kWaves / HS;
-  const int64_t tiles = pg::max_row_tiles(f.n_requests, f.n_tokens, f.group, kRowTile);
-  const int64_t items = pg::max_items(tiles, f.target, f.capacity, kKeyWaves), joins = tiles * f.by_heads.d * HS;
-  hipLaunchKernelGGL((paged_own_kernel<T, kF8, NT, HS>), dim3(static_cast<uint32_t>(items * f.by_heads.d)), dim3(kThreads), 0, s, FIRST(f), p, gr);
+int launch_prefix(First f, const AttnParams &p, const Groups &gr, hipStream_t s) {
+  constexpr int kRowTile = kRows * NT;
+  const dim3 grid(static_cast<uint32_t>(gr.shared_turns + gr.own_turns) * pg::kTurn);
+  hipLaunchKernelGGL((paged_prefix_kernel<T, kF8, NT, HS>), grid, dim3(kThreads), 0, s, FIRST(f), gr, p);
   SDVG_HIP_CHECK(hipGetLastError());
-  f.by_heads = sdvg::FastDiv::of(f.by_heads.d * HS);
+  f.by_heads = gr.by_heads;
+  // the fewer rows, the more sets of threads share a row's pieces
+  const int64_t all_rows = static_cast<int64_t>(f.n_tokens) * f.group * f.by_heads.d;
+  const int per = all_rows <= 1024 ? 8 : all_rows <= 2048 ? 4 : all_rows <= 4096 ? 2 : 1;
   int64_t rows = (static_cast<int64_t>(f.n_tokens) + f.n_requests - 1) / f.n_requests * f.group;
-  rows = ((rows < kRowTile ? rows : kRowTile) + 7) / 8;
-  hipLaunchKernelGGL((paged_shared_join_kernel<T, kF8, NT, HS>), dim3(static_cast<uint32_t>(joins), static_cast<uint32_t>(rows)), dim3(kJoinThreads),
-                     0, s, f, p.to, gr);
+  rows = ((rows < kRowTile ? rows : kRowTile) * per + 7) / 8;
+  const int64_t joins = pg::max_row_tiles(f.n_requests, f.n_tokens, f.group, kRowTile) * f.by_heads.d;
+  hipLaunchKernelGGL((paged_prefix_join_kernel<T, kF8, NT, HS>), dim3(static_cast<uint32_t>(joins), static_cast<uint32_t>(rows)),
+                     dim3(kJoinThreads), 0, s, f, p.to, gr, per);
   SDVG_HIP_CHECK(hipGetLastError());
   return SDVG_OK;
 }
 template <typename T, bool kF8>
-int launch_prefix(const First &f, const AttnParams &p, const Groups &gr, const Layout &w, int n_kv_heads, hipStream_t s) {
-  if (w.shared_slots > 0) {
-    First shared = f;
-    shared.by_heads = sdvg::FastDiv::of(n_kv_heads);
-    const dim3 grid(static_cast<uint32_t>(w.shared_slots * n_kv_heads));
-    if (w.shared_tile == 64)
-      hipLaunchKernelGGL((paged_shared_kernel<T, kF8, 2>), grid, dim3(kSharedThreads), 0, s, shared, gr, p);
-    else
-      hipLaunchKernelGGL((paged_shared_kernel<T, kF8, 4>), grid, dim3(kSharedThreads), 0, s, shared, gr, p);
-    SDVG_HIP_CHECK(hipGetLastError());
-  }
+int launch_prefix(const First &f, const AttnParams &p, const Groups &gr, const Layout &w, hipStream_t s) {
   if (w.sets == 2) {
     if constexpr (kF8)
-      if (w.own_tile == 32) return launch_own<T, kF8, 2, 2>(f, p, gr, s);
-    return launch_own<T, kF8, 1, 2>(f, p, gr, s);
+      if (w.own_tile == 32) return launch_prefix<T, kF8, 2, 2>(f, p, gr, s);
+    return launch_prefix<T, kF8, 1, 2>(f, p, gr, s);
   }
-  return w.own_tile == 16 ? launch_own<T, kF8, 1, 1>(f, p, gr, s) : launch_own<T, kF8, 2, 1>(f, p, gr, s);
+  return w.own_tile == 16 ? launch_prefix<T, kF8, 1, 1>(f, p, gr, s) : launch_prefix<T, kF8, 2, 1>(f, p, gr, s);
 }
 
 }  // namespace
@@ -542,20 +571,20 @@ extern "C" int sdvg_paged_prefix_attn(const sdvg_paged_attn_desc *desc, const sd
   if (n_groups == 0 || !workspace || workspace_bytes < w.bytes())
     return sdvg_paged_attn(desc, cache, q, block_table, q_start, kv_lens, out, lse, workspace, workspace_bytes, stream);
   const int32_t n_kv = cache->n_kv_heads;
-  const int64_t own_items = pg::max_items(pg::max_row_tiles(desc->n_requests, desc->n_tokens, desc->n_heads / n_kv, w.own_tile), w.target,
-                                          capacity_of(*desc, *cache), kWaves / w.sets);
-  if (w.shared_slots * n_kv >= (1 << 23) || own_items * n_kv >= (1 << 23) || w.own_slots * n_kv >= (1 << 23)) return SDVG_ERR_UNSUPPORTED;
+  const int32_t shared_turns = pg::turns_of(w.shared_slots * n_kv), own_turns = pg::turns_of(w.own_items * (n_kv / w.sets));
+  if ((int64_t{shared_turns} + own_turns) * pg::kTurn >= (1 << 23) || w.own_slots * n_kv >= (1 << 23)) return SDVG_ERR_UNSUPPORTED;
   First f = first_of(*desc, *cache, q_start, kv_lens);
   AttnParams p = params_of(*desc, *cache, q, block_table, out, lse);
   f.by_heads = sdvg::FastDiv::of(n_kv / w.sets);
   f.target = w.target;
-  Groups gr{group_start, prefix_lens, n_groups, static_cast<int32_t>(w.own_slots), static_cast<int32_t>(w.shared_slots), w.shared_target, w.shared_tile, nullptr, nullptr};
+  Groups gr{group_start, prefix_lens, n_groups, static_cast<int32_t>(w.own_slots), static_cast<int32_t>(w.shared_slots), w.shared_target,
+            shared_turns, own_turns, sdvg::FastDiv::of(n_kv), nullptr, nullptr};
   p.to.part_o = static_cast<float *>(workspace);
   gr.part_o = p.to.part_o + w.own_rows * 128;
   p.to.part_ml = gr.part_o + w.shared_rows * 128;
   gr.part_ml = p.to.part_ml + w.own_rows * 2;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool f8 = cache->dtype == SDVG_E4M3;
-  if (desc->dtype == SDVG_BF16) return f8 ? launch_prefix<Bf16, true>(f, p, gr, w, n_kv, s) : launch_prefix<Bf16, false>(f, p, gr, w, n_kv, s);
-  return f8 ? launch_prefix<F16, true>(f, p, gr, w, n_kv, s) : launch_prefix<F16, false>(f, p, gr, w, n_kv, s);
+  if (desc->dtype == SDVG_BF16) return f8 ? launch_prefix<Bf16, true>(f, p, gr, w, s) : launch_prefix<Bf16, false>(f, p, gr, w, s);
+  return f8 ? launch_prefix<F16, true>(f, p, gr, w, s) : launch_prefix<F16, false>(f, p, gr, w, s);
 }

@@ -5,6 +5,7 @@
 #include <stdlib.h>
 
 #include <set>
+#include <utility>
 #include <vector>
 
 #include "paged_prefix_plan.h"
@@ -26,7 +27,10 @@ static uint32_t rnd() {
     }                                                                                                                         \
   } while (0)
 
-static void one(int G, int longest, int most_tokens, int group, int row_tile, int window, int target, int64_t capacity) {
+static int tokens_of(const pg::SharedKeys &s, int group) { return s.tokens * group; }
+
+static void one(int G, int longest, int most_tokens, int group, int window, int target, int64_t capacity) {
+  constexpr int row_tile = pg::kSharedRows;
   std::vector<int32_t> token(G + 1), n(G);
   for (int g = 0; g < G; ++g) {
     token[g + 1] = token[g] + rnd() % (most_tokens + 1);
@@ -36,7 +40,7 @@ static void one(int G, int longest, int most_tokens, int group, int row_tile, in
   int64_t total = 0, row_tiles = 0;
   std::vector<pg::SharedKeys> q(G);
   for (int g = 0; g < G; ++g) {
-    q[g] = pg::shared_of(g, g + 1, token[g], token[g + 1], n[g], tokens, group, row_tile, window, capacity);
+    q[g] = pg::shared_of(g, g + 1, token[g], token[g + 1], n[g], tokens, group, window, capacity);
     total += pg::work_of(q[g]);
     row_tiles += q[g].row_tiles;
     CHECK(q[g].token0 == token[g] && q[g].tokens == token[g + 1] - token[g]);
@@ -52,23 +56,26 @@ static void one(int G, int longest, int most_tokens, int group, int row_tile, in
   }
   const int32_t chunk = pg::shared_chunk(total, row_tiles, target);
   CHECK(chunk >= 1);
-  const int64_t most_row_tiles = pg::max_shared_row_tiles(G, tokens, group, row_tile), most = pg::max_shared_items(most_row_tiles, target, capacity);
+  const int64_t most_row_tiles = pg::max_shared_row_tiles(G, tokens, group), most = pg::max_shared_items(most_row_tiles, target, capacity);
   CHECK(row_tiles <= most_row_tiles);
   std::set<int64_t> slots;
   int64_t items = 0;
   for (int g = 0; g < G; ++g) {
-    const int32_t pieces = pg::shared_pieces(q[g], chunk), mine = q[g].row_tiles * pieces;
+    const pg::SharedPieces pieces = pg::shared_pieces(q[g], chunk);
+    const int32_t mine = pg::shared_items(q[g], pieces);
     std::vector<std::vector<int>> seen(q[g].row_tiles, std::vector<int>(q[g].tiles));
     for (int i = 0; i < mine; ++i) {
-      const pg::Place at = pg::shared_place(q[g], i);
-      CHECK(at.tile >= 0 && at.tile < q[g].row_tiles && at.piece >= 0 && at.piece < pieces);
-      const pg::KeyTiles k = pg::shared_tiles_of(q[g], at.piece, chunk);
-      CHECK(k.begin < k.end && k.end - k.begin <= chunk);
+      const pg::Place at = pg::shared_place(q[g], pieces, i);
+      CHECK(at.tile >= 0 && at.tile < q[g].row_tiles && at.piece >= 0 && at.piece < (pg::is_half(q[g], at.tile) ? pieces.half : pieces.whole));
+      const int rows = tokens_of(q[g], group) - at.tile * row_tile;
+      CHECK(pg::is_half(q[g], at.tile) == (rows <= row_tile / 2));
+      const pg::KeyTiles k = pg::shared_tiles_of(q[g], at, chunk);
+      CHECK(k.begin < k.end && k.end - k.begin <= (pg::is_half(q[g], at.tile) ? 2 * chunk : chunk));
       for (int t = k.begin; t < k.end; ++t) {
         CHECK(t >= q[g].first_tile && t < q[g].first_tile + q[g].tiles);
         ++seen[at.tile][t - q[g].first_tile];
       }
-      const int64_t slot = items + int64_t{at.tile} * pieces + at.piece;
+      const int64_t slot = items + int64_t{at.tile} * pieces.whole + at.piece;
       CHECK(slot < most && slots.insert(slot).second);
     }
     for (const auto &row : seen)
@@ -84,16 +91,24 @@ int main() {
     for (int l : longest)
       for (int m : most)
         for (int group : heads)
-          for (int row_tile : {64, 128})
             for (int window : {0, 1, 100, 1 << 20})
               for (int target : {1, 4, 32, 512}) {
                 if (int64_t{G} * l * m > 3000000) continue;
-                one(G, l, m, group, row_tile, window, target, l + 5);
-                one(G, l, m, group, row_tile, window, target, l / 2 + 8);
+                one(G, l, m, group, window, target, l + 5);
+                one(G, l, m, group, window, target, l / 2 + 8);
               }
   // the largest numbers: nothing leaves 64 bits, and what is kept in 32 fits
-  const pg::SharedKeys s = pg::shared_of(0, 1, -5, INT32_MAX, INT32_MAX, 1 << 27, 16, 64, 0, INT32_MAX - 64);
-  if (s.row_tiles != (1 << 25) || s.tiles <= 0 || pg::work_of(s) != (int64_t{1} << 25) * s.tiles || pg::shared_chunk(pg::work_of(s), s.row_tiles, 512) < 1) return 1;
+  const pg::SharedKeys s = pg::shared_of(0, 1, -5, INT32_MAX, INT32_MAX, 1 << 27, 16, 0, INT32_MAX - 64);
+  if (s.row_tiles != (1 << 24) || s.half || s.tiles <= 0 || pg::work_of(s) != (int64_t{1} << 25) * s.tiles || pg::shared_chunk(pg::work_of(s), s.row_tiles, 512) < 1) return 1;
+  // every block of both kinds has its turn, once
+  for (int shared : {0, 1, 2, 5, 40})
+    for (int own : {1, 2, 7, 40}) {
+      std::set<std::pair<bool, int>> turns;
+      for (int b = 0; b < (shared + own) * pg::kTurn; ++b) {
+        const pg::Turn t = pg::turn_of(b, shared, own);
+        if (t.block < 0 || t.block >= (t.shared ? shared : own) * pg::kTurn || t.block % 8 != b % 8 || !turns.insert({t.shared, t.block}).second) return 1;
+      }
+    }
   printf("ok\n");
   return 0;
 }

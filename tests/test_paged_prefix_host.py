@@ -68,4 +68,4 @@ def test_binding_checks(b, monkeypatch):  # noqa: F811
 
 def test_kernels_do_not_spill():
     from test_kernel_resources import test_paged_kernels_do_not_spill as check
-    check("paged_prefix.hip", ("paged_shared_kernel", "paged_own_kernel", "paged_shared_join_kernel"))
+    check("paged_prefix.hip", ("paged_prefix_kernel", "paged_prefix_join_kernel"))
