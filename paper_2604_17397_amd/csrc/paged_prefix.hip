@@ -143,18 +143,14 @@ __device__ __forceinline__ void seen_by(const First &p, const FoundShared &f, in
   from = p.window > 0 && sees > p.window ? sees - p.window : 0;
 }
 
-// The shared keys of a row tile. Its waves have 32 rows each; where that leaves two of them without, two sets of two waves have the same rows
-// and half of every key tile each.
-template <typename T, bool kF8>
-__device__ __forceinline__ void attend_shared(const First &first, const Groups &gr, const AttnParams &p, uint32_t block, char *lds) {
-  constexpr int kRowTile = pg::kSharedRows, kBytes = kF8 ? 1 : 2;
-  FoundShared f;
-  const int item = gr.by_heads.div(block), head = block - item * gr.by_heads.d;
-  if (!find_shared<true>(first, gr, item, f)) return;
+// The shared keys of a row tile. Its waves have 32 rows each; where that leaves two of them without (kHalf), two sets of two waves have the
+// same rows and half of every key tile each.
+template <typename T, bool kF8, bool kHalf>
+__device__ __forceinline__ void attend_shared(const First &first, const Groups &gr, const AttnParams &p, const FoundShared &f, int head, char *lds) {
+  constexpr int kRowTile = pg::kSharedRows, kBytes = kF8 ? 1 : 2, kHalves = kHalf ? 1 : 2;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, hh = lane >> 5;
   const int left = f.q.tokens * first.group - f.at.tile * kRowTile, rows = left < kRowTile ? left : kRowTile;
-  const bool half = pg::is_half(f.q, f.at.tile);
-  const int rw = half ? wave & 1 : wave, set = wave >> 1;
+  const int rw = kHalf ? wave & 1 : wave, set = kHalf ? wave >> 1 : 0;
   const int row = rw * 32 + col;
   const bool any_row = rw * 32 < rows;
 
@@ -315,59 +311,83 @@ __device__ __forceinline__ void attend_shared(const First &first, const Groups &
         }
         barrier_after_lds();
       }
-      const char *const k_tile = lds + slot * (2 * kTileBytes), *const v_tile = k_tile + kTileBytes;
-      const auto take = [&](int kb) {   // 32 keys of the tile
-          f32x16 s;
+      if (any_row) {
+        // (kHalf: this wave's half of the tile, otherwise both)
+        const char *const k_tile = lds + slot * (2 * kTileBytes) + set * (32 * 256), *const v_tile = k_tile + kTileBytes;
+        const auto read_k = [&](int c, int kb) { return *reinterpret_cast<const u32x4 *>(k_tile + ai::k_read_offset(lane, c, kb)); };
+        const auto read_v = [&](int step, int d) {
+          const char *const at = v_tile + ai::v_read_offset(lane, step, d, 0);
+          const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at)),
+                      b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * 256)));
+          return u32x4{a[0], a[1], b[0], b[1]};
+        };
+        f32x16 s[kHalves];
+        u32x4 kf[8], vt[2][4];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        for (int c = 0; c < 8; ++c) kf[c] = read_k(c, 0);
 #pragma unroll
-          for (int c = 0; c < 8; ++c) s = mfma32<T>(*reinterpret_cast<const u32x4 *>(k_tile + ai::k_read_offset(lane, c, kb)), qf[c], s);
-          const int first_key = key0 + 32 * kb;
-          if (special || first_key + 32 > all_sees || first_key < all_from) {
+        for (int kb = 0; kb < kHalves; ++kb) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int key = first_key + 8 * (i >> 2) + 4 * hh + (i & 3);
-              const bool ok = ((valid >> (4 * kb + (i >> 2))) & 1) && key >= lo && key < hi && key >= from && key < sees;
-              s[i] = ok ? s[i] : -INFINITY;
-            }
-          }
-          float high = s[0];
-#pragma unroll
-          for (int i = 1; i < 16; ++i) high = fmaxf(high, s[i]);
-          high *= scale;
-          // m is raised only when some row's scores pass it by more than kSlack
-          if (__any(high > m + T::kSlack)) {
-            const float top = fmaxf(m, pair_max(high));
-            const float keep = m == -INFINITY ? 0.f : exp2_of(m - top);
-            m = top;
-            l *= keep;
-#pragma unroll
-            for (int d = 0; d < 4; ++d) o[d] *= keep;
-          }
-          const float base = m == -INFINITY ? 0.f : T::kShift - m;
-          u32x4 pf[2], rest[2];   // probabilities in 16 bits, and what is left of them
+          for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int c = 0; c < 8; ++c) {
-            const float a = exp2_of(fmaf(s[2 * c], scale, base)), b = exp2_of(fmaf(s[2 * c + 1], scale, base));
+            s[kb] = mfma32<T>(kf[c], qf[c], s[kb]);
+            if (kb + 1 < kHalves)
+              kf[c] = read_k(c, kb + 1);
+            else if (c < 4)
+              vt[0][c] = read_v(0, c);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const int first_key = key0 + 32 * set;
+        if (special || first_key + 32 * kHalves > all_sees || first_key < all_from) {
+#pragma unroll
+          for (int kb = 0; kb < kHalves; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int in = 32 * kb + 8 * (i >> 2) + 4 * hh + (i & 3), key = first_key + in;
+              const bool ok = ((valid >> (4 * set + (in >> 3))) & 1) && key >= lo && key < hi && key >= from && key < sees;
+              s[kb][i] = ok ? s[kb][i] : -INFINITY;
+            }
+        }
+        float high = s[0][0];
+#pragma unroll
+        for (int kb = 0; kb < kHalves; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) high = fmaxf(high, s[kb][i]);
+        high *= scale;
+        // m is raised only when some row's scores pass it by more than kSlack
+        if (__any(high > m + T::kSlack)) {
+          const float top = fmaxf(m, pair_max(high));
+          const float keep = m == -INFINITY ? 0.f : exp2_of(m - top);
+          m = top;
+          l *= keep;
+#pragma unroll
+          for (int d = 0; d < 4; ++d) o[d] *= keep;
+        }
+        const float base = m == -INFINITY ? 0.f : T::kShift - m;
+#pragma unroll
+        for (int step = 0; step < 2 * kHalves; ++step) {   // 16 keys
+          u32x4 pf, rest;   // probabilities in 16 bits, and what is left of them
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const int i = 8 * (step & 1) + 2 * c;
+            const float a = exp2_of(fmaf(s[step >> 1][i], scale, base)), b = exp2_of(fmaf(s[step >> 1][i + 1], scale, base));
             const unsigned w = T::pack(a, b);
-            pf[c >> 2][c & 3] = w;
-            rest[c >> 2][c & 3] = T::pack(a - T::first(w), b - T::second(w));
+            pf[c] = w;
+            rest[c] = T::pack(a - T::first(w), b - T::second(w));
             l += a + b;
           }
+          if (step + 1 < 2 * kHalves) {
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
+            for (int d = 0; d < 4; ++d) vt[(step + 1) & 1][d] = read_v(step + 1, d);
+          }
 #pragma unroll
-            for (int d = 0; d < 4; ++d) {
-              const char *const at = v_tile + ai::v_read_offset(lane, 2 * kb + j, d, 0);
-              const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 8 * 256));
-              const u32x2 a2 = __builtin_bit_cast(u32x2, a), b2 = __builtin_bit_cast(u32x2, b);
-              const u32x4 vt = {a2[0], a2[1], b2[0], b2[1]};
-              o[d] = mfma32<T>(vt, pf[j], mfma32<T>(vt, rest[j], o[d]));
-            }
-      };
-      if (any_row) {
-#pragma unroll 1
-        for (int kb = half ? set : 0; kb < (half ? set + 1 : 2); ++kb) take(kb);
+          for (int d = 0; d < 4; ++d) o[d] = mfma32<T>(vt[step & 1][d], rest, o[d]);
+#pragma unroll
+          for (int d = 0; d < 4; ++d) o[d] = mfma32<T>(vt[step & 1][d], pf, o[d]);
+        }
       }
       valid = valid_next;
     }
@@ -375,7 +395,7 @@ __device__ __forceinline__ void attend_shared(const First &first, const Groups &
 
   // the sets' results meet
   l = pair_sum(l) * T::kUnit;
-  if (half) {
+  if constexpr (kHalf) {
     __syncthreads();
     float *const os = reinterpret_cast<float *>(lds) + rw * 64 * 64, *const ml = reinterpret_cast<float *>(lds) + 2 * 64 * 64 + rw * 128;
     if (set == 1) {
@@ -416,7 +436,13 @@ __global__ __launch_bounds__(kThreads, kPerUnit) void paged_prefix_kernel(FIRST_
   const First first{q_start, kv_lens, n_requests, n_tokens, group, window, target, capacity, {heads_d, heads_m, heads_s}};
   const pg::Turn turn = pg::turn_of(blockIdx.x, gr.shared_turns, gr.own_turns);
   if (turn.shared) {
-    attend_shared<T, kF8>(first, gr, p, turn.block, lds);
+    FoundShared f;
+    const int item = gr.by_heads.div(turn.block), head = turn.block - item * gr.by_heads.d;
+    if (!find_shared<true>(first, gr, item, f)) return;
+    if (pg::is_half(f.q, f.at.tile))
+      attend_shared<T, kF8, true>(first, gr, p, f, head, lds);
+    else
+      attend_shared<T, kF8, false>(first, gr, p, f, head, lds);
   } else {
     float(*const o_s)[kRows][kPad] = reinterpret_cast<float(*)[kRows][kPad]>(lds);
     attend<T, kF8, NT, HS, true>(first, p, gr, turn.block, o_s, reinterpret_cast<float(*)[kRows][2]>(o_s + kWaves));
