@@ -462,7 +462,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_prefix_join_kernel(First f
   const int left = f.q.n * first.group - f.tile * kRowTile, rows = left < kRowTile ? left : kRowTile;
   FoundShared s{};
   const int g = gr.group_of(f.request, first.n_requests);
-  if (g >= 0) find_shared<false>(first, gr, g, s);
+  if (g >= 0 && !find_shared<false>(first, gr, g, s)) s = FoundShared{};   // (no slots)
   const int64_t own_step = static_cast<int64_t>(heads) * kRowTile, shared_step = static_cast<int64_t>(heads) * pg::kSharedRows;
   const int d4 = threadIdx.x & 31, set = threadIdx.x >> 5, sub = set % per, at_once = kSets / per;
   for (int row0 = blockIdx.y * at_once; row0 < rows; row0 += gridDim.y * at_once) {   // (all threads come round as often)

@@ -2,8 +2,8 @@
 // kernels do on the device and a host test repeats. (The requests' own keys are cut as paged_attn_plan.h says.)
 //
 // The rows of a group that share a key head (the new tokens of all its requests x the query heads of a key head) are cut into tiles
-// of kSharedRows rows, the shared keys into pieces of `chunk` key tiles at most; twice as many where the last row tile has no more than half
-// of the rows, whose key tiles take half the time. Every item (row tile, piece) leaves a partial result in a numbered slot; a row tile's are
+// of kSharedRows rows, the shared keys into pieces of `chunk` key tiles at most; a third more where the last row tile has no more than half
+// of the rows, whose key tiles take some three quarters of the time (half the products, the same copies). Every item (row tile, piece) leaves a partial result in a numbered slot; a row tile's are
 // consecutive.
 #pragma once
 #include "paged_attn_plan.h"
@@ -41,8 +41,8 @@ SDVG_PAGED_HD SharedKeys shared_of(int32_t start, int32_t end, int32_t token0, i
   s.half = s.row_tiles > 0 && rows - (s.row_tiles - int64_t{1}) * kSharedRows <= kSharedRows / 2;
   return s;
 }
-// In halves of a (row tile, key tile) pair.
-SDVG_PAGED_HD int64_t work_of(const SharedKeys &s) { return (2 * static_cast<int64_t>(s.row_tiles) - s.half) * s.tiles; }
+// In quarters of a (row tile, key tile) pair.
+SDVG_PAGED_HD int64_t work_of(const SharedKeys &s) { return (4 * static_cast<int64_t>(s.row_tiles) - s.half) * s.tiles; }
 
 // Key tiles per item at most: total = the sum of work_of over all groups, row_tiles that of theirs, target the items that fill the chip.
 // Where the row tiles are few, the items are made to fit the chip once; rounding up adds one per row tile at most.
@@ -50,20 +50,21 @@ constexpr int kSharedRounds = 2, kSharedLeast = 8;
 SDVG_PAGED_HD int32_t shared_chunk(int64_t total, int64_t row_tiles, int32_t target) {
   int64_t c;
   if (2 * row_tiles <= target) {
-    c = ceil_div(total, 2 * (target - static_cast<int32_t>(row_tiles)));
+    c = ceil_div(total, 4 * (target - static_cast<int32_t>(row_tiles)));
   } else {
-    c = ceil_div(total, 2 * kSharedRounds * target);
+    c = ceil_div(total, 4 * kSharedRounds * target);
     if (c < kSharedLeast) c = kSharedLeast;
   }
-  return c < 1 ? 1 : c < INT32_MAX / 2 ? static_cast<int32_t>(c) : INT32_MAX / 2;
+  return c < 1 ? 1 : c < INT32_MAX / 4 ? static_cast<int32_t>(c) : INT32_MAX / 4;
 }
 // Pieces of a row tile, of the last one where it is a half; items of a group.
 struct SharedPieces {
   int32_t whole, half;
 };
+SDVG_PAGED_HD int32_t half_chunk(int32_t chunk) { return chunk + (chunk + 2) / 3; }   // (not less than 4 / 3: the items' bound rests on it)
 SDVG_PAGED_HD SharedPieces shared_pieces(const SharedKeys &s, int32_t chunk) {
-  const uint32_t t = static_cast<uint32_t>(s.tiles), c = static_cast<uint32_t>(chunk);
-  return SharedPieces{static_cast<int32_t>((t + c - 1) / c), static_cast<int32_t>((t + 2 * c - 1) / (2 * c))};
+  const uint32_t t = static_cast<uint32_t>(s.tiles), c = static_cast<uint32_t>(chunk), h = static_cast<uint32_t>(half_chunk(chunk));
+  return SharedPieces{static_cast<int32_t>((t + c - 1) / c), static_cast<int32_t>((t + h - 1) / h)};
 }
 SDVG_PAGED_HD int32_t shared_items(const SharedKeys &s, const SharedPieces &n) { return (s.row_tiles - s.half) * n.whole + s.half * n.half; }
 SDVG_PAGED_HD bool is_half(const SharedKeys &s, int32_t tile) { return s.half && tile == s.row_tiles - 1; }
@@ -76,11 +77,11 @@ SDVG_PAGED_HD Place shared_place(const SharedKeys &s, const SharedPieces &n, int
   return Place{i - piece * wholes, piece};
 }
 SDVG_PAGED_HD KeyTiles shared_tiles_of(const SharedKeys &s, const Place &at, int32_t chunk) {
-  const int32_t c = is_half(s, at.tile) ? 2 * chunk : chunk, before = at.piece ? at.piece * c : 0;
+  const int32_t c = is_half(s, at.tile) ? half_chunk(chunk) : chunk, before = at.piece ? at.piece * c : 0;
   return KeyTiles{s.first_tile + before, s.first_tile + (s.tiles - before < c ? s.tiles : before + c)};
 }
 
-// Bounds for the launch from what the host knows: row tiles, and items (and slots). total / (2 chunk) <= target - row_tiles, or
+// Bounds for the launch from what the host knows: row tiles, and items (and slots). total / (4 chunk) <= target - row_tiles, or
 // kSharedRounds * target; and one more per row tile.
 SDVG_PAGED_HD int64_t max_shared_row_tiles(int64_t n_groups, int64_t n_tokens, int32_t group) {
   const int64_t rows = n_tokens * group, bound = rows / kSharedRows + n_groups;

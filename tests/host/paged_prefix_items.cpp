@@ -30,7 +30,7 @@ static uint32_t rnd() {
 static int tokens_of(const pg::SharedKeys &s, int group) { return s.tokens * group; }
 
 static void one(int G, int longest, int most_tokens, int group, int window, int target, int64_t capacity) {
-  constexpr int row_tile = pg::kSharedRows;
+  constexpr int row_tile = pg::kSharedRows, kT = pg::kSharedTile;
   std::vector<int32_t> token(G + 1), n(G);
   for (int g = 0; g < G; ++g) {
     token[g + 1] = token[g] + rnd() % (most_tokens + 1);
@@ -47,8 +47,8 @@ static void one(int G, int longest, int most_tokens, int group, int window, int 
     const int64_t hi = n[g] < capacity ? n[g] : capacity, first = int64_t{n[g]} + 1 - window, lo = window > 0 && first > 0 ? first : 0;
     CHECK(q[g].lo == lo && q[g].hi == hi);
     if (hi > lo && q[g].tokens > 0) {
-      CHECK(q[g].first_tile * 64ll <= lo && (q[g].first_tile + 1) * 64ll > lo);
-      CHECK((q[g].first_tile + int64_t{q[g].tiles}) * 64 >= hi && (q[g].first_tile + int64_t{q[g].tiles} - 1) * 64 < hi);
+      CHECK(q[g].first_tile * int64_t{kT} <= lo && (q[g].first_tile + 1) * int64_t{kT} > lo);
+      CHECK((q[g].first_tile + int64_t{q[g].tiles}) * kT >= hi && (q[g].first_tile + int64_t{q[g].tiles} - 1) * kT < hi);
       CHECK(int64_t{q[g].row_tiles} * row_tile >= int64_t{q[g].tokens} * group && (q[g].row_tiles - 1ll) * row_tile < int64_t{q[g].tokens} * group);
     } else {
       CHECK(q[g].tiles == 0 && q[g].row_tiles == 0);
@@ -70,7 +70,7 @@ static void one(int G, int longest, int most_tokens, int group, int window, int 
       const int rows = tokens_of(q[g], group) - at.tile * row_tile;
       CHECK(pg::is_half(q[g], at.tile) == (rows <= row_tile / 2));
       const pg::KeyTiles k = pg::shared_tiles_of(q[g], at, chunk);
-      CHECK(k.begin < k.end && k.end - k.begin <= (pg::is_half(q[g], at.tile) ? 2 * chunk : chunk));
+      CHECK(k.begin < k.end && k.end - k.begin <= (pg::is_half(q[g], at.tile) ? pg::half_chunk(chunk) : chunk));
       for (int t = k.begin; t < k.end; ++t) {
         CHECK(t >= q[g].first_tile && t < q[g].first_tile + q[g].tiles);
         ++seen[at.tile][t - q[g].first_tile];
@@ -99,7 +99,7 @@ int main() {
               }
   // the largest numbers: nothing leaves 64 bits, and what is kept in 32 fits
   const pg::SharedKeys s = pg::shared_of(0, 1, -5, INT32_MAX, INT32_MAX, 1 << 27, 16, 0, INT32_MAX - 64);
-  if (s.row_tiles != (1 << 24) || s.half || s.tiles <= 0 || pg::work_of(s) != (int64_t{1} << 25) * s.tiles || pg::shared_chunk(pg::work_of(s), s.row_tiles, 512) < 1) return 1;
+  if (s.row_tiles != (1 << 24) || s.half || s.tiles <= 0 || pg::work_of(s) != (int64_t{1} << 26) * s.tiles || pg::shared_chunk(pg::work_of(s), s.row_tiles, 512) < 1) return 1;
   // every block of both kinds has its turn, once
   for (int shared : {0, 1, 2, 5, 40})
     for (int own : {1, 2, 7, 40}) {
