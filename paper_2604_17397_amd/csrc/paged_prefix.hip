@@ -127,18 +127,20 @@ __device__ __forceinline__ bool find_shared(const First &p, const Groups &gr, in
   return false;
 }
 
-// Keys that the row of token `token` sees, from and up to: of the request among f's that has the token. (All lanes of the wave come here.)
+// Keys that the row of token `token` sees, from and up to: of the request among f's that has the token. A batch of 64 requests at a time, each
+// lane looks for its token among them in 6 steps. (All lanes of the wave come here.)
 __device__ __forceinline__ void seen_by(const First &p, const FoundShared &f, int token, int &from, int &sees) {
   const int lane = threadIdx.x & 63;
   sees = 0;
   for (int b = 0; b < f.q.requests; b += 64) {
-    const int r = b + lane < f.q.requests ? f.q.request0 + b + lane : f.q.request0 + f.q.requests - 1;
+    const int r = f.q.request0 + (b + lane < f.q.requests ? b + lane : f.q.requests - 1);
     const int start = p.q_start[r], end = p.q_start[r + 1], len = p.kv_lens[r];
-    const int n = f.q.requests - b < 64 ? f.q.requests - b : 64;
-    for (int i = 0; i < n; ++i) {
-      const int s = __builtin_amdgcn_readlane(start, i), e = __builtin_amdgcn_readlane(end, i), l = __builtin_amdgcn_readlane(len, i);
-      if (token >= s && token < e) sees = l - (e - token) + 1;
-    }
+    int at = 0;
+#pragma unroll
+    for (int step = 32; step > 0; step /= 2)
+      if (__shfl(start, at + step) <= token) at += step;
+    const int s = __shfl(start, at), e = __shfl(end, at), l = __shfl(len, at);
+    if (token >= s && token < e) sees = l - (e - token) + 1;
   }
   from = p.window > 0 && sees > p.window ? sees - p.window : 0;
 }
@@ -161,15 +163,17 @@ __device__ __forceinline__ void attend_shared(const First &first, const Groups &
   int from = 0, sees = INT32_MAX;
   {
     const uint32_t all = f.at.tile * kRowTile + (row < rows ? row : rows - 1), i = p.to.by_group.div(all), h = all - i * first.group;
+    if (row < rows) {
+      const uint16_t *src = static_cast<const uint16_t *>(p.q) + (f.q.token0 + static_cast<int64_t>(i)) * p.q_ts +
+                            (static_cast<int64_t>(head) * first.group + h) * p.q_hs + 8 * hh;
+#pragma unroll
+      for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const u32x4 *>(src + 16 * s);
+    }
     int a, b;
     seen_by(first, f, f.q.token0 + static_cast<int>(i), a, b);
     if (row < rows) {
       from = a;
       sees = b;
-      const uint16_t *src = static_cast<const uint16_t *>(p.q) + (f.q.token0 + static_cast<int64_t>(i)) * p.q_ts +
-                            (static_cast<int64_t>(head) * first.group + h) * p.q_hs + 8 * hh;
-#pragma unroll
-      for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const u32x4 *>(src + 16 * s);
     }
   }
   const int all_sees = wave_min(sees), all_from = -wave_min(-from);
