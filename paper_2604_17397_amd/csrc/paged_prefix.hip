@@ -93,11 +93,10 @@ __device__ __forceinline__ pg::SharedKeys load_group(const First &p, const Group
   const int32_t n = gr.lens[g];
   return pg::shared_of(start, end, p.q_start[start], p.q_start[end], n > 0 ? n : 0, p.n_tokens, p.group, p.window, p.capacity);
 }
-// Item number x (kItems), or the slots of group x.
+// Item number x (kItems), or the slots of group x. mine0: load_group of this lane.
 template <bool kItems>
-__device__ __forceinline__ bool find_shared(const First &p, const Groups &gr, int x, FoundShared &f) {
+__device__ __forceinline__ bool find_shared(const First &p, const Groups &gr, const pg::SharedKeys &mine0, int x, FoundShared &f) {
   const int lane = threadIdx.x & 63;
-  const pg::SharedKeys mine0 = load_group(p, gr, lane);
   int64_t total = 0, row_tiles = 0;
   for (int b = 0; b < gr.n; b += 64) {
     const pg::SharedKeys q = b ? load_group(p, gr, b + lane) : mine0;
@@ -442,7 +441,7 @@ __global__ __launch_bounds__(kThreads, kPerUnit) void paged_prefix_kernel(FIRST_
   if (turn.shared) {
     FoundShared f;
     const int item = gr.by_heads.div(turn.block), head = turn.block - item * gr.by_heads.d;
-    if (!find_shared<true>(first, gr, item, f)) return;
+    if (!find_shared<true>(first, gr, load_group(first, gr, threadIdx.x & 63), item, f)) return;
     if (pg::is_half(f.q, f.at.tile))
       attend_shared<T, kF8, true>(first, gr, p, f, head, lds);
     else
@@ -462,11 +461,12 @@ __global__ __launch_bounds__(kJoinThreads) void paged_prefix_join_kernel(First f
   __shared__ float ml_s[kSets][2];
   Found f;
   const int heads = first.by_heads.d, index = first.by_heads.div(blockIdx.x), head = blockIdx.x - index * heads;
+  const pg::SharedKeys groups = load_group(first, gr, threadIdx.x & 63);   // (asked for ahead of the requests')
   if (!find<kRowTile, kWaves / HS, false, true>(first, gr, index, f)) return;
   const int left = f.q.n * first.group - f.tile * kRowTile, rows = left < kRowTile ? left : kRowTile;
   FoundShared s{};
   const int g = gr.group_of(f.request, first.n_requests);
-  if (g >= 0 && !find_shared<false>(first, gr, g, s)) s = FoundShared{};   // (no slots)
+  if (g >= 0 && !find_shared<false>(first, gr, groups, g, s)) s = FoundShared{};   // (no slots)
   const int64_t own_step = static_cast<int64_t>(heads) * kRowTile, shared_step = static_cast<int64_t>(heads) * pg::kSharedRows;
   const int d4 = threadIdx.x & 31, set = threadIdx.x >> 5, sub = set % per, at_once = kSets / per;
   for (int row0 = blockIdx.y * at_once; row0 < rows; row0 += gridDim.y * at_once) {   // (all threads come round as often)
