@@ -7,12 +7,15 @@
 //
 // What bounds it: the logits are read from memory once (and once more from the caches where a cut has to be found); a launch or a fp64 operation
 // per token cost as much. So a row is never sorted. It is cut into slices, a workgroup each:
-//   1 slices   the largest logit; a histogram of tokens and their weights over bins of a quarter octave (factor 2^(1/4)) of weight. Where there is no filter the sum of weights alone.
-//   2 collect  (filters only) every slice's workgroup adds up the row's histograms, sees in which bins the cuts lie, and writes those bins' tokens to a list.
-//   3 draw     a workgroup per row: sorts what of the list the cuts need, then finds the slice with the drawn token from the slices' kept weights, and the token
-//              in it.
-// A weight in a histogram is an integer in steps of 2^-35 of its bin's upper end, in 64 bits beside the count; without filters it is
-// rounded to 2^-34 of its octave. So it is at most 2^-35 off, equal logits have equal weights, and sums of equal weights are exact.
+//   1 slices   the largest logit; a histogram of tokens and their weights over bins of a quarter octave (factor 2^(1/4)) of weight. Where there
+//              is no filter the sum of weights alone.
+//   2 decide   (filters only, a workgroup per row) adds up the row's histograms and sees in which bins the cuts lie.
+//   3 collect  (filters only) every slice's workgroup makes a finer histogram of those bins, 256 parts, and a list of their tokens.
+//   4 draw     a workgroup per row: finds the parts in which the cuts lie, compares the few tokens of such a part with each other, then finds
+//              the slice with the drawn token from the slices' kept weights, and the token in it.
+// A weight in a histogram is an integer in steps of 2^-35 of its bin's middle, in 64 bits beside the count; without filters it is
+// rounded to 2^-34 of its octave's middle. So it is at most 2^-35 off, equal logits have equal weights, and sums of equal weights are exact.
+#include <float.h>
 #include <math.h>
 
 #include "paged_kv.h"
@@ -24,9 +27,11 @@ typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 constexpr int kBins = 256;                 // of weight; the last one has all that is lighter, whose weight does not count (2^-63 of the largest)
 constexpr int kCountBits = 14;             // of a slice's bin: tokens below, weight in steps of kStep above
 constexpr double kStep = 0x1p-35;
-constexpr int kSliceThreads = 256, kMostSlice = 8192, kLeastSlice = 2048;
-constexpr int kDrawThreads = 1024, kSorted = 2048;
-constexpr int kListMost = 16384;           // tokens of a row's cut bins that are listed; more are looked for in the row again
+constexpr int kCopies = 4;                 // of a histogram, so that neighbours seldom add to one number at once
+constexpr int kSliceThreads = 256, kMostSlice = 8192, kLeastSlice = 4096;
+constexpr int kDrawThreads = 1024, kHeld = 2048, kRanked = 256;   // tokens that are held in LDS, and that are compared with each other
+constexpr int kParts = 256;                // of the cut bins
+constexpr int kListed = 1024;              // tokens of a slice's cut bins that are listed; where it has more, they are looked for in the slice again
 constexpr int kMostVocab = 1 << 20, kMostSlices = kMostVocab / kLeastSlice + 1;
 
 struct Slice {
@@ -38,12 +43,11 @@ struct Slice {
 };
 // What a row's filters come to, by bins.
 struct Cut {
-  int32_t from, upto;      // bins in which the last kept token may be
-  int32_t k_bin, k_left;   // bin in which top-k ends, tokens it keeps there; 256: nowhere
-  int32_t p_on;
-  int32_t listed;          // tokens in bins from .. upto and, where it counts, k_bin
+  int32_t from, upto;      // bins in which the last kept token may be; kBins: all are kept
+  int32_t k_bin, k_left;   // bin in which top-k ends, tokens it keeps there; kBins: nowhere
+  int32_t p_on, k_too;     // k_too: that bin, behind `upto`, matters for the weight that top-p takes a share of
   double all;              // weight of all tokens
-  double upto_weight[kBins];   // weight of bins 0 .. b, relative to the upper end of bin 0
+  double upto_weight[kBins];   // weight of bins 0 .. b, relative to the middle of bin 0
   int32_t upto_count[kBins];
 };
 struct Entry {
@@ -59,11 +63,13 @@ struct Params {
   float all_temperature, all_top_p, all_min_p;
   int32_t all_top_k;
   int64_t row_stride;      // elements
-  int32_t n_rows, vocab, slice, n_slices, list_most;
+  int32_t n_rows, vocab, slice, n_slices;
   Slice *slices;           // [row][slice]
   unsigned long long *bins;   // [row][slice][kBins]
   Cut *cuts;               // [row]
-  Entry *lists;            // [row][list_most]
+  unsigned long long *parts;   // [row][slice][2][kParts]: of bins from .. upto, as many of each; of the bin of top-k where k_too
+  int32_t *listed;         // [row][slice]: tokens in them
+  Entry *lists;            // [row][slice][kListed]
 };
 
 struct Row {
@@ -131,103 +137,125 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); }
 // Larger logits first, of equal ones the lower index.
 __device__ __forceinline__ unsigned long long rank_of(uint32_t key, uint32_t index) { return static_cast<unsigned long long>(~key) << 32 | index; }
-// A logit's place on the scale of bins. +infinity is a number that all others are far from. (The product is rounded by itself: what a fused
-// subtraction of its floor would keep beside it is no fraction where the place is a number beyond 2^52.)
-__device__ __forceinline__ double place_of(float x, double per_bin) {
+// A logit's place on the scale of bins (or octaves): the middle of its bin, and how far it is from it, -1/2 to 1/2. (+infinity is a number that all
+// others are far from. The product is rounded by itself: a fused subtraction would keep what is beyond it, which is no fraction where the
+// place is a number beyond 2^52.)
+struct Place {
+  double at, bin, rest;
+};
+__device__ __forceinline__ Place place_of(double x, double per_bin) {
 #pragma clang fp contract(off)
-  return (x == INFINITY ? 0x1p200 : static_cast<double>(x)) * per_bin;
+  Place a;
+  a.at = x * per_bin;
+  a.bin = rint(a.at);
+  a.rest = a.at - a.bin;
+  return a;
 }
-__device__ __forceinline__ int bin_of(double top, double floor_x) {
-  const double d = top - floor_x;
-  return d < kBins - 1 ? static_cast<int>(d) : kBins - 1;
+__device__ __forceinline__ double number_of(float x) { return x == INFINITY ? 0x1p200 : static_cast<double>(x); }
+__device__ __forceinline__ int bin_of(double top, double bin) { return static_cast<int>(fmin(top - bin, kBins - 1.0)); }   // (a NaN's: the last one)
+
+// 2^(z / 4) for |z| <= 1/2 in steps of kStep, with 1 added in the kCountBits bits below: a polynomial through the function's values at Chebyshev's
+// points, 1.3e-13 off at most, times 2^49. The last addition leaves its whole part in the sum's mantissa.
+__device__ __forceinline__ unsigned long long step_and_one(double z) {
+  double s = 0x1p49 * 3.7615098597694156e-08;
+  s = fma(s, z, 0x1p49 * 1.3025126327701222e-06);
+  s = fma(s, z, 0x1p49 * 3.757081572373334e-05);
+  s = fma(s, z, 0x1p49 * 0.0008672516469677146);
+  s = fma(s, z, 0x1p49 * 0.01501415668497826);
+  s = fma(s, z, 0x1p49 * 0.1732867951415776);
+  s = fma(s, z, 0x1p52 + 0x1p49 + (1 << (kCountBits - 1)));
+  const unsigned long long b = __double_as_longlong(s);
+  return static_cast<unsigned long long>(static_cast<uint32_t>(b >> 32) & 0xfffff) << 32 | ((static_cast<uint32_t>(b) & (0u - (1u << kCountBits))) | 1u);
+}
+static_assert(kCountBits == 14, "2^49 of weight and the count's bits make steps of 2^-35");
+__device__ __forceinline__ unsigned long long steps_of(double z) { return step_and_one(z) >> kCountBits; }
+// 2^z for |z| <= 1/2, rounded to 2^-34: the same, 1.1e-12 off at most.
+__device__ __forceinline__ double in_octave(double z) {
+  double s = 1.3255224883636123e-06;
+  s = fma(s, z, 1.531007940226575e-05);
+  s = fma(s, z, 0.000154034558524266);
+  s = fma(s, z, 0.001333345056800051);
+  s = fma(s, z, 0.009618129159402605);
+  s = fma(s, z, 0.05550410941205933);
+  s = fma(s, z, 0.24022650695812986);
+  s = fma(s, z, 0.6931471805459334);
+  return fma(s, z, 1.0 + 0x1.8p18) - 0x1.8p18;
+}
+// 2^(-b / 4): the middle of bin b, relative to that of bin 0
+__device__ __forceinline__ double middle_of(int b) {
+  const double r = b & 2 ? 0.7071067811865476 : 1.0;
+  return ldexp(b & 1 ? r * 0.8408964152537145 : r, -(b >> 2));
 }
 
-// 2^((f - 1) / 4) for 0 <= f < 1: exp's series to the 8th power, 4e-13 off at most.
-__device__ __forceinline__ double in_bin(double f) {
-  const double y = fma(f, 0.17328679513998632, -0.17328679513998632);
-  double s = 1.0 / 40320;
-  s = fma(s, y, 1.0 / 5040);
-  s = fma(s, y, 1.0 / 720);
-  s = fma(s, y, 1.0 / 120);
-  s = fma(s, y, 1.0 / 24);
-  s = fma(s, y, 1.0 / 6);
-  s = fma(s, y, 0.5);
-  s = fma(s, y, 1.0);
-  return fma(s, y, 1.0);
-}
-// 2^f for 0 <= f < 1, from the middle, rounded to 2^-34.
-__device__ __forceinline__ double in_octave(double f) {
-  const double y = fma(f, 0.6931471805599453, -0.34657359027997264);
-  double s = 1.0 / 479001600;
-  s = fma(s, y, 1.0 / 39916800);
-  s = fma(s, y, 1.0 / 3628800);
-  s = fma(s, y, 1.0 / 362880);
-  s = fma(s, y, 1.0 / 40320);
-  s = fma(s, y, 1.0 / 5040);
-  s = fma(s, y, 1.0 / 720);
-  s = fma(s, y, 1.0 / 120);
-  s = fma(s, y, 1.0 / 24);
-  s = fma(s, y, 1.0 / 6);
-  s = fma(s, y, 0.5);
-  s = fma(s, y, 1.0);
-  s = fma(s, y, 1.0);
-  return fma(s, 1.4142135623730951, 0x1p18) - 0x1p18;
-}
-// 2^(-b / 4)
-__device__ __forceinline__ double end_of_bin(int b) {
-  const double q[4] = {1.0, 0.8408964152537145, 0.7071067811865476, 0.5946035575013605};
-  return ldexp(q[b & 3], -(b >> 2));
-}
-__device__ __forceinline__ unsigned long long steps_of(double weight) {   // weight <= 1
-  return static_cast<unsigned long long>(__double_as_longlong(fma(weight, 1.0 / kStep, 0x1p52))) & ((1ull << 40) - 1);   // (rounded by the addition)
-}
-
-__device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
-  return x;
-}
-__device__ __forceinline__ int wave_min(int x) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int y = __shfl_xor(x, d);
-    x = y < x ? y : x;
+// Over the lanes of a wave: within rows of 16, then rows to the rows behind them.
+template <int kControl, int kRowMask, typename V>
+__device__ __forceinline__ V moved(V x, V none) {
+  static_assert(sizeof(V) == 4 || sizeof(V) == 8, "");
+  if constexpr (sizeof(V) == 4) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, x), kControl, kRowMask, 0xf, false));
+  } else {
+    const unsigned long long a = __builtin_bit_cast(unsigned long long, x), n = __builtin_bit_cast(unsigned long long, none);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(static_cast<int>(n), static_cast<int>(a), kControl, kRowMask, 0xf, false),
+                   hi = __builtin_amdgcn_update_dpp(static_cast<int>(n >> 32), static_cast<int>(a >> 32), kControl, kRowMask, 0xf, false);
+    return __builtin_bit_cast(V, static_cast<unsigned long long>(hi) << 32 | lo);
   }
-  return x;
 }
-__device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
-  return x;
+template <typename V, typename F>
+__device__ __forceinline__ V wave_scan(V x, V none, F &&join) {   // inclusive
+  x = join(moved<0x111, 0xf>(x, none), x);
+  x = join(moved<0x112, 0xf>(x, none), x);
+  x = join(moved<0x114, 0xf>(x, none), x);
+  x = join(moved<0x118, 0xf>(x, none), x);
+  x = join(moved<0x142, 0xa>(x, none), x);
+  return join(moved<0x143, 0xc>(x, none), x);
 }
 template <typename V>
-__device__ __forceinline__ V wave_scan(V x) {   // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const V y = __shfl_up(x, d);
-    if (lane >= d) x += y;
+__device__ __forceinline__ V of_last_lane(V x) {
+  if constexpr (sizeof(V) == 4) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+  } else {
+    const unsigned long long a = __builtin_bit_cast(unsigned long long, x);
+    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(a), 63), hi = __builtin_amdgcn_readlane(static_cast<int>(a >> 32), 63);
+    return __builtin_bit_cast(V, static_cast<unsigned long long>(hi) << 32 | lo);
   }
-  return x;
 }
-// Inclusive sums over a workgroup's threads; `waves` is LDS of a number per wave.
+template <typename V>
+__device__ __forceinline__ V wave_sums(V x) {
+  return wave_scan(x, V(0), [](V a, V b) { return a + b; });
+}
+template <typename V>
+__device__ __forceinline__ V wave_sum(V x) { return of_last_lane(wave_sums(x)); }
+__device__ __forceinline__ float wave_max(float x) { return of_last_lane(wave_scan(x, -INFINITY, [](float a, float b) { return fmaxf(a, b); })); }
+template <typename V>
+__device__ __forceinline__ V wave_min(V x, V most) {
+  return of_last_lane(wave_scan(x, most, [](V a, V b) { return a < b ? a : b; }));
+}
+// Inclusive sums over a workgroup's threads; `waves` is LDS of a number per wave (16 at most).
 template <int kThreads, typename V>
 __device__ __forceinline__ V block_scan(V x, V *waves) {
-  const int wave = threadIdx.x >> 6;
-  x = wave_scan(x);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  x = wave_sums(x);
   __syncthreads();
-  if ((threadIdx.x & 63) == 63) waves[wave] = x;
+  if (lane == 63) waves[wave] = x;
   __syncthreads();
-  V before = 0;
-  for (int w = 0; w < wave; ++w) before += waves[w];
-  return before + x;
+  return x + wave_sum(lane < wave ? waves[lane & (kThreads / 64 - 1)] : V(0));
+}
+
+// The first, or last, thread of a workgroup for which `is`: one lane of a wave asks, for atomics of many lanes to one address go one by one.
+__device__ __forceinline__ void first_thread(bool is, int *found) {
+  const unsigned long long m = __ballot(is);
+  if (m != 0 && (threadIdx.x & 63) == 0) atomicMin(found, static_cast<int>(threadIdx.x) + __ffsll(m) - 1);
+}
+__device__ __forceinline__ void last_thread(bool is, int *found) {
+  const unsigned long long m = __ballot(is);
+  if (m != 0 && (threadIdx.x & 63) == 0) atomicMax(found, static_cast<int>(threadIdx.x) + 63 - __clzll(m));
 }
 
 // ---- 1
 template <typename T, int kVectors>   // 16-byte vectors per thread
 __device__ __forceinline__ void one_slice(const Params &p, int r, int s) {
   constexpr int N = 16 / sizeof(T);
-  __shared__ unsigned long long hist[kBins];
+  __shared__ unsigned long long hist[kCopies][kBins + 1];
   __shared__ double sums[kSliceThreads / 64];
   __shared__ float tops[kSliceThreads / 64];
   __shared__ int firsts[kSliceThreads / 64];
@@ -238,7 +266,9 @@ __device__ __forceinline__ void one_slice(const Params &p, int r, int s) {
   bool nan = false;
 #pragma unroll
   for (int v = 0; v < kVectors; ++v) load16(row.grid, s * p.slice + (v * kSliceThreads + static_cast<int>(threadIdx.x)) * N, row.skew, p.vocab, x[v]);
-  hist[threadIdx.x] = 0;
+  if (w.filtered)
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) hist[i][threadIdx.x] = 0;
 #pragma unroll
   for (int v = 0; v < kVectors; ++v)
 #pragma unroll
@@ -255,6 +285,12 @@ __device__ __forceinline__ void one_slice(const Params &p, int r, int s) {
   out.most = most;
   out.nan = any_nan;
   if (!any_nan && most > -INFINITY) {
+    const auto each = [&](auto &&f) {
+#pragma unroll
+      for (int v = 0; v < kVectors; ++v)
+#pragma unroll
+        for (int i = 0; i < N; ++i) f(x[v][i]);
+    };
     if (w.greedy) {
       int first = INT32_MAX;
 #pragma unroll
@@ -264,45 +300,48 @@ __device__ __forceinline__ void one_slice(const Params &p, int r, int s) {
           const int at = s * p.slice + (v * kSliceThreads + static_cast<int>(threadIdx.x)) * N + i - row.skew;
           if (x[v][i] == most && at < first) first = at;
         }
-      first = wave_min(first);
+      first = wave_min(first, INT32_MAX);
       if (lane == 0) firsts[wave] = first;
       __syncthreads();
       for (int i = 0; i < kSliceThreads / 64; ++i) first = firsts[i] < first ? firsts[i] : first;
       out.first = first;
     } else if (!w.filtered) {
       const double per_octave = 0.25 * w.per_bin;
-      out.top = floor(place_of(most, per_octave));
+      const double top = out.top = place_of(number_of(most), per_octave).bin;
       double sum = 0.0;
-#pragma unroll
-      for (int v = 0; v < kVectors; ++v)
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (x[v][i] > -INFINITY) {
-            const double y = place_of(x[v][i], per_octave), f = floor(y), d = fmax(f - out.top, -2000.0);
-            sum += ldexp(in_octave(y - f), static_cast<int>(d));
-          }
+      const auto add = [&](double y) {   // (-infinity too, whose rest is a NaN: its weight is 0)
+        const Place a = place_of(y, per_octave);
+        sum += ldexp(in_octave(fmax(a.rest, -0.5)), static_cast<int>(fmax(a.bin - top, -2000.0)));
+      };
+      if (most < INFINITY)
+        each([&](float y) { add(static_cast<double>(y)); });
+      else
+        each([&](float y) { sum += y == INFINITY ? in_octave(place_of(0x1p200, per_octave).rest) : 0.0; });
       sum = wave_sum(sum);
       if (lane == 0) sums[wave] = sum;
       __syncthreads();
       out.sum = 0.0;
       for (int i = 0; i < kSliceThreads / 64; ++i) out.sum += sums[i];
     } else {
-      out.top = floor(place_of(most, w.per_bin));
-#pragma unroll
-      for (int v = 0; v < kVectors; ++v)
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (x[v][i] > -INFINITY) {
-            const double y = place_of(x[v][i], w.per_bin), f = floor(y);
-            const int b = bin_of(out.top, f);
-            const unsigned long long steps = b < kBins - 1 ? steps_of(in_bin(y - f)) : 0;
-            atomicAdd(&hist[b], steps << kCountBits | 1);
-          }
+      const double top = out.top = place_of(number_of(most), w.per_bin).bin;
+      unsigned long long *const mine = hist[threadIdx.x % kCopies];
+      // (-infinity comes to the last bin, which is not read)
+      const auto add = [&](double y) {
+        const Place a = place_of(y, w.per_bin);
+        atomicAdd(&mine[bin_of(top, a.bin)], step_and_one(a.rest));
+      };
+      if (most < INFINITY)
+        each([&](float y) { add(static_cast<double>(y)); });
+      else
+        each([&](float y) { add(number_of(y)); });
     }
   }
   if (w.filtered) {
     __syncthreads();
-    p.bins[(static_cast<int64_t>(r) * p.n_slices + s) * kBins + threadIdx.x] = hist[threadIdx.x];
+    unsigned long long sum = 0;
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) sum += hist[i][threadIdx.x];
+    p.bins[(static_cast<int64_t>(r) * p.n_slices + s) * kBins + threadIdx.x] = sum;
   }
   if (threadIdx.x == 0) p.slices[static_cast<int64_t>(r) * p.n_slices + s] = out;
 }
@@ -329,61 +368,68 @@ __device__ __forceinline__ Whole whole_of(const Params &p, int r) {   // by ever
   a.nan = __any(a.nan);
   return a;
 }
+// Place of the lightest token that min-p keeps.
+__device__ __forceinline__ double least_of(float most, const Row &w) { return place_of(number_of(most), w.per_bin).at + 4.0 * log2(static_cast<double>(w.m)); }
 // Bins that a slice's are behind the row's.
 __device__ __forceinline__ int behind(double top, double slice_top) { return static_cast<int>(fmin(top - slice_top, 1e6)); }
 
 // ---- 2
-template <typename T, int kVectors>
-__device__ __forceinline__ void collect(const Params &p, int r, int s) {
-  constexpr int N = 16 / sizeof(T);
+__global__ __launch_bounds__(kBins) void sample_decide_kernel(Params p) {
   __shared__ double weight[kBins];
-  __shared__ int count[kBins];
-  __shared__ double dwaves[kSliceThreads / 64];
-  __shared__ int iwaves[kSliceThreads / 64];
-  __shared__ int found[3];
+  __shared__ unsigned long long steps[kBins];
+  __shared__ int count[kBins], off[kMostSlices], found[3];
+  __shared__ double dwaves[kBins / 64];
+  __shared__ int iwaves[kBins / 64];
+  const int r = blockIdx.x, b = threadIdx.x;
   const Row w = row_of(p, r);
   if (!w.filtered) return;
-  Whole all = whole_of(p, r);
-  if (all.nan || all.most == -INFINITY) return;
-  all.top = floor(place_of(all.most, w.per_bin));
-  const int b = threadIdx.x;
-  // the row's bin b, and what the slices ahead of this one have in it
-  unsigned long long steps = 0;
-  int n = 0, n_ahead = 0, n_mine = 0;
   const Slice *const slices = p.slices + static_cast<int64_t>(r) * p.n_slices;
   const unsigned long long *const bins = p.bins + static_cast<int64_t>(r) * p.n_slices * kBins;
-#pragma unroll 4
-  for (int i = 0; i < p.n_slices; ++i) {
-    const bool some = slices[i].most > -INFINITY;
-    const int off = some ? behind(all.top, slices[i].top) : 0, at = b - off;
-    const bool in = some && b < kBins - 1 && at >= 0;
-    const unsigned long long h = in ? bins[i * kBins + at] : 0;
-    const int c = static_cast<int>(h & ((1u << kCountBits) - 1));
-    steps += h >> kCountBits;
-    n += c;
-    if (i < s) n_ahead += c;
-    if (i == s) n_mine = c;
-  }
-  const double mine = static_cast<double>(steps) * kStep * end_of_bin(b);
-  weight[b] = block_scan<kSliceThreads>(mine, dwaves);
-  count[b] = block_scan<kSliceThreads>(n, iwaves);
+  steps[b] = 0;
+  count[b] = 0;
   if (b < 3) found[b] = kBins;
+  // the row's histogram, 16 slices at a time: their numbers are asked for before it is known how far they have to be moved
+  constexpr int kAtOnce = 16;
+  unsigned long long h[kAtOnce];
+  const auto ask = [&](int base) {
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) h[j] = base + j < p.n_slices ? bins[(base + j) * kBins + b] : 0;
+  };
+  ask(0);
+  Whole all = whole_of(p, r);
+  if (all.nan || all.most == -INFINITY) return;
+  all.top = place_of(number_of(all.most), w.per_bin).bin;
+  for (int i = b; i < p.n_slices; i += kBins) off[i] = slices[i].most > -INFINITY ? behind(all.top, slices[i].top) : kBins;
+  __syncthreads();
+  for (int base = 0; base < p.n_slices; base += kAtOnce) {
+    if (base > 0) ask(base);
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j)
+      if (base + j < p.n_slices && b < kBins - 1 && b + off[base + j] < kBins - 1 && h[j] != 0) {
+        atomicAdd(&steps[b + off[base + j]], h[j] >> kCountBits);
+        atomicAdd(&count[b + off[base + j]], static_cast<int>(h[j] & ((1u << kCountBits) - 1)));
+      }
+  }
+  __syncthreads();
+  weight[b] = block_scan<kBins>(static_cast<double>(steps[b]) * kStep * middle_of(b), dwaves);
+  const int upto_here = block_scan<kBins>(count[b], iwaves);
+  count[b] = upto_here;
   __syncthreads();
   const double total = weight[kBins - 1];
   // top-k ends in the first bin up to which there are k tokens
-  if (w.k > 0 && count[b] >= w.k) atomicMin(&found[0], b);
+  first_thread(w.k > 0 && count[b] >= w.k, &found[0]);
   __syncthreads();
   const int k_bin = found[0], k_ahead = k_bin > 0 && k_bin < kBins ? count[k_bin - 1] : 0, k_left = k_bin < kBins ? w.k - k_ahead : 0;
   const bool k_inside = k_bin < kBins && count[k_bin] > w.k;
   const bool p_on = w.p < 1.0f;
-  int from = kBins, upto = kBins;   // (kBins: all tokens are kept)
+  int from = kBins, upto = kBins;
   if (p_on) {
     // the weight that top-k leaves is known to within its last bin; the last token of top-p lies in one of these bins
-    const double k_low = k_bin == kBins ? total : k_inside ? (k_bin > 0 ? weight[k_bin - 1] : 0.0) + k_left * end_of_bin(k_bin + 1) : weight[k_bin];
+    const double k_low = k_bin == kBins ? total : k_inside ? (k_bin > 0 ? weight[k_bin - 1] : 0.0) + k_left * middle_of(k_bin + 1) : weight[k_bin];
     const double k_high = k_bin == kBins ? total : weight[k_bin];
     const double low = w.p * k_low * (1.0 - 1e-9), high = w.p * k_high * (1.0 + 1e-9);
-    if (weight[b] >= low) atomicMin(&found[1], b);
-    if (weight[b] >= high) atomicMin(&found[2], b);
+    first_thread(weight[b] >= low, &found[1]);
+    first_thread(weight[b] >= high, &found[2]);
     __syncthreads();
     from = found[1];
     upto = found[2];
@@ -393,7 +439,7 @@ __device__ __forceinline__ void collect(const Params &p, int r, int s) {
     from = upto = k_bin;
   }
   if (w.m > 0.0f) {
-    const int m_bin = bin_of(all.top, floor(place_of(all.most, w.per_bin) + 4.0 * log2(static_cast<double>(w.m))));
+    const int m_bin = bin_of(all.top, rint(least_of(all.most, w)));
     if (m_bin < from) from = m_bin;
     if (m_bin < upto) upto = m_bin;
   }
@@ -401,65 +447,91 @@ __device__ __forceinline__ void collect(const Params &p, int r, int s) {
     from = upto = kBins;
   else if (upto > kBins - 2)
     upto = kBins - 2;
-  const bool k_too = p_on && k_inside && k_bin > upto;   // (for the weight that top-p takes a share of)
-  // tokens to be listed: of the row, of the slices ahead, of this one
-  const bool asked = (b >= from && b <= upto) || (k_too && b == k_bin);
-  __syncthreads();
-  const int listed = block_scan<kSliceThreads>(asked ? n : 0, iwaves);
-  __syncthreads();
-  const int ahead = block_scan<kSliceThreads>(asked ? n_ahead : 0, iwaves);
-  __syncthreads();
-  const int here = block_scan<kSliceThreads>(asked ? n_mine : 0, iwaves);
-  __shared__ int sums[3];
-  if (b == kSliceThreads - 1) {
-    sums[0] = listed;
-    sums[1] = ahead;
-    sums[2] = here;
+  Cut *const c = p.cuts + r;
+  c->upto_weight[b] = weight[b];
+  c->upto_count[b] = count[b];
+  if (b == 0) {
+    c->from = from;
+    c->upto = upto;
+    c->k_bin = k_bin;
+    c->k_left = k_left;
+    c->k_too = p_on && k_inside && k_bin > upto;
+    c->p_on = p_on;
+    c->all = total;
   }
-  if (s == 0) {
-    Cut *const c = p.cuts + r;
-    c->upto_weight[b] = weight[b];
-    c->upto_count[b] = count[b];
-    if (b == kSliceThreads - 1) {
-      c->from = from;
-      c->upto = upto;
-      c->k_bin = k_bin;
-      c->k_left = k_left;
-      c->p_on = p_on;
-      c->listed = listed;
-      c->all = total;
-    }
-  }
-  __syncthreads();
-  if (sums[0] > p.list_most || sums[2] == 0) return;
-  // the tokens themselves; their order in the list does not matter
+}
+
+// Logits among which are all of bins `first` .. `last`, few others, and never -infinity.
+struct Interval {
+  float low, high;
+};
+__device__ __forceinline__ Interval interval_of(double top, double first, double last, double per_bin) {
+  if (!(per_bin > 0.0)) return Interval{-FLT_MAX, INFINITY};
+  const double high = (top - first + 0.5) / per_bin, low = (top - last - 0.5) / per_bin;
+  return Interval{fmaxf(static_cast<float>(low - fabs(low) * 1e-6 - 3e-45), -FLT_MAX), static_cast<float>(high + fabs(high) * 1e-6 + 3e-45)};
+}
+// A bin's part, of n: the lightest tokens are in the last one.
+__device__ __forceinline__ int part_of(double rest, int n) {
+  const int i = static_cast<int>((0.5 - rest) * n);
+  return i < n - 1 ? i : n - 1;
+}
+
+// ---- 3
+template <typename T, int kVectors>
+__device__ __forceinline__ void collect(const Params &p, int r, int s) {
+  constexpr int N = 16 / sizeof(T);
+  static_assert(kVectors * N <= 32, "a bit per logit");
+  __shared__ unsigned long long parts[2][kParts];
+  __shared__ int n;
   const RowAt<T> row(p, r);
-  int mine_n = 0;
   float x[kVectors][N];
-  uint32_t hit[kVectors];
 #pragma unroll
-  for (int v = 0; v < kVectors; ++v) load16(row.grid, s * p.slice + (v * kSliceThreads + b) * N, row.skew, p.vocab, x[v]);
-#pragma unroll
-  for (int v = 0; v < kVectors; ++v) {
-    hit[v] = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if (x[v][i] == -INFINITY) continue;
-      const int bin = bin_of(all.top, floor(place_of(x[v][i], w.per_bin)));
-      if (bin < kBins - 1 && ((bin >= from && bin <= upto) || (k_too && bin == k_bin))) hit[v] |= 1u << i;
-    }
-    mine_n += __popc(hit[v]);
-  }
-  int at = sums[1] + block_scan<kSliceThreads>(mine_n, iwaves) - mine_n;
-  Entry *const list = p.lists + static_cast<int64_t>(r) * p.list_most;
+  for (int v = 0; v < kVectors; ++v) load16(row.grid, s * p.slice + (v * kSliceThreads + static_cast<int>(threadIdx.x)) * N, row.skew, p.vocab, x[v]);
+  const Row w = row_of(p, r);
+  if (!w.filtered) return;
+  const Whole all = whole_of(p, r);
+  if (all.nan || all.most == -INFINITY) return;
+  const Cut &c = p.cuts[r];
+  const int from = c.from, upto = c.upto, k_bin = c.k_too ? c.k_bin : -1;
+  if (from == kBins && k_bin < 0) return;
+  const double top = place_of(number_of(all.most), w.per_bin).bin;
+  parts[0][threadIdx.x] = 0;
+  parts[1][threadIdx.x] = 0;
+  if (threadIdx.x == 0) n = 0;
+  __syncthreads();
+  Interval a = {INFINITY, -INFINITY}, b = a;   // (none)
+  if (from < kBins) a = interval_of(top, from, upto, w.per_bin);
+  if (k_bin >= 0) b = interval_of(top, k_bin, k_bin, w.per_bin);
+  uint32_t hits = 0;
 #pragma unroll
   for (int v = 0; v < kVectors; ++v)
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (hit[v] >> i & 1) {
-        if (at < p.list_most) list[at] = Entry{key_of(x[v][i]), static_cast<uint32_t>(s * p.slice + (v * kSliceThreads + b) * N + i - row.skew)};
-        ++at;
-      }
+      if ((x[v][i] >= a.low && x[v][i] <= a.high) || (x[v][i] >= b.low && x[v][i] <= b.high)) hits |= 1u << (v * N + i);
+  const int per_bin = kParts / (upto - from + 1);
+  Entry *const list = p.lists + (static_cast<int64_t>(r) * p.n_slices + s) * kListed;
+  while (hits) {
+    const int j = __ffs(hits) - 1;
+    hits &= hits - 1;
+    const int place = s * p.slice + (j / N * kSliceThreads + static_cast<int>(threadIdx.x)) * N + j % N;
+    const float y = as_float(row.grid[place]);
+    const Place q = place_of(number_of(y), w.per_bin);
+    const int bin = bin_of(top, q.bin);
+    if ((bin < from || bin > upto) && bin != k_bin) continue;
+    if (bin == k_bin)
+      atomicAdd(&parts[1][part_of(q.rest, kParts)], step_and_one(q.rest));
+    else
+      atomicAdd(&parts[0][(bin - from) * per_bin + part_of(q.rest, per_bin)], step_and_one(q.rest));
+    const int at = atomicAdd(&n, 1);   // (their order does not matter)
+    if (at < kListed) list[at] = Entry{key_of(y), static_cast<uint32_t>(place - row.skew)};
+  }
+  __syncthreads();
+  const int64_t slot = static_cast<int64_t>(r) * p.n_slices + s;
+  if (threadIdx.x == 0) p.listed[slot] = n;
+  if (n > 0) {
+    p.parts[slot * 2 * kParts + threadIdx.x] = parts[0][threadIdx.x];
+    if (k_bin >= 0) p.parts[(slot * 2 + 1) * kParts + threadIdx.x] = parts[1][threadIdx.x];
+  }
 }
 template <typename T, int kSlice>
 __global__ __launch_bounds__(kSliceThreads) void sample_collect_kernel(Params p) {
@@ -467,101 +539,129 @@ __global__ __launch_bounds__(kSliceThreads) void sample_collect_kernel(Params p)
   collect<T, kSlice * static_cast<int>(sizeof(T)) / 16 / kSliceThreads>(p, r, s);
 }
 
-// ---- 3
+// ---- 4
 struct DrawLds {
-  unsigned long long ranks[kSorted];
-  double upto[kSorted];
-  unsigned long long steps[kBins];
-  int count[kBins];
+  unsigned long long ranks[kHeld];
+  unsigned long long near[kRanked], steps[kRanked];
+  unsigned long long part[kDrawThreads];
+  int part_count[kDrawThreads];
   double dwaves[kDrawThreads / 64];
   int iwaves[kDrawThreads / 64];
+  unsigned long long low, high, rank;
   double of_slice[kMostSlices];
   unsigned long long cut_steps[kMostSlices];
-  unsigned long long low, high;
+  int listed[kMostSlices];
+  bool unlisted;   // some slice's are not listed
   double d[2];
   int i[4];
 };
-
-// The tokens in the cut bins: from the list, or where it did not hold them from the row.
-template <typename T, typename F>
-__device__ __forceinline__ void each_candidate(const Params &p, int r, int listed, F &&f) {
-  if (listed <= p.list_most) {
-    const Entry *const list = p.lists + static_cast<int64_t>(r) * p.list_most;
-    for (int i = threadIdx.x; i < listed; i += kDrawThreads) f(list[i].key, list[i].index);
-  } else {
-    constexpr int N = 16 / sizeof(T);
+// A row that is drawn from.
+template <typename T>
+struct Drawn {
+  const Params &p;
+  DrawLds &l;
+  const Row &w;
+  int r;
+  double top;
+  int from, upto, k_bin;   // k_bin: -1 where it has no parts of its own
+  __device__ __forceinline__ Place place(uint32_t key) const { return place_of(number_of(of_key(key)), w.per_bin); }
+  __device__ __forceinline__ int parts_of(int bin) const { return bin == k_bin ? kParts : kParts / (upto - from + 1); }
+  __device__ __forceinline__ int first_part(int bin) const { return bin == k_bin ? kParts : (bin - from) * parts_of(bin); }
+  // Calls f(key, index) for the tokens in the cut bins, or for those of them that `in` has.
+  template <typename F>
+  __device__ __forceinline__ void each(Interval in, F &&f) const {
+    // the lists: some threads per slice
+    int set = kDrawThreads;
+    while (set * p.n_slices > kDrawThreads) set >>= 1;
+    const int mine = threadIdx.x / set;
+    if (mine < p.n_slices && l.listed[mine] <= kListed) {
+      const Entry *const list = p.lists + (static_cast<int64_t>(r) * p.n_slices + mine) * kListed;
+#pragma unroll 2
+      for (int i = threadIdx.x & (set - 1); i < l.listed[mine]; i += set) f(list[i].key, list[i].index);
+    }
+    if (!l.unlisted) return;
+    constexpr int N = 16 / sizeof(T), kUnits = 4;   // a slice is the work of 4 waves
     const RowAt<T> row(p, r);
-    for (int at = threadIdx.x * N; at < row.skew + p.vocab; at += kDrawThreads * N) {
-      float x[N];
-      load16(row.grid, at, row.skew, p.vocab, x);
+#pragma unroll 1
+    for (int u = threadIdx.x >> 6; u < p.n_slices * kUnits; u += kDrawThreads / 64) {
+      const int s = u / kUnits;
+      if (l.listed[s] <= kListed) continue;
+      const int begin = s * p.slice + u % kUnits * (p.slice / kUnits), end = begin + p.slice / kUnits;
+#pragma unroll 2
+      for (int at = begin + static_cast<int>(threadIdx.x & 63) * N; at < end; at += 64 * N) {
+        float x[N];
+        load16(row.grid, at, row.skew, p.vocab, x);
+        uint32_t hits = 0;
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (x[i] > -INFINITY) f(key_of(x[i]), static_cast<uint32_t>(at + i - row.skew));
+        for (int i = 0; i < N; ++i)
+          if (x[i] >= in.low && x[i] <= in.high) hits |= 1u << i;
+        while (hits) {
+          const int i = __ffs(hits) - 1;
+          hits &= hits - 1;
+          f(key_of(as_float(row.grid[at + i])), static_cast<uint32_t>(at + i - row.skew));
+        }
+      }
     }
   }
-}
+};
 
 struct Reached {
   unsigned long long rank;   // of the last token
   double weight;             // up to it
+  int part;                  // of its bin
+  int held;                  // tokens of this part, if l.ranks has them all; -1: it does not
 };
-// The last token of bin `bin` (with `n` tokens, weight `before` ahead of it) that is kept: the `left`th one, or (left == 0) the
-// first one at which the weight reaches `goal`.
+// The last token of bin `bin` (with the weight `before` ahead of it) that is kept: the `left`th one, or (left == 0) the first one at which the weight
+// reaches `goal`. It is in one part of the bin; where that has many tokens, they are cut into 256 by their ranks until few are left, and
+// these are compared with each other.
 template <typename T>
-__device__ Reached resolve(const Params &p, int r, int listed, const Row &w, double top, int bin, int n, double before, int left, double goal, DrawLds &l) {
-  unsigned long long low = 0, high = ~0ull;
-  const double end = end_of_bin(bin);
-  const auto in_it = [&](uint32_t key) { return bin_of(top, floor(place_of(of_key(key), w.per_bin))) == bin; };
-  const auto steps_in = [&](uint32_t key) {
-    const double y = place_of(of_key(key), w.per_bin);
-    return steps_of(in_bin(y - floor(y)));
-  };
-  const auto weigh = [&](uint32_t key) { return static_cast<double>(steps_in(key)) * kStep * end; };
-  while (n > kSorted) {
-    // too many to sort: 256 parts of the ranks that there are
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      l.low = ~0ull;
-      l.high = 0;
+__device__ __forceinline__ Reached resolve(const Drawn<T> &row, int bin, double before, int left, double goal) {
+  const Params &p = row.p;
+  DrawLds &l = row.l;
+  const int t = threadIdx.x, n_parts = row.parts_of(bin);
+  const double unit = kStep * middle_of(bin);
+  Reached out;
+  // the part
+  {
+    const int j = t & (kParts - 1), set = t / kParts;
+    unsigned long long steps = 0;
+    int count = 0;
+    if (j < n_parts) {
+      const unsigned long long *const parts = p.parts + static_cast<int64_t>(row.r) * p.n_slices * 2 * kParts + row.first_part(bin) + j;
+#pragma unroll 4
+      for (int s = set; s < p.n_slices; s += kDrawThreads / kParts) {
+        const unsigned long long h = l.listed[s] > 0 ? parts[s * 2 * kParts] : 0;
+        steps += h >> kCountBits;
+        count += static_cast<int>(h & ((1u << kCountBits) - 1));
+      }
     }
-    if (threadIdx.x < kBins) {
-      l.steps[threadIdx.x] = 0;
-      l.count[threadIdx.x] = 0;
+    __syncthreads();
+    l.part[t] = steps;
+    l.part_count[t] = count;
+    if (t == 0) {
+      l.i[0] = INT32_MAX;
+      l.i[1] = 0;
     }
     __syncthreads();
-    unsigned long long least = ~0ull, most = 0;
-    each_candidate<T>(p, r, listed, [&](uint32_t key, uint32_t index) {
-      const unsigned long long rank = rank_of(key, index);
-      if (rank < low || rank > high || !in_it(key)) return;
-      least = rank < least ? rank : least;
-      most = rank > most ? rank : most;
-    });
-    atomicMin(&l.low, least);
-    atomicMax(&l.high, most);
-    __syncthreads();
-    low = l.low;
-    high = l.high;
-    int shift = 0;
-    while (((high - low) >> shift) >= kBins) ++shift;
-    each_candidate<T>(p, r, listed, [&](uint32_t key, uint32_t index) {
-      const unsigned long long rank = rank_of(key, index);
-      if (rank < low || rank > high || !in_it(key)) return;
-      const int part = static_cast<int>((rank - low) >> shift);
-      atomicAdd(&l.count[part], 1);
-      atomicAdd(&l.steps[part], steps_in(key));
-    });
-    __syncthreads();
-    const int t = threadIdx.x < kBins ? threadIdx.x : kBins - 1;
-    const int c = threadIdx.x < kBins ? l.count[t] : 0;
-    const double m = threadIdx.x < kBins ? static_cast<double>(l.steps[t]) * kStep * end : 0.0;
+  }
+  int n = 0;
+  // the first of up to 256 numbers in l.part at which the goal is reached (the last one that has tokens, if rounding leaves none)
+  const auto choose = [&](int sets) {
+    int c = 0;
+    unsigned long long steps = 0;
+    if (t < kParts)
+      for (int set = 0; set < sets; ++set) {
+        c += l.part_count[set * kParts + t];
+        steps += l.part[set * kParts + t];
+      }
+    const double m = static_cast<double>(steps) * unit;
     const int c_upto = block_scan<kDrawThreads>(c, l.iwaves);
     const double m_upto = before + block_scan<kDrawThreads>(m, l.dwaves);
-    if (threadIdx.x == 0) l.i[0] = static_cast<int>((high - low) >> shift);
+    first_thread(c > 0 && (left > 0 ? c_upto >= left : m_upto >= goal), &l.i[0]);
+    last_thread(c > 0, &l.i[1]);
     __syncthreads();
-    if (c > 0 && (left > 0 ? c_upto >= left : m_upto >= goal)) atomicMin(&l.i[0], static_cast<int>(threadIdx.x));
-    __syncthreads();
-    const int part = l.i[0];   // (the last one, if rounding leaves none)
-    if (static_cast<int>(threadIdx.x) == part) {
+    const int part = l.i[0] != INT32_MAX ? l.i[0] : l.i[1];
+    if (t == part) {
       l.i[2] = c;
       l.i[3] = c_upto - c;
       l.d[0] = m_upto - m;
@@ -570,59 +670,129 @@ __device__ Reached resolve(const Params &p, int r, int listed, const Row &w, dou
     n = l.i[2];
     if (left > 0) left -= l.i[3];
     before = l.d[0];
-    const unsigned long long part_low = low + (static_cast<unsigned long long>(part) << shift);
-    const unsigned long long part_high = part_low + ((1ull << shift) - 1);
-    low = part_low;
+    return part;
+  };
+  out.part = choose(kDrawThreads / kParts);
+  out.held = -1;
+  unsigned long long low = 0, high = ~0ull;
+  const Interval in = interval_of(row.top, bin + (out.part - 0.01) / n_parts, bin - 1 + (out.part + 1.01) / n_parts, row.w.per_bin);
+  int n_held = -1;   // tokens in l.ranks, if all that are left are there
+  const auto each = [&](auto &&f) {
+    if (n_held >= 0) {
+      for (int i = t; i < n_held; i += kDrawThreads) {
+        const unsigned long long rank = l.ranks[i];
+        if (rank >= low && rank <= high) f(rank);
+      }
+    } else {
+      row.each(in, [&](uint32_t key, uint32_t index) {
+        const unsigned long long rank = rank_of(key, index);
+        if (rank < low || rank > high) return;
+        const Place a = row.place(key);
+        if (bin_of(row.top, a.bin) == bin && part_of(a.rest, n_parts) == out.part) f(rank);
+      });
+    }
+  };
+  bool whole = true;
+  while (n_held < 0 || n > kRanked) {
+    if (n_held < 0 && n <= kHeld) {
+      if (t == 0) l.i[0] = 0;
+      __syncthreads();
+      each([&](unsigned long long rank) {
+        const int at = atomicAdd(&l.i[0], 1);
+        if (at < kHeld) l.ranks[at] = rank;
+      });
+      __syncthreads();
+      n_held = l.i[0] < kHeld ? l.i[0] : kHeld;
+      if (whole) out.held = n_held;
+      continue;
+    }
+    whole = false;
+    __syncthreads();
+    if (t == 0) {
+      l.low = ~0ull;
+      l.high = ~0ull;
+      l.i[0] = INT32_MAX;
+      l.i[1] = 0;
+    }
+    if (t < kParts) {
+      l.part[t] = 0;
+      l.part_count[t] = 0;
+    }
+    __syncthreads();
+    unsigned long long least = ~0ull, most = 0;
+    each([&](unsigned long long rank) {
+      least = rank < least ? rank : least;
+      most = rank > most ? rank : most;
+    });
+    least = wave_min(least, ~0ull);
+    most = wave_min(~most, ~0ull);   // (the complement of the largest)
+    if ((t & 63) == 0) {
+      atomicMin(&l.low, least);
+      atomicMin(&l.high, most);
+    }
+    __syncthreads();
+    low = l.low;
+    high = ~l.high;
+    int shift = 0;
+    while (((high - low) >> shift) >= kParts) ++shift;
+    each([&](unsigned long long rank) {
+      const int part = static_cast<int>((rank - low) >> shift);
+      atomicAdd(&l.part_count[part], 1);
+      atomicAdd(&l.part[part], steps_of(row.place(~static_cast<uint32_t>(rank >> 32)).rest));
+    });
+    __syncthreads();
+    low += static_cast<unsigned long long>(choose(1)) << shift;
+    const unsigned long long part_high = low + ((1ull << shift) - 1);
     high = part_high < high ? part_high : high;
   }
+  // the few that are left, and their weights
   __syncthreads();
-  if (threadIdx.x == 0) l.i[0] = 0;
-  __syncthreads();
-  each_candidate<T>(p, r, listed, [&](uint32_t key, uint32_t index) {
-    const unsigned long long rank = rank_of(key, index);
-    if (rank < low || rank > high || !in_it(key)) return;
-    const int at = atomicAdd(&l.i[0], 1);
-    if (at < kSorted) l.ranks[at] = rank;
-  });
-  __syncthreads();
-  n = l.i[0] < kSorted ? l.i[0] : kSorted;
-  int size = 64;
-  while (size < n) size *= 2;
-  for (int i = threadIdx.x; i < size; i += kDrawThreads)
-    if (i >= n) l.ranks[i] = ~0ull;
-  for (int k = 2; k <= size; k *= 2)
-    for (int j = k / 2; j > 0; j /= 2) {
-      __syncthreads();
-      for (int i = threadIdx.x; i < size / 2; i += kDrawThreads) {
-        const int a = (i / j) * 2 * j + i % j, c = a + j;
-        const unsigned long long x = l.ranks[a], y = l.ranks[c];
-        if ((x > y) == ((a & k) == 0)) {
-          l.ranks[a] = y;
-          l.ranks[c] = x;
-        }
-      }
-    }
-  __syncthreads();
-  // weights in that order, two per thread
-  const int a = 2 * threadIdx.x;
-  const double x = a < n ? weigh(~static_cast<uint32_t>(l.ranks[a] >> 32)) : 0.0, y = a + 1 < n ? weigh(~static_cast<uint32_t>(l.ranks[a + 1] >> 32)) : 0.0;
-  const double sum = before + block_scan<kDrawThreads>(x + y, l.dwaves);
-  l.upto[a] = sum - y;
-  l.upto[a + 1] = sum;
-  if (threadIdx.x == 0) l.i[0] = n - 1;
-  __syncthreads();
-  if (left > 0) {
-    if (threadIdx.x == 0) l.i[0] = left < n ? left - 1 : n - 1;
-  } else {
-    for (int i = a; i < a + 2; ++i)
-      if (i < n && l.upto[i] >= goal) {
-        atomicMin(&l.i[0], i);
-        break;
-      }
+  if (t == 0) {
+    l.i[0] = 0;
+    l.rank = 0;
   }
   __syncthreads();
-  const int at = l.i[0] < 0 ? 0 : l.i[0];
-  return Reached{l.ranks[at], l.upto[at]};
+  each([&](unsigned long long rank) {
+    const int at = atomicAdd(&l.i[0], 1);
+    if (at < kRanked) {
+      l.near[at] = rank;
+      l.steps[at] = steps_of(row.place(~static_cast<uint32_t>(rank >> 32)).rest);
+    }
+  });
+  __syncthreads();
+  const int n_near = l.i[0] < kRanked ? l.i[0] : kRanked;
+  constexpr int kSets = kDrawThreads / kRanked;   // threads per token, each compares it with some of the others
+  const int mine = t & (kRanked - 1), set = t / kRanked, each_set = (n_near + kSets - 1) / kSets;
+  const unsigned long long rank = mine < n_near ? l.near[mine] : 0;
+  int ahead = 0;
+  unsigned long long steps = 0;
+#pragma unroll 4
+  for (int j = set * each_set; j < (set + 1) * each_set && j < n_near; ++j) {
+    const bool before_it = l.near[j] < rank;
+    ahead += before_it;
+    steps += before_it ? l.steps[j] : 0;
+  }
+  l.part_count[t] = ahead;
+  l.part[t] = steps;
+  __syncthreads();
+  if (t < n_near) {
+    for (int i = 1; i < kSets; ++i) {
+      ahead += l.part_count[i * kRanked + t];
+      steps += l.part[i * kRanked + t];
+    }
+    const double upto = before + static_cast<double>(steps + l.steps[t]) * unit;
+    // (the last of all, if rounding leaves none)
+    const bool last = left > 0 ? ahead + 1 == (left < n_near ? left : n_near)
+                               : (upto >= goal || ahead + 1 == n_near) && !(before + static_cast<double>(steps) * unit >= goal && ahead > 0);
+    if (last) {
+      l.rank = rank;
+      l.d[0] = upto;
+    }
+  }
+  __syncthreads();
+  out.rank = l.rank;
+  out.weight = l.d[0];
+  return out;
 }
 
 template <typename T>
@@ -644,7 +814,7 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Params p) {
     int first = INT32_MAX;
     for (int i = threadIdx.x & 63; i < p.n_slices; i += 64)
       if (slices[i].most == all.most && slices[i].first < first) first = slices[i].first;
-    first = wave_min(first);
+    first = wave_min(first, INT32_MAX);
     if (threadIdx.x == 0) {
       p.tokens[r] = first;
       if (p.logprob) p.logprob[r] = 0.0f;
@@ -652,149 +822,186 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Params p) {
     return;
   }
   const double unit = w.filtered ? w.per_bin : 0.25 * w.per_bin;   // what the slices' tops are in
-  all.top = floor(place_of(all.most, unit));
+  all.top = place_of(number_of(all.most), unit).bin;
   // ---- the kept tokens: rank <= last, place >= least
   unsigned long long last = ~0ull;
   double least = -INFINITY;
+  static_assert(kMostSlices <= kDrawThreads, "a slice per thread");
+  const int mine_s = threadIdx.x;
   if (!w.filtered) {
-    for (int i = threadIdx.x; i < p.n_slices; i += kDrawThreads)
-      l.of_slice[i] = slices[i].most > -INFINITY ? ldexp(slices[i].sum, static_cast<int>(fmax(slices[i].top - all.top, -2000.0))) : 0.0;
+    if (mine_s < p.n_slices)
+      l.of_slice[mine_s] = slices[mine_s].most > -INFINITY ? ldexp(slices[mine_s].sum, static_cast<int>(fmax(slices[mine_s].top - all.top, -2000.0))) : 0.0;
   } else {
     const Cut &c = p.cuts[r];
-    const int listed = c.listed;
-    if (w.m > 0.0f) least = place_of(all.most, w.per_bin) + 4.0 * log2(static_cast<double>(w.m));
-    int end = kBins;   // bin that has the last kept token
+    const int k_bin = c.k_bin, k_left = c.k_left, p_on = c.p_on;
+    const Drawn<T> row{p, l, w, r, all.top, c.from, c.upto, c.k_too ? k_bin : -1};
+    const bool any_parts = row.from < kBins || row.k_bin >= 0;
+    const int listed = any_parts && mine_s < p.n_slices ? p.listed[static_cast<int64_t>(r) * p.n_slices + mine_s] : 0;
+    if (mine_s < p.n_slices) {
+      l.listed[mine_s] = listed;
+      l.cut_steps[mine_s] = 0;
+    }
+    const bool unlisted = __syncthreads_or(listed > kListed);
+    if (mine_s == 0) l.unlisted = unlisted;
+    __syncthreads();
+    if (w.m > 0.0f) least = least_of(all.most, w);
+    int end = kBins, end_part = 0, held = -1;   // bin and part that have the last kept token
     double goal = 0.0;
     const auto weight_ahead = [&](int b) { return b > 0 ? c.upto_weight[b - 1] : 0.0; };
     const auto tokens_in = [&](int b) { return c.upto_count[b] - (b > 0 ? c.upto_count[b - 1] : 0); };
-    // top-k's last token is looked for where it can be the last one, and where top-p takes a share of the weight up to it
-    double kept = c.all;
-    if (c.k_bin < kBins) {
-      kept = c.upto_weight[c.k_bin];
-      if (c.k_bin <= c.upto || (c.p_on && tokens_in(c.k_bin) > c.k_left)) {
-        const Reached at = resolve<T>(p, r, listed, w, all.top, c.k_bin, tokens_in(c.k_bin), weight_ahead(c.k_bin), c.k_left, 0.0, l);
-        last = at.rank;
-        kept = at.weight;
-        end = c.k_bin;
+    // first top-k's last token, where it can be the last one and where top-p takes a share of the weight up to it; then top-p's
+    double kept = k_bin < kBins ? c.upto_weight[k_bin] : c.all;
+#pragma unroll 1
+    for (int turn = 0; turn < 2; ++turn) {
+      int bin = k_bin, left = k_left;
+      if (turn == 0) {
+        if (bin == kBins || (bin > row.upto && row.k_bin < 0)) continue;
+      } else {
+        if (!p_on || row.from == kBins) break;
+        goal = static_cast<double>(w.p) * kept;
+        left = 0;
+        bin = row.from;
+        while (bin < row.upto && c.upto_weight[bin] < goal) ++bin;
+        // (where min-p ends ahead of it, the bin has no token that counts)
+        if (tokens_in(bin) == 0 || c.upto_weight[bin] < goal * (1.0 - 1e-9)) break;
       }
-    }
-    if (c.p_on && c.from < kBins) {
-      goal = static_cast<double>(w.p) * kept;
-      int b = c.from;
-      while (b < c.upto && c.upto_weight[b] < goal) ++b;
-      // (where min-p ends ahead of it, the bin has no token that counts)
-      if (b < kBins && tokens_in(b) > 0 && c.upto_weight[b] >= goal * (1.0 - 1e-9)) {
-        const Reached at = resolve<T>(p, r, listed, w, all.top, b, tokens_in(b), weight_ahead(b), 0, goal, l);
-        if (at.rank < last) last = at.rank;
-        if (b < end) end = b;
+      const Reached at = resolve<T>(row, bin, weight_ahead(bin), left, goal);
+      if (turn == 0) kept = at.weight;
+      if (at.rank < last) {
+        last = at.rank;
+        end = bin;
+        end_part = at.part;
+        held = at.held;
+      } else {
+        held = -1;
       }
     }
     if (w.m > 0.0f) {
-      const int m_bin = bin_of(all.top, floor(least));
-      if (m_bin < end) end = m_bin;
+      const int m_bin = bin_of(all.top, rint(least)), m_part = m_bin <= row.upto && row.upto < kBins ? part_of(least - rint(least), row.parts_of(m_bin)) : 0;
+      if (m_bin < end || (m_bin == end && m_part < end_part)) {
+        end = m_bin;
+        end_part = m_part;
+        held = -1;
+      }
     }
-    // ---- the slices' kept weights: all bins ahead of `end`, and what is kept in it
-    for (int i = threadIdx.x; i < p.n_slices; i += kDrawThreads) l.cut_steps[i] = 0;
-    __syncthreads();
-    if (end < kBins - 1) {
-      const int skew = RowAt<T>(p, r).skew;
-      each_candidate<T>(p, r, listed, [&](uint32_t key, uint32_t index) {
-        const double y = place_of(of_key(key), w.per_bin), f = floor(y);
-        if (bin_of(all.top, f) != end || rank_of(key, index) > last || y < least) return;
-        atomicAdd(&l.cut_steps[(index + skew) / p.slice], steps_of(in_bin(y - f)));
-      });
+    // ---- the slices' kept weights: all bins ahead of `end`, of that the parts ahead of `end_part`, and what is kept in it
+    const bool inside = end < kBins - 1;
+    if (inside) {
+      __syncthreads();
+      const int skew = RowAt<T>(p, r).skew, n_parts = row.parts_of(end);
+      const auto keep = [&](unsigned long long rank) {
+        const Place a = row.place(~static_cast<uint32_t>(rank >> 32));
+        if (rank <= last && a.at >= least) atomicAdd(&l.cut_steps[(static_cast<uint32_t>(rank) + skew) / p.slice], steps_of(a.rest));
+      };
+      if (held >= 0)
+        for (int i = threadIdx.x; i < held; i += kDrawThreads) keep(l.ranks[i]);
+      else
+        row.each(interval_of(all.top, end + (end_part - 0.01) / n_parts, end - 1 + (end_part + 1.01) / n_parts, w.per_bin), [&](uint32_t key, uint32_t index) {
+          const Place a = row.place(key);
+          if (bin_of(all.top, a.bin) == end && part_of(a.rest, n_parts) == end_part) keep(rank_of(key, index));
+        });
     }
     __syncthreads();
     const unsigned long long *const bins = p.bins + static_cast<int64_t>(r) * p.n_slices * kBins;
+    const unsigned long long *const parts = p.parts + static_cast<int64_t>(r) * p.n_slices * 2 * kParts + (inside ? row.first_part(end) : 0);
     const int lane = threadIdx.x & 63;
+#pragma unroll 1
     for (int i = threadIdx.x >> 6; i < p.n_slices; i += kDrawThreads / 64) {
       double sum = 0.0;
+      unsigned long long steps = 0;
       if (slices[i].most > -INFINITY) {
         const int off = behind(all.top, slices[i].top);
 #pragma unroll
         for (int j = 0; j < kBins / 64; ++j) {
           const int b = 64 * j + lane;
-          if (b < kBins - 1 && b + off < end && b + off < kBins - 1) sum += static_cast<double>(bins[i * kBins + b] >> kCountBits) * kStep * end_of_bin(b + off);
+          if (b < kBins - 1 && b + off < end && b + off < kBins - 1) sum += static_cast<double>(bins[i * kBins + b] >> kCountBits) * kStep * middle_of(b + off);
         }
+        if (inside && l.listed[i] > 0)
+#pragma unroll
+          for (int j = 0; j < kParts / 64; ++j)
+            if (64 * j + lane < end_part) steps += parts[i * 2 * kParts + 64 * j + lane] >> kCountBits;
       }
       sum = wave_sum(sum);
-      if (lane == 0) l.of_slice[i] = sum + (end < kBins - 1 ? static_cast<double>(l.cut_steps[i]) * kStep * end_of_bin(end) : 0.0);
+      steps = wave_sum(steps);
+      if (lane == 0) l.of_slice[i] = sum + (inside ? static_cast<double>(steps + l.cut_steps[i]) * kStep * middle_of(end) : 0.0);
     }
   }
   __syncthreads();
-  // ---- the slice
+  // ---- the slice: the first one up to which the weight passes the goal (the last one that has any, if rounding leaves none)
   float u = p.u[r];
   u = u > 0.0f ? (u < 1.0f ? u : 0x1.fffffep-1f) : 0.0f;
-  double total = 0.0;
-  for (int i = 0; i < p.n_slices; ++i) total += l.of_slice[i];
-  const double goal = static_cast<double>(u) * total;
-  double before = 0.0, upto = 0.0;
-  int slice = 0;
-  for (int i = 0; i < p.n_slices; ++i) {
-    const double x = l.of_slice[i];
-    if (x > 0.0) {   // (the last one that has any, if rounding leaves none)
-      slice = i;
-      before = upto;
-    }
-    upto += x;
-    if (upto > goal) break;
-  }
-  // ---- the token: eight neighbours per thread
-  const RowAt<T> row(p, r);
-  const int at = slice * p.slice + 8 * static_cast<int>(threadIdx.x);
-  double weight[8], sum = 0.0;
-#pragma unroll
-  for (int v = 0; v < 8 / N; ++v) {
-    float x[N];
-    if (8 * static_cast<int>(threadIdx.x) < p.slice) {
-      load16(row.grid, at + v * N, row.skew, p.vocab, x);
-    } else {
-#pragma unroll
-      for (int i = 0; i < N; ++i) x[i] = -INFINITY;
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const double y = place_of(x[i], w.per_bin);
-      const bool kept = x[i] > -INFINITY && y >= least && rank_of(key_of(x[i]), at + v * N + i - row.skew) <= last;
-      double one = 0.0;   // as in the slices' sums
-      if (kept && w.filtered) {
-        const double f = floor(y);
-        const int b = bin_of(all.top, f);
-        if (b < kBins - 1) one = static_cast<double>(steps_of(in_bin(y - f))) * kStep * end_of_bin(b);
-      } else if (kept) {
-        const double o = 0.25 * y, f = floor(o);
-        one = ldexp(in_octave(o - f), static_cast<int>(fmax(f - all.top, -2000.0)));
-      }
-      weight[v * N + i] = one;
-      sum += one;
-    }
-  }
-  const double ahead = before + block_scan<kDrawThreads>(sum, l.dwaves) - sum;
-  if (threadIdx.x == 0) {
+  const double x_s = mine_s < p.n_slices ? l.of_slice[mine_s] : 0.0, upto_s = block_scan<kDrawThreads>(x_s, l.dwaves);
+  if (mine_s == kDrawThreads - 1) l.d[0] = upto_s;
+  if (mine_s == 0) {
     l.i[0] = INT32_MAX;
-    l.i[1] = -1;
+    l.i[1] = 0;
+    l.i[2] = INT32_MAX;
+    l.i[3] = -1;
   }
   __syncthreads();
-  double run = ahead;
+  const double total = l.d[0], goal = static_cast<double>(u) * total;
+  first_thread(x_s > 0.0 && upto_s > goal, &l.i[0]);
+  last_thread(x_s > 0.0, &l.i[1]);
+  __syncthreads();
+  const int slice = l.i[0] != INT32_MAX ? l.i[0] : l.i[1];
+  if (mine_s == slice) l.d[1] = upto_s - x_s;
+  __syncthreads();
+  const double before = l.d[1];
+  // ---- the token: 8 neighbours per thread
+  constexpr int kEach = kMostSlice / kDrawThreads;
+  static_assert(kEach == 8 && kEach % N == 0, "");
+  const RowAt<T> row(p, r);
+  const int at = slice * p.slice + kEach * static_cast<int>(threadIdx.x);
+  double weight[kEach], sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) weight[i] = 0.0;
+  if (kEach * static_cast<int>(threadIdx.x) < p.slice) {
+    float x[kEach / N][N];
+#pragma unroll
+    for (int v = 0; v < kEach / N; ++v) load16(row.grid, at + v * N, row.skew, p.vocab, x[v]);
+    const auto kept_place = [&](int i, Place &a) {   // as in the slices' sums
+      const float y = x[i / N][i % N];
+      a = place_of(number_of(y), unit);
+      return y > -INFINITY && rank_of(key_of(y), at + i - row.skew) <= last && a.at >= least;
+    };
+    if (w.filtered) {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        Place a;
+        const bool kept = kept_place(i, a);
+        const int b = bin_of(all.top, a.bin);
+        if (kept && b < kBins - 1) weight[i] = static_cast<double>(steps_of(a.rest)) * kStep * middle_of(b);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        Place a;
+        if (kept_place(i, a)) weight[i] = ldexp(in_octave(a.rest), static_cast<int>(fmax(a.bin - all.top, -2000.0)));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) sum += weight[i];
+  }
+  double run = before + block_scan<kDrawThreads>(sum, l.dwaves) - sum;
   int mine = INT32_MAX, any = -1;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < kEach; ++i) {
     run += weight[i];
     if (weight[i] > 0.0) {
       any = at + i;
       if (run > goal && mine == INT32_MAX) mine = at + i;
     }
   }
-  if (mine != INT32_MAX) atomicMin(&l.i[0], mine);
-  if (any >= 0) atomicMax(&l.i[1], any);
+  first_thread(mine != INT32_MAX, &l.i[2]);
+  last_thread(any >= 0, &l.i[3]);
   __syncthreads();
-  const int token = l.i[0] != INT32_MAX ? l.i[0] : l.i[1];
-  if (token >= at && token < at + 8) {
+  if (static_cast<int>(threadIdx.x) == (l.i[2] != INT32_MAX ? l.i[2] : l.i[3])) {
+    const int token = l.i[2] != INT32_MAX ? mine : any;
     p.tokens[r] = token - row.skew;
     if (p.logprob) {
       double one = 0.0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < kEach; ++i)
         if (token == at + i) one = weight[i];
       p.logprob[r] = static_cast<float>(log(one / total));
     }
@@ -804,26 +1011,27 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Params p) {
 // ---- host
 int slice_of(int64_t rows, int vocab) {
   int s = kMostSlice;
-  while (s > kLeastSlice && rows * ((vocab + s - 1) / s) < 512) s /= 2;
+  while (s > kLeastSlice && rows * ((vocab + s - 1) / s) < 256) s /= 2;
   return s;
 }
 int slices_of(int vocab, int slice) { return (vocab + 7 + slice - 1) / slice; }   // (a row may begin 7 places behind an aligned one)
-int list_of(int vocab) { return vocab < kListMost ? vocab : kListMost; }
 
 struct Space {
-  int slice, n_slices, list_most;
-  int64_t bins, cuts, lists, bytes;   // offsets; the slices are first
+  int slice, n_slices;
+  int64_t bins, parts, cuts, listed, lists, bytes;   // offsets; the slices are first
 };
 Space space_of(int64_t rows, int vocab) {
   Space s;
   const auto up = [](int64_t x) { return (x + 255) / 256 * 256; };
   s.slice = slice_of(rows, vocab);
   s.n_slices = slices_of(vocab, s.slice);
-  s.list_most = list_of(vocab);
-  s.bins = up(rows * s.n_slices * static_cast<int64_t>(sizeof(Slice)));
-  s.cuts = s.bins + rows * s.n_slices * kBins * 8;
-  s.lists = s.cuts + up(rows * static_cast<int64_t>(sizeof(Cut)));
-  s.bytes = s.lists + rows * s.list_most * static_cast<int64_t>(sizeof(Entry));
+  const int64_t all = rows * s.n_slices;
+  s.bins = up(all * static_cast<int64_t>(sizeof(Slice)));
+  s.parts = s.bins + all * kBins * 8;
+  s.cuts = s.parts + all * 2 * kParts * 8;
+  s.listed = s.cuts + up(rows * static_cast<int64_t>(sizeof(Cut)));
+  s.lists = s.listed + up(all * 4);
+  s.bytes = s.lists + all * kListed * static_cast<int64_t>(sizeof(Entry));
   return s;
 }
 
@@ -839,6 +1047,8 @@ int launch(const Params &p, bool filters, hipStream_t s) {
   hipLaunchKernelGGL((sample_slices_kernel<T, kSlice>), grid, dim3(kSliceThreads), 0, s, p);
   SDVG_HIP_CHECK(hipGetLastError());
   if (filters) {
+    hipLaunchKernelGGL(sample_decide_kernel, dim3(p.n_rows), dim3(kBins), 0, s, p);
+    SDVG_HIP_CHECK(hipGetLastError());
     hipLaunchKernelGGL((sample_collect_kernel<T, kSlice>), grid, dim3(kSliceThreads), 0, s, p);
     SDVG_HIP_CHECK(hipGetLastError());
   }
@@ -848,7 +1058,7 @@ int launch(const Params &p, bool filters, hipStream_t s) {
 }
 template <typename T>
 int launch(const Params &p, bool filters, hipStream_t s) {
-  return p.slice == 2048 ? launch<T, 2048>(p, filters, s) : p.slice == 4096 ? launch<T, 4096>(p, filters, s) : launch<T, 8192>(p, filters, s);
+  return p.slice == kLeastSlice ? launch<T, kLeastSlice>(p, filters, s) : launch<T, kMostSlice>(p, filters, s);
 }
 
 }  // namespace
@@ -887,8 +1097,9 @@ extern "C" int sdvg_sample_tokens(const sdvg_sample_args *a, void *workspace, in
   char *const at = static_cast<char *>(workspace);
   const Params p{static_cast<const char *>(a->logits), a->u, a->temperature, a->top_p, a->min_p, a->top_k, a->tokens, a->logprob,
                  a->all_temperature, a->all_top_p, a->all_min_p, a->all_top_k, a->n_rows > 1 ? a->row_stride : 0, a->n_rows, a->vocab, s.slice,
-                 s.n_slices, s.list_most, reinterpret_cast<Slice *>(at), reinterpret_cast<unsigned long long *>(at + s.bins),
-                 reinterpret_cast<Cut *>(at + s.cuts), reinterpret_cast<Entry *>(at + s.lists)};
+                 s.n_slices, reinterpret_cast<Slice *>(at), reinterpret_cast<unsigned long long *>(at + s.bins),
+                 reinterpret_cast<Cut *>(at + s.cuts), reinterpret_cast<unsigned long long *>(at + s.parts), reinterpret_cast<int32_t *>(at + s.listed),
+                 reinterpret_cast<Entry *>(at + s.lists)};
   const bool filters = a->top_k || a->top_p || a->min_p || (a->all_top_k > 0 && a->all_top_k < a->vocab) || a->all_top_p < 1.0f || a->all_min_p > 0.0f;
   hipStream_t q = static_cast<hipStream_t>(stream);
   return a->dtype == SDVG_F32 ? launch<float>(p, filters, q) : a->dtype == SDVG_BF16 ? launch<__bf16>(p, filters, q) : launch<_Float16>(p, filters, q);

@@ -44,8 +44,8 @@ def test_workspace_grows_with_the_rows_and_holds_every_slice(b):  # noqa: F811
     for vocab in (1, 1000, 32000, 262144, 1 << 20):
         for rows in (1, 2, 7, 64, 500, 777):
             n = need(rows, vocab)
-            # a histogram of 256 numbers and a record for every slice of at most 8192 tokens, one list per row
-            assert n >= rows * (-(-vocab // 8192) * (256 * 8 + 32) + 256 * 12 + min(vocab, 16384) * 8)
+            # a record, three histograms of 256 numbers and a list of 1024 tokens for every slice of at most 8192 tokens, and a row's own histogram
+            assert n >= rows * (-(-vocab // 8192) * (3 * 256 * 8 + 32 + 1024 * 8) + 256 * 12)
 
 
 def test_binding_checks(b, monkeypatch):  # noqa: F811
