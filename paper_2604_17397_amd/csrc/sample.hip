@@ -27,9 +27,11 @@ typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 constexpr int kBins = 256;                 // of weight; the last one has all that is lighter, whose weight does not count (2^-63 of the largest)
 constexpr int kCountBits = 14;             // of a slice's bin: tokens below, weight in steps of kStep above
 constexpr double kStep = 0x1p-35;
-constexpr int kCopies = 4;                 // of a histogram, so that neighbours seldom add to one number at once
+// A slice's histogram in LDS: neighbours add to different copies, and what is too light for the bins goes to places of its own per lane, or masked
+// tokens would all wait for one (200 x 150001 tokens, 70 % of them masked: 55 us with 1 copy and 1 place, 38 with 4 copies and 1 place, 30 with both).
+constexpr int kCopies = 4, kPlaces = kBins - 1 + 64;
 constexpr int kSliceThreads = 256, kMostSlice = 8192, kLeastSlice = 4096;
-constexpr int kDrawThreads = 1024, kHeld = 2048, kRanked = 256;   // tokens that are held in LDS, and that are compared with each other
+constexpr int kMostDraw = 1024, kHeld = 2048, kRanked = 256;   // tokens that are held in LDS, and that are compared with each other
 constexpr int kParts = 256;                // of the cut bins
 constexpr int kListed = 1024;              // tokens of a slice's cut bins that are listed; where it has more, they are looked for in the slice again
 constexpr int kMostVocab = 1 << 20, kMostSlices = kMostVocab / kLeastSlice + 1;
@@ -63,7 +65,7 @@ struct Params {
   float all_temperature, all_top_p, all_min_p;
   int32_t all_top_k;
   int64_t row_stride;      // elements
-  int32_t n_rows, vocab, slice, n_slices;
+  int32_t n_rows, vocab, slice, n_slices, filters;
   Slice *slices;           // [row][slice]
   unsigned long long *bins;   // [row][slice][kBins]
   Cut *cuts;               // [row]
@@ -128,6 +130,28 @@ struct RowAt {
     grid = reinterpret_cast<const T *>(a) - skew;
   }
 };
+
+// A slice's logits, kVectors x 16 bytes per thread, neighbours by neighbours. All are asked for before any is waited for, which takes a branch
+// that is the same for all of them.
+template <typename T, int kVectors, int N = 16 / sizeof(T)>
+__device__ __forceinline__ void load_slice(const RowAt<T> &row, const Params &p, int s, float (&x)[kVectors][N]) {
+  const int at = s * p.slice + static_cast<int>(threadIdx.x) * N;
+  if (s * p.slice >= row.skew && (s + 1) * p.slice <= row.skew + p.vocab) {
+    u32x4 w[kVectors];
+#pragma unroll
+    for (int v = 0; v < kVectors; ++v) w[v] = *reinterpret_cast<const u32x4 *>(row.grid + at + v * kSliceThreads * N);
+#pragma unroll
+    for (int v = 0; v < kVectors; ++v) {
+      T t[N];
+      __builtin_memcpy(t, &w[v], 16);
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[v][i] = as_float(t[i]);
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < kVectors; ++v) load16(row.grid, at + v * kSliceThreads * N, row.skew, p.vocab, x[v]);
+  }
+}
 
 // Order-preserving key; -0 is 0.
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -255,7 +279,7 @@ __device__ __forceinline__ void last_thread(bool is, int *found) {
 template <typename T, int kVectors>   // 16-byte vectors per thread
 __device__ __forceinline__ void one_slice(const Params &p, int r, int s) {
   constexpr int N = 16 / sizeof(T);
-  __shared__ unsigned long long hist[kCopies][kBins + 1];
+  __shared__ unsigned long long hist[kCopies][kPlaces];
   __shared__ double sums[kSliceThreads / 64];
   __shared__ float tops[kSliceThreads / 64];
   __shared__ int firsts[kSliceThreads / 64];
@@ -264,8 +288,7 @@ __device__ __forceinline__ void one_slice(const Params &p, int r, int s) {
   float x[kVectors][N];
   float most = -INFINITY;
   bool nan = false;
-#pragma unroll
-  for (int v = 0; v < kVectors; ++v) load16(row.grid, s * p.slice + (v * kSliceThreads + static_cast<int>(threadIdx.x)) * N, row.skew, p.vocab, x[v]);
+  load_slice(row, p, s, x);
   if (w.filtered)
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) hist[i][threadIdx.x] = 0;
@@ -291,6 +314,8 @@ __device__ __forceinline__ void one_slice(const Params &p, int r, int s) {
 #pragma unroll
         for (int i = 0; i < N; ++i) f(x[v][i]);
     };
+    const bool far = most == INFINITY;   // then the others weigh nothing beside it
+    if (far && !w.greedy) each([&](float &y) { y = y == INFINITY ? 0.0f : -INFINITY; });
     if (w.greedy) {
       int first = INT32_MAX;
 #pragma unroll
@@ -307,33 +332,27 @@ __device__ __forceinline__ void one_slice(const Params &p, int r, int s) {
       out.first = first;
     } else if (!w.filtered) {
       const double per_octave = 0.25 * w.per_bin;
-      const double top = out.top = place_of(number_of(most), per_octave).bin;
+      out.top = place_of(number_of(most), per_octave).bin;
+      const double top = far ? 0.0 : out.top;
       double sum = 0.0;
-      const auto add = [&](double y) {   // (-infinity too, whose rest is a NaN: its weight is 0)
-        const Place a = place_of(y, per_octave);
+      each([&](float y) {   // (-infinity too, whose rest is a NaN: its weight is 0)
+        const Place a = place_of(static_cast<double>(y), per_octave);
         sum += ldexp(in_octave(fmax(a.rest, -0.5)), static_cast<int>(fmax(a.bin - top, -2000.0)));
-      };
-      if (most < INFINITY)
-        each([&](float y) { add(static_cast<double>(y)); });
-      else
-        each([&](float y) { sum += y == INFINITY ? in_octave(place_of(0x1p200, per_octave).rest) : 0.0; });
+      });
       sum = wave_sum(sum);
       if (lane == 0) sums[wave] = sum;
       __syncthreads();
       out.sum = 0.0;
       for (int i = 0; i < kSliceThreads / 64; ++i) out.sum += sums[i];
     } else {
-      const double top = out.top = place_of(number_of(most), w.per_bin).bin;
-      unsigned long long *const mine = hist[threadIdx.x % kCopies];
-      // (-infinity comes to the last bin, which is not read)
-      const auto add = [&](double y) {
-        const Place a = place_of(y, w.per_bin);
-        atomicAdd(&mine[bin_of(top, a.bin)], step_and_one(a.rest));
-      };
-      if (most < INFINITY)
-        each([&](float y) { add(static_cast<double>(y)); });
-      else
-        each([&](float y) { add(number_of(y)); });
+      out.top = place_of(number_of(most), w.per_bin).bin;
+      const double top = far ? 0.0 : out.top, lightest = kBins - 1.0 + lane;
+      unsigned long long *mine = hist[threadIdx.x % kCopies];
+      each([&](float y) {
+        const Place a = place_of(static_cast<double>(y), w.per_bin);
+        const int b = static_cast<int>(fmin(top - a.bin, lightest));   // (of -infinity: the lane's own, whether the difference is infinite or a NaN)
+        atomicAdd(&mine[b], step_and_one(a.rest));
+      });
     }
   }
   if (w.filtered) {
@@ -485,8 +504,7 @@ __device__ __forceinline__ void collect(const Params &p, int r, int s) {
   __shared__ int n;
   const RowAt<T> row(p, r);
   float x[kVectors][N];
-#pragma unroll
-  for (int v = 0; v < kVectors; ++v) load16(row.grid, s * p.slice + (v * kSliceThreads + static_cast<int>(threadIdx.x)) * N, row.skew, p.vocab, x[v]);
+  load_slice(row, p, s, x);
   const Row w = row_of(p, r);
   if (!w.filtered) return;
   const Whole all = whole_of(p, r);
@@ -543,12 +561,16 @@ __global__ __launch_bounds__(kSliceThreads) void sample_collect_kernel(Params p)
 struct DrawLds {
   unsigned long long ranks[kHeld];
   unsigned long long near[kRanked], steps[kRanked];
-  unsigned long long part[kDrawThreads];
-  int part_count[kDrawThreads];
-  double dwaves[kDrawThreads / 64];
-  int iwaves[kDrawThreads / 64];
+  unsigned long long part[kMostDraw];
+  int part_count[kMostDraw];
+  double dwaves[kMostDraw / 64];
+  int iwaves[kMostDraw / 64];
   unsigned long long low, high, rank;
   double of_slice[kMostSlices];
+  int off[kMostSlices];       // bins of a slice behind the row's; kBins or more: none that counts
+  double upto_weight[kBins];
+  int upto_count[kBins];
+  float tops[kMostDraw / 64];
   unsigned long long cut_steps[kMostSlices];
   int listed[kMostSlices];
   bool unlisted;   // some slice's are not listed
@@ -556,7 +578,7 @@ struct DrawLds {
   int i[4];
 };
 // A row that is drawn from.
-template <typename T>
+template <typename T, int kDrawThreads>
 struct Drawn {
   const Params &p;
   DrawLds &l;
@@ -614,8 +636,8 @@ struct Reached {
 // The last token of bin `bin` (with the weight `before` ahead of it) that is kept: the `left`th one, or (left == 0) the first one at which the weight
 // reaches `goal`. It is in one part of the bin; where that has many tokens, they are cut into 256 by their ranks until few are left, and
 // these are compared with each other.
-template <typename T>
-__device__ __forceinline__ Reached resolve(const Drawn<T> &row, int bin, double before, int left, double goal) {
+template <typename T, int kDrawThreads>
+__device__ __forceinline__ Reached resolve(const Drawn<T, kDrawThreads> &row, int bin, double before, int left, double goal) {
   const Params &p = row.p;
   DrawLds &l = row.l;
   const int t = threadIdx.x, n_parts = row.parts_of(bin);
@@ -655,8 +677,19 @@ __device__ __forceinline__ Reached resolve(const Drawn<T> &row, int bin, double 
         steps += l.part[set * kParts + t];
       }
     const double m = static_cast<double>(steps) * unit;
-    const int c_upto = block_scan<kDrawThreads>(c, l.iwaves);
-    const double m_upto = before + block_scan<kDrawThreads>(m, l.dwaves);
+    int c_upto = wave_sums(c);
+    double m_upto = wave_sums(m);
+    if (t < kParts && (t & 63) == 63) {
+      l.iwaves[t >> 6] = c_upto;
+      l.dwaves[t >> 6] = m_upto;
+    }
+    __syncthreads();
+    for (int i = 0; i < kParts / 64 - 1; ++i)
+      if (i < t >> 6) {
+        c_upto += l.iwaves[i];
+        m_upto += l.dwaves[i];
+      }
+    m_upto += before;
     first_thread(c > 0 && (left > 0 ? c_upto >= left : m_upto >= goal), &l.i[0]);
     last_thread(c > 0, &l.i[1]);
     __syncthreads();
@@ -795,28 +828,52 @@ __device__ __forceinline__ Reached resolve(const Drawn<T> &row, int bin, double 
   return out;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Params p) {
+template <typename T, int kDrawThreads>
+__global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) {
   constexpr int N = 16 / sizeof(T);
   __shared__ DrawLds l;
-  const int r = blockIdx.x;
+  const int r = blockIdx.x, t = threadIdx.x;
+  static_assert(kMostSlices <= kDrawThreads && kBins <= kDrawThreads, "one per thread");
+  // all that the first kernels wrote is asked for at once (what they left out is not used)
+  const Slice slice_t = t < p.n_slices ? p.slices[static_cast<int64_t>(r) * p.n_slices + t] : Slice{0.0, 0.0, -INFINITY, INT32_MAX, 0, 0};
+  const Cut &c = p.cuts[r];
+  double upto_weight = 0.0, weight_of_all = 0.0;
+  int upto_count = 0, listed = 0, from = 0, upto = 0, k_bin = 0, k_left = 0, p_on = 0, k_too = 0;
+  if (p.filters) {
+    from = c.from;
+    upto = c.upto;
+    k_bin = c.k_bin;
+    k_left = c.k_left;
+    p_on = c.p_on;
+    k_too = c.k_too;
+    weight_of_all = c.all;
+    if (t < kBins) {
+      upto_weight = c.upto_weight[t];
+      upto_count = c.upto_count[t];
+    }
+    if (t < p.n_slices) listed = p.listed[static_cast<int64_t>(r) * p.n_slices + t];
+  }
+  float u = p.u[r];
   const Row w = row_of(p, r);
-  const Slice *const slices = p.slices + static_cast<int64_t>(r) * p.n_slices;
-  Whole all = whole_of(p, r);
+  Whole all{wave_max(slice_t.most), false, 0.0};
+  if ((t & 63) == 0) l.tops[t >> 6] = all.most;
+  all.nan = __syncthreads_or(slice_t.nan);
+  for (int i = 0; i < kDrawThreads / 64; ++i) all.most = fmaxf(all.most, l.tops[i]);
   if (all.nan || all.most == -INFINITY) {
-    if (threadIdx.x == 0) {
+    if (t == 0) {
       p.tokens[r] = -1;
       if (p.logprob) p.logprob[r] = NAN;
     }
     return;
   }
   if (w.greedy) {
-    int first = INT32_MAX;
-    for (int i = threadIdx.x & 63; i < p.n_slices; i += 64)
-      if (slices[i].most == all.most && slices[i].first < first) first = slices[i].first;
-    first = wave_min(first, INT32_MAX);
-    if (threadIdx.x == 0) {
-      p.tokens[r] = first;
+    if (t == 0) l.i[0] = INT32_MAX;
+    __syncthreads();
+    const int first = wave_min(slice_t.most == all.most ? slice_t.first : INT32_MAX, INT32_MAX);
+    if ((t & 63) == 0) atomicMin(&l.i[0], first);
+    __syncthreads();
+    if (t == 0) {
+      p.tokens[r] = l.i[0];
       if (p.logprob) p.logprob[r] = 0.0f;
     }
     return;
@@ -826,31 +883,30 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Params p) {
   // ---- the kept tokens: rank <= last, place >= least
   unsigned long long last = ~0ull;
   double least = -INFINITY;
-  static_assert(kMostSlices <= kDrawThreads, "a slice per thread");
-  const int mine_s = threadIdx.x;
   if (!w.filtered) {
-    if (mine_s < p.n_slices)
-      l.of_slice[mine_s] = slices[mine_s].most > -INFINITY ? ldexp(slices[mine_s].sum, static_cast<int>(fmax(slices[mine_s].top - all.top, -2000.0))) : 0.0;
+    if (t < p.n_slices) l.of_slice[t] = slice_t.most > -INFINITY ? ldexp(slice_t.sum, static_cast<int>(fmax(slice_t.top - all.top, -2000.0))) : 0.0;
   } else {
-    const Cut &c = p.cuts[r];
-    const int k_bin = c.k_bin, k_left = c.k_left, p_on = c.p_on;
-    const Drawn<T> row{p, l, w, r, all.top, c.from, c.upto, c.k_too ? k_bin : -1};
-    const bool any_parts = row.from < kBins || row.k_bin >= 0;
-    const int listed = any_parts && mine_s < p.n_slices ? p.listed[static_cast<int64_t>(r) * p.n_slices + mine_s] : 0;
-    if (mine_s < p.n_slices) {
-      l.listed[mine_s] = listed;
-      l.cut_steps[mine_s] = 0;
+    const Drawn<T, kDrawThreads> row{p, l, w, r, all.top, from, upto, k_too ? k_bin : -1};
+    if (row.from == kBins && row.k_bin < 0) listed = 0;
+    if (t < p.n_slices) {
+      l.listed[t] = listed;
+      l.cut_steps[t] = 0;
+      l.off[t] = slice_t.most > -INFINITY ? behind(all.top, slice_t.top) : kBins;
+    }
+    if (t < kBins) {
+      l.upto_weight[t] = upto_weight;
+      l.upto_count[t] = upto_count;
     }
     const bool unlisted = __syncthreads_or(listed > kListed);
-    if (mine_s == 0) l.unlisted = unlisted;
+    if (t == 0) l.unlisted = unlisted;
     __syncthreads();
     if (w.m > 0.0f) least = least_of(all.most, w);
     int end = kBins, end_part = 0, held = -1;   // bin and part that have the last kept token
     double goal = 0.0;
-    const auto weight_ahead = [&](int b) { return b > 0 ? c.upto_weight[b - 1] : 0.0; };
-    const auto tokens_in = [&](int b) { return c.upto_count[b] - (b > 0 ? c.upto_count[b - 1] : 0); };
+    const auto weight_ahead = [&](int b) { return b > 0 ? l.upto_weight[b - 1] : 0.0; };
+    const auto tokens_in = [&](int b) { return l.upto_count[b] - (b > 0 ? l.upto_count[b - 1] : 0); };
     // first top-k's last token, where it can be the last one and where top-p takes a share of the weight up to it; then top-p's
-    double kept = k_bin < kBins ? c.upto_weight[k_bin] : c.all;
+    double kept = k_bin < kBins ? l.upto_weight[k_bin] : weight_of_all;
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
       int bin = k_bin, left = k_left;
@@ -861,11 +917,11 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Params p) {
         goal = static_cast<double>(w.p) * kept;
         left = 0;
         bin = row.from;
-        while (bin < row.upto && c.upto_weight[bin] < goal) ++bin;
+        while (bin < row.upto && l.upto_weight[bin] < goal) ++bin;
         // (where min-p ends ahead of it, the bin has no token that counts)
-        if (tokens_in(bin) == 0 || c.upto_weight[bin] < goal * (1.0 - 1e-9)) break;
+        if (tokens_in(bin) == 0 || l.upto_weight[bin] < goal * (1.0 - 1e-9)) break;
       }
-      const Reached at = resolve<T>(row, bin, weight_ahead(bin), left, goal);
+      const Reached at = resolve(row, bin, weight_ahead(bin), left, goal);
       if (turn == 0) kept = at.weight;
       if (at.rank < last) {
         last = at.rank;
@@ -909,8 +965,8 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Params p) {
     for (int i = threadIdx.x >> 6; i < p.n_slices; i += kDrawThreads / 64) {
       double sum = 0.0;
       unsigned long long steps = 0;
-      if (slices[i].most > -INFINITY) {
-        const int off = behind(all.top, slices[i].top);
+      const int off = l.off[i];
+      if (off < kBins) {
 #pragma unroll
         for (int j = 0; j < kBins / 64; ++j) {
           const int b = 64 * j + lane;
@@ -928,11 +984,10 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Params p) {
   }
   __syncthreads();
   // ---- the slice: the first one up to which the weight passes the goal (the last one that has any, if rounding leaves none)
-  float u = p.u[r];
   u = u > 0.0f ? (u < 1.0f ? u : 0x1.fffffep-1f) : 0.0f;
-  const double x_s = mine_s < p.n_slices ? l.of_slice[mine_s] : 0.0, upto_s = block_scan<kDrawThreads>(x_s, l.dwaves);
-  if (mine_s == kDrawThreads - 1) l.d[0] = upto_s;
-  if (mine_s == 0) {
+  const double x_s = t < p.n_slices ? l.of_slice[t] : 0.0, upto_s = block_scan<kDrawThreads>(x_s, l.dwaves);
+  if (t == kDrawThreads - 1) l.d[0] = upto_s;
+  if (t == 0) {
     l.i[0] = INT32_MAX;
     l.i[1] = 0;
     l.i[2] = INT32_MAX;
@@ -944,12 +999,11 @@ __global__ __launch_bounds__(kDrawThreads) void sample_draw_kernel(Params p) {
   last_thread(x_s > 0.0, &l.i[1]);
   __syncthreads();
   const int slice = l.i[0] != INT32_MAX ? l.i[0] : l.i[1];
-  if (mine_s == slice) l.d[1] = upto_s - x_s;
+  if (t == slice) l.d[1] = upto_s - x_s;
   __syncthreads();
   const double before = l.d[1];
-  // ---- the token: 8 neighbours per thread
+  // ---- the token: neighbours per thread
   constexpr int kEach = kMostSlice / kDrawThreads;
-  static_assert(kEach == 8 && kEach % N == 0, "");
   const RowAt<T> row(p, r);
   const int at = slice * p.slice + kEach * static_cast<int>(threadIdx.x);
   double weight[kEach], sum = 0.0;
@@ -1014,7 +1068,7 @@ int slice_of(int64_t rows, int vocab) {
   while (s > kLeastSlice && rows * ((vocab + s - 1) / s) < 256) s /= 2;
   return s;
 }
-int slices_of(int vocab, int slice) { return (vocab + 7 + slice - 1) / slice; }   // (a row may begin 7 places behind an aligned one)
+int slices_of(int vocab, int slice, int skew = 7) { return (vocab + skew + slice - 1) / slice; }   // (a row may begin 7 places behind an aligned one)
 
 struct Space {
   int slice, n_slices;
@@ -1042,23 +1096,28 @@ int check_sizes(int32_t rows, int32_t vocab) {
 }
 
 template <typename T, int kSlice>
-int launch(const Params &p, bool filters, hipStream_t s) {
+int launch(const Params &p, hipStream_t s) {
   const dim3 grid(static_cast<uint32_t>(p.n_rows) * p.n_slices);
   hipLaunchKernelGGL((sample_slices_kernel<T, kSlice>), grid, dim3(kSliceThreads), 0, s, p);
   SDVG_HIP_CHECK(hipGetLastError());
-  if (filters) {
+  if (p.filters) {
     hipLaunchKernelGGL(sample_decide_kernel, dim3(p.n_rows), dim3(kBins), 0, s, p);
     SDVG_HIP_CHECK(hipGetLastError());
     hipLaunchKernelGGL((sample_collect_kernel<T, kSlice>), grid, dim3(kSliceThreads), 0, s, p);
     SDVG_HIP_CHECK(hipGetLastError());
   }
-  hipLaunchKernelGGL((sample_draw_kernel<T>), dim3(p.n_rows), dim3(kDrawThreads), 0, s, p);
+  // (a compute unit takes one workgroup of 1024 threads or two of 512: a row is drawn in fewer rounds with the larger one, rows that come in more
+  // than one round sooner with the smaller one; 1 row of 262144 tokens 26 and 31 us, 200 of 150001 24 and 30, 777 of 32768 53 and 38)
+  if (p.n_rows > 256)
+    hipLaunchKernelGGL((sample_draw_kernel<T, kMostDraw / 2>), dim3(p.n_rows), dim3(kMostDraw / 2), 0, s, p);
+  else
+    hipLaunchKernelGGL((sample_draw_kernel<T, kMostDraw>), dim3(p.n_rows), dim3(kMostDraw), 0, s, p);
   SDVG_HIP_CHECK(hipGetLastError());
   return SDVG_OK;
 }
 template <typename T>
-int launch(const Params &p, bool filters, hipStream_t s) {
-  return p.slice == kLeastSlice ? launch<T, kLeastSlice>(p, filters, s) : launch<T, kMostSlice>(p, filters, s);
+int launch(const Params &p, hipStream_t s) {
+  return p.slice == kLeastSlice ? launch<T, kLeastSlice>(p, s) : launch<T, kMostSlice>(p, s);
 }
 
 }  // namespace
@@ -1095,12 +1154,13 @@ extern "C" int sdvg_sample_tokens(const sdvg_sample_args *a, void *workspace, in
   }
   if (a->logprob && !sdvg::disjoint(a->logprob, n4, a->tokens, n4)) return SDVG_ERR_RANGE;
   char *const at = static_cast<char *>(workspace);
-  const Params p{static_cast<const char *>(a->logits), a->u, a->temperature, a->top_p, a->min_p, a->top_k, a->tokens, a->logprob,
+  Params p{static_cast<const char *>(a->logits), a->u, a->temperature, a->top_p, a->min_p, a->top_k, a->tokens, a->logprob,
                  a->all_temperature, a->all_top_p, a->all_min_p, a->all_top_k, a->n_rows > 1 ? a->row_stride : 0, a->n_rows, a->vocab, s.slice,
-                 s.n_slices, reinterpret_cast<Slice *>(at), reinterpret_cast<unsigned long long *>(at + s.bins),
+                 s.n_slices, 0, reinterpret_cast<Slice *>(at), reinterpret_cast<unsigned long long *>(at + s.bins),
                  reinterpret_cast<Cut *>(at + s.cuts), reinterpret_cast<unsigned long long *>(at + s.parts), reinterpret_cast<int32_t *>(at + s.listed),
                  reinterpret_cast<Entry *>(at + s.lists)};
-  const bool filters = a->top_k || a->top_p || a->min_p || (a->all_top_k > 0 && a->all_top_k < a->vocab) || a->all_top_p < 1.0f || a->all_min_p > 0.0f;
+  if ((reinterpret_cast<uintptr_t>(a->logits) | static_cast<uintptr_t>(p.row_stride * size)) % 16 == 0) p.n_slices = slices_of(a->vocab, s.slice, 0);
+  p.filters = a->top_k || a->top_p || a->min_p || (a->all_top_k > 0 && a->all_top_k < a->vocab) || a->all_top_p < 1.0f || a->all_min_p > 0.0f;
   hipStream_t q = static_cast<hipStream_t>(stream);
-  return a->dtype == SDVG_F32 ? launch<float>(p, filters, q) : a->dtype == SDVG_BF16 ? launch<__bf16>(p, filters, q) : launch<_Float16>(p, filters, q);
+  return a->dtype == SDVG_F32 ? launch<float>(p, q) : a->dtype == SDVG_BF16 ? launch<__bf16>(p, q) : launch<_Float16>(p, q);
 }
