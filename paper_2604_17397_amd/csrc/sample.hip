@@ -15,6 +15,10 @@
 //              the slice with the drawn token from the slices' kept weights, and the token in it.
 // A weight in a histogram is an integer in steps of 2^-35 of its bin's middle, in 64 bits beside the count; without filters it is
 // rounded to 2^-34 of its octave's middle. So it is at most 2^-35 off, equal logits have equal weights, and sums of equal weights are exact.
+//
+// us of the four kernels: 1 row of 32000 tokens, bf16, all filters 4, 5, 5, 20 (chains of latencies: the draw's are some 15 steps of 0.3 to 2); 128 rows of 131072,
+// bf16 17, 6, 13, 27; 200 of 150001, f16, top-p 28, 7, 22, 24; 777 of 32768, fp32 26, 6, 23, 37; 64 of 131072, fp32, no filter 12 and 9. The first kernel without
+// its histogram takes 11, 14 and 20 of the 17, 28 and 26: 18 operations and an atomic per token, and what a launch of so many loads takes to begin and end.
 #include <float.h>
 #include <math.h>
 
@@ -28,16 +32,17 @@ constexpr int kBins = 256;                 // of weight; the last one has all th
 constexpr int kCountBits = 14;             // of a slice's bin: tokens below, weight in steps of kStep above
 constexpr double kStep = 0x1p-35;
 // A slice's histogram in LDS: neighbours add to different copies, and what is too light for the bins goes to places of its own per lane, or masked
-// tokens would all wait for one (200 x 150001 tokens, 70 % of them masked: 55 us with 1 copy and 1 place, 38 with 4 copies and 1 place, 30 with both).
+// tokens would all wait for one (200 x 150001 tokens, 70 % of them masked: 86 us with 1 copy and 1 place, 38 with 4 copies and 1 place, 30 with both).
 constexpr int kCopies = 4, kPlaces = kBins - 1 + 64;
-constexpr int kSliceThreads = 256, kMostSlice = 8192, kLeastSlice = 4096;
+// Tokens of a slice. (Half as many, twice as many slices: 1 row of 32000 tokens 33.6 us for 34.8, 1 of 262144 45 for 40.)
+constexpr int kSlice = 8192, kSliceThreads = 256;
 constexpr int kMostDraw = 1024, kHeld = 2048, kRanked = 256;   // tokens that are held in LDS, and that are compared with each other
 constexpr int kParts = 256;                // of the cut bins
 constexpr int kListed = 1024;              // tokens of a slice's cut bins that are listed; where it has more, they are looked for in the slice again
-constexpr int kMostVocab = 1 << 20, kMostSlices = kMostVocab / kLeastSlice + 1;
+constexpr int kMostVocab = 1 << 20, kMostSlices = kMostVocab / kSlice + 1;
 
 struct Slice {
-  double top;       // floor of the largest x in bins, or in octaves (no filter)
+  double top;       // middle of the bin, or octave (no filter), of the largest x
   double sum;       // weights relative to 2^top (no filter)
   float most;       // largest logit; -infinity: none
   int32_t first;    // its lowest index (greedy)
@@ -65,7 +70,7 @@ struct Params {
   float all_temperature, all_top_p, all_min_p;
   int32_t all_top_k;
   int64_t row_stride;      // elements
-  int32_t n_rows, vocab, slice, n_slices, filters;
+  int32_t n_rows, vocab, n_slices, filters;
   Slice *slices;           // [row][slice]
   unsigned long long *bins;   // [row][slice][kBins]
   Cut *cuts;               // [row]
@@ -135,8 +140,8 @@ struct RowAt {
 // that is the same for all of them.
 template <typename T, int kVectors, int N = 16 / sizeof(T)>
 __device__ __forceinline__ void load_slice(const RowAt<T> &row, const Params &p, int s, float (&x)[kVectors][N]) {
-  const int at = s * p.slice + static_cast<int>(threadIdx.x) * N;
-  if (s * p.slice >= row.skew && (s + 1) * p.slice <= row.skew + p.vocab) {
+  const int at = s * kSlice + static_cast<int>(threadIdx.x) * N;
+  if (s * kSlice >= row.skew && (s + 1) * kSlice <= row.skew + p.vocab) {
     u32x4 w[kVectors];
 #pragma unroll
     for (int v = 0; v < kVectors; ++v) w[v] = *reinterpret_cast<const u32x4 *>(row.grid + at + v * kSliceThreads * N);
@@ -322,7 +327,7 @@ __device__ __forceinline__ void one_slice(const Params &p, int r, int s) {
       for (int v = 0; v < kVectors; ++v)
 #pragma unroll
         for (int i = N - 1; i >= 0; --i) {
-          const int at = s * p.slice + (v * kSliceThreads + static_cast<int>(threadIdx.x)) * N + i - row.skew;
+          const int at = s * kSlice + (v * kSliceThreads + static_cast<int>(threadIdx.x)) * N + i - row.skew;
           if (x[v][i] == most && at < first) first = at;
         }
       first = wave_min(first, INT32_MAX);
@@ -364,7 +369,7 @@ __device__ __forceinline__ void one_slice(const Params &p, int r, int s) {
   }
   if (threadIdx.x == 0) p.slices[static_cast<int64_t>(r) * p.n_slices + s] = out;
 }
-template <typename T, int kSlice>
+template <typename T>
 __global__ __launch_bounds__(kSliceThreads) void sample_slices_kernel(Params p) {
   const int r = blockIdx.x / p.n_slices, s = blockIdx.x - r * p.n_slices;
   one_slice<T, kSlice * static_cast<int>(sizeof(T)) / 16 / kSliceThreads>(p, r, s);
@@ -531,7 +536,7 @@ __device__ __forceinline__ void collect(const Params &p, int r, int s) {
   while (hits) {
     const int j = __ffs(hits) - 1;
     hits &= hits - 1;
-    const int place = s * p.slice + (j / N * kSliceThreads + static_cast<int>(threadIdx.x)) * N + j % N;
+    const int place = s * kSlice + (j / N * kSliceThreads + static_cast<int>(threadIdx.x)) * N + j % N;
     const float y = as_float(row.grid[place]);
     const Place q = place_of(number_of(y), w.per_bin);
     const int bin = bin_of(top, q.bin);
@@ -551,7 +556,7 @@ __device__ __forceinline__ void collect(const Params &p, int r, int s) {
     if (k_bin >= 0) p.parts[(slot * 2 + 1) * kParts + threadIdx.x] = parts[1][threadIdx.x];
   }
 }
-template <typename T, int kSlice>
+template <typename T>
 __global__ __launch_bounds__(kSliceThreads) void sample_collect_kernel(Params p) {
   const int r = blockIdx.x / p.n_slices, s = blockIdx.x - r * p.n_slices;
   collect<T, kSlice * static_cast<int>(sizeof(T)) / 16 / kSliceThreads>(p, r, s);
@@ -608,7 +613,7 @@ struct Drawn {
     for (int u = threadIdx.x >> 6; u < p.n_slices * kUnits; u += kDrawThreads / 64) {
       const int s = u / kUnits;
       if (l.listed[s] <= kListed) continue;
-      const int begin = s * p.slice + u % kUnits * (p.slice / kUnits), end = begin + p.slice / kUnits;
+      const int begin = s * kSlice + u % kUnits * (kSlice / kUnits), end = begin + kSlice / kUnits;
 #pragma unroll 2
       for (int at = begin + static_cast<int>(threadIdx.x & 63) * N; at < end; at += 64 * N) {
         float x[N];
@@ -947,7 +952,7 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
       const int skew = RowAt<T>(p, r).skew, n_parts = row.parts_of(end);
       const auto keep = [&](unsigned long long rank) {
         const Place a = row.place(~static_cast<uint32_t>(rank >> 32));
-        if (rank <= last && a.at >= least) atomicAdd(&l.cut_steps[(static_cast<uint32_t>(rank) + skew) / p.slice], steps_of(a.rest));
+        if (rank <= last && a.at >= least) atomicAdd(&l.cut_steps[(static_cast<uint32_t>(rank) + skew) / kSlice], steps_of(a.rest));
       };
       if (held >= 0)
         for (int i = threadIdx.x; i < held; i += kDrawThreads) keep(l.ranks[i]);
@@ -1003,13 +1008,13 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
   __syncthreads();
   const double before = l.d[1];
   // ---- the token: neighbours per thread
-  constexpr int kEach = kMostSlice / kDrawThreads;
+  constexpr int kEach = kSlice / kDrawThreads;
   const RowAt<T> row(p, r);
-  const int at = slice * p.slice + kEach * static_cast<int>(threadIdx.x);
+  const int at = slice * kSlice + kEach * static_cast<int>(threadIdx.x);
   double weight[kEach], sum = 0.0;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) weight[i] = 0.0;
-  if (kEach * static_cast<int>(threadIdx.x) < p.slice) {
+  if (kEach * static_cast<int>(threadIdx.x) < kSlice) {
     float x[kEach / N][N];
 #pragma unroll
     for (int v = 0; v < kEach / N; ++v) load16(row.grid, at + v * N, row.skew, p.vocab, x[v]);
@@ -1063,22 +1068,16 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
 }
 
 // ---- host
-int slice_of(int64_t rows, int vocab) {
-  int s = kMostSlice;
-  while (s > kLeastSlice && rows * ((vocab + s - 1) / s) < 256) s /= 2;
-  return s;
-}
-int slices_of(int vocab, int slice, int skew = 7) { return (vocab + skew + slice - 1) / slice; }   // (a row may begin 7 places behind an aligned one)
+int slices_of(int vocab, int skew = 7) { return (vocab + skew + kSlice - 1) / kSlice; }   // (a row may begin 7 places behind an aligned one)
 
 struct Space {
-  int slice, n_slices;
+  int n_slices;
   int64_t bins, parts, cuts, listed, lists, bytes;   // offsets; the slices are first
 };
 Space space_of(int64_t rows, int vocab) {
   Space s;
   const auto up = [](int64_t x) { return (x + 255) / 256 * 256; };
-  s.slice = slice_of(rows, vocab);
-  s.n_slices = slices_of(vocab, s.slice);
+  s.n_slices = slices_of(vocab);
   const int64_t all = rows * s.n_slices;
   s.bins = up(all * static_cast<int64_t>(sizeof(Slice)));
   s.parts = s.bins + all * kBins * 8;
@@ -1091,19 +1090,19 @@ Space space_of(int64_t rows, int vocab) {
 
 int check_sizes(int32_t rows, int32_t vocab) {
   if (rows < 0 || vocab < 1) return SDVG_ERR_SHAPE;
-  if (vocab > kMostVocab || static_cast<int64_t>(rows) * slices_of(vocab, kMostSlice) >= (1 << 23)) return SDVG_ERR_UNSUPPORTED;
+  if (vocab > kMostVocab || static_cast<int64_t>(rows) * slices_of(vocab) >= (1 << 23)) return SDVG_ERR_UNSUPPORTED;
   return SDVG_OK;
 }
 
-template <typename T, int kSlice>
+template <typename T>
 int launch(const Params &p, hipStream_t s) {
   const dim3 grid(static_cast<uint32_t>(p.n_rows) * p.n_slices);
-  hipLaunchKernelGGL((sample_slices_kernel<T, kSlice>), grid, dim3(kSliceThreads), 0, s, p);
+  hipLaunchKernelGGL((sample_slices_kernel<T>), grid, dim3(kSliceThreads), 0, s, p);
   SDVG_HIP_CHECK(hipGetLastError());
   if (p.filters) {
     hipLaunchKernelGGL(sample_decide_kernel, dim3(p.n_rows), dim3(kBins), 0, s, p);
     SDVG_HIP_CHECK(hipGetLastError());
-    hipLaunchKernelGGL((sample_collect_kernel<T, kSlice>), grid, dim3(kSliceThreads), 0, s, p);
+    hipLaunchKernelGGL((sample_collect_kernel<T>), grid, dim3(kSliceThreads), 0, s, p);
     SDVG_HIP_CHECK(hipGetLastError());
   }
   // (a compute unit takes one workgroup of 1024 threads or two of 512: a row is drawn in fewer rounds with the larger one, rows that come in more
@@ -1115,11 +1114,6 @@ int launch(const Params &p, hipStream_t s) {
   SDVG_HIP_CHECK(hipGetLastError());
   return SDVG_OK;
 }
-template <typename T>
-int launch(const Params &p, hipStream_t s) {
-  return p.slice == kLeastSlice ? launch<T, kLeastSlice>(p, s) : launch<T, kMostSlice>(p, s);
-}
-
 }  // namespace
 
 extern "C" int64_t sdvg_sample_tokens_workspace_bytes(int32_t n_rows, int32_t vocab) {
@@ -1155,11 +1149,11 @@ extern "C" int sdvg_sample_tokens(const sdvg_sample_args *a, void *workspace, in
   if (a->logprob && !sdvg::disjoint(a->logprob, n4, a->tokens, n4)) return SDVG_ERR_RANGE;
   char *const at = static_cast<char *>(workspace);
   Params p{static_cast<const char *>(a->logits), a->u, a->temperature, a->top_p, a->min_p, a->top_k, a->tokens, a->logprob,
-                 a->all_temperature, a->all_top_p, a->all_min_p, a->all_top_k, a->n_rows > 1 ? a->row_stride : 0, a->n_rows, a->vocab, s.slice,
+                 a->all_temperature, a->all_top_p, a->all_min_p, a->all_top_k, a->n_rows > 1 ? a->row_stride : 0, a->n_rows, a->vocab,
                  s.n_slices, 0, reinterpret_cast<Slice *>(at), reinterpret_cast<unsigned long long *>(at + s.bins),
                  reinterpret_cast<Cut *>(at + s.cuts), reinterpret_cast<unsigned long long *>(at + s.parts), reinterpret_cast<int32_t *>(at + s.listed),
                  reinterpret_cast<Entry *>(at + s.lists)};
-  if ((reinterpret_cast<uintptr_t>(a->logits) | static_cast<uintptr_t>(p.row_stride * size)) % 16 == 0) p.n_slices = slices_of(a->vocab, s.slice, 0);
+  if ((reinterpret_cast<uintptr_t>(a->logits) | static_cast<uintptr_t>(p.row_stride * size)) % 16 == 0) p.n_slices = slices_of(a->vocab, 0);
   p.filters = a->top_k || a->top_p || a->min_p || (a->all_top_k > 0 && a->all_top_k < a->vocab) || a->all_top_p < 1.0f || a->all_min_p > 0.0f;
   hipStream_t q = static_cast<hipStream_t>(stream);
   return a->dtype == SDVG_F32 ? launch<float>(p, q) : a->dtype == SDVG_BF16 ? launch<__bf16>(p, q) : launch<_Float16>(p, q);
