@@ -33,7 +33,7 @@ typedef enum {
   SDVG_ERR_DEVICE = -6       /* a HIP runtime call failed (see sdvg_last_device_error) */
 } sdvg_status;
 
-enum { SDVG_BF16 = 0, SDVG_F32 = 1, SDVG_F16 = 2, SDVG_E4M3 = 3 }; /* the last two: paged cache only */
+enum { SDVG_BF16 = 0, SDVG_F32 = 1, SDVG_F16 = 2, SDVG_E4M3 = 3 }; /* F16: paged cache and logits only, E4M3: the cache */
 
 /* Key-split policy of sdvg_block_attn_batch (see there). */
 enum { SDVG_SPLIT_NEVER = 0, SDVG_SPLIT_AUTO = 1, SDVG_SPLIT_ALWAYS = 2 };
@@ -456,8 +456,8 @@ int64_t sdvg_paged_attn_workspace_bytes(const sdvg_paged_attn_desc *desc, const 
  *   n_groups  >= 0; with 0 the call is sdvg_paged_attn.
  *   workspace as in sdvg_paged_attn, of sdvg_paged_prefix_attn_workspace_bytes(desc, cache, n_groups) bytes; without one, or with one that is
  *             too small, the call is sdvg_paged_attn with that workspace. A need of 0 means that there is nothing to do.
- * Made for many rows per group (its requests' tokens x the query heads of a key head): every 64 or 128 of them read the shared keys again.
- * Every workgroup looks through all groups and requests. Up to three launches; asynchronous on `stream`.
+ * Made for many rows per group (its requests' tokens x the query heads of a key head): every 128 of them read the shared keys again.
+ * Every workgroup looks through all groups and requests. Two launches; asynchronous on `stream`.
  */
 int sdvg_paged_prefix_attn(const sdvg_paged_attn_desc *desc, const sdvg_paged_kv *cache, const void *q, const int32_t *block_table,
                            const int32_t *q_start, const int32_t *kv_lens, int32_t n_groups, const int32_t *group_start,
@@ -486,7 +486,7 @@ int64_t sdvg_paged_prefix_attn_workspace_bytes(const sdvg_paged_attn_desc *desc,
  *   tokens    device int32 [n_rows]; logprob device float [n_rows], nullable. They must not overlap the inputs or each other (SDVG_ERR_RANGE).
  *   workspace device, 16-byte aligned, of at least sdvg_sample_tokens_workspace_bytes(n_rows, vocab) bytes (SDVG_ERR_RANGE if it is
  *             smaller). Scratch: overlapping calls need their own.
- * 1 <= vocab <= 2^20; n_rows slices of 8192 tokens below some 2^23 (SDVG_ERR_UNSUPPORTED); n_rows may be 0. Two launches, three with any
+ * 1 <= vocab <= 2^20; n_rows slices of 8192 tokens below some 2^23 (SDVG_ERR_UNSUPPORTED); n_rows may be 0. Two launches, four with any
  * filter; asynchronous on `stream`.
  */
 typedef struct {

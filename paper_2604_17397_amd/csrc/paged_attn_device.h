@@ -51,16 +51,23 @@ struct Groups {
   float *part_o, *part_ml;            // their partial results: O [slot][key head][kSharedRows][128], (m, l) [slot][key head][kSharedRows][2]
 
   __device__ __forceinline__ int32_t first(int g, int32_t n_requests) const { return start ? start[g] : g ? n_requests : 0; }
-  // the group that has request r, or -1
-  __device__ __forceinline__ int group_of(int r, int32_t n_requests) const {
+  // The groups of requests b + lane, or -1. All lanes of a wave come here, for one batch of 64 requests after the other; `seen` is the caller's, 0 for
+  // the first: starts that none of the later requests lies ahead of. So all batches together look at every start about once. (us of a call, with
+  // a loop over all starts per batch for the same: 300 groups of 3 requests 327, 3424; 16 of 8 31, 36; 6 of 7 as long; 1 of 128 with the
+  // search 35, compared at once 30.)
+  __device__ __forceinline__ int group_of(int b, int &seen) const {
     if (!start) return 0;
-    int g = -1;
-    for (int i = 0; i <= n; ++i) g += start[i] <= r;
-    return g < n ? g : -1;
-  }
-  __device__ __forceinline__ int32_t keys_of(int r, int32_t n_requests) const {
-    const int g = group_of(r, n_requests);
-    return g < 0 ? 0 : lens[g];
+    const int lane = threadIdx.x & 63;
+    if (n == 1) return start[0] <= b + lane && start[1] > b + lane ? 0 : -1;
+    int g = seen - 1;
+    for (;; seen += 64) {
+      const int s = seen + lane <= n ? start[seen + lane] : INT32_MAX, last = __builtin_amdgcn_readlane(s, 63);
+      int at = 0;   // of these starts, those up to the request
+#pragma unroll
+      for (int d = 32; d > 0; d /= 2) at += __shfl(s, at + d - 1) <= b + lane ? d : 0;
+      g += last <= b + lane ? 64 : at;
+      if (last > b + 63) return g < n ? g : -1;
+    }
   }
 };
 
@@ -177,24 +184,28 @@ __device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readl
 // Found by every wave for itself: lane i looks at request 64 b + i. Batches of 64 requests at a time.
 struct Found {
   pg::Request q;
-  int32_t request, tile, piece, pieces, slot, chunk;   // row tile of the request; slot of its first piece; key tiles of a piece
+  int32_t request, group, tile, piece, pieces, slot, chunk;   // row tile of the request; slot of its first piece; key tiles of a piece
 };
+// Request b + lane, and its group.
 template <int kRowTile, bool kShared>
-__device__ __forceinline__ pg::Request load_request(const First &p, const Groups &gr, int r) {
+__device__ __forceinline__ pg::Request load_request(const First &p, const Groups &gr, int b, int &seen, int &g) {
+  const int r = b + static_cast<int>(threadIdx.x & 63);
+  g = kShared ? gr.group_of(b, seen) : -1;
   if (r >= p.n_requests) return pg::Request{0, 0, 0, 0, 0, 0, 0};
   return pg::request_of(p.q_start[r], p.q_start[r + 1], p.kv_lens[r], p.n_tokens, p.group, kRowTile, p.window, p.capacity,
-                        kShared ? gr.keys_of(r, p.n_requests) : 0);
+                        kShared && g >= 0 ? gr.lens[g] : 0);
 }
 // Number `x` among the items (kItems) or among the row tiles that are joined. kShared: the keys behind the groups' shared ones.
 template <int kRowTile, int kKeyWaves, bool kItems, bool kShared>
 __device__ __forceinline__ bool find(const First &p, const Groups &gr, int x, Found &f) {
   const int lane = threadIdx.x & 63;
-  const pg::Request mine0 = load_request<kRowTile, kShared>(p, gr, lane);
+  int seen0 = 0, g0;
+  const pg::Request mine0 = load_request<kRowTile, kShared>(p, gr, 0, seen0, g0);
   int32_t chunk = INT32_MAX;
   if (p.target > 0) {
     int64_t total = 0, row_tiles = 0;
-    for (int b = 0; b < p.n_requests; b += 64) {
-      const pg::Request q = b ? load_request<kRowTile, kShared>(p, gr, b + lane) : mine0;
+    for (int b = 0, seen = seen0, g; b < p.n_requests; b += 64) {
+      const pg::Request q = b ? load_request<kRowTile, kShared>(p, gr, b, seen, g) : mine0;
       const int64_t w = pg::work_of(q);
       row_tiles += wave_total(q.row_tiles);
       total += wave_total(static_cast<int>(w & 0xffff)) + (static_cast<int64_t>(wave_total(static_cast<int>(w >> 16))) << 16);
@@ -204,15 +215,15 @@ __device__ __forceinline__ bool find(const First &p, const Groups &gr, int x, Fo
   // items: the full pieces of all requests come before all others
   int n_full = 0;
   if (kItems && p.target > 0)
-    for (int b = 0; b < p.n_requests; b += 64) {
-      const pg::Request q = b ? load_request<kRowTile, kShared>(p, gr, b + lane) : mine0;
+    for (int b = 0, seen = seen0, g; b < p.n_requests; b += 64) {
+      const pg::Request q = b ? load_request<kRowTile, kShared>(p, gr, b, seen, g) : mine0;
       n_full += wave_total(pg::numbers_of(q, pg::full_pieces(q, chunk), 0, pg::kFull));
     }
   const pg::Range range = !kItems ? pg::kSplit : x < n_full ? pg::kFull : pg::kRest;
   if (range == pg::kRest) x -= n_full;
   int before = 0, slots_before = 0;
-  for (int b = 0; b < p.n_requests; b += 64) {
-    const pg::Request q = b ? load_request<kRowTile, kShared>(p, gr, b + lane) : mine0;
+  for (int b = 0, seen = seen0, g = g0; b < p.n_requests; b += 64) {
+    const pg::Request q = b ? load_request<kRowTile, kShared>(p, gr, b, seen, g) : mine0;
     const int32_t full = pg::full_pieces(q, chunk), pieces = pg::pieces_of(q, chunk, full);
     const int32_t slots = pg::slots_of(q, pieces, kShared);
     const int32_t mine = pg::numbers_of(q, full, pieces, range, kShared);
@@ -224,6 +235,7 @@ __device__ __forceinline__ bool find(const First &p, const Groups &gr, int x, Fo
       const auto get = [src](int v) { return __builtin_amdgcn_readlane(v, src); };
       f.q = pg::Request{get(q.row0), get(q.n), get(q.len), get(q.first_tile), get(q.tiles), get(q.row_tiles), kShared ? get(q.from) : 0};
       f.request = b + src;
+      f.group = kShared ? get(g) : -1;
       f.pieces = get(pieces);
       const pg::Place at_x = pg::place_of(f.q, get(at), get(full), range, p.by_heads.d);
       f.tile = at_x.tile;

@@ -1,17 +1,26 @@
 // Attention of a batch over a paged cache where groups of requests share their first keys (a prompt and its continuations): the
-// shared keys are read once for all rows of a group, the others as in paged_attn.hip, and a third launch joins both.
+// shared keys are read once for all rows of a group, the others as in paged_attn.hip, and a second launch joins both.
 //
 // What bounds it: the rows of a group that share a key head (new tokens x query heads of the key head, over all its requests) are one
 // matrix, so the shared keys cost 4 x 128 FLOP per row and key and 512 bytes per key and key head in 16 bits: the HBM's time below some
 // 150 rows per key head, the matrix cores' above.
 //
-// A workgroup is 4 waves with 32 rows each, RW of them with rows of their own; 4 / RW sets of waves share the keys of a tile. K and V tiles of 64 keys lie in LDS, the next
+// A workgroup has 128 of these rows, 32 for each of its 4 waves, so that a key is read again for every 128 rows; the last one, where it has no
+// more than 64, has two sets of waves with half of every key tile each. K and V tiles of 64 keys lie in LDS, the next
 // one on its way while one is used: 16-bit rows are copied there by the load itself, e4m3 rows pass registers, where they
 // become 16-bit numbers, once for all waves.
 //   S^T = K Q^T with v_mfma_f32_32x32x16: a lane then has 16 scores of one row (lane % 32), keys 8 g + 4 (lane / 32) .. + 3, g = 0 .. 3.
 //   O^T = V^T P^T: those are the B operand of this product as they are, if V^T's keys are read in the same order, which the
-//     transposing read from LDS does.
+//     transposing read from LDS does. P goes in as two 16-bit numbers, the rounded one and what that leaves: a third more products than one
+//     number takes, for an error that is the result's own rounding.
 // The 16-byte chunks of a row are permuted by the row's number (block_attn_index.h has the same), so that no read meets a bank twice.
+//
+// us (kernel and join): 128 requests of one token behind 8191 shared keys, 32 query and 8 key heads, f16 74 + 12; 64 behind 65520 keys, 40 / 8 heads, bf16
+// 160 + 13, 0.9 PFLOP/s with the second number of P counted: a wave has 3072 cycles of products in a tile's 5000 or so, next to another wave of its SIMD; the rest is
+// the softmax, which the two waves do at the same time as often as not, and barriers (121 cycles, the copies' own wait 23). One row of 12 heads 9 + 6, a
+// chain of latencies. Not kept: key tiles of 32 in a ring of four (these three cases with 90, 202 and 15 us a call, against 83, 170 and 15), the
+// scores of a 32-key step ahead of the probabilities of the one before (88, 202; registers spill), row tiles of even size (183 and 181), raised wave priority
+// around the products (no difference).
 #include "block_attn_index.h"
 #include "paged_attn_device.h"
 #include "paged_prefix_plan.h"
@@ -465,8 +474,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_prefix_join_kernel(First f
   if (!find<kRowTile, kWaves / HS, false, true>(first, gr, index, f)) return;
   const int left = f.q.n * first.group - f.tile * kRowTile, rows = left < kRowTile ? left : kRowTile;
   FoundShared s{};
-  const int g = gr.group_of(f.request, first.n_requests);
-  if (g >= 0 && !find_shared<false>(first, gr, groups, g, s)) s = FoundShared{};   // (no slots)
+  if (f.group >= 0 && !find_shared<false>(first, gr, groups, f.group, s)) s = FoundShared{};   // (no slots)
   const int64_t own_step = static_cast<int64_t>(heads) * kRowTile, shared_step = static_cast<int64_t>(heads) * pg::kSharedRows;
   const int d4 = threadIdx.x & 31, set = threadIdx.x >> 5, sub = set % per, at_once = kSets / per;
   for (int row0 = blockIdx.y * at_once; row0 < rows; row0 += gridDim.y * at_once) {   // (all threads come round as often)
@@ -535,6 +543,8 @@ Layout layout_of(int n_cu, const sdvg_paged_attn_desc &d, const sdvg_paged_kv &c
   w.own_tile = row_tile_of(d.n_requests, d.n_tokens, group);
   w.sets = head_sets(c, w.own_tile);
   w.target = target_of(n_cu, d, c, w.own_tile);
+  // (two workgroups per compute unit, which is what fits; us of a call, 128 x 8191 keys and 64 x 65520: 83 and 170, one per unit 74 and 231, three for two
+  // units 76 and 181, four 89 and 181)
   w.shared_target = 2 * n_cu / c.n_kv_heads > 1 ? 2 * n_cu / c.n_kv_heads : 1;
   const int64_t tiles = pg::max_row_tiles(d.n_requests, d.n_tokens, group, w.own_tile);
   w.own_items = pg::max_items(tiles, w.target, capacity_of(d, c), kWaves / w.sets);

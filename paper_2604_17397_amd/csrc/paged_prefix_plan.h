@@ -3,8 +3,8 @@
 //
 // The rows of a group that share a key head (the new tokens of all its requests x the query heads of a key head) are cut into tiles
 // of kSharedRows rows, the shared keys into pieces of `chunk` key tiles at most; a third more where the last row tile has no more than half
-// of the rows, whose key tiles take some three quarters of the time (half the products, the same copies). Every item (row tile, piece) leaves a partial result in a numbered slot; a row tile's are
-// consecutive.
+// of the rows, whose key tiles take some three quarters of the time (half the products, the same copies; 64 x 65520 keys of 320 rows 183 us with pieces of one
+// length, 174 so). Every item (row tile, piece) leaves a partial result in a numbered slot; a row tile's are consecutive.
 #pragma once
 #include "paged_attn_plan.h"
 
@@ -94,7 +94,8 @@ SDVG_PAGED_HD int64_t max_shared_items(int64_t row_tiles, int32_t target, int64_
 }
 
 // The launch has blocks of both kinds, the shared keys' and the requests' own, in turns of kTurn blocks (one for every compute unit, and
-// a multiple of the 8 XCDs, to which a block's number modulo 8 stays the same); what one kind has more comes last.
+// a multiple of the 8 XCDs, to which a block's number modulo 8 stays the same); what one kind has more comes last. (us of a call: 128 x 8191 shared keys 83, 64 x
+// 65520 171, 24 requests of up to 8 tokens 88; in turns of 8 blocks 85, 255, 139, of 64 81, 171, 92, all the shared ones first 95, 176, 83.)
 constexpr int kTurn = 256;
 struct Turn {
   bool shared;

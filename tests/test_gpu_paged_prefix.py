@@ -340,3 +340,11 @@ def test_pool_past_32_bits():
                 assert ((got[r, h] - p @ y[r, :, h].double()).abs() <= 2.0**-7 * (p @ y[r, :, h].double().abs())).all()
         del pools, k, v, c
         torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("sizes", [[2] * 200, [0] * 300 + [1] + [0] * 70 + [64, 65] + [0] * 129, [1] * 64 + [3] * 64 + [0, 0, 130]],
+                         ids=["many", "empty ones", "batches"])
+def test_more_groups_than_a_wave_has_lanes(sizes):
+    case = Shared([(11 * i % 190, [(1 + (i + j) % 40, 1) for j in range(n)]) for i, n in enumerate(sizes)], 4, 2, 16, pool="head")
+    case.check()
+    case.check(window=70)
