@@ -239,15 +239,17 @@ __device__ __forceinline__ V wave_scan(V x, V none, F &&join) {   // inclusive
   return join(moved<0x143, 0xc>(x, none), x);
 }
 template <typename V>
-__device__ __forceinline__ V of_last_lane(V x) {
+__device__ __forceinline__ V of_lane(V x, int lane) {   // (the same lane for all)
   if constexpr (sizeof(V) == 4) {
-    return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+    return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
   } else {
     const unsigned long long a = __builtin_bit_cast(unsigned long long, x);
-    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(a), 63), hi = __builtin_amdgcn_readlane(static_cast<int>(a >> 32), 63);
+    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(a), lane), hi = __builtin_amdgcn_readlane(static_cast<int>(a >> 32), lane);
     return __builtin_bit_cast(V, static_cast<unsigned long long>(hi) << 32 | lo);
   }
 }
+template <typename V>
+__device__ __forceinline__ V of_last_lane(V x) { return of_lane(x, 63); }
 template <typename V>
 __device__ __forceinline__ V wave_sums(V x) {
   return wave_scan(x, V(0), [](V a, V b) { return a + b; });
@@ -287,7 +289,7 @@ __device__ __forceinline__ void one_slice(const Params &p, int r, int s) {
   __shared__ unsigned long long hist[kCopies][kPlaces];
   __shared__ double sums[kSliceThreads / 64];
   __shared__ float tops[kSliceThreads / 64];
-  __shared__ int firsts[kSliceThreads / 64];
+  __shared__ int firsts[kSliceThreads / 64], nans[kSliceThreads / 64];
   const Row w = row_of(p, r);
   const RowAt<T> row(p, r);
   float x[kVectors][N];
@@ -306,9 +308,17 @@ __device__ __forceinline__ void one_slice(const Params &p, int r, int s) {
     }
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   most = wave_max(most);
-  if (lane == 0) tops[wave] = most;
-  const bool any_nan = __syncthreads_or(nan);
-  for (int i = 0; i < kSliceThreads / 64; ++i) most = fmaxf(most, tops[i]);
+  const bool wave_nan = __any(nan);
+  if (lane == 0) {
+    tops[wave] = most;
+    nans[wave] = wave_nan;
+  }
+  __syncthreads();
+  bool any_nan = false;
+  for (int i = 0; i < kSliceThreads / 64; ++i) {
+    most = fmaxf(most, tops[i]);
+    any_nan |= nans[i] != 0;
+  }
   Slice out{};
   out.most = most;
   out.nan = any_nan;
@@ -572,14 +582,14 @@ struct DrawLds {
   int iwaves[kMostDraw / 64];
   unsigned long long low, high, rank;
   double of_slice[kMostSlices];
-  int off[kMostSlices];       // bins of a slice behind the row's; kBins or more: none that counts
+  double top_of_slice[kMostSlices];   // -infinity: it has no token
   double upto_weight[kBins];
   int upto_count[kBins];
   float tops[kMostDraw / 64];
+  int flags[kMostDraw / 64];
   unsigned long long cut_steps[kMostSlices];
   int listed[kMostSlices];
-  bool unlisted;   // some slice's are not listed
-  double d[2];
+  double d;
   int i[4];
 };
 // A row that is drawn from.
@@ -591,31 +601,33 @@ struct Drawn {
   int r;
   double top;
   int from, upto, k_bin;   // k_bin: -1 where it has no parts of its own
+  bool unlisted;           // some slice's tokens are not listed
+  int lanes;               // threads per slice that read its list
+  Entry mine;              // first one that this thread reads
   __device__ __forceinline__ Place place(uint32_t key) const { return place_of(number_of(of_key(key)), w.per_bin); }
   __device__ __forceinline__ int parts_of(int bin) const { return bin == k_bin ? kParts : kParts / (upto - from + 1); }
   __device__ __forceinline__ int first_part(int bin) const { return bin == k_bin ? kParts : (bin - from) * parts_of(bin); }
   // Calls f(key, index) for the tokens in the cut bins, or for those of them that `in` has.
   template <typename F>
-  __device__ __forceinline__ void each(Interval in, F &&f) const {
-    // the lists: some threads per slice
-    int set = kDrawThreads;
-    while (set * p.n_slices > kDrawThreads) set >>= 1;
-    const int mine = threadIdx.x / set;
-    if (mine < p.n_slices && l.listed[mine] <= kListed) {
-      const Entry *const list = p.lists + (static_cast<int64_t>(r) * p.n_slices + mine) * kListed;
-#pragma unroll 2
-      for (int i = threadIdx.x & (set - 1); i < l.listed[mine]; i += set) f(list[i].key, list[i].index);
+  __device__ __forceinline__ void each(int t, int r, Interval in, F &&f) const {
+    const int s_mine = t / lanes, n = s_mine < p.n_slices && l.listed[s_mine] <= kListed ? l.listed[s_mine] : 0;
+    const Entry *const list = p.lists + (static_cast<int64_t>(r) * p.n_slices + s_mine) * kListed;
+    Entry e = mine;
+#pragma unroll 1
+    for (int i = t & (lanes - 1); i < n; i += lanes) {
+      if (i >= lanes) e = list[i];
+      f(e.key, e.index);
     }
-    if (!l.unlisted) return;
+    if (!unlisted) return;
     constexpr int N = 16 / sizeof(T), kUnits = 4;   // a slice is the work of 4 waves
     const RowAt<T> row(p, r);
 #pragma unroll 1
-    for (int u = threadIdx.x >> 6; u < p.n_slices * kUnits; u += kDrawThreads / 64) {
+    for (int u = t >> 6; u < p.n_slices * kUnits; u += kDrawThreads / 64) {
       const int s = u / kUnits;
       if (l.listed[s] <= kListed) continue;
       const int begin = s * kSlice + u % kUnits * (kSlice / kUnits), end = begin + kSlice / kUnits;
-#pragma unroll 2
-      for (int at = begin + static_cast<int>(threadIdx.x & 63) * N; at < end; at += 64 * N) {
+#pragma unroll 1
+      for (int at = begin + (t & 63) * N; at < end; at += 64 * N) {
         float x[N];
         load16(row.grid, at, row.skew, p.vocab, x);
         uint32_t hits = 0;
@@ -645,7 +657,9 @@ template <typename T, int kDrawThreads>
 __device__ __forceinline__ Reached resolve(const Drawn<T, kDrawThreads> &row, int bin, double before, int left, double goal) {
   const Params &p = row.p;
   DrawLds &l = row.l;
-  const int t = threadIdx.x, n_parts = row.parts_of(bin);
+  int t = threadIdx.x, r = row.r;
+  asm volatile("" : "+v"(t), "+s"(r));   // (or what depends on them alone would be held in registers across both calls)
+  const int n_parts = row.parts_of(bin);
   const double unit = kStep * middle_of(bin);
   Reached out;
   // the part
@@ -654,7 +668,7 @@ __device__ __forceinline__ Reached resolve(const Drawn<T, kDrawThreads> &row, in
     unsigned long long steps = 0;
     int count = 0;
     if (j < n_parts) {
-      const unsigned long long *const parts = p.parts + static_cast<int64_t>(row.r) * p.n_slices * 2 * kParts + row.first_part(bin) + j;
+      const unsigned long long *const parts = p.parts + static_cast<int64_t>(r) * p.n_slices * 2 * kParts + row.first_part(bin) + j;
 #pragma unroll 4
       for (int s = set; s < p.n_slices; s += kDrawThreads / kParts) {
         const unsigned long long h = l.listed[s] > 0 ? parts[s * 2 * kParts] : 0;
@@ -666,49 +680,55 @@ __device__ __forceinline__ Reached resolve(const Drawn<T, kDrawThreads> &row, in
     l.part[t] = steps;
     l.part_count[t] = count;
     if (t == 0) {
-      l.i[0] = INT32_MAX;
-      l.i[1] = 0;
+      l.i[0] = l.i[1] = 0;
+      l.rank = 0;
     }
     __syncthreads();
   }
-  int n = 0;
-  // the first of up to 256 numbers in l.part at which the goal is reached (the last one that has tokens, if rounding leaves none)
+  int n = 0;   // tokens that are left
+  // the first of 256 numbers in l.part at which the goal is reached (the last one that has tokens, if rounding leaves none): every wave looks
+  // for itself, 4 numbers per lane
   const auto choose = [&](int sets) {
-    int c = 0;
-    unsigned long long steps = 0;
-    if (t < kParts)
+    constexpr int kOwn = kParts / 64;
+    const int lane = t & 63;
+    int c[kOwn], c_upto[kOwn], c_sum = 0;
+    double m[kOwn], m_upto[kOwn], m_sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+      unsigned long long steps = 0;
+      c[i] = 0;
       for (int set = 0; set < sets; ++set) {
-        c += l.part_count[set * kParts + t];
-        steps += l.part[set * kParts + t];
+        c[i] += l.part_count[set * kParts + kOwn * lane + i];
+        steps += l.part[set * kParts + kOwn * lane + i];
       }
-    const double m = static_cast<double>(steps) * unit;
-    int c_upto = wave_sums(c);
-    double m_upto = wave_sums(m);
-    if (t < kParts && (t & 63) == 63) {
-      l.iwaves[t >> 6] = c_upto;
-      l.dwaves[t >> 6] = m_upto;
+      m[i] = static_cast<double>(steps) * unit;
+      c_upto[i] = c_sum += c[i];
+      m_upto[i] = m_sum += m[i];
     }
-    __syncthreads();
-    for (int i = 0; i < kParts / 64 - 1; ++i)
-      if (i < t >> 6) {
-        c_upto += l.iwaves[i];
-        m_upto += l.dwaves[i];
+    const int c_ahead = wave_sums(c_sum) - c_sum;
+    const double m_ahead = before + (wave_sums(m_sum) - m_sum);
+    int first = kOwn, last = -1;
+#pragma unroll
+    for (int i = kOwn - 1; i >= 0; --i)
+      if (c[i] > 0) {
+        if (left > 0 ? c_ahead + c_upto[i] >= left : m_ahead + m_upto[i] >= goal) first = i;
+        if (last < 0) last = i;
       }
-    m_upto += before;
-    first_thread(c > 0 && (left > 0 ? c_upto >= left : m_upto >= goal), &l.i[0]);
-    last_thread(c > 0, &l.i[1]);
-    __syncthreads();
-    const int part = l.i[0] != INT32_MAX ? l.i[0] : l.i[1];
-    if (t == part) {
-      l.i[2] = c;
-      l.i[3] = c_upto - c;
-      l.d[0] = m_upto - m;
-    }
-    __syncthreads();
-    n = l.i[2];
-    if (left > 0) left -= l.i[3];
-    before = l.d[0];
-    return part;
+    const unsigned long long reached = __ballot(first < kOwn), any = __ballot(last >= 0);
+    const int src = reached ? __ffsll(reached) - 1 : any ? 63 - __clzll(any) : 0, i_mine = reached ? first : last < 0 ? 0 : last;
+    int c_mine = 0, c_before = 0;
+    double m_before = 0.0;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i)
+      if (i == i_mine) {
+        c_mine = c[i];
+        c_before = c_ahead + c_upto[i] - c[i];
+        m_before = m_ahead + (m_upto[i] - m[i]);
+      }
+    n = of_lane(c_mine, src);
+    if (left > 0) left -= of_lane(c_before, src);
+    before = of_lane(m_before, src);
+    return kOwn * src + of_lane(i_mine, src);
   };
   out.part = choose(kDrawThreads / kParts);
   out.held = -1;
@@ -722,7 +742,7 @@ __device__ __forceinline__ Reached resolve(const Drawn<T, kDrawThreads> &row, in
         if (rank >= low && rank <= high) f(rank);
       }
     } else {
-      row.each(in, [&](uint32_t key, uint32_t index) {
+      row.each(t, r, in, [&](uint32_t key, uint32_t index) {
         const unsigned long long rank = rank_of(key, index);
         if (rank < low || rank > high) return;
         const Place a = row.place(key);
@@ -730,15 +750,16 @@ __device__ __forceinline__ Reached resolve(const Drawn<T, kDrawThreads> &row, in
       });
     }
   };
+  const auto hold = [&](unsigned long long rank, unsigned long long *ranks, int most, int *count) {
+    const int at = atomicAdd(count, 1);
+    if (at >= most) return;
+    ranks[at] = rank;
+    if (at < kRanked) l.steps[at] = steps_of(row.place(~static_cast<uint32_t>(rank >> 32)).rest);
+  };
   bool whole = true;
   while (n_held < 0 || n > kRanked) {
     if (n_held < 0 && n <= kHeld) {
-      if (t == 0) l.i[0] = 0;
-      __syncthreads();
-      each([&](unsigned long long rank) {
-        const int at = atomicAdd(&l.i[0], 1);
-        if (at < kHeld) l.ranks[at] = rank;
-      });
+      each([&](unsigned long long rank) { hold(rank, l.ranks, kHeld, &l.i[0]); });
       __syncthreads();
       n_held = l.i[0] < kHeld ? l.i[0] : kHeld;
       if (whole) out.held = n_held;
@@ -749,8 +770,6 @@ __device__ __forceinline__ Reached resolve(const Drawn<T, kDrawThreads> &row, in
     if (t == 0) {
       l.low = ~0ull;
       l.high = ~0ull;
-      l.i[0] = INT32_MAX;
-      l.i[1] = 0;
     }
     if (t < kParts) {
       l.part[t] = 0;
@@ -784,29 +803,21 @@ __device__ __forceinline__ Reached resolve(const Drawn<T, kDrawThreads> &row, in
     high = part_high < high ? part_high : high;
   }
   // the few that are left, and their weights
-  __syncthreads();
-  if (t == 0) {
-    l.i[0] = 0;
-    l.rank = 0;
+  const bool here = n_held <= kRanked;
+  if (!here) {
+    each([&](unsigned long long rank) { hold(rank, l.near, kRanked, &l.i[1]); });
+    __syncthreads();
   }
-  __syncthreads();
-  each([&](unsigned long long rank) {
-    const int at = atomicAdd(&l.i[0], 1);
-    if (at < kRanked) {
-      l.near[at] = rank;
-      l.steps[at] = steps_of(row.place(~static_cast<uint32_t>(rank >> 32)).rest);
-    }
-  });
-  __syncthreads();
-  const int n_near = l.i[0] < kRanked ? l.i[0] : kRanked;
+  const unsigned long long *const near = here ? l.ranks : l.near;
+  const int n_near = here ? n_held : l.i[1] < kRanked ? l.i[1] : kRanked;
   constexpr int kSets = kDrawThreads / kRanked;   // threads per token, each compares it with some of the others
   const int mine = t & (kRanked - 1), set = t / kRanked, each_set = (n_near + kSets - 1) / kSets;
-  const unsigned long long rank = mine < n_near ? l.near[mine] : 0;
+  const unsigned long long rank = mine < n_near ? near[mine] : 0;
   int ahead = 0;
   unsigned long long steps = 0;
 #pragma unroll 4
   for (int j = set * each_set; j < (set + 1) * each_set && j < n_near; ++j) {
-    const bool before_it = l.near[j] < rank;
+    const bool before_it = near[j] < rank;
     ahead += before_it;
     steps += before_it ? l.steps[j] : 0;
   }
@@ -824,12 +835,12 @@ __device__ __forceinline__ Reached resolve(const Drawn<T, kDrawThreads> &row, in
                                : (upto >= goal || ahead + 1 == n_near) && !(before + static_cast<double>(steps) * unit >= goal && ahead > 0);
     if (last) {
       l.rank = rank;
-      l.d[0] = upto;
+      l.d = upto;
     }
   }
   __syncthreads();
   out.rank = l.rank;
-  out.weight = l.d[0];
+  out.weight = l.d;
   return out;
 }
 
@@ -860,10 +871,39 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
   }
   float u = p.u[r];
   const Row w = row_of(p, r);
+  // the lists: some threads per slice
+  int lanes = kDrawThreads;
+  while (lanes * p.n_slices > kDrawThreads) lanes >>= 1;
+  static_assert(kDrawThreads <= kListed, "a thread's first entry lies in its slice's list");
+  Entry mine_e{0, 0};
+  if (p.filters && t / lanes < p.n_slices) mine_e = p.lists[(static_cast<int64_t>(r) * p.n_slices + t / lanes) * kListed + (t & (lanes - 1))];
+  if (!w.filtered || (from == kBins && !k_too)) listed = 0;
+  if (t < p.n_slices) {
+    l.listed[t] = listed;
+    l.cut_steps[t] = 0;
+    l.top_of_slice[t] = slice_t.most > -INFINITY ? slice_t.top : -INFINITY;
+  }
+  if (t < kBins) {
+    l.upto_weight[t] = upto_weight;
+    l.upto_count[t] = upto_count;
+  }
   Whole all{wave_max(slice_t.most), false, 0.0};
-  if ((t & 63) == 0) l.tops[t >> 6] = all.most;
-  all.nan = __syncthreads_or(slice_t.nan);
-  for (int i = 0; i < kDrawThreads / 64; ++i) all.most = fmaxf(all.most, l.tops[i]);
+  const int flags = __any(slice_t.nan) | __any(listed > kListed) << 1;
+  if ((t & 63) == 0) {
+    l.tops[t >> 6] = all.most;
+    l.flags[t >> 6] = flags;
+  }
+  if (t == 0) {
+    l.i[2] = INT32_MAX;
+    l.i[3] = -1;
+  }
+  __syncthreads();
+  int all_flags = 0;
+  for (int i = 0; i < kDrawThreads / 64; ++i) {
+    all.most = fmaxf(all.most, l.tops[i]);
+    all_flags |= l.flags[i];
+  }
+  all.nan = all_flags & 1;
   if (all.nan || all.most == -INFINITY) {
     if (t == 0) {
       p.tokens[r] = -1;
@@ -872,13 +912,11 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
     return;
   }
   if (w.greedy) {
-    if (t == 0) l.i[0] = INT32_MAX;
-    __syncthreads();
     const int first = wave_min(slice_t.most == all.most ? slice_t.first : INT32_MAX, INT32_MAX);
-    if ((t & 63) == 0) atomicMin(&l.i[0], first);
+    if ((t & 63) == 0) atomicMin(&l.i[2], first);
     __syncthreads();
     if (t == 0) {
-      p.tokens[r] = l.i[0];
+      p.tokens[r] = l.i[2];
       if (p.logprob) p.logprob[r] = 0.0f;
     }
     return;
@@ -891,20 +929,7 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
   if (!w.filtered) {
     if (t < p.n_slices) l.of_slice[t] = slice_t.most > -INFINITY ? ldexp(slice_t.sum, static_cast<int>(fmax(slice_t.top - all.top, -2000.0))) : 0.0;
   } else {
-    const Drawn<T, kDrawThreads> row{p, l, w, r, all.top, from, upto, k_too ? k_bin : -1};
-    if (row.from == kBins && row.k_bin < 0) listed = 0;
-    if (t < p.n_slices) {
-      l.listed[t] = listed;
-      l.cut_steps[t] = 0;
-      l.off[t] = slice_t.most > -INFINITY ? behind(all.top, slice_t.top) : kBins;
-    }
-    if (t < kBins) {
-      l.upto_weight[t] = upto_weight;
-      l.upto_count[t] = upto_count;
-    }
-    const bool unlisted = __syncthreads_or(listed > kListed);
-    if (t == 0) l.unlisted = unlisted;
-    __syncthreads();
+    const Drawn<T, kDrawThreads> row{p, l, w, r, all.top, from, upto, k_too ? k_bin : -1, (all_flags & 2) != 0, lanes, mine_e};
     if (w.m > 0.0f) least = least_of(all.most, w);
     int end = kBins, end_part = 0, held = -1;   // bin and part that have the last kept token
     double goal = 0.0;
@@ -957,7 +982,7 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
       if (held >= 0)
         for (int i = threadIdx.x; i < held; i += kDrawThreads) keep(l.ranks[i]);
       else
-        row.each(interval_of(all.top, end + (end_part - 0.01) / n_parts, end - 1 + (end_part + 1.01) / n_parts, w.per_bin), [&](uint32_t key, uint32_t index) {
+        row.each(t, r, interval_of(all.top, end + (end_part - 0.01) / n_parts, end - 1 + (end_part + 1.01) / n_parts, w.per_bin), [&](uint32_t key, uint32_t index) {
           const Place a = row.place(key);
           if (bin_of(all.top, a.bin) == end && part_of(a.rest, n_parts) == end_part) keep(rank_of(key, index));
         });
@@ -970,7 +995,7 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
     for (int i = threadIdx.x >> 6; i < p.n_slices; i += kDrawThreads / 64) {
       double sum = 0.0;
       unsigned long long steps = 0;
-      const int off = l.off[i];
+      const int off = behind(all.top, l.top_of_slice[i]);
       if (off < kBins) {
 #pragma unroll
         for (int j = 0; j < kBins / 64; ++j) {
@@ -990,23 +1015,27 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
   __syncthreads();
   // ---- the slice: the first one up to which the weight passes the goal (the last one that has any, if rounding leaves none)
   u = u > 0.0f ? (u < 1.0f ? u : 0x1.fffffep-1f) : 0.0f;
-  const double x_s = t < p.n_slices ? l.of_slice[t] : 0.0, upto_s = block_scan<kDrawThreads>(x_s, l.dwaves);
-  if (t == kDrawThreads - 1) l.d[0] = upto_s;
-  if (t == 0) {
-    l.i[0] = INT32_MAX;
-    l.i[1] = 0;
-    l.i[2] = INT32_MAX;
-    l.i[3] = -1;
+  int slice = 0;
+  double total = 0.0, before = 0.0;
+  // every wave for itself, 64 slices at a time
+  for (int b = 0; b < p.n_slices; b += 64) {
+    const int i = b + (t & 63);
+    total += wave_sum(i < p.n_slices ? l.of_slice[i] : 0.0);
   }
-  __syncthreads();
-  const double total = l.d[0], goal = static_cast<double>(u) * total;
-  first_thread(x_s > 0.0 && upto_s > goal, &l.i[0]);
-  last_thread(x_s > 0.0, &l.i[1]);
-  __syncthreads();
-  const int slice = l.i[0] != INT32_MAX ? l.i[0] : l.i[1];
-  if (t == slice) l.d[1] = upto_s - x_s;
-  __syncthreads();
-  const double before = l.d[1];
+  const double goal = static_cast<double>(u) * total;
+  double passed = 0.0;
+  for (int b = 0; b < p.n_slices; b += 64) {
+    const int i = b + (t & 63);
+    const double x = i < p.n_slices ? l.of_slice[i] : 0.0, upto_x = passed + wave_sums(x);
+    const unsigned long long any = __ballot(x > 0.0), over = __ballot(x > 0.0 && upto_x > goal);
+    const int src = over ? __ffsll(over) - 1 : any ? 63 - __clzll(any) : -1;
+    if (src >= 0) {
+      slice = b + src;
+      before = of_lane(upto_x - x, src);
+    }
+    if (over) break;
+    passed = of_last_lane(upto_x);
+  }
   // ---- the token: neighbours per thread
   constexpr int kEach = kSlice / kDrawThreads;
   const RowAt<T> row(p, r);
