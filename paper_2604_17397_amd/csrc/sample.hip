@@ -927,7 +927,8 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
   unsigned long long last = ~0ull;
   double least = -INFINITY;
   if (!w.filtered) {
-    if (t < p.n_slices) l.of_slice[t] = slice_t.most > -INFINITY ? ldexp(slice_t.sum, static_cast<int>(fmax(slice_t.top - all.top, -2000.0))) : 0.0;
+    // (a slice in which every token's weight is rounded to 0 has none, whatever their sum is)
+    if (t < p.n_slices) l.of_slice[t] = slice_t.most > -INFINITY && slice_t.top - all.top > -1075.0 ? ldexp(slice_t.sum, static_cast<int>(slice_t.top - all.top)) : 0.0;
   } else {
     const Drawn<T, kDrawThreads> row{p, l, w, r, all.top, from, upto, k_too ? k_bin : -1, (all_flags & 2) != 0, lanes, mine_e};
     if (w.m > 0.0f) least = least_of(all.most, w);

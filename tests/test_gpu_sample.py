@@ -313,3 +313,16 @@ def test_frequencies():
     w = torch.softmax(torch.tensor([1.0, 3.0, -math.inf, 2.0, -math.inf, 2.5], dtype=torch.float64) / 0.8, 0)
     count = torch.bincount(got.long().cpu(), minlength=6).double()
     assert ((count - 65536 * w).abs() <= 1).all()
+
+
+@pytest.mark.parametrize("low", [-745.5, -744.8, -743.0, -700.0, -1e30])
+@pytest.mark.parametrize("u", [0.0, 0.5])
+def test_slices_of_tokens_too_light_for_64_bits(low, u):
+    """Many tokens whose weights are 0, or the smallest numbers, ahead of the one that counts: their sum is no weight where theirs is none."""
+    import paper_2604_17397_amd as P
+    x = torch.full((1, 3 * 8192), low, device="cuda")
+    x[0, 2 * 8192 + 77] = 0.0
+    got = P.sample_tokens(x, torch.tensor([u], device="cuda"), out=torch.full((1,), -7, dtype=torch.int32, device="cuda")).item()
+    # (where one of the smallest numbers is a weight, and where 0, is the rounding's: -744.8 lies between half of it and itself)
+    allowed = {2 * 8192 + 77} if u > 0 or low < -745 else {0} if low > -744 else {0, 2 * 8192 + 77}
+    assert got in allowed
