@@ -1065,7 +1065,7 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
         Place a;
-        if (kept_place(i, a)) weight[i] = ldexp(in_octave(a.rest), static_cast<int>(fmax(a.bin - all.top, -2000.0)));
+        if (kept_place(i, a) && a.bin - all.top > -1075.0) weight[i] = ldexp(in_octave(a.rest), static_cast<int>(a.bin - all.top));   // (lighter: 0)
       }
     }
 #pragma unroll
