@@ -16,9 +16,9 @@
 // A weight in a histogram is an integer in steps of 2^-35 of its bin's middle, in 64 bits beside the count; without filters it is
 // rounded to 2^-34 of its octave's middle. So it is at most 2^-35 off, equal logits have equal weights, and sums of equal weights are exact.
 //
-// us of the four kernels: 1 row of 32000 tokens, bf16, all filters 4, 5, 5, 20 (chains of latencies: the draw's are some 15 steps of 0.3 to 2); 128 rows of 131072,
-// bf16 17, 6, 13, 27; 200 of 150001, f16, top-p 28, 7, 22, 24; 777 of 32768, fp32 26, 6, 23, 37; 64 of 131072, fp32, no filter 12 and 9. The first kernel without
-// its histogram takes 11, 14 and 20 of the 17, 28 and 26: 18 operations and an atomic per token, and what a launch of so many loads takes to begin and end.
+// us of the four kernels: 1 row of 32000 tokens, bf16, all filters 5, 4, 6, 21 (chains of latencies: the draw's are some 15 steps of 0.3 to 2); 128 rows of 131072,
+// bf16 16, 6, 13, 27; 200 of 150001, f16, top-p 27, 6, 22, 23; 777 of 32768, fp32 25, 6, 23, 35; 64 of 131072, fp32, no filter 12 and 8. The first kernel without
+// its histogram takes 10, 13 and 19 of the 16, 27 and 25: 18 operations and an atomic per token, and what a launch of so many loads takes to begin and end.
 #include <float.h>
 #include <math.h>
 
