@@ -198,7 +198,6 @@ __device__ __forceinline__ pg::Request load_request(const First &p, const Groups
 // Number `x` among the items (kItems) or among the row tiles that are joined. kShared: the keys behind the groups' shared ones.
 template <int kRowTile, int kKeyWaves, bool kItems, bool kShared>
 __device__ __forceinline__ bool find(const First &p, const Groups &gr, int x, Found &f) {
-  const int lane = threadIdx.x & 63;
   int seen0 = 0, g0;
   const pg::Request mine0 = load_request<kRowTile, kShared>(p, gr, 0, seen0, g0);
   int32_t chunk = INT32_MAX;

@@ -579,7 +579,6 @@ struct DrawLds {
   unsigned long long part[kMostDraw];
   int part_count[kMostDraw];
   double dwaves[kMostDraw / 64];
-  int iwaves[kMostDraw / 64];
   unsigned long long low, high, rank;
   double of_slice[kMostSlices];
   double top_of_slice[kMostSlices];   // -infinity: it has no token
