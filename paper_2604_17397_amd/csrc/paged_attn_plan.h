@@ -30,13 +30,29 @@ struct Request {
 };
 SDVG_PAGED_HD int32_t clamp(int32_t x, int32_t lo, int32_t hi) { return x < lo ? lo : x > hi ? hi : x; }
 
-// start, end: q_start[r], q_start[r + 1]; capacity: keys that a row of the block table can name.
+// What a request's numbers name, whatever they are (start, end: q_start[r], q_start[r + 1]): n tokens from row0 on among the batch's n_tokens, the
+// last of which sees `len` keys.
+struct Rows {
+  int32_t row0, n, len;
+};
+SDVG_PAGED_HD Rows rows_of(int32_t start, int32_t end, int32_t len, int32_t n_tokens) {
+  Rows a;
+  a.row0 = clamp(start, 0, n_tokens);
+  a.n = clamp(end, a.row0, n_tokens) - a.row0;
+  a.len = len > 0 ? len : 0;
+  return a;
+}
+// Keys that token row0 + i of them sees, 0 <= i < n (none if not positive).
+SDVG_PAGED_HD int32_t sees_of(const Rows &a, int32_t i) { return a.len - a.n + i + 1; }
+
+// capacity: keys that a row of the block table can name.
 SDVG_PAGED_HD Request request_of(int32_t start, int32_t end, int32_t len, int32_t n_tokens, int32_t group, int32_t row_tile,
                                  int32_t window, int64_t capacity, int32_t prefix = 0) {
+  const Rows rows = rows_of(start, end, len, n_tokens);
   Request q;
-  q.row0 = clamp(start, 0, n_tokens);
-  q.n = clamp(end, q.row0, n_tokens) - q.row0;
-  q.len = len > 0 ? len : 0;
+  q.row0 = rows.row0;
+  q.n = rows.n;
+  q.len = rows.len;
   const int64_t first = static_cast<int64_t>(q.len) - q.n + 1 - window;  // of the first token's window
   const int32_t hi = q.len < capacity ? q.len : static_cast<int32_t>(capacity);
   int32_t lo = window > 0 && first > 0 ? static_cast<int32_t>(first) : 0;

@@ -135,20 +135,20 @@ __device__ __forceinline__ bool find_shared(const First &p, const Groups &gr, co
   return false;
 }
 
-// Keys that the row of token `token` sees, from and up to: of the request among f's that has the token. A batch of 64 requests at a time, each
-// lane looks for its token among them in 6 steps. (All lanes of the wave come here.)
+// Keys that the row of token `token` sees, from and up to: of the request among f's that has the token, whose numbers are clamped as for its own
+// keys. A batch of 64 requests at a time, each lane looks for its token among them in 6 steps. (All lanes of the wave come here.)
 __device__ __forceinline__ void seen_by(const First &p, const FoundShared &f, int token, int &from, int &sees) {
   const int lane = threadIdx.x & 63;
   sees = 0;
   for (int b = 0; b < f.q.requests; b += 64) {
     const int r = f.q.request0 + (b + lane < f.q.requests ? b + lane : f.q.requests - 1);
-    const int start = p.q_start[r], end = p.q_start[r + 1], len = p.kv_lens[r];
+    const pg::Rows mine = pg::rows_of(p.q_start[r], p.q_start[r + 1], p.kv_lens[r], p.n_tokens);
     int at = 0;
 #pragma unroll
     for (int step = 32; step > 0; step /= 2)
-      if (__shfl(start, at + step) <= token) at += step;
-    const int s = __shfl(start, at), e = __shfl(end, at), l = __shfl(len, at);
-    if (token >= s && token < e) sees = l - (e - token) + 1;
+      if (__shfl(mine.row0, at + step) <= token) at += step;
+    const pg::Rows q{__shfl(mine.row0, at), __shfl(mine.n, at), __shfl(mine.len, at)};
+    if (token >= q.row0 && token - q.row0 < q.n) sees = pg::sees_of(q, token - q.row0);
   }
   from = p.window > 0 && sees > p.window ? sees - p.window : 0;
 }
