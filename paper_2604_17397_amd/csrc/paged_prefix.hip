@@ -206,14 +206,15 @@ __device__ __forceinline__ void attend_shared(const First &first, const Groups &
     hi = __builtin_amdgcn_readfirstlane(hi < f.q.hi ? hi : f.q.hi);
   }
 
-  // (scores are compared ahead of their scale, which is positive then; -infinity times 0 would be no number)
+  // (scores are compared ahead of their scale, which is positive then; -infinity times 0 would be no number. A scale that is no number makes all scores
+  // none, ahead of the masks)
   float scale = p.scale_log2e * (kF8 && p.k_scale ? p.k_scale[head] : 1.0f);
-  if (scale < 0.f) {
-    scale = -scale;
+  const uint32_t flip = scale < 0.f ? 0x80008000u : 0u, nan = scale != scale ? 0xffffffffu : 0u;
+  if (flip | nan) {
 #pragma unroll
-    for (int s = 0; s < 8; ++s) qf[s] ^= 0x80008000u;
+    for (int s = 0; s < 8; ++s) qf[s] = (qf[s] ^ flip) | nan;
   }
-  scale = fmaxf(scale, 0x1p-126f);
+  scale = fmaxf(fabsf(scale), 0x1p-126f);
   f32x16 o[4];
 #pragma unroll
   for (int d = 0; d < 4; ++d)
