@@ -481,7 +481,8 @@ int64_t sdvg_paged_prefix_attn_workspace_bytes(const sdvg_paged_attn_desc *desc,
  *             nothing but -infinity, gets token -1 and a logprob of NaN.
  *   u         device float [n_rows], in [0, 1); other numbers are clamped, NaN is 0.
  *   temperature, top_k, top_p, min_p  device float / int32 / float / float [n_rows], nullable: then all rows have all_temperature, all_top_k,
- *             all_top_p, all_min_p. temperature <= 0 (or NaN): the token with the largest logit, the lowest index of several, logprob 0. top_k <= 0
+ *             all_top_p, all_min_p. temperature <= 0 (or NaN): the token with the largest logit, the lowest index of several, logprob 0; +infinity: all
+ *             logits that are numbers weigh the same. top_k <= 0
  *             or >= vocab, top_p >= 1 (or NaN) and min_p <= 0 (or NaN) are off; min_p > 1 is 1.
  *   tokens    device int32 [n_rows]; logprob device float [n_rows], nullable. They must not overlap the inputs or each other (SDVG_ERR_RANGE).
  *   workspace device, 16-byte aligned, of at least sdvg_sample_tokens_workspace_bytes(n_rows, vocab) bytes (SDVG_ERR_RANGE if it is

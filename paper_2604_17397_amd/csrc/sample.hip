@@ -80,7 +80,7 @@ struct Params {
 };
 
 struct Row {
-  double per_bin;          // bins per unit of logit
+  double per_bin;          // bins per unit of logit; not 0
   float p, m;
   int k;
   bool greedy, filtered;
@@ -95,9 +95,13 @@ __device__ __forceinline__ Row row_of(const Params &p, int r) {
   if (!(w.m > 0.0f)) w.m = 0.0f;
   if (w.m > 1.0f) w.m = 1.0f;
   if (w.k <= 0 || w.k >= p.vocab) w.k = 0;
+  // An infinite temperature: logits that are numbers weigh the same, so all of them lie within 2^-60 of a bin, and min-p cuts nothing; +infinity is
+  // far from them even then (number_of).
+  const bool hot = t == INFINITY;
+  if (hot) w.m = 0.0f;
   w.greedy = !(t > 0.0f);
   w.filtered = !w.greedy && (w.k > 0 || w.p < 1.0f || w.m > 0.0f);
-  w.per_bin = 4.0 * 1.4426950408889634 / static_cast<double>(t);
+  w.per_bin = hot ? 0x1p-190 : 4.0 * 1.4426950408889634 / static_cast<double>(t);
   return w;
 }
 
@@ -180,7 +184,7 @@ __device__ __forceinline__ Place place_of(double x, double per_bin) {
   a.rest = a.at - a.bin;
   return a;
 }
-__device__ __forceinline__ double number_of(float x) { return x == INFINITY ? 0x1p200 : static_cast<double>(x); }
+__device__ __forceinline__ double number_of(float x) { return x == INFINITY ? 0x1p300 : static_cast<double>(x); }
 __device__ __forceinline__ int bin_of(double top, double bin) { return static_cast<int>(fmin(top - bin, kBins - 1.0)); }   // (a NaN's: the last one)
 
 // 2^(z / 4) for |z| <= 1/2 in steps of kStep, with 1 added in the kCountBits bits below: a polynomial through the function's values at Chebyshev's
