@@ -474,7 +474,7 @@ int64_t sdvg_paged_prefix_attn_workspace_bytes(const sdvg_paged_attn_desc *desc,
  *   min-p: of these the ones with w_i >= min_p;
  *   tokens[r] = the lowest index i for which the sum of the kept weights up to i is more than u[r] times their total.
  * logprob[r] is the natural logarithm of its weight over that total. Weights and sums are held in 64 bits, a weight at most 2^-35
- * of itself off; one below 2^-63 of the largest counts as 0 where there is a filter, and one below 2^-1074 otherwise. The same call gives the same tokens, and so does a row alone
+ * of itself off (2^-34 in a row without filters), however large logit / t is; one below 2^-63 of the largest counts as 0 where there is a filter, and one below 2^-1074 otherwise. The same call gives the same tokens, and so does a row alone
  * or among others, but where u or top_p lie as near to a border as that.
  *   logits    device [n_rows][vocab] of type dtype (SDVG_F32, SDVG_BF16, SDVG_F16), row_stride elements apart (not looked at for one row),
  *             aligned to their own size. -infinity: the token is never drawn; -0 is 0; +infinity is more than all numbers. A row that has a NaN, or

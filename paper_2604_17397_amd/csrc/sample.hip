@@ -14,7 +14,9 @@
 //   4 draw     a workgroup per row: finds the parts in which the cuts lie, compares the few tokens of such a part with each other, then finds
 //              the slice with the drawn token from the slices' kept weights, and the token in it.
 // A weight in a histogram is an integer in steps of 2^-35 of its bin's middle, in 64 bits beside the count; without filters it is
-// rounded to 2^-34 of its octave's middle. So it is at most 2^-35 off, equal logits have equal weights, and sums of equal weights are exact.
+// rounded to 2^-34 of its octave's middle, at most 2^-34.5 of itself. A logit's place on the scale of bins is a product in twice 64 bits, so what all
+// logits of a row have in common, a large number at a low temperature, costs a weight nothing. Equal logits have equal weights, and the sum
+// of up to 2^17 tokens that all have the largest one is exact.
 //
 // us of the four kernels: 1 row of 32000 tokens, bf16, all filters 5, 4, 6, 21 (chains of latencies: the draw's are some 15 steps of 0.3 to 2); 128 rows of 131072,
 // bf16 16, 6, 13, 27; 200 of 150001, f16, top-p 27, 6, 22, 23; 777 of 32768, fp32 25, 6, 23, 35; 64 of 131072, fp32, no filter 12 and 8. The first kernel without
@@ -81,13 +83,14 @@ struct Params {
 
 struct Row {
   double per_bin;          // bins per unit of logit; not 0
-  float p, m;
+  float t, p, m;
   int k;
   bool greedy, filtered;
 };
 __device__ __forceinline__ Row row_of(const Params &p, int r) {
   Row w;
   const float t = p.temperature ? p.temperature[r] : p.all_temperature;
+  w.t = t;
   w.p = p.top_p ? p.top_p[r] : p.all_top_p;
   w.m = p.min_p ? p.min_p[r] : p.all_min_p;
   w.k = p.top_k ? p.top_k[r] : p.all_top_k;
@@ -170,18 +173,24 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); }
 // Larger logits first, of equal ones the lower index.
 __device__ __forceinline__ unsigned long long rank_of(uint32_t key, uint32_t index) { return static_cast<unsigned long long>(~key) << 32 | index; }
-// A logit's place on the scale of bins (or octaves): the middle of its bin, and how far it is from it, -1/2 to 1/2. (+infinity is a number that all
-// others are far from. The product is rounded by itself: a fused subtraction would keep what is beyond it, which is no fraction where the
-// place is a number beyond 2^52.)
+// A logit's place on the scale of bins (or octaves): the nearest bin's middle by the rounded product, and how far from it the product itself is,
+// -1/2 to 1/2 and what its rounding may add. From places of 2^36 on (kFar) that is taken as 0: neighbouring logits in 32 bits are 2^12 bins apart
+// there, so what is not equal to the largest one weighs nothing beside it (596 bins are the lightest weight that min-p can keep, 1075 octaves the
+// lightest number). Places never decrease with the logit, bin by bin and within a bin.
+constexpr double kFar = 0x1p36;
 struct Place {
-  double at, bin, rest;
+  double bin, rest;
 };
-__device__ __forceinline__ Place place_of(double x, double per_bin) {
-#pragma clang fp contract(off)
+// Not of places beyond kFar, whose rest may be anything.
+__device__ __forceinline__ Place near_place_of(double x, double per_bin) {
   Place a;
-  a.at = x * per_bin;
-  a.bin = rint(a.at);
-  a.rest = a.at - a.bin;
+  a.bin = rint(x * per_bin);
+  a.rest = fma(x, per_bin, -a.bin);
+  return a;
+}
+__device__ __forceinline__ Place place_of(double x, double per_bin) {
+  Place a = near_place_of(x, per_bin);
+  if (!(fabs(a.bin) < kFar)) a.rest = 0.0;
   return a;
 }
 __device__ __forceinline__ double number_of(float x) { return x == INFINITY ? 0x1p300 : static_cast<double>(x); }
@@ -333,8 +342,11 @@ __device__ __forceinline__ void one_slice(const Params &p, int r, int s) {
 #pragma unroll
         for (int i = 0; i < N; ++i) f(x[v][i]);
     };
-    const bool far = most == INFINITY;   // then the others weigh nothing beside it
-    if (far && !w.greedy) each([&](float &y) { y = y == INFINITY ? 0.0f : -INFINITY; });
+    const double unit = w.filtered ? w.per_bin : 0.25 * w.per_bin;
+    out.top = place_of(number_of(most), unit).bin;
+    const bool far = fabs(out.top) >= kFar;   // then what is not equal to the largest logit weighs nothing
+    if (far && !w.greedy) each([&](float &y) { y = y == most ? 0.0f : -INFINITY; });
+    const double top = far ? 0.0 : out.top;
     if (w.greedy) {
       int first = INT32_MAX;
 #pragma unroll
@@ -350,13 +362,10 @@ __device__ __forceinline__ void one_slice(const Params &p, int r, int s) {
       for (int i = 0; i < kSliceThreads / 64; ++i) first = firsts[i] < first ? firsts[i] : first;
       out.first = first;
     } else if (!w.filtered) {
-      const double per_octave = 0.25 * w.per_bin;
-      out.top = place_of(number_of(most), per_octave).bin;
-      const double top = far ? 0.0 : out.top;
       double sum = 0.0;
-      each([&](float y) {   // (-infinity too, whose rest is a NaN: its weight is 0)
-        const Place a = place_of(static_cast<double>(y), per_octave);
-        sum += ldexp(in_octave(fmax(a.rest, -0.5)), static_cast<int>(fmax(a.bin - top, -2000.0)));
+      each([&](float y) {   // (far below the largest one, where `rest` is any number, or a NaN for -infinity, the weight is 0)
+        const Place a = near_place_of(static_cast<double>(y), unit);
+        sum += ldexp(in_octave(fmin(fmax(a.rest, -0.75), 0.75)), static_cast<int>(fmax(a.bin - top, -2000.0)));
       });
       sum = wave_sum(sum);
       if (lane == 0) sums[wave] = sum;
@@ -364,11 +373,10 @@ __device__ __forceinline__ void one_slice(const Params &p, int r, int s) {
       out.sum = 0.0;
       for (int i = 0; i < kSliceThreads / 64; ++i) out.sum += sums[i];
     } else {
-      out.top = place_of(number_of(most), w.per_bin).bin;
-      const double top = far ? 0.0 : out.top, lightest = kBins - 1.0 + lane;
+      const double lightest = kBins - 1.0 + lane;
       unsigned long long *mine = hist[threadIdx.x % kCopies];
       each([&](float y) {
-        const Place a = place_of(static_cast<double>(y), w.per_bin);
+        const Place a = near_place_of(static_cast<double>(y), unit);
         const int b = static_cast<int>(fmin(top - a.bin, lightest));   // (of -infinity: the lane's own, whether the difference is infinite or a NaN)
         atomicAdd(&mine[b], step_and_one(a.rest));
       });
@@ -406,8 +414,16 @@ __device__ __forceinline__ Whole whole_of(const Params &p, int r) {   // by ever
   a.nan = __any(a.nan);
   return a;
 }
-// Place of the lightest token that min-p keeps.
-__device__ __forceinline__ double least_of(float most, const Row &w) { return place_of(number_of(most), w.per_bin).at + 4.0 * log2(static_cast<double>(w.m)); }
+// The least number that a logit may be to be kept by min-p: the sum of the largest one and t log(m), rounded up (its rounding error is what the three
+// subtractions find). Rounding keeps the order of numbers, so a kept logit's place is not behind this one's, nor one that is not kept ahead.
+__device__ __forceinline__ double least_of(float most, const Row &w) {
+#pragma clang fp contract(off)
+  const double a = number_of(most), b = static_cast<double>(w.t) * log(static_cast<double>(w.m)), sum = a + b, of_b = sum - a;
+  const double lost = (a - (sum - of_b)) + (b - of_b);
+  if (!(lost > 0.0)) return sum;
+  const long long bits = __double_as_longlong(sum);
+  return __longlong_as_double(sum > 0.0 ? bits + 1 : bits - 1);   // (a sum of 0 is exact)
+}
 // Bins that a slice's are behind the row's.
 __device__ __forceinline__ int behind(double top, double slice_top) { return static_cast<int>(fmin(top - slice_top, 1e6)); }
 
@@ -477,7 +493,7 @@ __global__ __launch_bounds__(kBins) void sample_decide_kernel(Params p) {
     from = upto = k_bin;
   }
   if (w.m > 0.0f) {
-    const int m_bin = bin_of(all.top, rint(least_of(all.most, w)));
+    const int m_bin = bin_of(all.top, place_of(least_of(all.most, w), w.per_bin).bin);
     if (m_bin < from) from = m_bin;
     if (m_bin < upto) upto = m_bin;
   }
@@ -508,7 +524,7 @@ __device__ __forceinline__ Interval interval_of(double top, double first, double
   const double high = (top - first + 0.5) / per_bin, low = (top - last - 0.5) / per_bin;
   return Interval{fmaxf(static_cast<float>(low - fabs(low) * 1e-6 - 3e-45), -FLT_MAX), static_cast<float>(high + fabs(high) * 1e-6 + 3e-45)};
 }
-// A bin's part, of n: the lightest tokens are in the last one.
+// A bin's part, of n: the lightest tokens are in the last one. (`rest` may be past 1/2 by 2^-18, which the conversion makes part 0 as well.)
 __device__ __forceinline__ int part_of(double rest, int n) {
   const int i = static_cast<int>((0.5 - rest) * n);
   return i < n - 1 ? i : n - 1;
@@ -926,7 +942,7 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
   }
   const double unit = w.filtered ? w.per_bin : 0.25 * w.per_bin;   // what the slices' tops are in
   all.top = place_of(number_of(all.most), unit).bin;
-  // ---- the kept tokens: rank <= last, place >= least
+  // ---- the kept tokens: rank <= last, logit >= least
   unsigned long long last = ~0ull;
   double least = -INFINITY;
   if (!w.filtered) {
@@ -967,7 +983,8 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
       }
     }
     if (w.m > 0.0f) {
-      const int m_bin = bin_of(all.top, rint(least)), m_part = m_bin <= row.upto && row.upto < kBins ? part_of(least - rint(least), row.parts_of(m_bin)) : 0;
+      const Place at = place_of(least, w.per_bin);
+      const int m_bin = bin_of(all.top, at.bin), m_part = m_bin <= row.upto && row.upto < kBins ? part_of(at.rest, row.parts_of(m_bin)) : 0;
       if (m_bin < end || (m_bin == end && m_part < end_part)) {
         end = m_bin;
         end_part = m_part;
@@ -980,8 +997,9 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
       __syncthreads();
       const int skew = RowAt<T>(p, r).skew, n_parts = row.parts_of(end);
       const auto keep = [&](unsigned long long rank) {
-        const Place a = row.place(~static_cast<uint32_t>(rank >> 32));
-        if (rank <= last && a.at >= least) atomicAdd(&l.cut_steps[(static_cast<uint32_t>(rank) + skew) / kSlice], steps_of(a.rest));
+        const float x = of_key(~static_cast<uint32_t>(rank >> 32));
+        if (rank <= last && number_of(x) >= least)
+          atomicAdd(&l.cut_steps[(static_cast<uint32_t>(rank) + skew) / kSlice], steps_of(place_of(number_of(x), w.per_bin).rest));
       };
       if (held >= 0)
         for (int i = threadIdx.x; i < held; i += kDrawThreads) keep(l.ranks[i]);
@@ -1054,7 +1072,7 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
     const auto kept_place = [&](int i, Place &a) {   // as in the slices' sums
       const float y = x[i / N][i % N];
       a = place_of(number_of(y), unit);
-      return y > -INFINITY && rank_of(key_of(y), at + i - row.skew) <= last && a.at >= least;
+      return y > -INFINITY && rank_of(key_of(y), at + i - row.skew) <= last && number_of(y) >= least;
     };
     if (w.filtered) {
 #pragma unroll
