@@ -56,6 +56,7 @@ struct Cut {
   int32_t k_bin, k_left;   // bin in which top-k ends, tokens it keeps there; kBins: nowhere
   int32_t p_on, k_too;     // k_too: that bin, behind `upto`, matters for the weight that top-p takes a share of
   double all;              // weight of all tokens
+  double least;            // least number that a logit may be for min-p
   double upto_weight[kBins];   // weight of bins 0 .. b, relative to the middle of bin 0
   int32_t upto_count[kBins];
 };
@@ -414,11 +415,11 @@ __device__ __forceinline__ Whole whole_of(const Params &p, int r) {   // by ever
   a.nan = __any(a.nan);
   return a;
 }
-// The least number that a logit may be to be kept by min-p: the sum of the largest one and t log(m), rounded up (its rounding error is what the three
-// subtractions find). Rounding keeps the order of numbers, so a kept logit's place is not behind this one's, nor one that is not kept ahead.
-__device__ __forceinline__ double least_of(float most, const Row &w) {
+// The least number that a logit may be to be kept by min-p: the sum of the largest one and b = t log(m), rounded up (its rounding error is what the
+// three subtractions find). Rounding keeps the order of numbers, so a kept logit's place is not behind this one's, nor one that is not kept ahead.
+__device__ __forceinline__ double least_of(float most, double b) {
 #pragma clang fp contract(off)
-  const double a = number_of(most), b = static_cast<double>(w.t) * log(static_cast<double>(w.m)), sum = a + b, of_b = sum - a;
+  const double a = number_of(most), sum = a + b, of_b = sum - a;
   const double lost = (a - (sum - of_b)) + (b - of_b);
   if (!(lost > 0.0)) return sum;
   const long long bits = __double_as_longlong(sum);
@@ -450,6 +451,7 @@ __global__ __launch_bounds__(kBins) void sample_decide_kernel(Params p) {
     for (int j = 0; j < kAtOnce; ++j) h[j] = base + j < p.n_slices ? bins[(base + j) * kBins + b] : 0;
   };
   ask(0);
+  const double t_log_m = w.m > 0.0f ? static_cast<double>(w.t) * log(static_cast<double>(w.m)) : 0.0;   // (while the numbers are on their way)
   Whole all = whole_of(p, r);
   if (all.nan || all.most == -INFINITY) return;
   all.top = place_of(number_of(all.most), w.per_bin).bin;
@@ -492,8 +494,9 @@ __global__ __launch_bounds__(kBins) void sample_decide_kernel(Params p) {
   } else if (k_bin < kBins) {
     from = upto = k_bin;
   }
+  const double least = least_of(all.most, t_log_m);
   if (w.m > 0.0f) {
-    const int m_bin = bin_of(all.top, place_of(least_of(all.most, w), w.per_bin).bin);
+    const int m_bin = bin_of(all.top, place_of(least, w.per_bin).bin);
     if (m_bin < from) from = m_bin;
     if (m_bin < upto) upto = m_bin;
   }
@@ -512,6 +515,7 @@ __global__ __launch_bounds__(kBins) void sample_decide_kernel(Params p) {
     c->k_too = p_on && k_inside && k_bin > upto;
     c->p_on = p_on;
     c->all = total;
+    c->least = least;
   }
 }
 
@@ -872,7 +876,7 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
   // all that the first kernels wrote is asked for at once (what they left out is not used)
   const Slice slice_t = t < p.n_slices ? p.slices[static_cast<int64_t>(r) * p.n_slices + t] : Slice{0.0, 0.0, -INFINITY, INT32_MAX, 0, 0};
   const Cut &c = p.cuts[r];
-  double upto_weight = 0.0, weight_of_all = 0.0;
+  double upto_weight = 0.0, weight_of_all = 0.0, least_there = 0.0;
   int upto_count = 0, listed = 0, from = 0, upto = 0, k_bin = 0, k_left = 0, p_on = 0, k_too = 0;
   if (p.filters) {
     from = c.from;
@@ -882,6 +886,7 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
     p_on = c.p_on;
     k_too = c.k_too;
     weight_of_all = c.all;
+    least_there = c.least;
     if (t < kBins) {
       upto_weight = c.upto_weight[t];
       upto_count = c.upto_count[t];
@@ -950,7 +955,7 @@ __global__ __launch_bounds__(kDrawThreads, 4) void sample_draw_kernel(Params p) 
     if (t < p.n_slices) l.of_slice[t] = slice_t.most > -INFINITY && slice_t.top - all.top > -1075.0 ? ldexp(slice_t.sum, static_cast<int>(slice_t.top - all.top)) : 0.0;
   } else {
     const Drawn<T, kDrawThreads> row{p, l, w, r, all.top, from, upto, k_too ? k_bin : -1, (all_flags & 2) != 0, lanes, mine_e};
-    if (w.m > 0.0f) least = least_of(all.most, w);
+    if (w.m > 0.0f) least = least_there;
     int end = kBins, end_part = 0, held = -1;   // bin and part that have the last kept token
     double goal = 0.0;
     const auto weight_ahead = [&](int b) { return b > 0 ? l.upto_weight[b - 1] : 0.0; };
