@@ -55,7 +55,8 @@ def main():
     rc |= run([sys.executable, "-m", "pytest", "-x", "-q", "tests/test_abi.py", "tests/test_paged_abi.py", "tests/test_paged_prefix_host.py", "tests/test_sample_host.py"], env)
     # (3) the host programs over the kernels' index headers
     for name in ("attn_index_replay", "attn_groups_replay", "attn_rows32_replay", "attn_rows32_halves", "attn_split_check",
-                 "row_map_check", "paged_attn_plan", "paged_prefix_items", "paged_rows_of"):
+                 "row_map_check", "paged_attn_plan", "paged_prefix_items", "paged_prefix_own",
+                 "paged_rows_of"):
         exe = os.path.join(tmp, name + "_san")
         rc |= run(["g++", "-O1", "-g", "-std=c++17", "-fopenmp", "-fsanitize=address,undefined", "-fno-omit-frame-pointer",
                    "-I", os.path.join(ROOT, "paper_2604_17397_amd", "csrc"), "-I", os.path.join(ROOT, "include"),
