@@ -456,8 +456,12 @@ int64_t sdvg_paged_attn_workspace_bytes(const sdvg_paged_attn_desc *desc, const 
  *   n_groups  >= 0; with 0 the call is sdvg_paged_attn.
  *   workspace as in sdvg_paged_attn, of sdvg_paged_prefix_attn_workspace_bytes(desc, cache, n_groups) bytes; without one, or with one that is
  *             too small, the call is sdvg_paged_attn with that workspace. A need of 0 means that there is nothing to do.
- * Made for many rows per group (its requests' tokens x the query heads of a key head): every 128 of them read the shared keys again.
- * Every workgroup looks through all groups and requests. Two launches; asynchronous on `stream`.
+ * Numbers out of range are clamped as there, for the shared keys as for the others; where q_start or group_start decrease, rows may miss shared keys.
+ * When it pays: every row goes through the workspace and a second launch, 6 to 15 us of a call, so it is sdvg_paged_attn that is faster where little is
+ * shared. One group, bf16: from some 150000 to 200000 keys on that are not read again, (requests - 1) x shared keys x key heads (16 requests of 12
+ * / 12 heads x 1024 keys 15 us for 17, 64 of 32 / 8 x 16384 79 for 387; but 16 of 32 / 8 x 1024 17 for 14, 2 x 4096 16 for 12). Groups of one request
+ * never gain: 1.1 to 3.4 times the time. Made for many rows per group (its requests' tokens x the query heads of a key head): every 128 of them
+ * read the shared keys again. Every workgroup looks through all groups and requests. Two launches; asynchronous on `stream`.
  */
 int sdvg_paged_prefix_attn(const sdvg_paged_attn_desc *desc, const sdvg_paged_kv *cache, const void *q, const int32_t *block_table,
                            const int32_t *q_start, const int32_t *kv_lens, int32_t n_groups, const int32_t *group_start,
@@ -467,15 +471,16 @@ int64_t sdvg_paged_prefix_attn_workspace_bytes(const sdvg_paged_attn_desc *desc,
 /*
  * ---- Drawing tokens ---------------------------------------------------------------------------
  * One token per row of logits, from a random number that the caller gives: the last call of a step whose rows are the next tokens
- * of many requests, or of many continuations of one prompt. With t = temperature, M the row's largest logit and w_i = exp((logit_i - M) / t):
+ * of many requests, or of many continuations of one prompt. For programs that serve a model with a vocabulary from the paged cache; nothing
+ * else here makes logits or takes a token's number (sdvg_page_plan takes counts, sdvg_paged_commit rows). With t = temperature, M the row's largest logit and w_i = exp((logit_i - M) / t):
  *   the tokens in order, larger logits first, of equal ones the lower index;
  *   top-k: the first top_k of them;
  *   top-p: the shortest prefix of those whose weight is at least top_p times theirs (at least one token);
  *   min-p: of these the ones with w_i >= min_p;
  *   tokens[r] = the lowest index i for which the sum of the kept weights up to i is more than u[r] times their total.
  * logprob[r] is the natural logarithm of its weight over that total. Weights and sums are held in 64 bits, a weight at most 2^-35
- * of itself off (2^-34 in a row without filters), however large logit / t is; one below 2^-63 of the largest counts as 0 where there is a filter, and one below 2^-1074 otherwise. The same call gives the same tokens, and so does a row alone
- * or among others, but where u or top_p lie as near to a border as that.
+ * of itself off (2^-34 in a row without filters), however large logit / t is; one below 2^-63 of the largest counts
+ * as 0 where there is a filter, and one below 2^-1074 otherwise. The same call gives the same tokens, and so does a row alone or among others, but where u or top_p lie as near to a border as that.
  *   logits    device [n_rows][vocab] of type dtype (SDVG_F32, SDVG_BF16, SDVG_F16), row_stride elements apart (not looked at for one row),
  *             aligned to their own size. -infinity: the token is never drawn; -0 is 0; +infinity is more than all numbers. A row that has a NaN, or
  *             nothing but -infinity, gets token -1 and a logprob of NaN.
@@ -486,7 +491,7 @@ int64_t sdvg_paged_prefix_attn_workspace_bytes(const sdvg_paged_attn_desc *desc,
  *             or >= vocab, top_p >= 1 (or NaN) and min_p <= 0 (or NaN) are off; min_p > 1 is 1.
  *   tokens    device int32 [n_rows]; logprob device float [n_rows], nullable. They must not overlap the inputs or each other (SDVG_ERR_RANGE).
  *   workspace device, 16-byte aligned, of at least sdvg_sample_tokens_workspace_bytes(n_rows, vocab) bytes (SDVG_ERR_RANGE if it is
- *             smaller). Scratch: overlapping calls need their own.
+ *             smaller), some 14.4 KB for every 8192 tokens of a row, whatever the filters. Scratch: overlapping calls need their own.
  * 1 <= vocab <= 2^20; n_rows slices of 8192 tokens below some 2^23 (SDVG_ERR_UNSUPPORTED); n_rows may be 0. Two launches, four with any
  * filter; asynchronous on `stream`.
  */

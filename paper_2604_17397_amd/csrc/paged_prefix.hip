@@ -15,10 +15,10 @@
 //     number takes, for an error that is the result's own rounding.
 // The 16-byte chunks of a row are permuted by the row's number (block_attn_index.h has the same), so that no read meets a bank twice.
 //
-// us (kernel and join): 128 requests of one token behind 8191 shared keys, 32 query and 8 key heads, f16 74 + 12; 64 behind 65520 keys, 40 / 8 heads, bf16
-// 160 + 13, 0.8 PFLOP/s with the second number of P counted: products take three fifths of the 5000 cycles or so of a tile, next to another wave of the SIMD; the rest is
-// the softmax, which the two waves do at the same time as often as not, and barriers (121 cycles, the copies' own wait 23). One row of 12 heads 9 + 6, a
-// chain of latencies. Not kept: key tiles of 32 in a ring of four (these three cases with 90, 202 and 15 us a call, against 83, 170 and 15), the
+// us of a call (and of kernel and join, traced, when the kernel takes longer than in a loop of calls): 128 requests of one token behind 8191 shared keys,
+// 32 query and 8 key heads, f16 86 (79 + 14); 64 behind 65520 keys, 40 / 8 heads, bf16 171 (187 + 15), of which products at the full rate, the second
+// number of P counted, would take 104; the rest is the softmax, which two waves of a SIMD do at the same time as often as not, and barriers. Four requests
+// of 12 heads behind 936 keys 14.9 (9.6 + 5.8), a chain of latencies. Not kept: key tiles of 32 in a ring of four (these three cases with 90, 202 and 15 us a call, against 83, 170 and 15), the
 // scores of a 32-key step ahead of the probabilities of the one before (88, 202; registers spill), row tiles of even size (183 and 181), raised wave priority
 // around the products (no difference).
 #include "block_attn_index.h"

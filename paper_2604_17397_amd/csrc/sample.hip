@@ -19,7 +19,7 @@
 // of up to 2^17 tokens that all have the largest one is exact.
 //
 // us of the four kernels: 1 row of 32000 tokens, bf16, all filters 5, 4, 6, 21 (chains of latencies: the draw's are some 15 steps of 0.3 to 2); 128 rows of 131072,
-// bf16 16, 6, 13, 27; 200 of 150001, f16, top-p 27, 6, 22, 23; 777 of 32768, fp32 25, 6, 23, 35; 64 of 131072, fp32, no filter 12 and 8. The first kernel without
+// bf16 16, 6, 13, 28; 200 of 150001, f16, top-p 27, 7, 22, 24; 777 of 32768, fp32 26, 6, 23, 36; 64 of 131072, fp32, no filter 12 and 8. The first kernel without
 // its histogram takes 10, 13 and 19 of the 16, 27 and 25: 18 operations and an atomic per token, and what a launch of so many loads takes to begin and end.
 #include <float.h>
 #include <math.h>
