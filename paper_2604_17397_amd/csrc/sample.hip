@@ -822,8 +822,8 @@ __device__ __forceinline__ Reached resolve(const Drawn<T, kDrawThreads> &row, in
     });
     __syncthreads();
     low += static_cast<unsigned long long>(choose(1)) << shift;
-    const unsigned long long part_high = low + ((1ull << shift) - 1);
-    high = part_high < high ? part_high : high;
+    const unsigned long long rest = (1ull << shift) - 1;   // (low + rest may leave 64 bits, behind the lowest logits)
+    if (high - low > rest) high = low + rest;
   }
   // the few that are left, and their weights
   const bool here = n_held <= kRanked;

@@ -34,3 +34,21 @@ def test_infinite_temperature(kind, filters, vocab):
     for u in (0.0, 0.5, 0.75, 1 - 2.0**-24):
         check(x, [u] * 10, temperature=INF, **FILTERS[filters])
         check(x, [u] * 10, temperature=[INF, 1.0, INF, INF, 2.0, INF, INF, 0.5, INF, INF], **FILTERS[filters])
+
+
+@pytest.mark.parametrize("kind", list(DT))
+@pytest.mark.parametrize("t", [INF, 3.4028234e38, 1e37])
+@pytest.mark.parametrize("vocab", [300, 453, 5000, 30001])
+def test_the_lowest_numbers_among_others_of_the_same_weight(kind, t, vocab):
+    """Ties of weight from one end of the numbers to the other, more than are compared with each other: they go by logit, then by index."""
+    big = torch.finfo(DT[kind]).max
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(vocab)
+    x = torch.randn((8, vocab), generator=gen, device="cuda").to(DT[kind])
+    x[torch.rand((8, vocab), generator=gen, device="cuda") < 0.5] = -big
+    x[4:6] = -x[4:6]                                # the largest number instead
+    x[6:][torch.rand((2, vocab), generator=gen, device="cuda") < 0.3] = big
+    x[7][torch.rand(vocab, generator=gen, device="cuda") < 0.5] = -INF
+    for u in (0.1, 0.7):
+        for kw in (dict(top_k=vocab - 5), dict(top_k=vocab // 2), dict(top_k=vocab // 3, top_p=0.7), dict(top_p=0.6), dict(top_p=0.99), dict(top_k=vocab - 2, min_p=0.25)):
+            check(x, [u] * 8, temperature=t, **kw)
